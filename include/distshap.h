@@ -58,6 +58,9 @@ enum ds_dtype {
                             accumulate in fp32; the product X_c W_1, formed once per target, stays fp32 */
 };
 
+/* Element types of the operators on rows of features. */
+enum ds_element { DS_ELEM_F32 = 0, DS_ELEM_BF16 = 1, DS_ELEM_F16 = 2 };
+
 enum ds_score { DS_SCORE_PROB = 0, DS_SCORE_LOGIT = 1 };
 enum ds_solver { DS_SOLVER_AUTO = 0, DS_SOLVER_GRAM_CHOL = 1, DS_SOLVER_CGLS = 2 };
 /* Regression weight of a sampled row (paper, "Shapley value" / sample-distribution equation: rho_s is the
@@ -351,6 +354,64 @@ int ds_solve(ds_ctx* ctx, int64_t n, int64_t k, const uint64_t* Z, const float* 
  * (device) receiving row 2t = G_s and row 2t+1 = its complement. 1 <= num_k <= 4096. */
 int ds_fidelity(ds_ctx* ctx, const ds_cgraph* cg, const float* phi, const int64_t* topk, int32_t num_k,
                 int32_t score, float* fid_plus, float* fid_minus, uint64_t* masks_out);
+
+/* ---- operators on rows of features ------------------------------------------------
+ *
+ * What a learned encoder of node features computes and trains on: layer norm, dropout with a residual sum, rows grouped
+ * by a type (or by the expert that a router chose), and products with the weights of a row's group. Rows are of ds_element
+ * `dtype`, `*_stride` elements apart (at least a row's width for outputs; 0 repeats one row of an input), at any alignment that the
+ * element itself has; parameters of a norm, biases, their gradients and statistics are fp32. Sums are held in fp32 and every result is rounded once.
+ * An output may be the same buffer as an input of the same rows for ds_layer_norm (x), ds_dropout (x, residual) and
+ * ds_layer_norm_backward (dy, x), with equal strides; otherwise outputs overlap nothing. The calls queue their kernels on the context's
+ * stream and return: they allocate nothing, copy nothing to the host and wait for nothing, so they may be
+ * captured into a HIP graph. A call that needs scratch memory says how much (`*_workspace`, pure host functions); the
+ * caller gives it, aligned to 16 bytes, and may reuse it once the stream has passed the call. The same inputs give
+ * the same bits. */
+
+/* y = (x - mean) rstd weight + bias over the columns of each row, rstd = 1 / sqrt(variance + eps). 1 <= cols <= 4096.
+ * weight, bias: float[cols] or NULL (1 and 0). mean, rstd: float[rows] out or NULL, what the backward pass needs. */
+int ds_layer_norm(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, const float* weight,
+                  const float* bias, float eps, void* y, int64_t y_stride, float* mean, float* rstd);
+
+/* Gradients of ds_layer_norm: dx, dweight float[cols] = sum over rows of dy (x - mean) rstd, dbias float[cols] = sum of dy
+ * (zeros where rows is 0). mean, rstd: what the forward pass left. */
+int ds_layer_norm_backward_workspace(int64_t rows, int64_t cols, int64_t* bytes /* [host] */);
+int ds_layer_norm_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t dy_stride, const void* x,
+                           int64_t x_stride, const float* mean, const float* rstd, const float* weight, void* dx,
+                           int64_t dx_stride, float* dweight, float* dbias, void* workspace, int64_t workspace_bytes);
+
+/* y = residual + (kept ? x * 65536 / (65536 - t) : 0) with t = round(65536 p) (halves to even); residual NULL: 0. Element
+ * (r, c) is kept where a 16-bit draw is not below t: half c % 2 (0: the low one) of word c % 8 / 2 of Philox4x32-10 with
+ * counter (c / 8, r mod 2^32, r / 2^32, tag) and key `seed`. The mask is not stored: the gradient of x is this call on the
+ * gradient of y with the same p, seed and tag and no residual. A dropped element leaves 0 whatever it was. 0 <= p <= 1. */
+int ds_dropout(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, const void* residual,
+               int64_t residual_stride, double p, uint64_t seed, uint32_t tag, void* y, int64_t y_stride);
+
+/* Rows by group. ids: int32[rows], the group of every row (outside of [0, groups): none). offsets: int64[groups + 1] out,
+ * offsets[g] = rows in the groups before g; order: int32[rows] out, the rows by group, ascending within each, those of
+ * no group last. 1 <= groups <= 1024, rows <= 2^30. */
+int ds_group_rows_workspace(int64_t rows, int64_t groups, int64_t* bytes /* [host] */);
+int ds_group_rows(ds_ctx* ctx, const int32_t* ids, int64_t rows, int64_t groups, int64_t* offsets, int32_t* order, void* workspace,
+                  int64_t workspace_bytes);
+
+/* y[r] = x[r] w[g] + bias[g] for the rows r = order[offsets[g] .. offsets[g + 1]) of every group g, zeros for the rows of no
+ * group (order[offsets[groups] ..)); relu != 0: max(., 0). order NULL: rows are sorted by group. w: [groups x inner x outer]
+ * of `dtype`, contiguous; bias: float[groups x outer] or NULL. offsets ascend from 0 and order names every row once, as
+ * ds_group_rows leaves them; where they do not, some rows of y are left unwritten or written with another row's group, and nothing
+ * outside of the buffers is touched. */
+int ds_grouped_mm(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, const void* x,
+                  int64_t x_stride, const void* w, const int64_t* offsets, const int32_t* order, const float* bias, int32_t relu,
+                  void* y, int64_t y_stride);
+
+/* Gradients of ds_grouped_mm without its ReLU: dx[r] = dy[r] w[g]^T (zeros for rows of no group), dw[g] = sum over the
+ * group's rows of x[r]^T dy[r], db: float[groups x outer] = sum of dy[r] (zeros for an empty group). gate: NULL, or rows like x:
+ * dx is 0 where gate is not above 0 (the ReLU whose output x was). */
+int ds_grouped_mm_backward_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups,
+                                     int64_t* bytes /* [host] */);
+int ds_grouped_mm_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, const void* dy,
+                           int64_t dy_stride, const void* x, int64_t x_stride, const void* w, const int64_t* offsets,
+                           const int32_t* order, const void* gate, int64_t gate_stride, void* dx, int64_t dx_stride, void* dw,
+                           float* db, void* workspace, int64_t workspace_bytes);
 
 /* Measurement aid: a plain device-to-device copy of `bytes` bytes (multiple of 16) by a simple
  * streaming kernel on the context's stream. Profilers' HBM byte counters are calibrated against it

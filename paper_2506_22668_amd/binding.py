@@ -13,12 +13,15 @@ DS_F32, DS_BF16_IN_F32_ACC = 0, 1
 DS_SCORE_PROB, DS_SCORE_LOGIT = 0, 1
 DS_SOLVER_AUTO, DS_SOLVER_GRAM_CHOL, DS_SOLVER_CGLS = 0, 1, 2
 DS_WEIGHT_CLASS_MASS, DS_WEIGHT_UNIFORM = 0, 1
+DS_ELEM_F32, DS_ELEM_BF16, DS_ELEM_F16 = 0, 1, 2
 
 EXPORTED_SYMBOLS = [
     "ds_create", "ds_destroy", "ds_last_error", "ds_set_tuning", "ds_set_graph", "ds_set_features", "ds_set_gcn", "ds_set_gat",
     "ds_explain", "ds_explain_cgraph", "ds_explain_batch", "ds_extract", "ds_cgraph_get_info", "ds_cgraph_edges",
     "ds_cgraph_nodes", "ds_cgraph_first_transform", "ds_cgraph_free", "ds_sample_plan", "ds_sample",
     "ds_plan_tables", "ds_plan_tables_ex", "ds_sample_ex", "ds_sample_range", "ds_eval", "ds_eval_pairs", "ds_eval_noalloc", "ds_solve", "ds_fidelity", "ds_copy_probe", "ds_version",
+    "ds_layer_norm", "ds_layer_norm_backward_workspace", "ds_layer_norm_backward", "ds_dropout", "ds_group_rows_workspace",
+    "ds_group_rows", "ds_grouped_mm", "ds_grouped_mm_backward_workspace", "ds_grouped_mm_backward",
 ]
 
 
@@ -114,6 +117,15 @@ def load_library():
         "ds_solve": [p, i64, i64, p, p, p, C.POINTER(Options), p, C.POINTER(Report)],
         "ds_copy_probe": [p, p, p, i64],
         "ds_fidelity": [p, p, p, C.POINTER(i64), i32, i32, C.POINTER(C.c_float), C.POINTER(C.c_float), p],
+        "ds_layer_norm": [p, i32, i64, i64, p, i64, p, p, C.c_float, p, i64, p, p],
+        "ds_layer_norm_backward_workspace": [i64, i64, C.POINTER(i64)],
+        "ds_layer_norm_backward": [p, i32, i64, i64, p, i64, p, i64, p, p, p, p, i64, p, p, p, i64],
+        "ds_dropout": [p, i32, i64, i64, p, i64, p, i64, dbl, u64, u32, p, i64],
+        "ds_group_rows_workspace": [i64, i64, C.POINTER(i64)],
+        "ds_group_rows": [p, p, i64, i64, p, p, p, i64],
+        "ds_grouped_mm": [p, i32, i64, i64, i64, i64, p, i64, p, p, p, p, i32, p, i64],
+        "ds_grouped_mm_backward_workspace": [i32, i64, i64, i64, i64, C.POINTER(i64)],
+        "ds_grouped_mm_backward": [p, i32, i64, i64, i64, i64, p, i64, p, i64, p, p, p, p, i64, p, i64, p, p, p, i64],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -179,6 +191,9 @@ class Context:
             raise DistShapError(rc, "ds_create failed")
         self.h = handle
         self._keep = {}
+        self._index = idx
+        self._raw_stream = stream.cuda_stream if stream is not None else 0
+        self._elements = {torch.float32: DS_ELEM_F32, torch.bfloat16: DS_ELEM_BF16, torch.float16: DS_ELEM_F16}
 
     def close(self):
         if getattr(self, "h", None):
@@ -435,3 +450,167 @@ class Context:
                                            C.byref(opts), _ptr(phi), C.byref(rep)),
                          allow=(DS_ENOTCONV,) if allow_not_converged else ())
         return phi, rep, rc
+
+    # -- operators on rows of features ---------------------------------------------
+    # Queued on the context's stream, which is ordered behind torch's current stream and in front of what that stream
+    # does next; nothing waits on the host. Under graph capture the context has to be one made for the captured stream.
+    def _queue(self, fn, *args):
+        t = self.torch
+        current = t.cuda.current_stream(self._index)
+        if current.cuda_stream == self._raw_stream:
+            self._check(fn(self.h, *args))
+            return
+        if t.cuda.is_current_stream_capturing():
+            raise DistShapError(DS_EINVAL, "the stream being captured is not the context's")
+        own = self._stream if self._stream is not None else t.cuda.default_stream(self._index)
+        own.wait_stream(current)
+        try:
+            self._check(fn(self.h, *args))
+        finally:
+            current.wait_stream(own)
+
+    def _refuse(self, message):
+        raise DistShapError(DS_EINVAL, message)
+
+    def _rows(self, a, name, shape=None, dtype=None):
+        """(tensor, its rows' distance): rows may lie apart, columns have to be neighbours (copied if they are not)."""
+        if a.dim() != 2 or (shape is not None and tuple(a.shape) != shape):
+            self._refuse(f"{name} has shape {tuple(a.shape)}, {'two dimensions are' if shape is None else f'{shape} is'} needed")
+        if a.dtype not in self._elements or (dtype is not None and a.dtype != dtype):
+            self._refuse(f"{name} is {a.dtype}, {'float32, bfloat16 or float16' if dtype is None else dtype} is needed")
+        if a.get_device() != self._index:
+            self._refuse(f"{name} is not on {self.device}")
+        step, inner = a.stride()
+        if inner != 1 and a.shape[1] > 1:
+            a = a.contiguous()
+            step = a.shape[1]
+        return a, step
+
+    def _values(self, a, name, shape, dtype):
+        """A contiguous tensor of the given shape and type, or None; its address."""
+        if a is None:
+            return None, None
+        if tuple(a.shape) != shape or a.dtype != dtype:
+            self._refuse(f"{name} is {a.dtype} of shape {tuple(a.shape)}, {dtype} of shape {shape} is needed")
+        if a.get_device() != self._index:
+            self._refuse(f"{name} is not on {self.device}")
+        a = a.contiguous()
+        return a, a.data_ptr()
+
+    def _workspace(self, fn, *args):
+        need = C.c_int64()
+        rc = fn(*args, C.byref(need))
+        if rc != DS_OK:
+            raise DistShapError(rc, "sizes out of range")
+        if need.value == 0:
+            return None, None, 0
+        ws = self.torch.empty(need.value, dtype=self.torch.uint8, device=self.device)
+        return ws, ws.data_ptr(), need.value
+
+    def layer_norm(self, x, weight=None, bias=None, eps=1e-5, want_stats=False):
+        """y = (x - mean) rstd weight + bias over the columns of each row; with `want_stats` (y, mean, rstd), the
+        last two for layer_norm_backward. x: [rows, cols] in fp32, bf16 or fp16, cols <= 4096; the others fp32."""
+        t = self.torch
+        x, xs = self._rows(x, "x")
+        rows, cols = x.shape
+        weight, wp = self._values(weight, "weight", (cols,), t.float32)
+        bias, bp = self._values(bias, "bias", (cols,), t.float32)
+        y = t.empty((rows, cols), dtype=x.dtype, device=x.device)
+        mean = rstd = mp = rp = None
+        if want_stats:
+            mean, rstd = t.empty((2, rows), dtype=t.float32, device=x.device)
+            mp, rp = mean.data_ptr(), rstd.data_ptr()
+        self._queue(self.lib.ds_layer_norm, self._elements[x.dtype], rows, cols, x.data_ptr(), xs, wp, bp, eps, y.data_ptr(),
+                    cols, mp, rp)
+        return (y, mean, rstd) if want_stats else y
+
+    def layer_norm_backward(self, dy, x, mean, rstd, weight=None):
+        """(dx, dweight, dbias) of layer_norm; mean and rstd are what it gave for x."""
+        t = self.torch
+        x, xs = self._rows(x, "x")
+        rows, cols = x.shape
+        dy, dys = self._rows(dy, "dy", (rows, cols), x.dtype)
+        if mean is None or rstd is None:
+            self._refuse("mean and rstd of the forward pass are needed")
+        mean, mp = self._values(mean, "mean", (rows,), t.float32)
+        rstd, rp = self._values(rstd, "rstd", (rows,), t.float32)
+        weight, wp = self._values(weight, "weight", (cols,), t.float32)
+        dx = t.empty((rows, cols), dtype=x.dtype, device=x.device)
+        dweight, dbias = t.empty((2, cols), dtype=t.float32, device=x.device)
+        ws, wsp, wsn = self._workspace(self.lib.ds_layer_norm_backward_workspace, rows, cols)
+        self._queue(self.lib.ds_layer_norm_backward, self._elements[x.dtype], rows, cols, dy.data_ptr(), dys, x.data_ptr(), xs, mp,
+                    rp, wp, dx.data_ptr(), cols, dweight.data_ptr(), dbias.data_ptr(), wsp, wsn)
+        return dx, dweight, dbias
+
+    def dropout(self, x, p, seed, tag=0, residual=None):
+        """residual + dropout(x): the mask is a function of (row, column, seed, tag) and never stored, so the gradient is
+        `dropout(dy, p, seed, tag)`."""
+        t = self.torch
+        x, xs = self._rows(x, "x")
+        rows, cols = x.shape
+        rp, rs = None, 0
+        if residual is not None:
+            residual, rs = self._rows(residual, "residual", (rows, cols), x.dtype)
+            rp = residual.data_ptr()
+        y = t.empty((rows, cols), dtype=x.dtype, device=x.device)
+        self._queue(self.lib.ds_dropout, self._elements[x.dtype], rows, cols, x.data_ptr(), xs, rp, rs, p, int(seed),
+                    int(tag) & 0xFFFFFFFF, y.data_ptr(), cols)
+        return y
+
+    def group_rows(self, ids, groups):
+        """(offsets int64[groups + 1], order int32[rows]): the rows by group, ascending within each, those whose id
+        (int32[rows]) is outside of [0, groups) last."""
+        t = self.torch
+        if ids is None or ids.dim() != 1:
+            self._refuse("ids: one for every row")
+        rows = ids.shape[0]
+        ids, ip = self._values(ids, "ids", (rows,), t.int32)
+        groups = int(groups)
+        ws, wsp, wsn = self._workspace(self.lib.ds_group_rows_workspace, rows, groups)
+        offsets = t.empty(groups + 1, dtype=t.int64, device=ids.device)
+        order = t.empty(rows, dtype=t.int32, device=ids.device)
+        self._queue(self.lib.ds_group_rows, ip, rows, groups, offsets.data_ptr(), order.data_ptr(), wsp, wsn)
+        return offsets, order
+
+    def _grouped(self, x, w, offsets, order):
+        t = self.torch
+        x, xs = self._rows(x, "x")
+        if w is None or w.dim() != 3 or w.shape[1] != x.shape[1]:
+            self._refuse(f"w is [groups, {x.shape[1]}, outer] for rows of {x.shape[1]} columns")
+        w, wp = self._values(w, "w", tuple(w.shape), x.dtype)
+        if offsets is None:
+            self._refuse("offsets are needed")
+        offsets, op = self._values(offsets, "offsets", (w.shape[0] + 1,), t.int64)
+        order, rp = self._values(order, "order", (x.shape[0],), t.int32)
+        return x, xs, w, wp, (offsets, order), op, rp
+
+    def grouped_mm(self, x, w, offsets, order=None, bias=None, relu=False):
+        """y[r] = x[r] @ w[g] + bias[g] (then ReLU) for the rows of every group g (see group_rows; order None: rows sorted by
+        group), zeros for rows of no group. x: [rows, inner], w: [groups, inner, outer] of x's type, bias fp32."""
+        t = self.torch
+        x, xs, w, wp, keep, op, rp = self._grouped(x, w, offsets, order)
+        (rows, inner), (groups, _, outer) = x.shape, w.shape
+        bias, bp = self._values(bias, "bias", (groups, outer), t.float32)
+        y = t.empty((rows, outer), dtype=x.dtype, device=x.device)
+        self._queue(self.lib.ds_grouped_mm, self._elements[x.dtype], rows, inner, outer, groups, x.data_ptr(), xs, wp, op, rp, bp,
+                    int(bool(relu)), y.data_ptr(), outer)
+        return y
+
+    def grouped_mm_backward(self, dy, x, w, offsets, order=None, gate=None):
+        """(dx, dw, dbias fp32) of grouped_mm without its ReLU; dx is 0 where `gate` (rows like x) is not above 0."""
+        t = self.torch
+        x, xs, w, wp, keep, op, rp = self._grouped(x, w, offsets, order)
+        (rows, inner), (groups, _, outer) = x.shape, w.shape
+        dy, dys = self._rows(dy, "dy", (rows, outer), x.dtype)
+        gp, gs = None, 0
+        if gate is not None:
+            gate, gs = self._rows(gate, "gate", (rows, inner), x.dtype)
+            gp = gate.data_ptr()
+        dx = t.empty((rows, inner), dtype=x.dtype, device=x.device)
+        dw = t.empty((groups, inner, outer), dtype=x.dtype, device=x.device)
+        db = t.empty((groups, outer), dtype=t.float32, device=x.device)
+        element = self._elements[x.dtype]
+        ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_workspace, element, rows, inner, outer, groups)
+        self._queue(self.lib.ds_grouped_mm_backward, element, rows, inner, outer, groups, dy.data_ptr(), dys, x.data_ptr(), xs, wp, op,
+                    rp, gp, gs, dx.data_ptr(), inner, dw.data_ptr(), db.data_ptr(), wsp, wsn)
+        return dx, dw, db

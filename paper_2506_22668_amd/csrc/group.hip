@@ -1,0 +1,171 @@
+// Rows by group: offsets[g] rows lie in the groups before g, and the order lists the rows group by group, ascending within a
+// group, those of no group (an id outside of [0, groups)) last.
+//
+// A stable counting sort with one key digit. A workgroup of 16 waves has a stretch of the rows, every wave a sixteenth of it in
+// steps of 64. Within a step the lanes of one group find each other by a ballot for every bit of the id, so that a row's rank is
+// a popcount and the lowest lane adds the step's count in LDS: no atomic decides an order, and the result is the
+// only one there is. Several workgroups: a first launch leaves every stretch's counts, a second adds up the ones before its own
+// (ids are read twice, from the caches the second time).
+#include "feature_ops.h"
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kStretch = 4096;    // rows of a workgroup, at the least, where there are several
+
+struct GroupArgs {
+  const int32_t* ids;
+  int rows, groups, per_wave;   // rows of a wave, a multiple of 64
+  int64_t* offsets;
+  int32_t *order, *counts;      // counts: [block][groups + 1]
+};
+
+// the lanes whose key is this lane's
+__device__ __forceinline__ unsigned long long same_key(int key, int bits) {
+  unsigned long long same = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long set = __ballot((key >> b) & 1);
+    same &= (key >> b) & 1 ? set : ~set;
+  }
+  return same;
+}
+
+__device__ __forceinline__ int key_of(const GroupArgs& a, int row, int end) {
+  if (row >= end) return a.groups + 1;   // (counted nowhere)
+  const int id = a.ids[row];
+  return id >= 0 && id < a.groups ? id : a.groups;
+}
+
+// Goes through a wave's rows: calls each(row, key, rank among the step's rows of the key, how many) for the rows there are
+template <typename Each>
+__device__ __forceinline__ void walk(const GroupArgs& a, int wave, Each each) {
+  const int lane = threadIdx.x & 63, bits = 32 - __clz(a.groups + 1);
+  const int64_t first = ((int64_t)blockIdx.x * kWaves + wave) * a.per_wave;
+  const int begin = first < a.rows ? (int)first : a.rows;
+  const int end = a.rows - begin < a.per_wave ? a.rows : begin + a.per_wave;
+  int key = key_of(a, begin + lane, end);
+  for (int at = begin; at < end; at += 64) {
+    const int now = key;
+    if (end - at > 64) key = key_of(a, at + 64 + lane, end);
+    const unsigned long long same = same_key(now, bits);
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    each(at + lane, now, rank, __popcll(same));
+  }
+}
+
+// counts of this workgroup's rows by wave and group
+__device__ __forceinline__ void count_rows(const GroupArgs& a, int* count) {
+  const int wave = threadIdx.x >> 6, keys = a.groups + 1;
+  for (int i = threadIdx.x; i < kWaves * keys; i += kThreads) count[i] = 0;
+  __syncthreads();
+  volatile int* mine = count + wave * keys;   // (lanes of the wave take turns at it)
+  walk(a, wave, [&](int, int key, int rank, int of) {
+    if (rank == 0 && key < keys) mine[key] = mine[key] + of;   // (one lane a group)
+  });
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a) {
+  extern __shared__ int count[];
+  count_rows(a, count);
+  const int keys = a.groups + 1;
+  for (int g = threadIdx.x; g < keys; g += kThreads) {
+    int n = 0;
+    for (int w = 0; w < kWaves; ++w) n += count[w * keys + g];
+    a.counts[(int64_t)blockIdx.x * keys + g] = n;
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a) {
+  extern __shared__ int count[];   // [waves][keys], then the rows of a group in the whole and before this workgroup
+  __shared__ int wave_sum[kWaves];
+  const int keys = a.groups + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int *whole = count + kWaves * keys, *before = whole + keys;
+  count_rows(a, count);
+  if (gridDim.x == 1) {
+    for (int g = threadIdx.x; g < keys; g += kThreads) {
+      int n = 0;
+      for (int w = 0; w < kWaves; ++w) n += count[w * keys + g];
+      whole[g] = n;
+      before[g] = 0;
+    }
+  } else {
+    for (int g = threadIdx.x; g < keys; g += kThreads) whole[g] = before[g] = 0;
+    __syncthreads();
+    const int all = (int)gridDim.x * keys, mine = (int)blockIdx.x * keys;
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+      const int n = a.counts[i];
+      if (n == 0) continue;
+      const int g = i % keys;
+      atomicAdd(&whole[g], n);   // (whole numbers: any order gives the same)
+      if (i < mine) atomicAdd(&before[g], n);
+    }
+  }
+  __syncthreads();
+  // where each group starts
+  const int n = (int)threadIdx.x < a.groups ? whole[threadIdx.x] : 0;
+  int upto = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += up;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  int start = upto - n, held = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) start += wave_sum[w];
+    held += wave_sum[w];
+  }
+  for (int g = threadIdx.x; g < keys; g += kThreads) {
+    // (thread g has group g's start; the rows of no group start behind all others)
+    int at = (g < a.groups ? start : held) + before[g];
+    if (blockIdx.x == 0) a.offsets[g] = at;
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = count[w * keys + g];
+      count[w * keys + g] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  volatile int* mine = count + wave * keys;
+  walk(a, wave, [&](int row, int key, int rank, int of) {
+    if (key >= keys) return;
+    const int at = mine[key];
+    a.order[at + rank] = row;
+    if (rank == 0) mine[key] = at + of;   // (a wave's LDS accesses keep their order)
+  });
+}
+
+}  // namespace
+
+// One workgroup takes up to four stretches by itself: a second launch costs more than the rest of its walk does.
+int ds_group_blocks(int rows, int groups) {
+  (void)groups;
+  const int blocks = (rows + kStretch - 1) / kStretch;
+  return blocks <= 4 ? 1 : blocks < 256 ? blocks : 256;
+}
+
+int ds_launch_group_rows(ds_ctx* ctx, const int32_t* ids, int rows, int groups, int64_t* offsets, int32_t* order, int32_t* counts) {
+  const int blocks = ds_group_blocks(rows, groups);
+  GroupArgs a = {};
+  a.ids = ids;
+  a.rows = rows;
+  a.groups = groups;
+  const int64_t waves = (int64_t)blocks * kWaves, each = ((int64_t)rows + waves - 1) / waves;
+  a.per_wave = (int)((each + 63) / 64 * 64);
+  a.offsets = offsets;
+  a.order = order;
+  a.counts = counts;
+  const int lds = (kWaves + 2) * (groups + 1) * (int)sizeof(int);
+  if (lds > 48 * 1024) {
+    DS_HIP(ctx, hipFuncSetAttribute((const void*)group_count_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    DS_HIP(ctx, hipFuncSetAttribute((const void*)group_place_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  }
+  if (blocks > 1) hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kThreads), lds, ctx->stream, a);
+  hipLaunchKernelGGL(group_place_kernel, dim3(blocks > 0 ? blocks : 1), dim3(kThreads), lds, ctx->stream, a);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}

@@ -1,0 +1,307 @@
+// Products of rows with the weights of their group, and their gradients.
+//
+//   forward:   y[r] = x[r] W_g + b_g (ReLU)              for the rows r of group g, zeros for the rows of no group
+//   backward:  dx[r] = (gate[r] > 0) dy[r] W_g^T,  dW_g = sum_r x[r]^T dy[r],  db_g = sum_r dy[r]
+//
+// The rows of group g are those at positions offsets[g] .. offsets[g + 1] of `order`. Sizes of groups are known on the GPU
+// alone: the grid has a tile for every one that there can be, and a workgroup finds its rows from the offsets.
+// All products go through the matrix cores, fp32 ones on their fp32 form, and are summed in fp32.
+#include "feature_ops.h"
+#include "rows.h"
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+using PieceV = typename Piece<T>::V;
+
+// d += a b on 16 x 16 with a lane's piece of both operands: lane l gives row (column) l % 16 and the contraction's indices
+// N (l / 16) .. + N - 1; d: column l % 16, rows 4 (l / 16) .. + 3.
+__device__ __forceinline__ f32x4 multiply(PieceV<__bf16> a, PieceV<__bf16> b, f32x4 d) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(PieceV<_Float16> a, PieceV<_Float16> b, f32x4 d) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, d, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(PieceV<float> a, PieceV<float> b, f32x4 d) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], d, 0, 0, 0);
+  return d;
+}
+
+struct MmArgs {
+  int rows, inner, outer, groups;
+  const void *w, *x, *dy, *gate;
+  int64_t xs, dys, gs, ys;
+  const int64_t* offsets;
+  const int32_t* order;
+  const float* bias;
+  int relu, col_tiles;
+  void* y;            // the product by rows (y, or dx)
+  void* dw;
+  float* db;
+};
+
+constexpr int kWaves = 4;   // of a workgroup: they share the contraction
+
+// ---- few rows to a group --------------------------------------------------------------------------------------------------
+// A workgroup takes 16 RB rows of one group and 16 N columns (N = elements of a 16-byte piece), each of its waves every
+// fourth step of the contraction; their sums meet in LDS. No operand is shared between waves, so none goes through LDS: a
+// wave has eight pieces of W a step in flight without a barrier. W is read in its own order: where its rows run along the
+// columns of the result (TRANSPOSED false: N steps of the contraction by 8 columns to a lane) the lane turns its square of
+// elements around in registers; column j of the squares of 16 lanes is an operand, so that a lane ends up with N neighbouring columns of a
+// row. TRANSPOSED: the product with W^T, whose pieces are operands as they are.
+template <typename T, int RB, bool TRANSPOSED>
+__global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
+  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
+  __shared__ float meet[kWaves][4][64][N];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+  const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
+  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N;
+  GroupTile gt;
+  if (!find_group_tile(a.offsets, a.groups, a.rows, SHIFT, tile, &gt)) return;
+  int row[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) row[r] = gt.begin + 16 * r + m < gt.end ? ds_ordered_row(a.order, a.rows, gt.begin + 16 * r + m) : -1;
+  f32x4 acc[RB][N] = {};
+  const int64_t xs = TRANSPOSED ? a.dys : a.xs;
+  const T* x = (const T*)(TRANSPOSED ? a.dy : a.x);
+  if (gt.group < a.groups) {
+    const T* w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer;
+    const int n0 = col + N * m;   // the lane's columns
+    PieceV<T> wp[N], xp[RB];
+    const auto fetch = [&](int k) {
+      k += N * q;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if constexpr (TRANSPOSED) wp[i] = load_piece<T>(w + (int64_t)(n0 + i) * a.outer + k, n0 + i < width ? depth - k : 0);
+        else wp[i] = load_piece<T>(w + (int64_t)(k + i) * a.outer + n0, k + i < depth ? width - n0 : 0);
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) xp[r] = load_piece<T>(x + row[r] * xs + k, row[r] >= 0 ? depth - k : 0);
+    };
+    int k = wave * 4 * N;
+    if (k < depth) fetch(k);
+    while (k < depth) {
+      PieceV<T> wn[N], xn[RB];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if constexpr (TRANSPOSED) {
+          wn[j] = wp[j];
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) wn[j][i] = wp[i][j];
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) xn[r] = xp[r];
+      k += kWaves * 4 * N;
+      if (k < depth) fetch(k);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) acc[r][j] = multiply(wn[j], xn[r], acc[r][j]);
+    }
+  }
+  const T* gate = (const T*)a.gate;
+  T* y = (T*)a.y;
+  // wave w ends up with the four columns' quarter w of every row block: columns col + N (4 q + w) .. + N - 1
+  const int n = col + N * (4 * q + wave);
+  float bias[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    bias[j] = a.bias && gt.group < a.groups && n + j < width ? a.bias[(int64_t)gt.group * width + n + j] : 0.f;
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    if (r) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) meet[wave][i][lane][j] = acc[r][j][i];
+    __syncthreads();
+    if (row[r] >= 0) {
+      PieceV<T> out;
+      const PieceV<T> open = gate ? load_piece<T>(gate + row[r] * a.gs + n, width - n) : PieceV<T>{};
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float v = bias[j];
+#pragma unroll
+        for (int s = 0; s < kWaves; ++s) v += meet[s][wave][lane][j];
+        if (a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
+        if (gate) v = (float)open[j] > 0.f ? v : 0.f;
+        out[j] = (T)v;
+      }
+      store_piece<T>(y + row[r] * a.ys + n, out, width - n);
+    }
+  }
+}
+
+// dW and db of a group: 16 N outer by 8 N inner columns to a workgroup, the waves share the group's rows. Both operands
+// run across the contraction (the rows), so both are turned around in registers. db is one more product, with ones for x.
+template <typename T>
+__global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a) {
+  constexpr int N = Piece<T>::N, H = N / 2;
+  typedef T Half __attribute__((ext_vector_type(H), aligned(sizeof(T))));
+  __shared__ float meet[kWaves][4][64][N];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+  const int group = (int)blockIdx.y;
+  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N, in0 = ((int)blockIdx.x / a.col_tiles) * 16 * H;
+  int begin, end;
+  ds_group_range(a.offsets, a.groups, a.rows, group, &begin, &end);
+  const T *x = (const T*)a.x, *dy = (const T*)a.dy;
+  const int n0 = col + N * m, c0 = in0 + H * m;
+  f32x4 acc[H][N] = {}, sum[N] = {};
+  PieceV<T> ones;
+#pragma unroll
+  for (int i = 0; i < N; ++i) ones[i] = (T)1.f;
+  const bool with_sum = in0 == 0;
+  for (int at = begin + wave * 4 * N; at < end; at += kWaves * 4 * N) {
+    PieceV<T> dp[N], dn[N], xn[H];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int pos = at + N * q + i, row = pos < end ? ds_ordered_row(a.order, a.rows, pos) : -1;
+      dp[i] = load_piece<T>(dy + row * a.dys + n0, row >= 0 ? a.outer - n0 : 0);
+      const T* px = x + row * a.xs + c0;
+      const int have = row >= 0 ? a.inner - c0 : 0;
+      if (have >= H) {
+        const Half h = *reinterpret_cast<const Half*>(px);
+#pragma unroll
+        for (int j = 0; j < H; ++j) xn[j][i] = h[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < H; ++j) xn[j][i] = j < have ? px[j] : (T)0.f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dn[j][i] = dp[i][j];
+#pragma unroll
+      for (int h = 0; h < H; ++h) acc[h][j] = multiply(dn[j], xn[h], acc[h][j]);
+      if (with_sum) sum[j] = multiply(dn[j], ones, sum[j]);
+    }
+  }
+  T* dw = (T*)a.dw + (int64_t)group * a.inner * a.outer;
+  const int n = col + N * (4 * q + wave);
+#pragma unroll
+  for (int h = 0; h <= H; ++h) {
+    if (h == H && !with_sum) break;
+    if (h) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) meet[wave][i][lane][j] = h < H ? acc[h < H ? h : 0][j][i] : sum[j][i];
+    __syncthreads();
+    float v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      v[j] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kWaves; ++s) v[j] += meet[s][wave][lane][j];
+    }
+    if (h < H) {
+      PieceV<T> out;
+#pragma unroll
+      for (int j = 0; j < N; ++j) out[j] = (T)v[j];
+      if (c0 + h < a.inner) store_piece<T>(dw + (int64_t)(c0 + h) * a.outer + n, out, a.outer - n);
+    } else if (m == 0) {   // (every column of the product with ones is the sum)
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (n + j < a.outer) a.db[(int64_t)group * a.outer + n + j] = v[j];
+    }
+  }
+}
+
+MmArgs arguments(const ds_grouped& p) {
+  MmArgs a = {};
+  a.rows = p.rows;
+  a.inner = p.inner;
+  a.outer = p.outer;
+  a.groups = p.groups;
+  a.w = p.w;
+  a.offsets = p.offsets;
+  a.order = p.order;
+  return a;
+}
+
+// tiles of 2^shift rows that the groups and the rows of none can have: every group may end inside one
+int64_t most_tiles(const ds_grouped& p, int shift) {
+  const int64_t partial = p.groups + 1 < p.rows ? p.groups + 1 : p.rows;
+  return ((int64_t)p.rows >> shift) + partial;
+}
+
+template <typename T, bool TRANSPOSED>
+int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
+  if (p.rows == 0) return DS_OK;
+  constexpr int N = Piece<T>::N;
+  hipStream_t stream = ctx->stream;
+  a.col_tiles = ((TRANSPOSED ? p.inner : p.outer) + 16 * N - 1) / (16 * N);
+  const int64_t mean = p.rows / p.groups;
+  const int shift = mean <= 16 ? 4 : mean <= 32 ? 5 : 6;
+  const int64_t tiles = most_tiles(p, shift) * a.col_tiles;
+  if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
+  const dim3 grid((unsigned)tiles), block(64 * kWaves);
+  if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, TRANSPOSED>), grid, block, 0, stream, a);
+  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, TRANSPOSED>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, TRANSPOSED>), grid, block, 0, stream, a);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+template <typename T>
+int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
+  constexpr int N = Piece<T>::N;
+  a.col_tiles = (p.outer + 16 * N - 1) / (16 * N);
+  const dim3 grid((unsigned)(((p.inner + 8 * N - 1) / (8 * N)) * a.col_tiles), p.groups), block(64 * kWaves);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T>), grid, block, 0, ctx->stream, a);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+template <typename T>
+int backward(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
+  DS_TRY((launch_rows<T, true>(ctx, p, a)));
+  return launch_weights<T>(ctx, p, a);
+}
+
+}  // namespace
+
+int ds_launch_grouped_mm(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows x, const float* bias, int relu, ds_rows y) {
+  if (p.rows == 0) return DS_OK;
+  MmArgs a = arguments(p);
+  a.x = x.data;
+  a.xs = x.stride;
+  a.bias = bias;
+  a.relu = relu;
+  a.y = (void*)y.data;
+  a.ys = y.stride;
+  if (dtype == DS_ELEM_F32) return launch_rows<float, false>(ctx, p, a);
+  if (dtype == DS_ELEM_BF16) return launch_rows<__bf16, false>(ctx, p, a);
+  return launch_rows<_Float16, false>(ctx, p, a);
+}
+
+int64_t ds_grouped_mm_backward_bytes(int dtype, const ds_grouped& p) {
+  (void)dtype;
+  (void)p;
+  return 0;
+}
+
+int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, ds_rows x, ds_rows gate, ds_rows dx,
+                                  void* dw, float* db, void* workspace) {
+  (void)workspace;
+  MmArgs a = arguments(p);
+  a.dy = dy.data;
+  a.dys = dy.stride;
+  a.x = x.data;
+  a.xs = x.stride;
+  a.gate = gate.data;
+  a.gs = gate.stride;
+  a.y = (void*)dx.data;
+  a.ys = dx.stride;
+  a.dw = dw;
+  a.db = db;
+  if (dtype == DS_ELEM_F32) return backward<float>(ctx, p, a);
+  if (dtype == DS_ELEM_BF16) return backward<__bf16>(ctx, p, a);
+  return backward<_Float16>(ctx, p, a);
+}

@@ -1,0 +1,115 @@
+// What the operators on rows of features share: 16-byte pieces of a row at any alignment, sums over the lanes of a row, and the
+// rows of a group.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "group_range.h"
+
+namespace {
+
+// 16 bytes of a row. `U` is only as aligned as an element: rows of any width, stride and start are read and written in
+// 16-byte accesses (the GPU runs with unaligned access enabled), so that no second form for odd rows is needed.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<float> {
+  static constexpr int N = 4;
+  typedef float V __attribute__((ext_vector_type(4)));
+  typedef float U __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Piece<__bf16> {
+  static constexpr int N = 8;
+  typedef __bf16 V __attribute__((ext_vector_type(8)));
+  typedef __bf16 U __attribute__((ext_vector_type(8), aligned(2)));
+};
+template <>
+struct Piece<_Float16> {
+  static constexpr int N = 8;
+  typedef _Float16 V __attribute__((ext_vector_type(8)));
+  typedef _Float16 U __attribute__((ext_vector_type(8), aligned(2)));
+};
+
+// the first `have` elements from p on, zeros behind them; nothing outside of them is read
+template <typename T>
+__device__ __forceinline__ typename Piece<T>::V load_piece(const T* p, int have) {
+  if (have >= Piece<T>::N) return *reinterpret_cast<const typename Piece<T>::U*>(p);
+  typename Piece<T>::V v = {};
+#pragma unroll
+  for (int i = 0; i < Piece<T>::N - 1; ++i)
+    if (i < have) v[i] = p[i];
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, typename Piece<T>::V v, int have) {
+  if (have >= Piece<T>::N) {
+    *reinterpret_cast<typename Piece<T>::U*>(p) = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < Piece<T>::N - 1; ++i)
+    if (i < have) p[i] = v[i];
+}
+
+template <int CTRL>
+__device__ __forceinline__ float add_across(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over groups of LANES neighbouring lanes, in every lane of the group: exchanges inside the registers, no LDS.
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float v) {
+  if constexpr (LANES >= 2) v = add_across<0xB1>(v);    // lane ^ 1
+  if constexpr (LANES >= 4) v = add_across<0x4E>(v);    // lane ^ 2
+  if constexpr (LANES >= 8) v = add_across<0x141>(v);   // 7 - lane: the other four
+  if constexpr (LANES >= 16) v = add_across<0x140>(v);  // 15 - lane: the other eight
+  if constexpr (LANES >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  if constexpr (LANES >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  return v;
+}
+
+struct GroupTile {
+  int group;            // == groups: rows of no group
+  int begin, end;       // positions in the order
+};
+
+// Tile `tile` of the rows cut into tiles of 2^shift, group by group, the rows of no group last. Called by whole waves, with
+// the same answer in every lane; false behind the last tile.
+__device__ __forceinline__ bool find_group_tile(const int64_t* offsets, int groups, int rows, int shift, int tile, GroupTile* out) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int base = 0; base <= groups; base += 64) {
+    const int g = base + lane;
+    int begin = 0, end = 0;
+    if (g <= groups) ds_group_range(offsets, groups, rows, g, &begin, &end);
+    const int tiles = (int)(((int64_t)(end - begin) + (1 << shift) - 1) >> shift);
+    int upto = tiles;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += up;
+    }
+    const unsigned long long reach = __ballot(before + upto > tile);
+    if (reach) {
+      const int src = __ffsll((long long)reach) - 1;
+      const int first = __shfl(before + upto - tiles, src, 64);
+      const int b = __shfl(begin, src, 64), e = __shfl(end, src, 64);
+      out->group = __builtin_amdgcn_readfirstlane(base + src);
+      out->begin = __builtin_amdgcn_readfirstlane(b + ((tile - first) << shift));
+      out->end = __builtin_amdgcn_readfirstlane(min(e, b + ((tile - first + 1) << shift)));
+      return true;
+    }
+    before += __shfl(upto, 63, 64);
+  }
+  return false;
+}
+
+}  // namespace
