@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libdistshap_hip.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "sampler.hip", "extract.hip", "eval.hip", "eval_zt.hip", "gat_eval.hip", "bitmat.hip", "tiles.hip",
            "gram_chol.hip", "cgls.hip", "fidelity.hip", "plan.cpp", "feature_api.hip", "norm.hip", "dropout.hip", "group.hip",
-           "grouped_mm.hip"]
+           "grouped_mm.hip", "grouped_tiles.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # The one flag list of the shipped code objects (tests that inspect the generated code import it).
 COMPILE_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off",

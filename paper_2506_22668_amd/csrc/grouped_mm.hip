@@ -6,7 +6,9 @@
 // The rows of group g are those at positions offsets[g] .. offsets[g + 1] of `order`. Sizes of groups are known on the GPU
 // alone: the grid has a tile for every one that there can be, and a workgroup finds its rows from the offsets.
 // All products go through the matrix cores, fp32 ones on their fp32 form, and are summed in fp32.
-#include "feature_ops.h"
+#include <type_traits>
+
+#include "grouped_mm.h"
 #include "rows.h"
 
 namespace {
@@ -29,19 +31,6 @@ __device__ __forceinline__ f32x4 multiply(PieceV<float> a, PieceV<float> b, f32x
   for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], d, 0, 0, 0);
   return d;
 }
-
-struct MmArgs {
-  int rows, inner, outer, groups;
-  const void *w, *x, *dy, *gate;
-  int64_t xs, dys, gs, ys;
-  const int64_t* offsets;
-  const int32_t* order;
-  const float* bias;
-  int relu, col_tiles;
-  void* y;            // the product by rows (y, or dx)
-  void* dw;
-  float* db;
-};
 
 constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 
@@ -225,10 +214,9 @@ MmArgs arguments(const ds_grouped& p) {
   return a;
 }
 
-// tiles of 2^shift rows that the groups and the rows of none can have: every group may end inside one
-int64_t most_tiles(const ds_grouped& p, int shift) {
-  const int64_t partial = p.groups + 1 < p.rows ? p.groups + 1 : p.rows;
-  return ((int64_t)p.rows >> shift) + partial;
+template <typename T>
+int element_of() {
+  return sizeof(T) == 4 ? DS_ELEM_F32 : std::is_same<T, __bf16>::value ? DS_ELEM_BF16 : DS_ELEM_F16;
 }
 
 template <typename T, bool TRANSPOSED>
@@ -238,8 +226,9 @@ int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   hipStream_t stream = ctx->stream;
   a.col_tiles = ((TRANSPOSED ? p.inner : p.outer) + 16 * N - 1) / (16 * N);
   const int64_t mean = p.rows / p.groups;
+  if (mean > 64) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
   const int shift = mean <= 16 ? 4 : mean <= 32 ? 5 : 6;
-  const int64_t tiles = most_tiles(p, shift) * a.col_tiles;
+  const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
   if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
   const dim3 grid((unsigned)tiles), block(64 * kWaves);
   if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, TRANSPOSED>), grid, block, 0, stream, a);
