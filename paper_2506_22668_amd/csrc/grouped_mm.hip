@@ -214,6 +214,8 @@ MmArgs arguments(const ds_grouped& p) {
   return a;
 }
 
+bool many_rows(const ds_grouped& p) { return p.rows / p.groups > 64; }
+
 template <typename T>
 int element_of() {
   return sizeof(T) == 4 ? DS_ELEM_F32 : std::is_same<T, __bf16>::value ? DS_ELEM_BF16 : DS_ELEM_F16;
@@ -226,7 +228,7 @@ int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   hipStream_t stream = ctx->stream;
   a.col_tiles = ((TRANSPOSED ? p.inner : p.outer) + 16 * N - 1) / (16 * N);
   const int64_t mean = p.rows / p.groups;
-  if (mean > 64) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
+  if (many_rows(p)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
   const int shift = mean <= 16 ? 4 : mean <= 32 ? 5 : 6;
   const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
   if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
@@ -249,8 +251,9 @@ int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
 }
 
 template <typename T>
-int backward(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
+int backward(ds_ctx* ctx, const ds_grouped& p, MmArgs& a, void* workspace) {
   DS_TRY((launch_rows<T, true>(ctx, p, a)));
+  if (many_rows(p)) return ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
   return launch_weights<T>(ctx, p, a);
 }
 
@@ -271,14 +274,11 @@ int ds_launch_grouped_mm(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows x,
 }
 
 int64_t ds_grouped_mm_backward_bytes(int dtype, const ds_grouped& p) {
-  (void)dtype;
-  (void)p;
-  return 0;
+  return many_rows(p) ? ds_weight_tiles_bytes(dtype) : 0;
 }
 
 int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, ds_rows x, ds_rows gate, ds_rows dx,
                                   void* dw, float* db, void* workspace) {
-  (void)workspace;
   MmArgs a = arguments(p);
   a.dy = dy.data;
   a.dys = dy.stride;
@@ -290,7 +290,7 @@ int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, d
   a.ys = dx.stride;
   a.dw = dw;
   a.db = db;
-  if (dtype == DS_ELEM_F32) return backward<float>(ctx, p, a);
-  if (dtype == DS_ELEM_BF16) return backward<__bf16>(ctx, p, a);
-  return backward<_Float16>(ctx, p, a);
+  if (dtype == DS_ELEM_F32) return backward<float>(ctx, p, a, workspace);
+  if (dtype == DS_ELEM_BF16) return backward<__bf16>(ctx, p, a, workspace);
+  return backward<_Float16>(ctx, p, a, workspace);
 }

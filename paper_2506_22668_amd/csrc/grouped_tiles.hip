@@ -1,5 +1,6 @@
 // Products of rows with the weights of their group where a group has many rows: tiles through LDS.
 #include "grouped_mm.h"
+#include "mm_split.h"
 #include "rows.h"
 
 namespace {
@@ -253,6 +254,277 @@ int launch_one(ds_ctx* ctx, MmArgs& a) {
 
 bool sixteen(const void* p, int64_t stride, size_t element) { return (uintptr_t)p % 16 == 0 && stride * element % 16 == 0; }
 
+// ---- the gradient of the weights ------------------------------------------------------------------------------------------------
+// dW_g = sum_r x[r]^T dy[r]: both operands run across the contraction, which is the group's rows. Groups are ragged and there are about
+// as many tiles as compute units, so the steps of all tiles of all groups lie in one line (group by group, tile by tile) that is cut
+// evenly, a stretch to a workgroup. Where a cut falls inside a tile, the workgroups on both sides leave fp32 sums (at most two a
+// workgroup), which a second launch adds up in order: no atomics, the same bits every time.
+// the steps of a group's contraction
+__device__ __forceinline__ int group_steps(const MmArgs& a, int g, int depth, int* begin, int* end) {
+  ds_group_range(a.offsets, a.groups, a.rows, g, begin, end);
+  return (*end - *begin + depth - 1) / depth;
+}
+
+// Steps of all groups (each tile's), and where unit `unit` of the line falls: its group (-1: behind the end) and the steps before it
+// there, of all tiles. Called by whole waves, the same answer in every lane.
+__device__ __forceinline__ int64_t locate_unit(const MmArgs& a, int depth, int tiles, int64_t unit, int* group, int64_t* within) {
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  *group = -1;
+  for (int base = 0; base < a.groups; base += 64) {
+    int begin, end;
+    const int g = base + lane;
+    const int64_t own = g < a.groups ? (int64_t)group_steps(a, g, depth, &begin, &end) * tiles : 0;
+    int64_t upto = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t up = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += up;
+    }
+    const unsigned long long reach = __ballot(before + upto > unit);
+    if (reach && *group < 0) {
+      const int src = __ffsll((long long)reach) - 1;
+      *group = __builtin_amdgcn_readfirstlane(base + src);
+      *within = unit - __shfl(before + upto - own, src, 64);
+    }
+    before += __shfl(upto, 63, 64);
+  }
+  return before;
+}
+
+template <typename T, int BR, int BN, int WR, int WN, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial) {
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
+  constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLICES = DEPTH / (2 * N), SLOT = BR * BN + BN;
+  using XOp = Operand<T, BR, true>;
+  using DOp = Operand<T, BN, true>;
+  constexpr int STAGE = XOp::BYTES + DOp::BYTES;
+  constexpr int PARTS = THREADS / BN, EACH = DEPTH / PARTS;   // of the sums for db: threads to a column, steps of each
+  __shared__ __attribute__((aligned(128))) char even[STAGE], odd[STAGE];
+  __shared__ float sums[PARTS][BN];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wr = (wave / WN) * (BR / WR), wn = (wave % WN) * (BN / WN);
+  const int tiles = (a.inner + BR - 1) / BR * a.col_tiles;
+  int group;
+  int64_t within, dummy;
+  int none;
+  const int64_t units = locate_unit(a, DEPTH, tiles, 0, &none, &dummy);
+  const int64_t wgs = units < (int64_t)gridDim.x ? units : (int64_t)gridDim.x;   // (none without a unit: the join reads all that there are)
+  if ((int64_t)blockIdx.x >= wgs) return;
+  int64_t unit = ds_mm_even_begin(blockIdx.x, wgs, units);
+  const int64_t last = ds_mm_even_begin(blockIdx.x + 1, wgs, units);
+  locate_unit(a, DEPTH, tiles, unit, &group, &within);
+  const T *x = (const T*)a.x, *dy = (const T*)a.dy;
+  const Reader<T, BR, true, false> rx(lane);
+  const Reader<T, BN, true, true> rd(lane);
+  while (unit < last && group < a.groups) {
+    int begin, end;
+    const int steps = group_steps(a, group, DEPTH, &begin, &end);
+    if (within >= (int64_t)steps * tiles) {   // on to the next group
+      ++group;
+      within = 0;
+      continue;
+    }
+    const int tile = (int)(within / steps), first = (int)(within % steps);
+    const int upto = last - unit < steps - first ? first + (int)(last - unit) : steps;
+    const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
+    f32x16 acc[NR][NN] = {};
+    float sum = 0.f;
+    Loader<T, BR, true, THREADS, DIRECT> lx;
+    Loader<T, BN, true, THREADS, DIRECT> ld;
+    static_assert(BR == BN, "both operands' pieces of a thread lie in the same rows");
+    int row[lx.PIECES];
+#pragma unroll
+    for (int u = 0; u < lx.PIECES; ++u) {
+      const int n = u * THREADS + (int)threadIdx.x;
+      lx.from[u] = x + in0 + XOp::piece(n) * N;
+      lx.limit[u] = a.inner - in0 - XOp::piece(n) * N;
+      ld.from[u] = dy + col0 + DOp::piece(n) * N;
+      ld.limit[u] = a.outer - col0 - DOp::piece(n) * N;
+    }
+    const auto find_rows = [&](int s) {
+#pragma unroll
+      for (int u = 0; u < lx.PIECES; ++u) {
+        const int pos = begin + s * DEPTH + XOp::line(u * THREADS + (int)threadIdx.x);
+        row[u] = s < upto && pos < end ? ds_ordered_row(a.order, a.rows, pos) : -1;
+      }
+    };
+    const auto fetch = [&](char* stage) {
+#pragma unroll
+      for (int u = 0; u < ld.PIECES; ++u) ld.fetch(u, ld.from[u] + row[u] * a.dys, row[u] < 0 ? 0 : ld.limit[u], stage);
+#pragma unroll
+      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, lx.from[u] + row[u] * a.xs, row[u] < 0 ? 0 : lx.limit[u], stage + DOp::BYTES);
+    };
+    const auto step = [&](int s, char* now, char* then) {
+      __syncthreads();
+      if (s + 1 < upto) {
+        fetch(then);
+        find_rows(s + 2);
+      }
+#pragma unroll
+      for (int c = 0; c < SLICES; ++c) {
+        PieceV<T> fx[NR], fd[NN];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) fx[r] = rx.read(now + DOp::BYTES, wr + r * 32, c);
+#pragma unroll
+        for (int n = 0; n < NN; ++n) fd[n] = rd.read(now, wn + n * 32, c);
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fd[n], fx[r], acc[r][n]);
+      }
+      if (in0 == 0) {   // db: the column sums of what is in LDS anyway
+        const int col = (int)threadIdx.x % BN, part = (int)threadIdx.x / BN;
+        float v = 0.f;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+          const int line = part * EACH + k;
+          const int p = sizeof(T) == 2 ? (col / N) ^ ((line & 3) << 2) : col / N;
+          v += (float)*reinterpret_cast<const T*>(now + line * (BN * (int)sizeof(T)) + p * 16 + col % N * (int)sizeof(T));
+        }
+        sum += v;
+      }
+      if (s + 1 < upto) {
+        ld.store(then);
+        lx.store(then + DOp::BYTES);
+      }
+    };
+    __syncthreads();   // (the last tile's readers are through)
+    find_rows(first);
+    fetch(even);
+    find_rows(first + 1);
+    ld.store(even);
+    lx.store(even + DOp::BYTES);
+    for (int s = first; s < upto; s += 2) {
+      step(s, even, odd);
+      if (s + 1 < upto) step(s + 1, odd, even);
+    }
+    if (in0 == 0) {
+      sums[threadIdx.x / BN][threadIdx.x % BN] = sum;
+      __syncthreads();
+      if (threadIdx.x < BN) {
+        sum = 0.f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) sum += sums[p][threadIdx.x];
+      }
+    }
+    if (first == 0 && upto == steps) {
+      T* dw = (T*)a.dw + (int64_t)group * a.inner * a.outer;
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const int in = in0 + wr + r * 32 + (lane & 31);
+#pragma unroll
+        for (int n = 0; n < NN; ++n)
+#pragma unroll
+          for (int p = 0; p < 16 / N; ++p) {
+            const int c = col0 + wn + n * 32 + 16 * (lane >> 5) + p * N;
+            if (in < a.inner && c < a.outer) {
+              PieceV<T> out;
+#pragma unroll
+              for (int i = 0; i < N; ++i) out[i] = (T)acc[r][n][p * N + i];
+              store_piece<T>(dw + (int64_t)in * a.outer + c, out, a.outer - c);
+            }
+          }
+      }
+      if (in0 == 0 && threadIdx.x < BN && col0 + (int)threadIdx.x < a.outer) a.db[(int64_t)group * a.outer + col0 + threadIdx.x] = sum;
+    } else {
+      // slot 0: the tile began with an earlier workgroup; 1: it begins here and a later one goes on
+      float* to = partial + ((int64_t)blockIdx.x * 2 + (first == 0)) * SLOT;
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int n = 0; n < NN; ++n)
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const float4 v = {acc[r][n][4 * p], acc[r][n][4 * p + 1], acc[r][n][4 * p + 2], acc[r][n][4 * p + 3]};
+            reinterpret_cast<float4*>(to)[((r * NN + n) * 4 + p) * THREADS + threadIdx.x] = v;
+          }
+      if (in0 == 0 && threadIdx.x < BN) to[BR * BN + threadIdx.x] = sum;
+    }
+    unit += upto - first;
+    within += upto - first;
+  }
+}
+
+// Adds up the sums of tiles that were cut, and clears the gradients of empty groups: a workgroup to a tile and 32 x 32 block of each wave
+template <typename T, int BR, int BN, int WR, int WN>
+__global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, const float* partial, int wgs) {
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
+  constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wr = (wave / WN) * (BR / WR), wn = (wave % WN) * (BN / WN);
+  const int tiles = (a.inner + BR - 1) / BR * a.col_tiles;
+  const int group = (int)blockIdx.y, tile = (int)blockIdx.x / (NR * NN), block = (int)blockIdx.x % (NR * NN), r = block / NN, n = block % NN;
+  const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
+  int begin, end;
+  const int steps = group_steps(a, group, DEPTH, &begin, &end);
+  int64_t first = 0, last = -1, from = 0;
+  if (steps > 0) {
+    // where the tile's steps lie in the line: those of the groups before it first
+    int64_t mine = 0, all = 0;
+    for (int g = lane; g < a.groups; g += 64) {
+      int b, e;
+      const int64_t own = (int64_t)group_steps(a, g, DEPTH, &b, &e) * tiles;
+      all += own;
+      if (g < group) mine += own;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      all += __shfl_xor(all, o, 64);
+      mine += __shfl_xor(mine, o, 64);
+    }
+    from = mine + (int64_t)tile * steps;
+    const int64_t shares = all < wgs ? all : wgs;
+    first = ds_mm_even_owner(from, shares, all);
+    last = ds_mm_even_owner(from + steps - 1, shares, all);
+    if (first == last) return;
+  }
+  f32x16 v = {};
+  float sum = 0.f;
+  const bool with_sum = in0 == 0 && block == 0 && threadIdx.x < BN;
+  for (int64_t b = first; b <= last; ++b) {
+    const float* p = partial + (b * 2 + (b == first)) * SLOT;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 f = reinterpret_cast<const float4*>(p)[(block * 4 + q) * THREADS + threadIdx.x];
+      v[4 * q] += f.x;
+      v[4 * q + 1] += f.y;
+      v[4 * q + 2] += f.z;
+      v[4 * q + 3] += f.w;
+    }
+    if (with_sum) sum += p[BR * BN + threadIdx.x];
+  }
+  T* dw = (T*)a.dw + (int64_t)group * a.inner * a.outer;
+  const int in = in0 + wr + r * 32 + (lane & 31);
+#pragma unroll
+  for (int p = 0; p < 16 / N; ++p) {
+    const int c = col0 + wn + n * 32 + 16 * (lane >> 5) + p * N;
+    if (in < a.inner && c < a.outer) {
+      PieceV<T> out;
+#pragma unroll
+      for (int i = 0; i < N; ++i) out[i] = (T)v[p * N + i];
+      store_piece<T>(dw + (int64_t)in * a.outer + c, out, a.outer - c);
+    }
+  }
+  if (with_sum && col0 + (int)threadIdx.x < a.outer) a.db[(int64_t)group * a.outer + col0 + threadIdx.x] = sum;
+}
+
+constexpr int kWeightGroups = 256;   // workgroups of the even cut
+
+template <typename T, int BR, int BN, int WR, int WN>
+int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
+  a.col_tiles = (a.outer + BN - 1) / BN;
+  const int64_t blocks = (int64_t)((a.inner + BR - 1) / BR) * a.col_tiles * (BR / WR / 32) * (BN / WN / 32);
+  if (blocks > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
+  const bool direct = sixteen(a.x, a.xs, sizeof(T)) && sixteen(a.dy, a.dys, sizeof(T)) && a.inner % Piece<T>::N == 0 && a.outer % Piece<T>::N == 0;
+  const dim3 block(64 * WR * WN);
+  if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true>), dim3(kWeightGroups), block, 0, ctx->stream, a, partial);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, false>), dim3(kWeightGroups), block, 0, ctx->stream, a, partial);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_join_kernel<T, BR, BN, WR, WN>), dim3((unsigned)blocks, a.groups), block, 0, ctx->stream, a, partial, kWeightGroups);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED>
 int launch(ds_ctx* ctx, MmArgs& a) {
   const void* x = TRANSPOSED ? a.dy : a.x;
@@ -267,4 +539,15 @@ int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a) {
   if (dtype == DS_ELEM_F32) return transposed ? launch<float, 128, 128, 2, 2, true>(ctx, a) : launch<float, 128, 128, 2, 2, false>(ctx, a);
   if (dtype == DS_ELEM_BF16) return transposed ? launch<__bf16, 256, 256, 2, 4, true>(ctx, a) : launch<__bf16, 256, 256, 2, 4, false>(ctx, a);
   return transposed ? launch<_Float16, 256, 256, 2, 4, true>(ctx, a) : launch<_Float16, 256, 256, 2, 4, false>(ctx, a);
+}
+
+int64_t ds_weight_tiles_bytes(int dtype) {
+  const int64_t side = dtype == DS_ELEM_F32 ? 128 : 256;
+  return kWeightGroups * 2 * (side * side + side) * (int64_t)sizeof(float);
+}
+
+int ds_launch_weight_tiles(ds_ctx* ctx, int dtype, MmArgs& a, void* partial) {
+  if (dtype == DS_ELEM_F32) return launch_weights<float, 128, 128, 2, 2>(ctx, a, (float*)partial);
+  if (dtype == DS_ELEM_BF16) return launch_weights<__bf16, 256, 256, 2, 4>(ctx, a, (float*)partial);
+  return launch_weights<_Float16, 256, 256, 2, 4>(ctx, a, (float*)partial);
 }
