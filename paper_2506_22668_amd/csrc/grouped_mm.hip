@@ -48,8 +48,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
   const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N;
-  GroupTile gt;
-  if (!find_group_tile(a.offsets, a.groups, a.rows, SHIFT, tile, &gt)) return;
+  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT);
+  if (tile >= all.count()) return;
+  const GroupTile gt = all.find(tile);
   int row[RB];
 #pragma unroll
   for (int r = 0; r < RB; ++r) row[r] = gt.begin + 16 * r + m < gt.end ? ds_ordered_row(a.order, a.rows, gt.begin + 16 * r + m) : -1;

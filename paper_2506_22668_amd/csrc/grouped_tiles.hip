@@ -85,21 +85,14 @@ struct Reader {
   }
 };
 
-// Brings a step of an operand into LDS: piece u of thread t is piece number u * threads + t of the tile.
-template <typename T, int COLS, bool ACROSS, int THREADS, bool DIRECT>
+// Brings pieces of an operand into LDS: piece u of thread t is piece number u * THREADS + t of the tile. Direct loads go there by
+// themselves; rows that are not aligned for them come through registers.
+template <typename T, int COLS, int THREADS, bool DIRECT>
 struct Loader {
-  using Op = Operand<T, COLS, ACROSS>;
-  static constexpr int N = Op::N, PIECES = Op::BYTES / 16 / THREADS;
-  const T* from[PIECES];   // of the thread's pieces, at step 0
-  int limit[PIECES];       // not ACROSS: the contraction's end, as seen from the piece, or 0 (no such column); ACROSS: elements from the piece's column on
+  static constexpr int N = Piece<T>::N, PIECES = COLS * kDepthBytes / 16 / THREADS;
   PieceV<T> held[DIRECT ? 1 : PIECES];
 
-  __device__ __forceinline__ void store(char* tile) {
-    if constexpr (!DIRECT) {
-#pragma unroll
-      for (int u = 0; u < PIECES; ++u) *reinterpret_cast<PieceV<T>*>(tile + (u * THREADS + (int)threadIdx.x) * 16) = held[u];
-    }
-  }
+  // have: elements that there are from p on (zeros behind them)
   __device__ __forceinline__ void fetch(int u, const T* p, int have, char* tile) {
     if constexpr (DIRECT) {
       const T* src = have > 0 ? p : reinterpret_cast<const T*>(&kZeros);
@@ -109,145 +102,208 @@ struct Loader {
       held[u] = load_piece<T>(p, have);
     }
   }
+  __device__ __forceinline__ void store(char* tile) {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int u = 0; u < PIECES; ++u) *reinterpret_cast<PieceV<T>*>(tile + (u * THREADS + (int)threadIdx.x) * 16) = held[u];
+    }
+  }
 };
 
+// Workgroups stay: one to a compute unit, which goes through tiles of BR rows and BN columns. A step of the contraction (128 bytes of
+// every row) is computed on from one half of the LDS while the next but one comes into the other; a wave's operands for a slice of the
+// step are read while the matrix cores work on the slice before.
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
-  constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLICES = DEPTH / (2 * N);
+  constexpr int TR = BR / WR, TN = BN / WN, NR = TR / 32, NN = TN / 32, SLICES = DEPTH / (2 * N);
   constexpr int SHIFT = BR == 256 ? 8 : BR == 128 ? 7 : 6;
   using XOp = Operand<T, BR, false>;
   using WOp = Operand<T, BN, !TRANSPOSED>;
   constexpr int STAGE = XOp::BYTES + WOp::BYTES;
+  // results on their way out: a wave's rows, PASS blocks of 32 at a time, lie in `odd`
+  constexpr int OUT_ROW = TN * (int)sizeof(T), PASS = STAGE / (WR * WN) / (32 * OUT_ROW) < NR ? STAGE / (WR * WN) / (32 * OUT_ROW) : NR;
+  constexpr int CHUNKS = OUT_ROW / 16, ROWS_AT_ONCE = 64 / CHUNKS;
   // (two arrays, not halves of one: only then does the compiler know that what is read of one does not wait for what comes into the other)
   __shared__ __attribute__((aligned(128))) char even[STAGE], odd[STAGE];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wr = (wave / WN) * (BR / WR), wn = (wave % WN) * (BN / WN);
+  __shared__ int row_of[2][BR];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = (wave / WN) * TR, wn = (wave % WN) * TN;
   const int width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
-  // Workgroups go to the eight XCDs in turn: each XCD takes a stretch of the tiles, so that the column tiles of a row tile share an L2
-  const int per = (int)gridDim.x >> 3;
-  const int at = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
-  const int tile = at / a.col_tiles, col0 = at % a.col_tiles * BN;
+  const T* x = (const T*)(TRANSPOSED ? a.dy : a.x);
+  const int64_t xs = TRANSPOSED ? a.dys : a.xs;
+  const T* gate = (const T*)a.gate;
+  T* y = (T*)a.y;
+  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT);
+  // Workgroups go to the eight XCDs in turn. Each XCD has a stretch of the tiles, column tiles of a row tile next to each other, so that they
+  // share its L2; its workgroups take them in turn.
+  const int64_t tiles = (int64_t)all.count() * a.col_tiles;
+  const int xcd = (int)blockIdx.x & 7, step_by = (int)gridDim.x >> 3;
+  const int64_t stretch = tiles * (xcd + 1) / 8;
+  int64_t at = tiles * xcd / 8 + ((int)blockIdx.x >> 3);
+
+  Loader<T, BR, THREADS, DIRECT> lx;
+  Loader<T, BN, THREADS, DIRECT> lw;
+  const Reader<T, BR, false, false> rx(lane);
+  const Reader<T, BN, !TRANSPOSED, true> rw(lane);
+  const int steps = (depth + DEPTH - 1) / DEPTH;
+  // A thread's pieces of a step lie in one place of lines that are a fixed number apart (the exchange of pieces goes by the last bits
+  // of a line, which that number leaves alone)
+  constexpr int XLINES = THREADS / XOp::PER_ROW, WLINES = THREADS / WOp::PER_ROW;
+  static_assert(XLINES % 8 == 0 && WLINES % 8 == 0, "");
+  const int xk = XOp::piece((int)threadIdx.x) * N, wline = WOp::line((int)threadIdx.x), wplace = WOp::piece((int)threadIdx.x) * N;
+  const T *from_x[lx.PIECES], *from_w;
   GroupTile gt;
-  if (!find_group_tile(a.offsets, a.groups, a.rows, SHIFT, tile, &gt)) return;
-  int row[NR];
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const int pos = gt.begin + wr + r * 32 + (lane & 31);
-    row[r] = pos < gt.end ? ds_ordered_row(a.order, a.rows, pos) : -1;
-  }
-  f32x16 acc[NR][NN] = {};
-  if (gt.group < a.groups) {
-    const T* x = (const T*)(TRANSPOSED ? a.dy : a.x);
-    const int64_t xs = TRANSPOSED ? a.dys : a.xs;
-    const T* w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer;
-    Loader<T, BR, false, THREADS, DIRECT> lx;
-    Loader<T, BN, !TRANSPOSED, THREADS, DIRECT> lw;
-#pragma unroll
-    for (int u = 0; u < lx.PIECES; ++u) {
-      const int n = u * THREADS + (int)threadIdx.x, pos = gt.begin + XOp::line(n), k = XOp::piece(n) * N;
-      const int r = pos < gt.end ? ds_ordered_row(a.order, a.rows, pos) : -1;
-      lx.from[u] = x + (r < 0 ? 0 : r) * xs + k;
-      lx.limit[u] = r < 0 ? 0 : depth - k;
-    }
+  int col0, turn = 0;
+  const auto fetch = [&](int s, char* stage) {
+    const int k = s * DEPTH;
 #pragma unroll
     for (int u = 0; u < lw.PIECES; ++u) {
-      const int n = u * THREADS + (int)threadIdx.x;
-      if constexpr (TRANSPOSED) {
-        const int col = col0 + WOp::line(n), k = WOp::piece(n) * N;
-        lw.from[u] = w + (int64_t)col * a.outer + k;
-        lw.limit[u] = col < width ? depth - k : 0;
-      } else {
-        const int col = col0 + WOp::piece(n) * N;
-        lw.from[u] = w + (int64_t)WOp::line(n) * a.outer + col;
-        lw.limit[u] = width - col;
-      }
+      const int line = u * WLINES + wline;
+      if constexpr (TRANSPOSED) lw.fetch(u, from_w + (int64_t)(u * WLINES) * a.outer + k, col0 + line < width ? depth - k - wplace : 0, stage);
+      else lw.fetch(u, from_w + (int64_t)(k + u * WLINES) * a.outer, k + line < depth ? width - col0 - wplace : 0, stage);
     }
-    const auto fetch = [&](int k, char* stage) {
 #pragma unroll
-      for (int u = 0; u < lw.PIECES; ++u) {
-        if constexpr (TRANSPOSED) {
-          lw.fetch(u, lw.from[u] + k, lw.limit[u] - k, stage);
-        } else {
-          const int line = WOp::line(u * THREADS + (int)threadIdx.x);
-          lw.fetch(u, lw.from[u] + (int64_t)k * a.outer, k + line < depth ? lw.limit[u] : 0, stage);
-        }
-      }
+    for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x[u] + k, depth - k - xk, stage + WOp::BYTES);
+  };
+  const auto put = [&](char* stage) {
+    lw.store(stage);
+    lx.store(stage + WOp::BYTES);
+  };
+  // what a thread brings of tile `at`, and its first step
+  const auto start = [&]() {
+    gt = all.find((int)(at / a.col_tiles));
+    col0 = (int)(at % a.col_tiles) * BN;
+    turn ^= 1;
+    if (threadIdx.x < BR) {
+      const int pos = gt.begin + (int)threadIdx.x;
+      row_of[turn][threadIdx.x] = pos < gt.end ? ds_ordered_row(a.order, a.rows, pos) : -1;
+    }
+    if (gt.group == a.groups) return;
 #pragma unroll
-      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, lx.from[u] + k, lx.limit[u] - k, stage + WOp::BYTES);
-    };
-    const Reader<T, BR, false, false> rx(lane);
-    const Reader<T, BN, !TRANSPOSED, true> rw(lane);
-    const auto compute = [&](const char* stage) {
+    for (int u = 0; u < lx.PIECES; ++u) {
+      const int pos = gt.begin + u * XLINES + XOp::line((int)threadIdx.x);
+      const int r = pos < gt.end ? ds_ordered_row(a.order, a.rows, pos) : 0;
+      from_x[u] = x + (r < 0 ? 0 : r) * xs + xk;   // (no row: any row, whose results go nowhere)
+    }
+    from_w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer +
+             (TRANSPOSED ? (int64_t)(col0 + wline) * a.outer + wplace : (int64_t)wline * a.outer + col0 + wplace);
+    fetch(0, even);
+    put(even);
+  };
+
+  if (at >= stretch) return;
+  start();
+  while (true) {
+    f32x16 acc[NR][NN] = {};
+    if (gt.group < a.groups) {
+      PieceV<T> fx[2][NR], fw[2][NN];
+      const auto read = [&](const char* stage, int c) {
 #pragma unroll
-      for (int s = 0; s < SLICES; ++s) {
-        PieceV<T> fx[NR], fw[NN];
+        for (int n = 0; n < NN; ++n) fw[c & 1][n] = rw.read(stage, wn + n * 32, c);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) fx[r] = rx.read(stage + WOp::BYTES, wr + r * 32, s);
-#pragma unroll
-        for (int n = 0; n < NN; ++n) fw[n] = rw.read(stage, wn + n * 32, s);
+        for (int r = 0; r < NR; ++r) fx[c & 1][r] = rx.read(stage + WOp::BYTES, wr + r * 32, c);
+      };
+      const auto work = [&](int c) {
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fw[n], fx[r], acc[r][n]);
-      }
-    };
-    const int steps = (depth + DEPTH - 1) / DEPTH;
-    const auto step = [&](int s, char* now, char* then) {
-      __syncthreads();
-      if (s + 1 < steps) fetch((s + 1) * DEPTH, then);
-      compute(now);
-      if (s + 1 < steps) {
-        lw.store(then);
-        lx.store(then + WOp::BYTES);
-      }
-    };
-    fetch(0, even);
-    lw.store(even);
-    lx.store(even + WOp::BYTES);
-    for (int s = 0; s < steps; s += 2) {
-      step(s, even, odd);
-      if (s + 1 < steps) step(s + 1, odd, even);
-    }
-  }
-  const T* gate = (const T*)a.gate;
-  T* y = (T*)a.y;
+          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fw[c & 1][n], fx[c & 1][r], acc[r][n]);
+      };
+      const auto step = [&](int s, char* now, char* then) {
 #pragma unroll
-  for (int n = 0; n < NN; ++n) {
-    const int col = col0 + wn + n * 32 + 16 * (lane >> 5);
-    float bias[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) bias[i] = a.bias && gt.group < a.groups && col + i < width ? a.bias[(int64_t)gt.group * width + col + i] : 0.f;
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      if (row[r] < 0) continue;
-#pragma unroll
-      for (int p = 0; p < 16 / N; ++p) {
-        const int c = col + p * N;
-        if (c >= width) continue;
-        const PieceV<T> open = gate ? load_piece<T>(gate + row[r] * a.gs + c, width - c) : PieceV<T>{};
-        PieceV<T> out;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          float v = acc[r][n][p * N + i] + bias[p * N + i];
-          if (a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
-          if (gate) v = (float)open[i] > 0.f ? v : 0.f;
-          out[i] = (T)v;
+        for (int c = 0; c + 1 < SLICES; ++c) {
+          read(now, c + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          work(c);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        store_piece<T>(y + row[r] * a.ys + c, out, width - c);
+        __syncthreads();   // step s + 1 is there, and nobody reads step s any more
+        if (s + 2 < steps) {
+          put(now);
+          fetch(DIRECT ? s + 2 : s + 3, now);
+        }
+        if (s + 1 < steps) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int n = 0; n < NN; ++n) fw[0][n] = rw.read(then, wn + n * 32, 0);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) fx[0][r] = rx.read(then + WOp::BYTES, wr + r * 32, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        work(SLICES - 1);
+      };
+      static_assert(SLICES % 2 == 0, "");
+      if (steps > 1) {
+        fetch(1, odd);
+        put(odd);
+        if (!DIRECT) fetch(2, even);
+      }
+      __syncthreads();
+      read(even, 0);
+      for (int s = 0; s < steps; s += 2) {
+        step(s, even, odd);
+        if (s + 1 < steps) step(s + 1, odd, even);
       }
     }
+    // the next tile's first step comes in while this one's results go out
+    const GroupTile done = gt;
+    const int col = col0 + wn, ids = turn;
+    at += step_by;
+    const bool more = at < stretch;
+    __syncthreads();
+    if (more) start();
+    char* mine = odd + wave * (STAGE / (WR * WN));
+#pragma unroll
+    for (int r0 = 0; r0 < NR; r0 += PASS) {
+#pragma unroll
+      for (int n = 0; n < NN; ++n) {
+        const int c = col + n * 32 + 16 * (lane >> 5);
+        float bias[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          bias[i] = a.bias && done.group < a.groups && c + i < width ? a.bias[(int64_t)done.group * width + c + i] : 0.f;
+#pragma unroll
+        for (int r = 0; r < PASS; ++r)
+#pragma unroll
+          for (int p = 0; p < 16 / N; ++p) {
+            PieceV<T> out;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              float v = acc[r0 + r][n][p * N + i] + bias[p * N + i];
+              if (a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
+              out[i] = (T)v;
+            }
+            const int line = r * 32 + (lane & 31), chunk = (n * 32 + 16 * (lane >> 5)) / N + p;
+            *reinterpret_cast<PieceV<T>*>(mine + line * OUT_ROW + ((chunk ^ (line & 7)) << 4)) = out;
+          }
+      }
+      // (a wave reads what it wrote itself: its LDS accesses keep their order)
+#pragma unroll
+      for (int i = 0; i < PASS * 32 / ROWS_AT_ONCE; ++i) {
+        const int line = i * ROWS_AT_ONCE + lane / CHUNKS, chunk = lane % CHUNKS, c = col + chunk * N;
+        const int row = row_of[ids][wr + r0 * 32 + line];
+        PieceV<T> out = *reinterpret_cast<const PieceV<T>*>(mine + line * OUT_ROW + ((chunk ^ (line & 7)) << 4));
+        if (row >= 0 && c < width) {
+          if (gate) {
+            const PieceV<T> open = load_piece<T>(gate + row * a.gs + c, width - c);
+#pragma unroll
+            for (int j = 0; j < N; ++j) out[j] = (float)open[j] > 0.f ? out[j] : (T)0.f;
+          }
+          store_piece<T>(y + row * a.ys + c, out, width - c);
+        }
+      }
+    }
+    if (!more) return;
+    __syncthreads();
   }
 }
 
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED, bool DIRECT>
 int launch_one(ds_ctx* ctx, MmArgs& a) {
-  constexpr int SHIFT = BR == 256 ? 8 : BR == 128 ? 7 : 6;
   a.col_tiles = ((TRANSPOSED ? a.inner : a.outer) + BN - 1) / BN;
-  const int64_t tiles = (ds_most_tiles(a, SHIFT) * a.col_tiles + 7) / 8 * 8;
-  if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", a.rows, TRANSPOSED ? a.inner : a.outer);
-  const auto kernel = row_tiles_kernel<T, BR, BN, WR, WN, TRANSPOSED, DIRECT>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(64 * WR * WN), 0, ctx->stream, a);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(row_tiles_kernel<T, BR, BN, WR, WN, TRANSPOSED, DIRECT>), dim3((unsigned)(ctx->num_cus + 7) / 8 * 8),
+                     dim3(64 * WR * WN), 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -330,30 +386,25 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
     const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
     f32x16 acc[NR][NN] = {};
     float sum = 0.f;
-    Loader<T, BR, true, THREADS, DIRECT> lx;
-    Loader<T, BN, true, THREADS, DIRECT> ld;
-    static_assert(BR == BN, "both operands' pieces of a thread lie in the same rows");
+    Loader<T, BR, THREADS, DIRECT> lx;
+    Loader<T, BN, THREADS, DIRECT> ld;
+    constexpr int LINES = THREADS / XOp::PER_ROW;   // (as in row_tiles_kernel)
+    static_assert(BR == BN && LINES % 4 == 0, "both operands' pieces of a thread lie in the same rows");
     int row[lx.PIECES];
-#pragma unroll
-    for (int u = 0; u < lx.PIECES; ++u) {
-      const int n = u * THREADS + (int)threadIdx.x;
-      lx.from[u] = x + in0 + XOp::piece(n) * N;
-      lx.limit[u] = a.inner - in0 - XOp::piece(n) * N;
-      ld.from[u] = dy + col0 + DOp::piece(n) * N;
-      ld.limit[u] = a.outer - col0 - DOp::piece(n) * N;
-    }
+    const int line = XOp::line((int)threadIdx.x), place = XOp::piece((int)threadIdx.x) * N;
+    const T *from_x = x + in0 + place, *from_dy = dy + col0 + place;
     const auto find_rows = [&](int s) {
 #pragma unroll
       for (int u = 0; u < lx.PIECES; ++u) {
-        const int pos = begin + s * DEPTH + XOp::line(u * THREADS + (int)threadIdx.x);
+        const int pos = begin + s * DEPTH + u * LINES + line;
         row[u] = s < upto && pos < end ? ds_ordered_row(a.order, a.rows, pos) : -1;
       }
     };
     const auto fetch = [&](char* stage) {
 #pragma unroll
-      for (int u = 0; u < ld.PIECES; ++u) ld.fetch(u, ld.from[u] + row[u] * a.dys, row[u] < 0 ? 0 : ld.limit[u], stage);
+      for (int u = 0; u < ld.PIECES; ++u) ld.fetch(u, from_dy + row[u] * a.dys, row[u] < 0 ? 0 : a.outer - col0 - place, stage);
 #pragma unroll
-      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, lx.from[u] + row[u] * a.xs, row[u] < 0 ? 0 : lx.limit[u], stage + DOp::BYTES);
+      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x + row[u] * a.xs, row[u] < 0 ? 0 : a.inner - in0 - place, stage + DOp::BYTES);
     };
     const auto step = [&](int s, char* now, char* then) {
       __syncthreads();
@@ -378,9 +429,9 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
         float v = 0.f;
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
-          const int line = part * EACH + k;
-          const int p = sizeof(T) == 2 ? (col / N) ^ ((line & 3) << 2) : col / N;
-          v += (float)*reinterpret_cast<const T*>(now + line * (BN * (int)sizeof(T)) + p * 16 + col % N * (int)sizeof(T));
+          const int at = part * EACH + k;
+          const int p = sizeof(T) == 2 ? (col / N) ^ ((at & 3) << 2) : col / N;
+          v += (float)*reinterpret_cast<const T*>(now + at * (BN * (int)sizeof(T)) + p * 16 + col % N * (int)sizeof(T));
         }
         sum += v;
       }

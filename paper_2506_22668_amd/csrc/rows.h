@@ -81,35 +81,56 @@ struct GroupTile {
   int begin, end;       // positions in the order
 };
 
-// Tile `tile` of the rows cut into tiles of 2^shift, group by group, the rows of no group last. Called by whole waves, with
-// the same answer in every lane; false behind the last tile.
-__device__ __forceinline__ bool find_group_tile(const int64_t* offsets, int groups, int rows, int shift, int tile, GroupTile* out) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int base = 0; base <= groups; base += 64) {
-    const int g = base + lane;
-    int begin = 0, end = 0;
-    if (g <= groups) ds_group_range(offsets, groups, rows, g, &begin, &end);
-    const int tiles = (int)(((int64_t)(end - begin) + (1 << shift) - 1) >> shift);
-    int upto = tiles;
+// The rows cut into tiles of 2^shift, group by group, the rows of no group last. Used by whole waves, with the same answer in every lane:
+// a lane holds one of 64 neighbouring groups, so that up to 63 groups are looked at once and a tile is found by a ballot.
+class GroupTiles {
+ public:
+  __device__ __forceinline__ GroupTiles(const int64_t* offsets, int groups, int rows, int shift)
+      : offsets_(offsets), groups_(groups), rows_(rows), shift_(shift) {
+    look(0, 0);
+  }
+  // number of tiles
+  __device__ __forceinline__ int count() {
+    while (base_ + 64 <= groups_) look(base_ + 64, last_);
+    return last_;
+  }
+  // tile 0 .. count() - 1
+  __device__ __forceinline__ GroupTile find(int tile) {
+    if (tile < before_) look(0, 0);
+    while (tile >= last_ && base_ + 64 <= groups_) look(base_ + 64, last_);
+    const unsigned long long reach = __ballot(upto_ > tile);
+    const int src = reach ? __ffsll((long long)reach) - 1 : 63;
+    const int g = __builtin_amdgcn_readfirstlane(src);
+    const int first = __builtin_amdgcn_readlane(upto_ - tiles_, g);
+    const int b = __builtin_amdgcn_readlane(begin_, g), e = __builtin_amdgcn_readlane(end_, g);
+    GroupTile t;
+    t.group = base_ + g;
+    t.begin = b + ((tile - first) << shift_);
+    t.end = min(e, t.begin + (1 << shift_));
+    return t;
+  }
+
+ private:
+  const int64_t* offsets_;
+  int groups_, rows_, shift_;
+  int base_, before_, last_;           // the first of the 64 groups; tiles in front of them and up to their end
+  int begin_, end_, tiles_, upto_;     // of the lane's group
+  __device__ __forceinline__ void look(int base, int before) {
+    const int lane = threadIdx.x & 63, g = base + lane;
+    base_ = base;
+    before_ = before;
+    begin_ = end_ = 0;
+    if (g <= groups_) ds_group_range(offsets_, groups_, rows_, g, &begin_, &end_);
+    tiles_ = (int)(((int64_t)(end_ - begin_) + (1 << shift_) - 1) >> shift_);
+    upto_ = tiles_;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += up;
+      const int up = __shfl_up(upto_, o, 64);
+      if (lane >= o) upto_ += up;
     }
-    const unsigned long long reach = __ballot(before + upto > tile);
-    if (reach) {
-      const int src = __ffsll((long long)reach) - 1;
-      const int first = __shfl(before + upto - tiles, src, 64);
-      const int b = __shfl(begin, src, 64), e = __shfl(end, src, 64);
-      out->group = __builtin_amdgcn_readfirstlane(base + src);
-      out->begin = __builtin_amdgcn_readfirstlane(b + ((tile - first) << shift));
-      out->end = __builtin_amdgcn_readfirstlane(min(e, b + ((tile - first + 1) << shift)));
-      return true;
-    }
-    before += __shfl(upto, 63, 64);
+    upto_ += before;
+    last_ = __builtin_amdgcn_readlane(upto_, 63);
   }
-  return false;
-}
+};
 
 }  // namespace
