@@ -48,7 +48,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
   const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N;
-  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT);
+  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT, true);
   if (tile >= all.count()) return;
   const GroupTile gt = all.find(tile);
   int row[RB];
@@ -215,7 +215,8 @@ MmArgs arguments(const ds_grouped& p) {
   return a;
 }
 
-bool many_rows(const ds_grouped& p) { return p.rows / p.groups > 64; }
+// (the tiles' loads need rows of 16 bytes at the least)
+bool many_rows(const ds_grouped& p) { return p.rows / p.groups > 64 && p.inner >= 8 && p.outer >= 8; }
 
 template <typename T>
 int element_of() {

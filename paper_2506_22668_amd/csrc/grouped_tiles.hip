@@ -10,7 +10,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define DS_LDS __attribute__((address_space(3)))
 #define DS_GLOBAL __attribute__((address_space(1)))
 
-constexpr int kDepthBytes = 128;   // of a step of the contraction
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
 
@@ -32,42 +31,43 @@ __device__ __forceinline__ f32x16 multiply(PieceV<float> a, PieceV<float> b, f32
 // column of the tile that row m of a matrix-core operand stands for: a lane's 16 results are then 16 neighbours
 __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
-// An operand in LDS. ACROSS false: [COLS][128 bytes of the contraction], 16-byte pieces of a column exchanged by its last three bits;
-// true: [steps of the contraction][COLS], pieces exchanged by the step's last two bits (16-bit types).
-template <typename T, int COLS, bool ACROSS>
+// A stage of an operand in LDS: DEPTH elements of the contraction (64 or 128 bytes of them). ACROSS false: [COLS][DEPTH], the 16-byte pieces of
+// a column exchanged by bits of its number; true: [DEPTH][COLS], pieces exchanged by the step's last two bits (16-bit types). Either way
+// the lanes that read together meet all banks.
+template <typename T, int COLS, bool ACROSS, int DEPTH_BYTES>
 struct Operand {
-  static constexpr int N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T), BYTES = COLS * kDepthBytes;
-  static constexpr int PER_ROW = ACROSS ? COLS / N : 8;
-  // the place of piece number `at` of the tile: its column (or step) and which piece of that
-  static __device__ __forceinline__ int line(int at) { return at / PER_ROW; }
-  static __device__ __forceinline__ int piece(int at) {
-    const int p = at % PER_ROW;
-    if constexpr (ACROSS) return sizeof(T) == 2 ? p ^ ((line(at) & 3) << 2) : p;
-    else return p ^ (line(at) & 7);
+  static constexpr int N = Piece<T>::N, DEPTH = DEPTH_BYTES / sizeof(T), BYTES = COLS * DEPTH_BYTES;
+  static constexpr int PER_ROW = ACROSS ? COLS / N : DEPTH_BYTES / 16;
+  static __device__ __forceinline__ int exchange(int line, int piece) {
+    if constexpr (ACROSS) return sizeof(T) == 2 ? piece ^ ((line & 3) << 2) : piece;
+    else return DEPTH_BYTES == 64 ? piece ^ ((line >> 1) & 3) : piece ^ (line & 7);
   }
+  // the place of piece number `at` of the stage: its column (or step) and which piece of that
+  static __device__ __forceinline__ int line(int at) { return at / PER_ROW; }
+  static __device__ __forceinline__ int piece(int at) { return exchange(line(at), at % PER_ROW); }
 };
 
 // A lane's operand pieces for 32 columns and 2 N steps of the contraction
-template <typename T, int COLS, bool ACROSS, bool ORDERED>
+template <typename T, int COLS, bool ACROSS, bool ORDERED, int DEPTH_BYTES>
 struct Reader {
-  using Op = Operand<T, COLS, ACROSS>;
+  using Op = Operand<T, COLS, ACROSS, DEPTH_BYTES>;
   int m, h, lane;
   __device__ __forceinline__ Reader(int lane_) : lane(lane_) {
     const int r = lane & 31;
     m = ORDERED ? column_of(r) : r;
     h = lane >> 5;
   }
-  // columns first .. first + 31, steps slice * 2 N ..
-  __device__ __forceinline__ PieceV<T> read(const char* tile, int first, int slice) const {
+  // columns first .. first + 31 (first: a multiple of 32), steps slice * 2 N ..
+  __device__ __forceinline__ PieceV<T> read(const char* stage, int first, int slice) const {
     constexpr int N = Op::N;
     if constexpr (!ACROSS) {
-      return *reinterpret_cast<const PieceV<T>*>(tile + (first + m) * kDepthBytes + (((2 * slice + h) ^ (m & 7)) << 4));
+      return *reinterpret_cast<const PieceV<T>*>(stage + (first + m) * DEPTH_BYTES + (Op::exchange(m, 2 * slice + h) << 4));
     } else if constexpr (sizeof(T) == 2) {
       const int i = lane & 15, four = ((lane >> 4) & 1) * 4 + (i & 3);
       const int col = first + (ORDERED ? 16 * (four & 1) + 4 * (four >> 1) : 4 * four);
-      const int byte = (slice * 16 + 8 * h + (i >> 2)) * (COLS * 2) + (((col >> 3) ^ ((i >> 2) << 2)) << 4) + (col & 7) * 2;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((DS_LDS s16x4*)(tile + byte));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((DS_LDS s16x4*)(tile + byte + 4 * COLS * 2));
+      const int byte = (slice * 16 + 8 * h + (i >> 2)) * (COLS * 2) + (Op::exchange(i >> 2, col >> 3) << 4) + (col & 7) * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((DS_LDS s16x4*)(stage + byte));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((DS_LDS s16x4*)(stage + byte + 4 * COLS * 2));
       union {
         s16x4 half[2];
         PieceV<T> whole;
@@ -79,27 +79,45 @@ struct Reader {
       PieceV<T> v;
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        v[i] = *reinterpret_cast<const float*>(tile + (slice * 2 * N + N * h + i) * (COLS * 4) + (first + m) * 4);
+        v[i] = *reinterpret_cast<const float*>(stage + (slice * 2 * N + N * h + i) * (COLS * 4) + (first + m) * 4);
       return v;
     }
   }
 };
 
+// The last `have` (at most N) elements of 16 bytes, brought to the front, zeros behind them
+template <typename T>
+__device__ __forceinline__ PieceV<T> last_elements(PieceV<T> v, int have) {
+  union {
+    PieceV<T> piece;
+    unsigned __int128 bits;
+  } u;
+  u.piece = v;
+  u.bits = have <= 0 ? 0 : u.bits >> (8 * (int)sizeof(T) * (Piece<T>::N - (have < Piece<T>::N ? have : Piece<T>::N)));
+  u.bits = have <= 0 ? 0 : u.bits;
+  return u.piece;
+}
+
 // Brings pieces of an operand into LDS: piece u of thread t is piece number u * THREADS + t of the tile. Direct loads go there by
-// themselves; rows that are not aligned for them come through registers.
-template <typename T, int COLS, int THREADS, bool DIRECT>
+// themselves; rows that are not aligned for them come through registers. A piece that reaches over its row's end is read as the row's last
+// 16 bytes and shifted: nothing outside of the row is read, element by element nothing either (rows have at least 16 bytes).
+template <typename T, int STAGE_BYTES, int THREADS, bool DIRECT>
 struct Loader {
-  static constexpr int N = Piece<T>::N, PIECES = COLS * kDepthBytes / 16 / THREADS;
+  static constexpr int N = Piece<T>::N, PIECES = STAGE_BYTES / 16 / THREADS;
   PieceV<T> held[DIRECT ? 1 : PIECES];
 
-  // have: elements that there are from p on (zeros behind them)
-  __device__ __forceinline__ void fetch(int u, const T* p, int have, char* tile) {
+  // have: elements that there are from p to the row's end; there: whether there is such a row; ends: whether any lane has no whole piece
+  __device__ __forceinline__ void fetch(int u, const T* p, int have, bool there, bool ends, char* tile) {
+    const T* zeros = reinterpret_cast<const T*>(&kZeros);
     if constexpr (DIRECT) {
-      const T* src = have > 0 ? p : reinterpret_cast<const T*>(&kZeros);
+      const T* src = there && have > 0 ? p : zeros;
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
       __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(tile + (u * THREADS + wave * 64) * 16), 16, 0, 0);
+    } else if (!ends) {
+      held[u] = *reinterpret_cast<const typename Piece<T>::U*>(p);
     } else {
-      held[u] = load_piece<T>(p, have);
+      const T* src = !there ? zeros : have >= N ? p : p + (have - N);
+      held[u] = last_elements<T>(*reinterpret_cast<const typename Piece<T>::U*>(src), there ? have : 0);
     }
   }
   __device__ __forceinline__ void store(char* tile) {
@@ -110,23 +128,97 @@ struct Loader {
   }
 };
 
-// Workgroups stay: one to a compute unit, which goes through tiles of BR rows and BN columns. A step of the contraction (128 bytes of
-// every row) is computed on from one half of the LDS while the next but one comes into the other; a wave's operands for a slice of the
-// step are read while the matrix cores work on the slice before.
+constexpr int kMostGroups = 1024;
+
+// Tiles up to the last of every group, in LDS: a tile's group is found by two ballots
+struct GroupTable {
+  int upto[kMostGroups], waves[16];
+};
+
+// Fills the table (all threads of the workgroup); the number of tiles
+template <int THREADS, int SHIFT>
+__device__ __forceinline__ int fill_table(GroupTable& t, const MmArgs& a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int base = 0; base < kMostGroups; base += THREADS) {
+    const int g = base + (int)threadIdx.x;
+    if (base >= a.groups) {
+      t.upto[g] = before;
+      continue;
+    }
+    int begin = 0, end = 0;
+    if (g < a.groups) ds_group_range(a.offsets, a.groups, a.rows, g, &begin, &end);
+    int upto = (int)(((int64_t)(end - begin) + (1 << SHIFT) - 1) >> SHIFT);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += up;
+    }
+    if (lane == 63) t.waves[wave] = upto;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) upto += t.waves[w];
+      all += t.waves[w];
+    }
+    t.upto[g] = before + upto;
+    before += all;
+    __syncthreads();
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(before);
+}
+
+// Tile `tile` (one that there is); the same answer in every lane
+template <int SHIFT>
+__device__ __forceinline__ GroupTile find_tile(const GroupTable& t, const MmArgs& a, int tile) {
+  const int lane = threadIdx.x & 63;
+  const int sixteen = __ffsll((long long)__ballot(t.upto[lane * 16 + 15] > tile)) - 1;
+  const int g = __builtin_amdgcn_readfirstlane(sixteen * 16 + __ffsll((long long)__ballot(t.upto[sixteen * 16 + (lane & 15)] > tile)) - 1);
+  int begin, end;
+  ds_group_range(a.offsets, a.groups, a.rows, g, &begin, &end);
+  begin += (tile - (g ? t.upto[g - 1] : 0)) << SHIFT;
+  GroupTile out;
+  out.group = g;
+  out.begin = __builtin_amdgcn_readfirstlane(begin);
+  out.end = __builtin_amdgcn_readfirstlane(min(end, begin + (1 << SHIFT)));
+  return out;
+}
+
+// Waits until all but the last LATER of the wave's loads and stores are done (-1: without that), then for the workgroup's other waves:
+// what they brought into LDS is there. (A plain barrier waits for LDS accesses, but not for loads that go to LDS directly.)
+template <int LATER>
+__device__ __forceinline__ void meet() {
+  if constexpr (LATER >= 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// The same value, of which the compiler knows nothing: what is computed from it stays where it stands, out of the registers of a loop around it.
+__device__ __forceinline__ int hidden(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// Workgroups stay: one to a compute unit, which goes through tiles of BR rows and BN columns as through one line of steps of the
+// contraction (128 bytes of every row). A step is computed on from one half of the LDS, the next one is in the other half already, and
+// what comes behind that, of this tile or the next, is asked for as soon as the first half is through; a wave's operands for a slice of the
+// step are read while the matrix cores work on the slice before. Results leave through LDS of their own, while the next tile's steps come in.
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 64 / sizeof(T);
   constexpr int TR = BR / WR, TN = BN / WN, NR = TR / 32, NN = TN / 32, SLICES = DEPTH / (2 * N);
   constexpr int SHIFT = BR == 256 ? 8 : BR == 128 ? 7 : 6;
-  using XOp = Operand<T, BR, false>;
-  using WOp = Operand<T, BN, !TRANSPOSED>;
-  constexpr int STAGE = XOp::BYTES + WOp::BYTES;
-  // results on their way out: a wave's rows, PASS blocks of 32 at a time, lie in `odd`
-  constexpr int OUT_ROW = TN * (int)sizeof(T), PASS = STAGE / (WR * WN) / (32 * OUT_ROW) < NR ? STAGE / (WR * WN) / (32 * OUT_ROW) : NR;
-  constexpr int CHUNKS = OUT_ROW / 16, ROWS_AT_ONCE = 64 / CHUNKS;
-  // (two arrays, not halves of one: only then does the compiler know that what is read of one does not wait for what comes into the other)
-  __shared__ __attribute__((aligned(128))) char even[STAGE], odd[STAGE];
-  __shared__ int row_of[2][BR];
+  using XOp = Operand<T, BR, false, 64>;
+  using WOp = Operand<T, BN, !TRANSPOSED, 64>;
+  constexpr int STAGE = XOp::BYTES + WOp::BYTES, LOADS = STAGE / 16 / THREADS;
+  constexpr int OUT_ROW = TN * (int)sizeof(T), CHUNKS = OUT_ROW / 16, AT_ONCE = 64 / CHUNKS, OUT_ROWS = 16, OUTS = OUT_ROWS / AT_ONCE;
+  // (arrays, not parts of one: only then does the compiler know that what is read of one does not wait for what comes into the other)
+  __shared__ __attribute__((aligned(128))) char stage0[STAGE], stage1[STAGE], stage2[STAGE], stage3[STAGE], leaving[WR * WN * OUT_ROWS * OUT_ROW];
+  __shared__ __attribute__((aligned(16))) float bias_of[WR * WN * TN];
+  __shared__ GroupTable table;
+  // of the tiles under way, by their number: the rows, and the group (a tile comes in at most five stages before it is computed on, and has two at the least)
+  __shared__ int row_of[8][BR], group_of[8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = (wave / WN) * TR, wn = (wave % WN) * TN;
   const int width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
@@ -134,174 +226,252 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
   const int64_t xs = TRANSPOSED ? a.dys : a.xs;
   const T* gate = (const T*)a.gate;
   T* y = (T*)a.y;
-  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT);
   // Workgroups go to the eight XCDs in turn. Each XCD has a stretch of the tiles, column tiles of a row tile next to each other, so that they
   // share its L2; its workgroups take them in turn.
-  const int64_t tiles = (int64_t)all.count() * a.col_tiles;
+  const int64_t tiles = (int64_t)fill_table<THREADS, SHIFT>(table, a) * a.col_tiles;
   const int xcd = (int)blockIdx.x & 7, step_by = (int)gridDim.x >> 3;
-  const int64_t stretch = tiles * (xcd + 1) / 8;
-  int64_t at = tiles * xcd / 8 + ((int)blockIdx.x >> 3);
+  const int stretch = __builtin_amdgcn_readfirstlane((int)(tiles * (xcd + 1) / 8));
+  int at = __builtin_amdgcn_readfirstlane((int)(tiles * xcd / 8) + ((int)blockIdx.x >> 3));
 
-  Loader<T, BR, THREADS, DIRECT> lx;
-  Loader<T, BN, THREADS, DIRECT> lw;
-  const Reader<T, BR, false, false> rx(lane);
-  const Reader<T, BN, !TRANSPOSED, true> rw(lane);
-  const int steps = (depth + DEPTH - 1) / DEPTH;
+  Loader<T, XOp::BYTES, THREADS, DIRECT> lx;
+  Loader<T, WOp::BYTES, THREADS, DIRECT> lw;
+  const Reader<T, BR, false, false, 64> rx(lane);
+  const Reader<T, BN, !TRANSPOSED, true, 64> rw(lane);
+  const int steps = (depth + 2 * DEPTH - 1) / (2 * DEPTH) * 2;   // stages of a tile, an even number (zeros behind the end)
   // A thread's pieces of a step lie in one place of lines that are a fixed number apart (the exchange of pieces goes by the last bits
   // of a line, which that number leaves alone)
   constexpr int XLINES = THREADS / XOp::PER_ROW, WLINES = THREADS / WOp::PER_ROW;
   static_assert(XLINES % 8 == 0 && WLINES % 8 == 0, "");
-  const int xk = XOp::piece((int)threadIdx.x) * N, wline = WOp::line((int)threadIdx.x), wplace = WOp::piece((int)threadIdx.x) * N;
+  const int xk = XOp::piece((int)threadIdx.x) * N;
+  const int wline = WOp::line((int)threadIdx.x), wplace = WOp::piece((int)threadIdx.x) * N;
+  // what comes in: step `coming` of the tile `coming_at`, whose rows were looked up while the tile before came in
   const T *from_x[lx.PIECES], *from_w;
-  GroupTile gt;
-  int col0, turn = 0;
-  const auto fetch = [&](int s, char* stage) {
-    const int k = s * DEPTH;
+  int row[lx.PIECES], coming = 0, coming_col = 0, coming_at = at, coming_group = 0, coming_number = 0;
+  const auto look_up = [&](int tile) __attribute__((always_inline)) {
+    const GroupTile found = find_tile<SHIFT>(table, a, tile / a.col_tiles);
+    coming_group = found.group;
+    const int line = XOp::line(hidden((int)threadIdx.x));
+#pragma unroll
+    for (int u = 0; u < lx.PIECES; ++u) {
+      const int pos = found.begin + u * XLINES + line;
+      row[u] = pos < found.end ? ds_ordered_row(a.order, a.rows, pos) : -1;
+    }
+  };
+  // Asks for the next stage: number `coming` of tile `coming_at`; behind the last one nothing.
+  const auto fetch = [&](char* stage) __attribute__((always_inline)) {
+    if (coming_at >= stretch) return;
+    if (coming == 0) {
+      coming_col = coming_at % a.col_tiles * BN;
+      from_w = (const T*)a.w + (int64_t)coming_group * a.inner * a.outer +
+               (TRANSPOSED ? (int64_t)(coming_col + wline) * a.outer + wplace : (int64_t)wline * a.outer + coming_col + wplace);
+      int* rows = row_of[coming_number & 7];
+      const int tid = hidden((int)threadIdx.x);
+#pragma unroll
+      for (int u = 0; u < lx.PIECES; ++u) {
+        from_x[u] = x + (row[u] < 0 ? 0 : row[u]) * xs + xk;   // (no row: any row, whose results go nowhere)
+        if (tid % XOp::PER_ROW == 0) rows[u * XLINES + XOp::line(tid)] = row[u];
+      }
+      group_of[coming_number & 7] = coming_group;
+      ++coming_number;
+      if (coming_at + step_by < stretch) look_up(coming_at + step_by);
+    }
+    const int k = coming * DEPTH;
+    const bool deep = k + DEPTH > depth, wide = coming_col + BN > width;
+#pragma unroll
+    for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x[u] + k, depth - k - xk, true, deep, stage + WOp::BYTES);
 #pragma unroll
     for (int u = 0; u < lw.PIECES; ++u) {
       const int line = u * WLINES + wline;
-      if constexpr (TRANSPOSED) lw.fetch(u, from_w + (int64_t)(u * WLINES) * a.outer + k, col0 + line < width ? depth - k - wplace : 0, stage);
-      else lw.fetch(u, from_w + (int64_t)(k + u * WLINES) * a.outer, k + line < depth ? width - col0 - wplace : 0, stage);
+      if constexpr (TRANSPOSED)
+        lw.fetch(u, from_w + (int64_t)(u * WLINES) * a.outer + k, depth - k - wplace, coming_col + line < width, deep || wide, stage);
+      else lw.fetch(u, from_w + (int64_t)(k + u * WLINES) * a.outer, width - coming_col - wplace, k + line < depth, deep || wide, stage);
     }
-#pragma unroll
-    for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x[u] + k, depth - k - xk, stage + WOp::BYTES);
+    if (++coming == steps) {
+      coming = 0;
+      coming_at += step_by;
+    }
   };
-  const auto put = [&](char* stage) {
+  const auto put = [&](char* stage) __attribute__((always_inline)) {
     lw.store(stage);
     lx.store(stage + WOp::BYTES);
   };
-  // what a thread brings of tile `at`, and its first step
-  const auto start = [&]() {
-    gt = all.find((int)(at / a.col_tiles));
-    col0 = (int)(at % a.col_tiles) * BN;
-    turn ^= 1;
-    if (threadIdx.x < BR) {
-      const int pos = gt.begin + (int)threadIdx.x;
-      row_of[turn][threadIdx.x] = pos < gt.end ? ds_ordered_row(a.order, a.rows, pos) : -1;
-    }
-    if (gt.group == a.groups) return;
-#pragma unroll
-    for (int u = 0; u < lx.PIECES; ++u) {
-      const int pos = gt.begin + u * XLINES + XOp::line((int)threadIdx.x);
-      const int r = pos < gt.end ? ds_ordered_row(a.order, a.rows, pos) : 0;
-      from_x[u] = x + (r < 0 ? 0 : r) * xs + xk;   // (no row: any row, whose results go nowhere)
-    }
-    from_w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer +
-             (TRANSPOSED ? (int64_t)(col0 + wline) * a.outer + wplace : (int64_t)wline * a.outer + col0 + wplace);
-    fetch(0, even);
-    put(even);
-  };
 
-  if (at >= stretch) return;
-  start();
-  while (true) {
+  if (at < stretch) {
     f32x16 acc[NR][NN] = {};
-    if (gt.group < a.groups) {
-      PieceV<T> fx[2][NR], fw[2][NN];
-      const auto read = [&](const char* stage, int c) {
+    PieceV<T> fx[2][NR], fw[2][NN];
+    const auto read = [&](const char* stage, int c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < NN; ++n) fw[c & 1][n] = rw.read(stage, wn + n * 32, c);
+      for (int n = 0; n < NN; ++n) fw[c & 1][n] = rw.read(stage, wn + n * 32, c);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) fx[c & 1][r] = rx.read(stage + WOp::BYTES, wr + r * 32, c);
-      };
-      const auto work = [&](int c) {
+      for (int r = 0; r < NR; ++r) fx[c & 1][r] = rx.read(stage + WOp::BYTES, wr + r * 32, c);
+    };
+    const auto work = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+      for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fw[c & 1][n], fx[c & 1][r], acc[r][n]);
-      };
-      const auto step = [&](int s, char* now, char* then) {
+        for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fw[c & 1][n], fx[c & 1][r], acc[r][n]);
+    };
+    // One stage, in two phases between barriers: the wave's operands out of LDS and loads of what comes three stages on, into the stage that
+    // was `before`; then nothing but products. The two waves of a SIMD are a phase apart, so that one fills the matrix cores while the other
+    // works off addresses and waits. Waits leave the loads of two stages under way. `fresh`: in the stages behind a tile's results,
+    // in front of whose stores all loads were waited for, so that the stores need not be.
+    const auto half = [&](bool fresh, char* now, char* before) __attribute__((always_inline)) {
+      read(now, 0);
+      read(now, 1);
+      put(before);
+      fetch(before);
+      if (DIRECT && !fresh) meet<2 * LOADS>();
+      else meet<-1>();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      work(0);
+      work(1);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      meet<-1>();
+    };
+    static_assert(SLICES == 2, "");
+    int number = 0;
+    const auto leave = [&]() __attribute__((always_inline)) {
+      const int lane = hidden((int)threadIdx.x & 63), col = at % a.col_tiles * BN + wn;
+      char* mine = leaving + wave * (OUT_ROWS * OUT_ROW);
+      float* bias = bias_of + wave * TN;
+      if constexpr (!TRANSPOSED) {
+        const float* from = a.bias + (a.bias ? (int64_t)__builtin_amdgcn_readfirstlane(group_of[number & 7]) * width : 0);
 #pragma unroll
-        for (int c = 0; c + 1 < SLICES; ++c) {
-          read(now, c + 1);
-          __builtin_amdgcn_sched_barrier(0);
-          work(c);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        __syncthreads();   // step s + 1 is there, and nobody reads step s any more
-        if (s + 2 < steps) {
-          put(now);
-          fetch(DIRECT ? s + 2 : s + 3, now);
-        }
-        if (s + 1 < steps) {
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int n = 0; n < NN; ++n) fw[0][n] = rw.read(then, wn + n * 32, 0);
-#pragma unroll
-          for (int r = 0; r < NR; ++r) fx[0][r] = rx.read(then + WOp::BYTES, wr + r * 32, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        work(SLICES - 1);
-      };
-      static_assert(SLICES % 2 == 0, "");
-      if (steps > 1) {
-        fetch(1, odd);
-        put(odd);
-        if (!DIRECT) fetch(2, even);
+        for (int j = 0; j < TN; j += 64)
+          if (TN % 64 == 0 || j + lane < TN) bias[j + lane] = a.bias ? from[min(col + j + lane, width - 1)] : 0.f;
       }
-      __syncthreads();
-      read(even, 0);
-      for (int s = 0; s < steps; s += 2) {
-        step(s, even, odd);
-        if (s + 1 < steps) step(s + 1, odd, even);
-      }
-    }
-    // the next tile's first step comes in while this one's results go out
-    const GroupTile done = gt;
-    const int col = col0 + wn, ids = turn;
-    at += step_by;
-    const bool more = at < stretch;
-    __syncthreads();
-    if (more) start();
-    char* mine = odd + wave * (STAGE / (WR * WN));
+      const float least = !TRANSPOSED && a.relu ? 0.f : -INFINITY;
+      const int chunk = lane % CHUNKS, c = col + chunk * N;
+      const int* rows = row_of[number & 7] + wr + lane / CHUNKS;
+      // (a gate is asked for two blocks of rows ahead, in front of stores that its coming would otherwise wait for)
+      PieceV<T> open[2 * NR][OUTS];
+      const auto ask = [&](int r) __attribute__((always_inline)) {
+        if constexpr (TRANSPOSED) {
+          if (gate && r < NR) {
 #pragma unroll
-    for (int r0 = 0; r0 < NR; r0 += PASS) {
+            for (int half = 2 * r; half < 2 * r + 2; ++half)
 #pragma unroll
-      for (int n = 0; n < NN; ++n) {
-        const int c = col + n * 32 + 16 * (lane >> 5);
-        float bias[16];
+              for (int i = 0; i < OUTS; ++i) {
+                const int to = rows[half * OUT_ROWS + i * AT_ONCE];
+                if (to >= 0 && c + N <= width) open[half][i] = *reinterpret_cast<const typename Piece<T>::U*>(gate + to * a.gs + c);
+              }
+          }
+        }
+      };
+      ask(0);
+      ask(1);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the next step has come in: see step)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          bias[i] = a.bias && done.group < a.groups && c + i < width ? a.bias[(int64_t)done.group * width + c + i] : 0.f;
+      for (int r = 0; r < NR; ++r) {
+        PieceV<T> out[NN][16 / N];
 #pragma unroll
-        for (int r = 0; r < PASS; ++r)
+        for (int n = 0; n < NN; ++n)
 #pragma unroll
-          for (int p = 0; p < 16 / N; ++p) {
-            PieceV<T> out;
+          for (int p = 0; p < 16 / N; ++p)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-              float v = acc[r0 + r][n][p * N + i] + bias[p * N + i];
-              if (a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
-              out[i] = (T)v;
+            for (int q = 0; q < N; q += 4) {
+              float4 b = {0.f, 0.f, 0.f, 0.f};
+              if constexpr (!TRANSPOSED) b = *reinterpret_cast<const float4*>(bias + n * 32 + 16 * (lane >> 5) + p * N + q);
+              const float plus[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float v = acc[r][n][p * N + q + i];
+                if constexpr (!TRANSPOSED) {
+                  v += plus[i];
+                  v = v < least ? least : v;   // (a NaN stays one)
+                }
+                out[n][p][q + i] = (T)v;
+              }
             }
-            const int line = r * 32 + (lane & 31), chunk = (n * 32 + 16 * (lane >> 5)) / N + p;
-            *reinterpret_cast<PieceV<T>*>(mine + line * OUT_ROW + ((chunk ^ (line & 7)) << 4)) = out;
-          }
-      }
-      // (a wave reads what it wrote itself: its LDS accesses keep their order)
+        if (r) ask(r + 1);
 #pragma unroll
-      for (int i = 0; i < PASS * 32 / ROWS_AT_ONCE; ++i) {
-        const int line = i * ROWS_AT_ONCE + lane / CHUNKS, chunk = lane % CHUNKS, c = col + chunk * N;
-        const int row = row_of[ids][wr + r0 * 32 + line];
-        PieceV<T> out = *reinterpret_cast<const PieceV<T>*>(mine + line * OUT_ROW + ((chunk ^ (line & 7)) << 4));
-        if (row >= 0 && c < width) {
-          if (gate) {
-            const PieceV<T> open = load_piece<T>(gate + row * a.gs + c, width - c);
+        for (int h = 0; h < 2; ++h) {   // 16 rows at a time
+          const int half = 2 * r + h;
+          if (((lane >> 4) & 1) == h) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) out[j] = (float)open[j] > 0.f ? out[j] : (T)0.f;
+            for (int n = 0; n < NN; ++n)
+#pragma unroll
+              for (int p = 0; p < 16 / N; ++p)
+                *reinterpret_cast<PieceV<T>*>(mine + (lane & 15) * OUT_ROW + ((((n * 32 + 16 * (lane >> 5)) / N + p) ^ (lane & 7)) << 4)) = out[n][p];
           }
-          store_piece<T>(y + row * a.ys + c, out, width - c);
+          // (a wave reads what it wrote itself: its LDS accesses keep their order)
+#pragma unroll
+          for (int i = 0; i < OUTS; ++i) {
+            const int line = i * AT_ONCE + lane / CHUNKS, to = rows[half * OUT_ROWS + i * AT_ONCE];
+            const char* held = mine + line * OUT_ROW + ((chunk ^ (line & 7)) << 4);
+            if (to < 0 || c >= width) continue;
+            T* target = y + to * a.ys + c;
+            if (c + N <= width) {
+              PieceV<T> v = *reinterpret_cast<const PieceV<T>*>(held);
+              if (TRANSPOSED && gate) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = (float)open[half][i][j] > 0.f ? v[j] : (T)0.f;
+              }
+              *reinterpret_cast<typename Piece<T>::U*>(target) = v;
+            } else {
+#pragma unroll 1
+              for (int j = 0; j < width - c; ++j) {
+                const T v = reinterpret_cast<const T*>(held)[j];
+                target[j] = !TRANSPOSED || !gate || (float)gate[to * a.gs + c + j] > 0.f ? v : (T)0.f;
+              }
+            }
+          }
         }
       }
+      ++number;
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int n = 0; n < NN; ++n) acc[r][n] = f32x16{};
+    };
+    look_up(at);
+    fetch(stage0);
+    put(stage0);
+    fetch(stage1);
+    put(stage1);
+    fetch(stage2);
+    put(stage2);
+    if (!DIRECT) fetch(stage3);
+    meet<0>();
+    const bool second = wave >= WR * WN / 2;   // the waves that are a phase behind; all leave a tile together
+    if (second) meet<-1>();
+    int s = 0;
+    bool left = true;
+    const auto two = [&](char* before, char* now, char* then) __attribute__((always_inline)) {
+      half(left, now, before);
+      half(left, then, now);
+      s += 2;
+      left = s == steps;
+      if (left) {
+        if (!second) meet<-1>();
+        leave();
+        s = 0;
+        at += step_by;
+        if (at >= stretch) return false;
+        if (second) meet<-1>();
+      }
+      return true;
+    };
+    while (two(stage3, stage0, stage1) && two(stage1, stage2, stage3)) {
     }
-    if (!more) return;
-    __syncthreads();
+  }
+  // rows of no group
+  int none, end;
+  ds_group_range(a.offsets, a.groups, a.rows, a.groups, &none, &end);
+  for (int pos = none + (int)blockIdx.x * WR * WN + wave; pos < end; pos += (int)gridDim.x * WR * WN) {
+    const int r = ds_ordered_row(a.order, a.rows, pos);
+    if (r >= 0)
+      for (int c = lane * N; c < width; c += 64 * N) store_piece<T>(y + r * a.ys + c, PieceV<T>{}, width - c);
   }
 }
 
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED, bool DIRECT>
 int launch_one(ds_ctx* ctx, MmArgs& a) {
   a.col_tiles = ((TRANSPOSED ? a.inner : a.outer) + BN - 1) / BN;
+  if (ds_most_tiles(a, BR == 256 ? 8 : 7) * a.col_tiles > 0x7fffffff)
+    return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than are counted", a.rows, TRANSPOSED ? a.inner : a.outer);
   hipLaunchKernelGGL(HIP_KERNEL_NAME(row_tiles_kernel<T, BR, BN, WR, WN, TRANSPOSED, DIRECT>), dim3((unsigned)(ctx->num_cus + 7) / 8 * 8),
                      dim3(64 * WR * WN), 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
@@ -350,10 +520,10 @@ __device__ __forceinline__ int64_t locate_unit(const MmArgs& a, int depth, int t
 
 template <typename T, int BR, int BN, int WR, int WN, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 128 / sizeof(T);
   constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLICES = DEPTH / (2 * N), SLOT = BR * BN + BN;
-  using XOp = Operand<T, BR, true>;
-  using DOp = Operand<T, BN, true>;
+  using XOp = Operand<T, BR, true, 128>;
+  using DOp = Operand<T, BN, true, 128>;
   constexpr int STAGE = XOp::BYTES + DOp::BYTES;
   constexpr int PARTS = THREADS / BN, EACH = DEPTH / PARTS;   // of the sums for db: threads to a column, steps of each
   __shared__ __attribute__((aligned(128))) char even[STAGE], odd[STAGE];
@@ -371,8 +541,8 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   const int64_t last = ds_mm_even_begin(blockIdx.x + 1, wgs, units);
   locate_unit(a, DEPTH, tiles, unit, &group, &within);
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
-  const Reader<T, BR, true, false> rx(lane);
-  const Reader<T, BN, true, true> rd(lane);
+  const Reader<T, BR, true, false, 128> rx(lane);
+  const Reader<T, BN, true, true, 128> rd(lane);
   while (unit < last && group < a.groups) {
     int begin, end;
     const int steps = group_steps(a, group, DEPTH, &begin, &end);
@@ -386,11 +556,12 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
     const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
     f32x16 acc[NR][NN] = {};
     float sum = 0.f;
-    Loader<T, BR, THREADS, DIRECT> lx;
-    Loader<T, BN, THREADS, DIRECT> ld;
+    Loader<T, XOp::BYTES, THREADS, DIRECT> lx;
+    Loader<T, DOp::BYTES, THREADS, DIRECT> ld;
     constexpr int LINES = THREADS / XOp::PER_ROW;   // (as in row_tiles_kernel)
     static_assert(BR == BN && LINES % 4 == 0, "both operands' pieces of a thread lie in the same rows");
     int row[lx.PIECES];
+    constexpr bool ends = true;
     const int line = XOp::line((int)threadIdx.x), place = XOp::piece((int)threadIdx.x) * N;
     const T *from_x = x + in0 + place, *from_dy = dy + col0 + place;
     const auto find_rows = [&](int s) {
@@ -402,12 +573,12 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
     };
     const auto fetch = [&](char* stage) {
 #pragma unroll
-      for (int u = 0; u < ld.PIECES; ++u) ld.fetch(u, from_dy + row[u] * a.dys, row[u] < 0 ? 0 : a.outer - col0 - place, stage);
+      for (int u = 0; u < ld.PIECES; ++u) ld.fetch(u, from_dy + row[u] * a.dys, a.outer - col0 - place, row[u] >= 0, ends, stage);
 #pragma unroll
-      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x + row[u] * a.xs, row[u] < 0 ? 0 : a.inner - in0 - place, stage + DOp::BYTES);
+      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x + row[u] * a.xs, a.inner - in0 - place, row[u] >= 0, ends, stage + DOp::BYTES);
     };
     const auto step = [&](int s, char* now, char* then) {
-      __syncthreads();
+      meet<0>();
       if (s + 1 < upto) {
         fetch(then);
         find_rows(s + 2);
@@ -500,7 +671,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
 // Adds up the sums of tiles that were cut, and clears the gradients of empty groups: a workgroup to a tile and 32 x 32 block of each wave
 template <typename T, int BR, int BN, int WR, int WN>
 __global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, const float* partial, int wgs) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 128 / sizeof(T);
   constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wr = (wave / WN) * (BR / WR), wn = (wave % WN) * (BN / WN);
@@ -587,7 +758,7 @@ int launch(ds_ctx* ctx, MmArgs& a) {
 }  // namespace
 
 int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a) {
-  if (dtype == DS_ELEM_F32) return transposed ? launch<float, 128, 128, 2, 2, true>(ctx, a) : launch<float, 128, 128, 2, 2, false>(ctx, a);
+  if (dtype == DS_ELEM_F32) return transposed ? launch<float, 128, 128, 2, 4, true>(ctx, a) : launch<float, 128, 128, 2, 4, false>(ctx, a);
   if (dtype == DS_ELEM_BF16) return transposed ? launch<__bf16, 256, 256, 2, 4, true>(ctx, a) : launch<__bf16, 256, 256, 2, 4, false>(ctx, a);
   return transposed ? launch<_Float16, 256, 256, 2, 4, true>(ctx, a) : launch<_Float16, 256, 256, 2, 4, false>(ctx, a);
 }
