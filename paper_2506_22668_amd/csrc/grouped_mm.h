@@ -24,5 +24,5 @@ static inline int64_t ds_most_tiles(const MmArgs& a, int shift) {
 // The product by rows in tiles through LDS (grouped_tiles.hip); transposed: dx = dy w^T
 int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a);
 // The gradient of the weights in tiles; partial: ds_weight_tiles_bytes of scratch
-int64_t ds_weight_tiles_bytes(int dtype);
+int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer);
 int ds_launch_weight_tiles(ds_ctx* ctx, int dtype, MmArgs& a, void* partial);

@@ -276,7 +276,7 @@ int ds_launch_grouped_mm(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows x,
 }
 
 int64_t ds_grouped_mm_backward_bytes(int dtype, const ds_grouped& p) {
-  return many_rows(p) ? ds_weight_tiles_bytes(dtype) : 0;
+  return many_rows(p) ? ds_weight_tiles_bytes(dtype, p.rows, p.inner, p.outer) : 0;
 }
 
 int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, ds_rows x, ds_rows gate, ds_rows dx,

@@ -257,9 +257,9 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
       row[u] = pos < found.end ? ds_ordered_row(a.order, a.rows, pos) : -1;
     }
   };
-  // Asks for the next stage: number `coming` of tile `coming_at`; behind the last one nothing.
+  // Asks for the next stage: number `coming` of tile `coming_at`; behind the last one nothing (false).
   const auto fetch = [&](char* stage) __attribute__((always_inline)) {
-    if (coming_at >= stretch) return;
+    if (coming_at >= stretch) return false;
     if (coming == 0) {
       coming_col = coming_at % a.col_tiles * BN;
       from_w = (const T*)a.w + (int64_t)coming_group * a.inner * a.outer +
@@ -290,6 +290,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
       coming = 0;
       coming_at += step_by;
     }
+    return true;
   };
   const auto put = [&](char* stage) __attribute__((always_inline)) {
     lw.store(stage);
@@ -313,15 +314,16 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
     };
     // One stage, in two phases between barriers: the wave's operands out of LDS and loads of what comes three stages on, into the stage that
     // was `before`; then nothing but products. The two waves of a SIMD are a phase apart, so that one fills the matrix cores while the other
-    // works off addresses and waits. Waits leave the loads of two stages under way. `fresh`: in the stages behind a tile's results,
-    // in front of whose stores all loads were waited for, so that the stores need not be.
+    // works off addresses and waits. Waits leave the loads of two stages under way (near the end, where there are no more, none). `fresh`: in the
+    // two stages behind a tile's results, in front of whose stores all loads were waited for, so that the stores need not be.
     const auto half = [&](bool fresh, char* now, char* before) __attribute__((always_inline)) {
       read(now, 0);
       read(now, 1);
       put(before);
-      fetch(before);
-      if (DIRECT && !fresh) meet<2 * LOADS>();
-      else meet<-1>();
+      const bool more = fetch(before);
+      if (!DIRECT || fresh) meet<-1>();
+      else if (more) meet<2 * LOADS>();
+      else meet<0>();
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
       work(0);
@@ -481,156 +483,190 @@ int launch_one(ds_ctx* ctx, MmArgs& a) {
 bool sixteen(const void* p, int64_t stride, size_t element) { return (uintptr_t)p % 16 == 0 && stride * element % 16 == 0; }
 
 // ---- the gradient of the weights ------------------------------------------------------------------------------------------------
-// dW_g = sum_r x[r]^T dy[r]: both operands run across the contraction, which is the group's rows. Groups are ragged and there are about
-// as many tiles as compute units, so the steps of all tiles of all groups lie in one line (group by group, tile by tile) that is cut
-// evenly, a stretch to a workgroup. Where a cut falls inside a tile, the workgroups on both sides leave fp32 sums (at most two a
-// workgroup), which a second launch adds up in order: no atomics, the same bits every time.
+// dW_g = sum_r x[r]^T dy[r]: both operands run across the contraction, which is the group's rows. Groups are ragged, and there are about
+// as many tiles as compute units or fewer, so the steps of all groups (UNIT rows each) lie in one line that is cut evenly into chunks, and a
+// workgroup takes one tile of the weights through one chunk. The tiles of a chunk run beside each other on one XCD and read the same rows: with
+// the steps of a tile in one line instead, neighbours read different rows, and all of them came from memory.
+// Where a cut falls inside a group, the chunks on both sides leave fp32 sums (at most two a workgroup), which a second launch
+// adds up in order: no atomics, the same bits every time.
 // the steps of a group's contraction
 __device__ __forceinline__ int group_steps(const MmArgs& a, int g, int depth, int* begin, int* end) {
   ds_group_range(a.offsets, a.groups, a.rows, g, begin, end);
   return (*end - *begin + depth - 1) / depth;
 }
 
-// Steps of all groups (each tile's), and where unit `unit` of the line falls: its group (-1: behind the end) and the steps before it
-// there, of all tiles. Called by whole waves, the same answer in every lane.
-__device__ __forceinline__ int64_t locate_unit(const MmArgs& a, int depth, int tiles, int64_t unit, int* group, int64_t* within) {
+// Steps of all groups, and where step `unit` of the line falls: its group (-1: behind the end) and the steps before it there. Called by whole
+// waves, the same answer in every lane.
+__device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit, int* group, int* within) {
   const int lane = threadIdx.x & 63;
-  int64_t before = 0;
+  int before = 0;
   *group = -1;
   for (int base = 0; base < a.groups; base += 64) {
     int begin, end;
-    const int g = base + lane;
-    const int64_t own = g < a.groups ? (int64_t)group_steps(a, g, depth, &begin, &end) * tiles : 0;
-    int64_t upto = own;
+    const int g = base + lane, own = g < a.groups ? group_steps(a, g, depth, &begin, &end) : 0;
+    int upto = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int64_t up = __shfl_up(upto, o, 64);
+      const int up = __shfl_up(upto, o, 64);
       if (lane >= o) upto += up;
     }
     const unsigned long long reach = __ballot(before + upto > unit);
     if (reach && *group < 0) {
-      const int src = __ffsll((long long)reach) - 1;
-      *group = __builtin_amdgcn_readfirstlane(base + src);
-      *within = unit - __shfl(before + upto - own, src, 64);
+      const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)reach) - 1);
+      *group = base + src;
+      *within = unit - __builtin_amdgcn_readlane(before + upto - own, src);
     }
-    before += __shfl(upto, 63, 64);
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
   return before;
 }
 
 template <typename T, int BR, int BN, int WR, int WN, bool DIRECT>
-__global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 128 / sizeof(T);
-  constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLICES = DEPTH / (2 * N), SLOT = BR * BN + BN;
-  using XOp = Operand<T, BR, true, 128>;
-  using DOp = Operand<T, BN, true, 128>;
-  constexpr int STAGE = XOp::BYTES + DOp::BYTES;
-  constexpr int PARTS = THREADS / BN, EACH = DEPTH / PARTS;   // of the sums for db: threads to a column, steps of each
-  __shared__ __attribute__((aligned(128))) char even[STAGE], odd[STAGE];
-  __shared__ float sums[PARTS][BN];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial, int most_chunks) {
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 64 / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
+  constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
+  using XOp = Operand<T, BR, true, 64>;
+  using DOp = Operand<T, BN, true, 64>;
+  constexpr int STAGE = XOp::BYTES + DOp::BYTES, LOADS = STAGE / 16 / THREADS;
+  constexpr int LINES = THREADS / DOp::PER_ROW, EACH = DEPTH / LINES;   // of a thread's pieces of a stage: lines apart, and how many
+  __shared__ __attribute__((aligned(128))) char stage0[STAGE], stage1[STAGE], stage2[STAGE], stage3[STAGE];
+  __shared__ float sums[LINES][BN];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = (wave / WN) * (BR / WR), wn = (wave % WN) * (BN / WN);
   const int tiles = (a.inner + BR - 1) / BR * a.col_tiles;
-  int group;
-  int64_t within, dummy;
-  int none;
-  const int64_t units = locate_unit(a, DEPTH, tiles, 0, &none, &dummy);
-  const int64_t wgs = units < (int64_t)gridDim.x ? units : (int64_t)gridDim.x;   // (none without a unit: the join reads all that there are)
-  if ((int64_t)blockIdx.x >= wgs) return;
-  int64_t unit = ds_mm_even_begin(blockIdx.x, wgs, units);
-  const int64_t last = ds_mm_even_begin(blockIdx.x + 1, wgs, units);
-  locate_unit(a, DEPTH, tiles, unit, &group, &within);
+  // Workgroups go to the eight XCDs in turn: each XCD has a stretch of the (chunk, tile) pairs
+  const int place_of = ((int)blockIdx.x & 7) * ((int)gridDim.x >> 3) + ((int)blockIdx.x >> 3);
+  const int chunk = place_of / tiles, tile = place_of % tiles;
+  int group, within, none;
+  const int units = locate_unit(a, UNIT, 0, &none, &within), chunks = min(units, most_chunks);   // (no chunk without a step)
+  if (chunk >= chunks) return;
+  int unit = (int)ds_mm_even_begin(chunk, chunks, units);
+  const int last = (int)ds_mm_even_begin(chunk + 1, chunks, units);
+  locate_unit(a, UNIT, unit, &group, &within);
+  const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
-  const Reader<T, BR, true, false, 128> rx(lane);
-  const Reader<T, BN, true, true, 128> rd(lane);
+  const Reader<T, BR, true, false, 64> rx(lane);
+  const Reader<T, BN, true, true, 64> rd(lane);
+  static_assert(BR == BN && LINES % 4 == 0, "both operands' pieces of a thread lie in the same rows");
+  const int line = DOp::line((int)threadIdx.x), place = DOp::piece((int)threadIdx.x) * N;
   while (unit < last && group < a.groups) {
     int begin, end;
-    const int steps = group_steps(a, group, DEPTH, &begin, &end);
-    if (within >= (int64_t)steps * tiles) {   // on to the next group
+    const int steps = group_steps(a, group, UNIT, &begin, &end);
+    if (within >= steps) {   // on to the next group
       ++group;
       within = 0;
       continue;
     }
-    const int tile = (int)(within / steps), first = (int)(within % steps);
-    const int upto = last - unit < steps - first ? first + (int)(last - unit) : steps;
-    const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
+    const int first = __builtin_amdgcn_readfirstlane(within);
+    const int upto = __builtin_amdgcn_readfirstlane(min(first + last - unit, steps));
     f32x16 acc[NR][NN] = {};
-    float sum = 0.f;
+    float sum[N] = {};
     Loader<T, XOp::BYTES, THREADS, DIRECT> lx;
     Loader<T, DOp::BYTES, THREADS, DIRECT> ld;
-    constexpr int LINES = THREADS / XOp::PER_ROW;   // (as in row_tiles_kernel)
-    static_assert(BR == BN && LINES % 4 == 0, "both operands' pieces of a thread lie in the same rows");
-    int row[lx.PIECES];
-    constexpr bool ends = true;
-    const int line = XOp::line((int)threadIdx.x), place = XOp::piece((int)threadIdx.x) * N;
-    const T *from_x = x + in0 + place, *from_dy = dy + col0 + place;
-    const auto find_rows = [&](int s) {
+    // The next stage to come in starts at position `coming` of the order, up to `stop`; its rows are looked up while the one before comes in.
+    const int stop = __builtin_amdgcn_readfirstlane(min(end, begin + upto * UNIT)), stages = 2 * (upto - first);
+    int coming = __builtin_amdgcn_readfirstlane(begin + first * UNIT), left = stages;
+    int row[EACH];
+    const auto look_up = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < lx.PIECES; ++u) {
-        const int pos = begin + s * DEPTH + u * LINES + line;
-        row[u] = s < upto && pos < end ? ds_ordered_row(a.order, a.rows, pos) : -1;
+      for (int u = 0; u < EACH; ++u) {
+        const int pos = at + u * LINES + line;
+        row[u] = pos < stop ? ds_ordered_row(a.order, a.rows, pos) : -1;
       }
     };
-    const auto fetch = [&](char* stage) {
+    const bool ends = a.outer - col0 < BN || a.inner - in0 < BR;   // (columns that there are not)
+    const auto fetch = [&](char* stage) __attribute__((always_inline)) {
+      if (left == 0) return false;
+      int now[EACH];
 #pragma unroll
-      for (int u = 0; u < ld.PIECES; ++u) ld.fetch(u, from_dy + row[u] * a.dys, a.outer - col0 - place, row[u] >= 0, ends, stage);
+      for (int u = 0; u < EACH; ++u) now[u] = row[u];
+      const bool over = ends || coming + DEPTH > stop || a.order;   // (an order may name rows that there are not)
+      look_up(coming + DEPTH);   // (in front of the loads: a wait for it does not wait for them)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x + row[u] * a.xs, a.inner - in0 - place, row[u] >= 0, ends, stage + DOp::BYTES);
+      for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + now[u] * a.dys + (col0 + place), a.outer - col0 - place, now[u] >= 0, over, stage);
+#pragma unroll
+      for (int u = 0; u < EACH; ++u) lx.fetch(u, x + now[u] * a.xs + (in0 + place), a.inner - in0 - place, now[u] >= 0, over, stage + DOp::BYTES);
+      coming += DEPTH;
+      --left;
+      return true;
     };
-    const auto step = [&](int s, char* now, char* then) {
-      meet<0>();
-      if (s + 1 < upto) {
-        fetch(then);
-        find_rows(s + 2);
+    const auto put = [&](char* stage) __attribute__((always_inline)) {
+      ld.store(stage);
+      lx.store(stage + DOp::BYTES);
+    };
+    // (in two phases, the waves of a SIMD a phase apart, as in row_tiles_kernel)
+    const auto half = [&](bool fresh, char* now, char* before) __attribute__((always_inline)) {
+      PieceV<T> fx[2][NR], fd[2][NN];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int n = 0; n < NN; ++n) fd[c][n] = rd.read(now, wn + n * 32, c);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) fx[c][r] = rx.read(now + DOp::BYTES, wr + r * 32, c);
       }
+      if (in0 == 0) {   // db: the column sums of what is in LDS anyway
 #pragma unroll
-      for (int c = 0; c < SLICES; ++c) {
-        PieceV<T> fx[NR], fd[NN];
+        for (int u = 0; u < EACH; ++u) {
+          const PieceV<T> v = *reinterpret_cast<const PieceV<T>*>(now + (u * THREADS + (int)threadIdx.x) * 16);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) fx[r] = rx.read(now + DOp::BYTES, wr + r * 32, c);
+          for (int i = 0; i < N; ++i) sum[i] += (float)v[i];
+        }
+      }
+      put(before);
+      const bool more = fetch(before);
+      if (!DIRECT || fresh) meet<-1>();
+      else if (more) meet<2 * LOADS>();
+      else meet<0>();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int n = 0; n < NN; ++n) fd[n] = rd.read(now, wn + n * 32, c);
+      for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fd[n], fx[r], acc[r][n]);
-      }
-      if (in0 == 0) {   // db: the column sums of what is in LDS anyway
-        const int col = (int)threadIdx.x % BN, part = (int)threadIdx.x / BN;
-        float v = 0.f;
-#pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-          const int at = part * EACH + k;
-          const int p = sizeof(T) == 2 ? (col / N) ^ ((at & 3) << 2) : col / N;
-          v += (float)*reinterpret_cast<const T*>(now + at * (BN * (int)sizeof(T)) + p * 16 + col % N * (int)sizeof(T));
-        }
-        sum += v;
-      }
-      if (s + 1 < upto) {
-        ld.store(then);
-        lx.store(then + DOp::BYTES);
-      }
+          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fd[c][n], fx[c][r], acc[r][n]);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      meet<-1>();
     };
-    __syncthreads();   // (the last tile's readers are through)
-    find_rows(first);
-    fetch(even);
-    find_rows(first + 1);
-    ld.store(even);
-    lx.store(even + DOp::BYTES);
-    for (int s = first; s < upto; s += 2) {
-      step(s, even, odd);
-      if (s + 1 < upto) step(s + 1, odd, even);
+    look_up(coming);
+    fetch(stage0);
+    put(stage0);
+    fetch(stage1);
+    put(stage1);
+    fetch(stage2);
+    put(stage2);
+    if (!DIRECT) fetch(stage3);
+    meet<0>();
+    const bool second = wave >= WR * WN / 2;
+    if (second) meet<-1>();
+    for (int s = 0; s < stages; s += 4) {
+      half(s == 0, stage0, stage3);
+      half(s == 0, stage1, stage0);
+      if (s + 2 < stages) {
+        half(false, stage2, stage1);
+        half(false, stage3, stage2);
+      }
     }
+    if (!second) meet<-1>();
+    const bool whole = first == 0 && upto == steps;
+    // slot 0: the group began in an earlier chunk; 1: it begins here and goes on in a later one
+    float* to = partial + ((int64_t)place_of * 2 + (first == 0)) * SLOT;
     if (in0 == 0) {
-      sums[threadIdx.x / BN][threadIdx.x % BN] = sum;
+#pragma unroll
+      for (int i = 0; i < N; ++i) sums[line][place + i] = sum[i];
       __syncthreads();
       if (threadIdx.x < BN) {
-        sum = 0.f;
+        float v = 0.f;
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) sum += sums[p][threadIdx.x];
+        for (int p = 0; p < LINES; ++p) v += sums[p][threadIdx.x];
+        if (!whole) to[BR * BN + threadIdx.x] = v;
+        else if (col0 + (int)threadIdx.x < a.outer) a.db[(int64_t)group * a.outer + col0 + threadIdx.x] = v;
       }
+      __syncthreads();
     }
-    if (first == 0 && upto == steps) {
+    if (whole) {
       T* dw = (T*)a.dw + (int64_t)group * a.inner * a.outer;
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -648,10 +684,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
             }
           }
       }
-      if (in0 == 0 && threadIdx.x < BN && col0 + (int)threadIdx.x < a.outer) a.db[(int64_t)group * a.outer + col0 + threadIdx.x] = sum;
     } else {
-      // slot 0: the tile began with an earlier workgroup; 1: it begins here and a later one goes on
-      float* to = partial + ((int64_t)blockIdx.x * 2 + (first == 0)) * SLOT;
 #pragma unroll
       for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -661,16 +694,15 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
             const float4 v = {acc[r][n][4 * p], acc[r][n][4 * p + 1], acc[r][n][4 * p + 2], acc[r][n][4 * p + 3]};
             reinterpret_cast<float4*>(to)[((r * NN + n) * 4 + p) * THREADS + threadIdx.x] = v;
           }
-      if (in0 == 0 && threadIdx.x < BN) to[BR * BN + threadIdx.x] = sum;
     }
     unit += upto - first;
     within += upto - first;
   }
 }
 
-// Adds up the sums of tiles that were cut, and clears the gradients of empty groups: a workgroup to a tile and 32 x 32 block of each wave
+// Adds up the sums of groups that were cut, and clears the gradients of empty ones: a workgroup to a tile and 32 x 32 block of each wave
 template <typename T, int BR, int BN, int WR, int WN>
-__global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, const float* partial, int wgs) {
+__global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, const float* partial, int most_chunks) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 128 / sizeof(T);
   constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -680,13 +712,13 @@ __global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, con
   const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
   int begin, end;
   const int steps = group_steps(a, group, DEPTH, &begin, &end);
-  int64_t first = 0, last = -1, from = 0;
+  int first = 0, last = -1;
   if (steps > 0) {
-    // where the tile's steps lie in the line: those of the groups before it first
-    int64_t mine = 0, all = 0;
+    // where the group's steps lie in the line: those of the groups before it first
+    int mine = 0, all = 0;
     for (int g = lane; g < a.groups; g += 64) {
       int b, e;
-      const int64_t own = (int64_t)group_steps(a, g, DEPTH, &b, &e) * tiles;
+      const int own = group_steps(a, g, DEPTH, &b, &e);
       all += own;
       if (g < group) mine += own;
     }
@@ -695,17 +727,16 @@ __global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, con
       all += __shfl_xor(all, o, 64);
       mine += __shfl_xor(mine, o, 64);
     }
-    from = mine + (int64_t)tile * steps;
-    const int64_t shares = all < wgs ? all : wgs;
-    first = ds_mm_even_owner(from, shares, all);
-    last = ds_mm_even_owner(from + steps - 1, shares, all);
+    const int chunks = min(all, most_chunks);
+    first = (int)ds_mm_even_owner(mine, chunks, all);
+    last = (int)ds_mm_even_owner(mine + steps - 1, chunks, all);
     if (first == last) return;
   }
   f32x16 v = {};
   float sum = 0.f;
   const bool with_sum = in0 == 0 && block == 0 && threadIdx.x < BN;
-  for (int64_t b = first; b <= last; ++b) {
-    const float* p = partial + (b * 2 + (b == first)) * SLOT;
+  for (int b = first; b <= last; ++b) {
+    const float* p = partial + (((int64_t)b * tiles + tile) * 2 + (b == first)) * SLOT;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float4 f = reinterpret_cast<const float4*>(p)[(block * 4 + q) * THREADS + threadIdx.x];
@@ -731,18 +762,33 @@ __global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, con
   if (with_sum && col0 + (int)threadIdx.x < a.outer) a.db[(int64_t)group * a.outer + col0 + threadIdx.x] = sum;
 }
 
-constexpr int kWeightGroups = 256;   // workgroups of the even cut
+// Chunks of the line of steps: as many as fill the compute units with every tile once, or twice where that leaves fewer of them idle in the last
+// round, but none of less than about 8 steps (512 rows of 16 bits), whose sums would cost more than they do.
+int chunks_of(int rows, int64_t tiles, int unit) {
+  constexpr int64_t kUnits = 256;
+  const auto idle = [&](int64_t p) { return (double)((p * tiles + kUnits - 1) / kUnits * kUnits) / (double)(p * tiles); };
+  const int64_t once = kUnits / tiles > 1 ? kUnits / tiles : 1, twice = 2 * kUnits / tiles > 1 ? 2 * kUnits / tiles : 1;
+  int64_t p = idle(twice) < 0.93 * idle(once) ? twice : once;
+  const int64_t most = rows / (8 * unit);
+  return (int)(p < most ? p : most > 1 ? most : 1);
+}
+
+template <typename T, int BR, int BN>
+int64_t weight_tiles(int inner, int outer) {
+  return (int64_t)((inner + BR - 1) / BR) * ((outer + BN - 1) / BN);
+}
 
 template <typename T, int BR, int BN, int WR, int WN>
 int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
   a.col_tiles = (a.outer + BN - 1) / BN;
-  const int64_t blocks = (int64_t)((a.inner + BR - 1) / BR) * a.col_tiles * (BR / WR / 32) * (BN / WN / 32);
-  if (blocks > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
+  const int64_t tiles = weight_tiles<T, BR, BN>(a.inner, a.outer), chunks = chunks_of(a.rows, tiles, 128 / (int)sizeof(T));
+  const int64_t wgs = (tiles * chunks + 7) / 8 * 8, blocks = tiles * (BR / WR / 32) * (BN / WN / 32);
+  if (wgs > 0x7fffffff || blocks > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
   const bool direct = sixteen(a.x, a.xs, sizeof(T)) && sixteen(a.dy, a.dys, sizeof(T)) && a.inner % Piece<T>::N == 0 && a.outer % Piece<T>::N == 0;
-  const dim3 block(64 * WR * WN);
-  if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true>), dim3(kWeightGroups), block, 0, ctx->stream, a, partial);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, false>), dim3(kWeightGroups), block, 0, ctx->stream, a, partial);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_join_kernel<T, BR, BN, WR, WN>), dim3((unsigned)blocks, a.groups), block, 0, ctx->stream, a, partial, kWeightGroups);
+  const dim3 grid((unsigned)wgs), block(64 * WR * WN);
+  if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, false>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_join_kernel<T, BR, BN, WR, WN>), dim3((unsigned)blocks, a.groups), block, 0, ctx->stream, a, partial, (int)chunks);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -763,13 +809,15 @@ int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a) {
   return transposed ? launch<_Float16, 256, 256, 2, 4, true>(ctx, a) : launch<_Float16, 256, 256, 2, 4, false>(ctx, a);
 }
 
-int64_t ds_weight_tiles_bytes(int dtype) {
+int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer) {
   const int64_t side = dtype == DS_ELEM_F32 ? 128 : 256;
-  return kWeightGroups * 2 * (side * side + side) * (int64_t)sizeof(float);
+  const int64_t tiles = dtype == DS_ELEM_F32 ? weight_tiles<float, 128, 128>(inner, outer) : weight_tiles<__bf16, 256, 256>(inner, outer);
+  const int64_t chunks = chunks_of(rows, tiles, dtype == DS_ELEM_F32 ? 32 : 64);
+  return chunks > 1 ? tiles * chunks * 2 * (side * side + side) * (int64_t)sizeof(float) : 0;
 }
 
 int ds_launch_weight_tiles(ds_ctx* ctx, int dtype, MmArgs& a, void* partial) {
-  if (dtype == DS_ELEM_F32) return launch_weights<float, 128, 128, 2, 2>(ctx, a, (float*)partial);
+  if (dtype == DS_ELEM_F32) return launch_weights<float, 128, 128, 2, 4>(ctx, a, (float*)partial);
   if (dtype == DS_ELEM_BF16) return launch_weights<__bf16, 256, 256, 2, 4>(ctx, a, (float*)partial);
   return launch_weights<_Float16, 256, 256, 2, 4>(ctx, a, (float*)partial);
 }
