@@ -85,45 +85,92 @@ struct Reader {
   }
 };
 
-// The last `have` (at most N) elements of 16 bytes, brought to the front, zeros behind them
+// without the first `by` (at most N) elements, zeros behind the others
 template <typename T>
-__device__ __forceinline__ PieceV<T> last_elements(PieceV<T> v, int have) {
+__device__ __forceinline__ PieceV<T> shifted(PieceV<T> v, unsigned by) {
   union {
     PieceV<T> piece;
     unsigned __int128 bits;
   } u;
   u.piece = v;
-  u.bits = have <= 0 ? 0 : u.bits >> (8 * (int)sizeof(T) * (Piece<T>::N - (have < Piece<T>::N ? have : Piece<T>::N)));
-  u.bits = have <= 0 ? 0 : u.bits;
+  u.bits = by >= Piece<T>::N ? 0 : u.bits >> (8 * (int)sizeof(T) * by);
   return u.piece;
 }
 
-// Brings pieces of an operand into LDS: piece u of thread t is piece number u * THREADS + t of the tile. Direct loads go there by
-// themselves; rows that are not aligned for them come through registers. A piece that reaches over its row's end is read as the row's last
-// 16 bytes and shifted: nothing outside of the row is read, element by element nothing either (rows have at least 16 bytes).
+// 16 bytes from p on; behind `end`, where the matrix ends, zeros, and nothing is read there. (A matrix has 16 bytes.)
+template <typename T>
+__device__ __forceinline__ PieceV<T> load_within(const T* p, const T* end) {
+  constexpr int N = Piece<T>::N;
+  const int64_t by = p + N - end;
+  const PieceV<T> v = *reinterpret_cast<const typename Piece<T>::U*>(by <= 0 ? p : end - N);
+  return by <= 0 ? v : shifted<T>(v, by < N ? (unsigned)by : N);
+}
+
+template <typename T>
+__device__ __forceinline__ PieceV<T> first_elements(PieceV<T> v, int have) {
+#pragma unroll
+  for (int i = 0; i < Piece<T>::N; ++i) v[i] = i < have ? v[i] : (T)0.f;
+  return v;
+}
+
+// the first `have` (1 to N - 1) elements
+template <typename T>
+__device__ __forceinline__ void store_first(T* p, PieceV<T> v, int have) {
+  constexpr int N = Piece<T>::N;
+  typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  typedef T Two __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+  if constexpr (N == 8) {
+    if (have & 4) {
+      *reinterpret_cast<Four*>(p) = Four{v[0], v[1], v[2], v[3]};
+      p += 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = v[i + 4];
+    }
+  }
+  if (have & 2) {
+    *reinterpret_cast<Two*>(p) = Two{v[0], v[1]};
+    p += 2;
+    v[0] = v[2];
+  }
+  if (have & 1) *p = v[0];
+}
+
+// Brings pieces of an operand into LDS: piece u of thread t is piece number u * THREADS + t of the stage. Direct loads go there by themselves;
+// rows that are not aligned for them come through registers.
 template <typename T, int STAGE_BYTES, int THREADS, bool DIRECT>
 struct Loader {
   static constexpr int N = Piece<T>::N, PIECES = STAGE_BYTES / 16 / THREADS;
   PieceV<T> held[DIRECT ? 1 : PIECES];
+  unsigned over = 0;   // four bits a piece: by how many elements it would reach over the matrix' end
 
-  // have: elements that there are from p to the row's end; there: whether there is such a row; ends: whether any lane has no whole piece
-  __device__ __forceinline__ void fetch(int u, const T* p, int have, bool there, bool ends, char* tile) {
+  // The piece at p, zeros if it is not `there`. Where columns end in it, what lies behind them comes along: the next row's, or what is between
+  // the rows, up to the matrix' `end`; it meets results only that nobody stores. (edge: whether any lane's piece may not be there
+  // or may reach over the end. One that would is read so that it ends there, and shifted on its way into LDS.)
+  __device__ __forceinline__ void fetch(int u, const T* p, bool there, bool edge, const T* end, char* stage) {
     const T* zeros = reinterpret_cast<const T*>(&kZeros);
-    if constexpr (DIRECT) {
-      const T* src = there && have > 0 ? p : zeros;
+    if constexpr (DIRECT) {   // (rows are whole pieces)
+      const T* src = there && p < end ? p : zeros;
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-      __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(tile + (u * THREADS + wave * 64) * 16), 16, 0, 0);
-    } else if (!ends) {
-      held[u] = *reinterpret_cast<const typename Piece<T>::U*>(p);
+      __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(stage + (u * THREADS + wave * 64) * 16), 16, 0, 0);
     } else {
-      const T* src = !there ? zeros : have >= N ? p : p + (have - N);
-      held[u] = last_elements<T>(*reinterpret_cast<const typename Piece<T>::U*>(src), there ? have : 0);
+      if (u == 0) over = 0;
+      if (edge) {
+        const int64_t by = there ? p + N - end : 0;
+        over |= (unsigned)(by <= 0 ? 0 : by < N ? by : N) << (4 * u);
+        p = !there ? zeros : by > 0 ? end - N : p;
+      }
+      held[u] = *reinterpret_cast<const typename Piece<T>::U*>(p);
     }
   }
-  __device__ __forceinline__ void store(char* tile) {
+  // into LDS; cut: of each piece its first `keep` elements alone (the contraction ends in it)
+  __device__ __forceinline__ void store(char* stage, bool cut, int keep) {
     if constexpr (!DIRECT) {
 #pragma unroll
-      for (int u = 0; u < PIECES; ++u) *reinterpret_cast<PieceV<T>*>(tile + (u * THREADS + (int)threadIdx.x) * 16) = held[u];
+      for (int u = 0; u < PIECES; ++u) {
+        if (__any(over >> (4 * u) & 15)) held[u] = shifted<T>(held[u], over >> (4 * u) & 15);
+        if (cut) held[u] = first_elements<T>(held[u], keep);
+        *reinterpret_cast<PieceV<T>*>(stage + (u * THREADS + (int)threadIdx.x) * 16) = held[u];
+      }
     }
   }
 };
@@ -224,7 +271,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
   const int width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
   const T* x = (const T*)(TRANSPOSED ? a.dy : a.x);
   const int64_t xs = TRANSPOSED ? a.dys : a.xs;
-  const T* gate = (const T*)a.gate;
+  const T *gate = (const T*)a.gate, *gate_end = gate + (int64_t)(a.rows - 1) * a.gs + width;
   T* y = (T*)a.y;
   // Workgroups go to the eight XCDs in turn. Each XCD has a stretch of the tiles, column tiles of a row tile next to each other, so that they
   // share its L2; its workgroups take them in turn.
@@ -235,6 +282,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
 
   Loader<T, XOp::BYTES, THREADS, DIRECT> lx;
   Loader<T, WOp::BYTES, THREADS, DIRECT> lw;
+  const T *x_end = x + (int64_t)(a.rows - 1) * xs + depth, *w_end = (const T*)a.w + (int64_t)a.groups * a.inner * a.outer;
   const Reader<T, BR, false, false, 64> rx(lane);
   const Reader<T, BN, !TRANSPOSED, true, 64> rw(lane);
   const int steps = (depth + 2 * DEPTH - 1) / (2 * DEPTH) * 2;   // stages of a tile, an even number (zeros behind the end)
@@ -278,13 +326,13 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
     const int k = coming * DEPTH;
     const bool deep = k + DEPTH > depth, wide = coming_col + BN > width;
 #pragma unroll
-    for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x[u] + k, depth - k - xk, true, deep, stage + WOp::BYTES);
+    for (int u = 0; u < lx.PIECES; ++u) lx.fetch(u, from_x[u] + k, k + xk < depth, deep, x_end, stage + WOp::BYTES);
 #pragma unroll
     for (int u = 0; u < lw.PIECES; ++u) {
       const int line = u * WLINES + wline;
       if constexpr (TRANSPOSED)
-        lw.fetch(u, from_w + (int64_t)(u * WLINES) * a.outer + k, depth - k - wplace, coming_col + line < width, deep || wide, stage);
-      else lw.fetch(u, from_w + (int64_t)(k + u * WLINES) * a.outer, width - coming_col - wplace, k + line < depth, deep || wide, stage);
+        lw.fetch(u, from_w + (int64_t)(u * WLINES) * a.outer + k, coming_col + line < width && k + wplace < depth, deep || wide, w_end, stage);
+      else lw.fetch(u, from_w + (int64_t)(k + u * WLINES) * a.outer, k + line < depth, deep || wide, w_end, stage);
     }
     if (++coming == steps) {
       coming = 0;
@@ -292,9 +340,11 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
     }
     return true;
   };
+  // what came through registers: the stage that was asked for last
   const auto put = [&](char* stage) __attribute__((always_inline)) {
-    lw.store(stage);
-    lx.store(stage + WOp::BYTES);
+    const int k = ((coming == 0 ? steps : coming) - 1) * DEPTH;
+    lw.store(stage, TRANSPOSED && k + DEPTH > depth, depth - k - wplace);
+    lx.store(stage + WOp::BYTES, k + DEPTH > depth, depth - k - xk);
   };
 
   if (at < stretch) {
@@ -357,7 +407,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
 #pragma unroll
               for (int i = 0; i < OUTS; ++i) {
                 const int to = rows[half * OUT_ROWS + i * AT_ONCE];
-                if (to >= 0 && c + N <= width) open[half][i] = *reinterpret_cast<const typename Piece<T>::U*>(gate + to * a.gs + c);
+                if (to >= 0 && c < width) open[half][i] = load_within<T>(gate + to * a.gs + c, gate_end);
               }
           }
         }
@@ -404,21 +454,14 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
             const int line = i * AT_ONCE + lane / CHUNKS, to = rows[half * OUT_ROWS + i * AT_ONCE];
             const char* held = mine + line * OUT_ROW + ((chunk ^ (line & 7)) << 4);
             if (to < 0 || c >= width) continue;
-            T* target = y + to * a.ys + c;
-            if (c + N <= width) {
-              PieceV<T> v = *reinterpret_cast<const PieceV<T>*>(held);
-              if (TRANSPOSED && gate) {
+            PieceV<T> v = *reinterpret_cast<const PieceV<T>*>(held);
+            if (TRANSPOSED && gate) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[j] = (float)open[half][i][j] > 0.f ? v[j] : (T)0.f;
-              }
-              *reinterpret_cast<typename Piece<T>::U*>(target) = v;
-            } else {
-#pragma unroll 1
-              for (int j = 0; j < width - c; ++j) {
-                const T v = reinterpret_cast<const T*>(held)[j];
-                target[j] = !TRANSPOSED || !gate || (float)gate[to * a.gs + c + j] > 0.f ? v : (T)0.f;
-              }
+              for (int j = 0; j < N; ++j) v[j] = (float)open[half][i][j] > 0.f ? v[j] : (T)0.f;
             }
+            T* target = y + to * a.ys + c;
+            if (c + N <= width) *reinterpret_cast<typename Piece<T>::U*>(target) = v;
+            else store_first<T>(target, v, width - c);
           }
         }
       }
@@ -545,6 +588,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   locate_unit(a, UNIT, unit, &group, &within);
   const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
+  const T *x_end = x + (int64_t)(a.rows - 1) * a.xs + a.inner, *dy_end = dy + (int64_t)(a.rows - 1) * a.dys + a.outer;
   const Reader<T, BR, true, false, 64> rx(lane);
   const Reader<T, BN, true, true, 64> rd(lane);
   static_assert(BR == BN && LINES % 4 == 0, "both operands' pieces of a thread lie in the same rows");
@@ -584,16 +628,16 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
       look_up(coming + DEPTH);   // (in front of the loads: a wait for it does not wait for them)
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + now[u] * a.dys + (col0 + place), a.outer - col0 - place, now[u] >= 0, over, stage);
+      for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + now[u] * a.dys + (col0 + place), now[u] >= 0, over, dy_end, stage);
 #pragma unroll
-      for (int u = 0; u < EACH; ++u) lx.fetch(u, x + now[u] * a.xs + (in0 + place), a.inner - in0 - place, now[u] >= 0, over, stage + DOp::BYTES);
+      for (int u = 0; u < EACH; ++u) lx.fetch(u, x + now[u] * a.xs + (in0 + place), now[u] >= 0, over, x_end, stage + DOp::BYTES);
       coming += DEPTH;
       --left;
       return true;
     };
     const auto put = [&](char* stage) __attribute__((always_inline)) {
-      ld.store(stage);
-      lx.store(stage + DOp::BYTES);
+      ld.store(stage, false, 0);
+      lx.store(stage + DOp::BYTES, false, 0);
     };
     // (in two phases, the waves of a SIMD a phase apart, as in row_tiles_kernel)
     const auto half = [&](bool fresh, char* now, char* before) __attribute__((always_inline)) {
