@@ -15,9 +15,6 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-template <typename T>
-using PieceV = typename Piece<T>::V;
-
 // d += a b on 16 x 16 with a lane's piece of both operands: lane l gives row (column) l % 16 and the contraction's indices
 // N (l / 16) .. + N - 1; d: column l % 16, rows 4 (l / 16) .. + 3.
 __device__ __forceinline__ f32x4 multiply(PieceV<__bf16> a, PieceV<__bf16> b, f32x4 d) {
@@ -41,9 +38,12 @@ constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 // columns of the result (TRANSPOSED false: N steps of the contraction by 8 columns to a lane) the lane turns its square of
 // elements around in registers; column j of the squares of 16 lanes is an operand, so that a lane ends up with N neighbouring columns of a
 // row. TRANSPOSED: the product with W^T, whose pieces are operands as they are.
-template <typename T, int RB, bool TRANSPOSED>
+// Loads have no branches, which they would be waited for at: a piece that reaches over its row's end brings the next row's elements along. Columns
+// that there are not lead to results that nobody stores; where the contraction ends, the last step clears them. A piece that would reach over
+// the matrix' end, which it can in its last N rows alone, is read so that it ends there, and shifted. (TINY: matrices of less than 16 bytes, element by element.)
+template <typename T, int RB, bool TRANSPOSED, bool TINY>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
-  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
+  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6, STEP = kWaves * 4 * N;
   __shared__ float meet[kWaves][4][64][N];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
@@ -58,22 +58,61 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
   const int64_t xs = TRANSPOSED ? a.dys : a.xs;
   const T* x = (const T*)(TRANSPOSED ? a.dy : a.x);
   if (gt.group < a.groups) {
-    const T* w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer;
+    const T *w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer, *w_end = (const T*)a.w + (int64_t)a.groups * a.inner * a.outer;
+    const T* x_end = x + (int64_t)(a.rows - 1) * xs + depth;
     const int n0 = col + N * m;   // the lane's columns
     PieceV<T> wp[N], xp[RB];
+    const auto over = [](const T* p, const T* end) -> unsigned {
+      const int64_t by = p + N - end;
+      return by <= 0 ? 0 : by < N ? (unsigned)by : N;
+    };
+    const auto w_at = [&](int k, int i) -> const T* {
+      if constexpr (TRANSPOSED) return w + (int64_t)min(n0 + i, width - 1) * a.outer + min(k, depth - 1);
+      else return w + (int64_t)min(k + i, depth - 1) * a.outer + min(n0, width - 1);
+    };
+    const auto x_at = [&](int k, int r) -> const T* { return x + (row[r] < 0 ? 0 : row[r]) * xs + min(k, depth - 1); };
     const auto fetch = [&](int k) {
       k += N * q;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if constexpr (TRANSPOSED) wp[i] = load_piece<T>(w + (int64_t)(n0 + i) * a.outer + k, n0 + i < width ? depth - k : 0);
-        else wp[i] = load_piece<T>(w + (int64_t)(k + i) * a.outer + n0, k + i < depth ? width - n0 : 0);
+        if constexpr (TINY) {
+          if constexpr (TRANSPOSED) wp[i] = load_piece<T>(w + (int64_t)(n0 + i) * a.outer + k, n0 + i < width ? depth - k : 0);
+          else wp[i] = load_piece<T>(w + (int64_t)(k + i) * a.outer + n0, k + i < depth ? width - n0 : 0);
+        } else {
+          const T* p = w_at(k, i);
+          wp[i] = *reinterpret_cast<const typename Piece<T>::U*>(p + N <= w_end ? p : w_end - N);
+        }
       }
 #pragma unroll
-      for (int r = 0; r < RB; ++r) xp[r] = load_piece<T>(x + row[r] * xs + k, row[r] >= 0 ? depth - k : 0);
+      for (int r = 0; r < RB; ++r) {
+        if constexpr (TINY) {
+          xp[r] = load_piece<T>(x + row[r] * xs + k, row[r] >= 0 ? depth - k : 0);
+        } else {
+          const T* p = x_at(k, r);
+          xp[r] = *reinterpret_cast<const typename Piece<T>::U*>(p + N <= x_end ? p : x_end - N);
+        }
+      }
+    };
+    // near the contraction's end: what lies behind it
+    const auto clear = [&](int k) {
+      k += N * q;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const unsigned by = over(w_at(k, i), w_end);
+        if (__any(by)) wp[i] = shifted<T>(wp[i], by);
+        wp[i] = first_elements<T>(wp[i], TRANSPOSED ? depth - k : k + i < depth ? N : 0);
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        const unsigned by = over(x_at(k, r), x_end);
+        if (__any(by)) xp[r] = shifted<T>(xp[r], by);
+        xp[r] = first_elements<T>(xp[r], depth - k);
+      }
     };
     int k = wave * 4 * N;
     if (k < depth) fetch(k);
     while (k < depth) {
+      if (!TINY && k + 5 * N > depth) clear(k);
       PieceV<T> wn[N], xn[RB];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -86,7 +125,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
       }
 #pragma unroll
       for (int r = 0; r < RB; ++r) xn[r] = xp[r];
-      k += kWaves * 4 * N;
+      k += STEP;
       if (k < depth) fetch(k);
 #pragma unroll
       for (int j = 0; j < N; ++j)
@@ -94,14 +133,22 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
         for (int r = 0; r < RB; ++r) acc[r][j] = multiply(wn[j], xn[r], acc[r][j]);
     }
   }
-  const T* gate = (const T*)a.gate;
+  const T *gate = (const T*)a.gate, *gate_end = gate + (int64_t)(a.rows - 1) * a.gs + width;
   T* y = (T*)a.y;
   // wave w ends up with the four columns' quarter w of every row block: columns col + N (4 q + w) .. + N - 1
   const int n = col + N * (4 * q + wave);
   float bias[N];
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    bias[j] = a.bias && gt.group < a.groups && n + j < width ? a.bias[(int64_t)gt.group * width + n + j] : 0.f;
+    bias[j] = !TRANSPOSED && a.bias && gt.group < a.groups ? a.bias[(int64_t)gt.group * width + min(n + j, width - 1)] : 0.f;
+  PieceV<T> open[RB];
+  if (TRANSPOSED && gate) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      if constexpr (TINY) open[r] = load_piece<T>(gate + row[r] * a.gs + n, row[r] >= 0 ? width - n : 0);
+      else open[r] = load_within<T>(gate + (row[r] < 0 ? 0 : row[r]) * a.gs + min(n, width - 1), gate_end);
+    }
+  }
 #pragma unroll
   for (int r = 0; r < RB; ++r) {
     if (r) __syncthreads();
@@ -110,29 +157,32 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
 #pragma unroll
       for (int j = 0; j < N; ++j) meet[wave][i][lane][j] = acc[r][j][i];
     __syncthreads();
-    if (row[r] >= 0) {
+    if (row[r] >= 0 && n < width) {
       PieceV<T> out;
-      const PieceV<T> open = gate ? load_piece<T>(gate + row[r] * a.gs + n, width - n) : PieceV<T>{};
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         float v = bias[j];
 #pragma unroll
         for (int s = 0; s < kWaves; ++s) v += meet[s][wave][lane][j];
-        if (a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
-        if (gate) v = (float)open[j] > 0.f ? v : 0.f;
+        if (!TRANSPOSED && a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
+        if (TRANSPOSED && gate) v = (float)open[r][j] > 0.f ? v : 0.f;
         out[j] = (T)v;
       }
-      store_piece<T>(y + row[r] * a.ys + n, out, width - n);
+      T* to = y + row[r] * a.ys + n;
+      if (n + N <= width) *reinterpret_cast<typename Piece<T>::U*>(to) = out;
+      else store_first<T>(to, out, width - n);
     }
   }
 }
 
 // dW and db of a group: 16 N outer by 8 N inner columns to a workgroup, the waves share the group's rows. Both operands
-// run across the contraction (the rows), so both are turned around in registers. db is one more product, with ones for x.
-template <typename T>
+// run across the contraction (the rows), so both are turned around in registers. db is one more product, with ones for x. The rows
+// of the next step are looked up, and those of this one's are on their way, while the products of the one before are formed.
+template <typename T, bool TINY>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a) {
-  constexpr int N = Piece<T>::N, H = N / 2;
-  typedef T Half __attribute__((ext_vector_type(H), aligned(sizeof(T))));
+  constexpr int N = Piece<T>::N, H = N / 2, STEP = kWaves * 4 * N;
+  typedef T Half __attribute__((ext_vector_type(H)));
+  typedef T HalfU __attribute__((ext_vector_type(H), aligned(sizeof(T))));
   __shared__ float meet[kWaves][4][64][N];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int group = (int)blockIdx.y;
@@ -140,33 +190,82 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
   int begin, end;
   ds_group_range(a.offsets, a.groups, a.rows, group, &begin, &end);
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
-  const int n0 = col + N * m, c0 = in0 + H * m;
+  const T *x_end = x + (int64_t)(a.rows - 1) * a.xs + a.inner, *dy_end = dy + (int64_t)(a.rows - 1) * a.dys + a.outer;
+  const int n0 = min(col + N * m, a.outer - 1), c0 = min(in0 + H * m, a.inner - 1);   // the lane's columns
   f32x4 acc[H][N] = {}, sum[N] = {};
   PieceV<T> ones;
 #pragma unroll
   for (int i = 0; i < N; ++i) ones[i] = (T)1.f;
   const bool with_sum = in0 == 0;
-  for (int at = begin + wave * 4 * N; at < end; at += kWaves * 4 * N) {
-    PieceV<T> dp[N], dn[N], xn[H];
+  int row[N], late[N];   // of the pieces under way, and of the next ones
+  PieceV<T> dp[N];
+  Half xp[N];
+  const auto look_up = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) late[i] = at + N * q + i < end ? ds_ordered_row(a.order, a.rows, at + N * q + i) : -1;
+  };
+  const auto fetch = [&]() {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int pos = at + N * q + i, row = pos < end ? ds_ordered_row(a.order, a.rows, pos) : -1;
-      dp[i] = load_piece<T>(dy + row * a.dys + n0, row >= 0 ? a.outer - n0 : 0);
-      const T* px = x + row * a.xs + c0;
-      const int have = row >= 0 ? a.inner - c0 : 0;
-      if (have >= H) {
-        const Half h = *reinterpret_cast<const Half*>(px);
+      row[i] = late[i];
+      if constexpr (TINY) {
+        dp[i] = load_piece<T>(dy + row[i] * a.dys + col + N * m, row[i] >= 0 ? a.outer - col - N * m : 0);
+        const int have = row[i] >= 0 ? a.inner - in0 - H * m : 0;
 #pragma unroll
-        for (int j = 0; j < H; ++j) xn[j][i] = h[j];
+        for (int j = 0; j < H; ++j) xp[i][j] = j < have ? x[row[i] * a.xs + in0 + H * m + j] : (T)0.f;
       } else {
+        const int r = row[i] < 0 ? 0 : row[i];
+        const T *pd = dy + r * a.dys + n0, *px = x + r * a.xs + c0;
+        dp[i] = *reinterpret_cast<const typename Piece<T>::U*>(pd + N <= dy_end ? pd : dy_end - N);
+        xp[i] = *reinterpret_cast<const HalfU*>(px + H <= x_end ? px : x_end - H);
+      }
+    }
+  };
+  int at = begin + wave * 4 * N;
+  if (at < end) {
+    look_up(at);
+    fetch();
+    if (at + STEP < end) look_up(at + STEP);
+  }
+  for (; at < end; at += STEP) {
+    PieceV<T> dn[N], xn[H];
+    if constexpr (!TINY) {
 #pragma unroll
-        for (int j = 0; j < H; ++j) xn[j][i] = j < have ? px[j] : (T)0.f;
+      for (int i = 0; i < N; ++i) {
+        // (rows that there are not are cleared; pieces that would reach over the end have been read so that they end there)
+        const int r = row[i] < 0 ? 0 : row[i];
+        const int64_t by = dy + r * a.dys + n0 + N - dy_end, bx = x + r * a.xs + c0 + H - x_end;
+        if (__any(by > 0)) dp[i] = shifted<T>(dp[i], by <= 0 ? 0 : by < N ? (unsigned)by : N);
+        if (__any(bx > 0)) {
+          Half moved = xp[i];
+#pragma unroll
+          for (int s = 1; s <= H; ++s)
+            if (bx >= s) {
+#pragma unroll
+              for (int j = 0; j + 1 < H; ++j) moved[j] = moved[j + 1];
+              moved[H - 1] = (T)0.f;
+            }
+          xp[i] = moved;
+        }
+        if (row[i] < 0) {
+          dp[i] = PieceV<T>{};
+          xp[i] = Half{};
+        }
       }
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
+    for (int i = 0; i < N; ++i) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) dn[j][i] = dp[i][j];
+      for (int j = 0; j < N; ++j) dn[j][i] = dp[i][j];
+#pragma unroll
+      for (int j = 0; j < H; ++j) xn[j][i] = xp[i][j];
+    }
+    if (at + STEP < end) {
+      fetch();
+      if (at + 2 * STEP < end) look_up(at + 2 * STEP);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
 #pragma unroll
       for (int h = 0; h < H; ++h) acc[h][j] = multiply(dn[j], xn[h], acc[h][j]);
       if (with_sum) sum[j] = multiply(dn[j], ones, sum[j]);
@@ -194,7 +293,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
       PieceV<T> out;
 #pragma unroll
       for (int j = 0; j < N; ++j) out[j] = (T)v[j];
-      if (c0 + h < a.inner) store_piece<T>(dw + (int64_t)(c0 + h) * a.outer + n, out, a.outer - n);
+      const int in = in0 + H * m + h;
+      if (in < a.inner && n < a.outer) {
+        T* to = dw + (int64_t)in * a.outer + n;
+        if (n + N <= a.outer) *reinterpret_cast<typename Piece<T>::U*>(to) = out;
+        else store_first<T>(to, out, a.outer - n);
+      }
     } else if (m == 0) {   // (every column of the product with ones is the sum)
 #pragma unroll
       for (int j = 0; j < N; ++j)
@@ -218,6 +322,12 @@ MmArgs arguments(const ds_grouped& p) {
 // (the tiles' loads need rows of 16 bytes at the least)
 bool many_rows(const ds_grouped& p) { return p.rows / p.groups > 64 && p.inner >= 8 && p.outer >= 8; }
 
+// whether a matrix has less than 16 bytes from its first element to its last
+template <typename T>
+bool tiny_matrix(int64_t stride, int64_t rows, int64_t cols) {
+  return (rows - 1) * stride + cols < Piece<T>::N;
+}
+
 template <typename T>
 int element_of() {
   return sizeof(T) == 4 ? DS_ELEM_F32 : std::is_same<T, __bf16>::value ? DS_ELEM_BF16 : DS_ELEM_F16;
@@ -235,9 +345,13 @@ int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
   if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
   const dim3 grid((unsigned)tiles), block(64 * kWaves);
-  if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, TRANSPOSED>), grid, block, 0, stream, a);
-  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, TRANSPOSED>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, TRANSPOSED>), grid, block, 0, stream, a);
+  // (rows of at least 16 bytes each would not be enough to ask for: an operand may have one row)
+  const bool tiny = tiny_matrix<T>(TRANSPOSED ? a.dys : a.xs, p.rows, TRANSPOSED ? p.outer : p.inner) ||
+                    tiny_matrix<T>((int64_t)p.inner * p.outer, p.groups, (int64_t)p.inner * p.outer) || (a.gate && tiny_matrix<T>(a.gs, p.rows, p.inner));
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, TRANSPOSED, true>), dim3((unsigned)(ds_most_tiles(a, 6) * a.col_tiles)), block, 0, stream, a);
+  else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, TRANSPOSED, false>), grid, block, 0, stream, a);
+  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, TRANSPOSED, false>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, TRANSPOSED, false>), grid, block, 0, stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -247,7 +361,9 @@ int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   constexpr int N = Piece<T>::N;
   a.col_tiles = (p.outer + 16 * N - 1) / (16 * N);
   const dim3 grid((unsigned)(((p.inner + 8 * N - 1) / (8 * N)) * a.col_tiles), p.groups), block(64 * kWaves);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T>), grid, block, 0, ctx->stream, a);
+  const bool tiny = tiny_matrix<T>(a.xs, p.rows, p.inner) || tiny_matrix<T>(a.dys, p.rows, p.outer);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true>), grid, block, 0, ctx->stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, false>), grid, block, 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }

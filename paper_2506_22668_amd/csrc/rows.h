@@ -53,6 +53,59 @@ __device__ __forceinline__ void store_piece(T* p, typename Piece<T>::V v, int ha
     if (i < have) p[i] = v[i];
 }
 
+template <typename T>
+using PieceV = typename Piece<T>::V;
+
+// without the first `by` (at most N) elements, zeros behind the others
+template <typename T>
+__device__ __forceinline__ PieceV<T> shifted(PieceV<T> v, unsigned by) {
+  union {
+    PieceV<T> piece;
+    unsigned __int128 bits;
+  } u;
+  u.piece = v;
+  u.bits = by >= Piece<T>::N ? 0 : u.bits >> (8 * (int)sizeof(T) * by);
+  return u.piece;
+}
+
+// 16 bytes from p on; behind `end`, where the matrix ends, zeros, and nothing is read there. (A matrix has 16 bytes.)
+template <typename T>
+__device__ __forceinline__ PieceV<T> load_within(const T* p, const T* end) {
+  constexpr int N = Piece<T>::N;
+  const int64_t by = p + N - end;
+  const PieceV<T> v = *reinterpret_cast<const typename Piece<T>::U*>(by <= 0 ? p : end - N);
+  return by <= 0 ? v : shifted<T>(v, by < N ? (unsigned)by : N);
+}
+
+template <typename T>
+__device__ __forceinline__ PieceV<T> first_elements(PieceV<T> v, int have) {
+#pragma unroll
+  for (int i = 0; i < Piece<T>::N; ++i) v[i] = i < have ? v[i] : (T)0.f;
+  return v;
+}
+
+// the first `have` (1 to N - 1) elements
+template <typename T>
+__device__ __forceinline__ void store_first(T* p, PieceV<T> v, int have) {
+  constexpr int N = Piece<T>::N;
+  typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  typedef T Two __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+  if constexpr (N == 8) {
+    if (have & 4) {
+      *reinterpret_cast<Four*>(p) = Four{v[0], v[1], v[2], v[3]};
+      p += 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = v[i + 4];
+    }
+  }
+  if (have & 2) {
+    *reinterpret_cast<Two*>(p) = Two{v[0], v[1]};
+    p += 2;
+    v[0] = v[2];
+  }
+  if (have & 1) *p = v[0];
+}
+
 template <int CTRL>
 __device__ __forceinline__ float add_across(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));

@@ -382,6 +382,33 @@ def test_grouped_mm_backward(ctx, t, rows, inner, outer, groups):
         assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), again))
 
 
+# widths below a 16-byte piece, contractions that end right behind a step, matrices of less than 16 bytes
+NARROW = [(3, 1, 1, 1), (1, 1, 2, 1), (2, 3, 1, 2), (40, 33, 3, 2), (40, 3, 33, 2), (90, 65, 1, 1), (90, 1, 65, 1), (700, 40, 5, 3), (700, 5, 40, 3),
+          (300, 34, 9, 1), (200, 129, 130, 2), (1, 33, 7, 1), (33, 128, 7, 1), (600, 8, 8, 2), (600, 9, 15, 2)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", NARROW)
+def test_grouped_mm_narrow(ctx, t, rows, inner, outer, groups):
+    say(f"narrow {t} rows={rows} inner={inner} outer={outer} groups={groups}")
+    test_grouped_mm(ctx, t, rows, inner, outer, groups)
+    test_grouped_mm_backward(ctx, t, rows, inner, outer, groups)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows", [1, 7, 100, 1000])
+def test_grouped_mm_of_one_row_for_all(ctx, t, rows):
+    """Rows that lie nowhere apart (an expanded row): their last piece is the buffer's last."""
+    say(f"expanded {t} rows={rows}")
+    g = generator(rows)
+    for inner, outer in [(37, 45), (64, 264)]:
+        x, dy, w = normal(g, 1, inner, t=t).expand(rows, inner), normal(g, 1, outer, t=t).expand(rows, outer), normal(g, 1, inner, outer, t=t)
+        offsets = torch.tensor([0, rows], device="cuda")
+        assert torch.equal(ctx.grouped_mm(x, w, offsets), ctx.grouped_mm(x.contiguous(), w, offsets))
+        got, want = ctx.grouped_mm_backward(dy, x, w, offsets, gate=x), ctx.grouped_mm_backward(dy.contiguous(), x.contiguous(), w, offsets, gate=x.contiguous())
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("t", TYPES)
 def test_grouped_mm_without_rows(ctx, t):
     say(f"grouped_mm without rows {t}")
