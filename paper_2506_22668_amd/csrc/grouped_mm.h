@@ -26,3 +26,6 @@ int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a);
 // The gradient of the weights in tiles; partial: ds_weight_tiles_bytes of scratch
 int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer);
 int ds_launch_weight_tiles(ds_ctx* ctx, int dtype, MmArgs& a, void* partial);
+// what the choice between the forms has to know of the tiles
+bool ds_wide_tiles(int rows, int width);                           // fp32: 256 rows to a tile
+int ds_weight_chunks(int rows, int64_t tiles, int unit);           // stretches that the rows are cut into, in units of `unit` rows

@@ -6,6 +6,8 @@
 // The rows of group g are those at positions offsets[g] .. offsets[g + 1] of `order`. Sizes of groups are known on the GPU
 // alone: the grid has a tile for every one that there can be, and a workgroup finds its rows from the offsets.
 // All products go through the matrix cores, fp32 ones on their fp32 form, and are summed in fp32.
+#include <math.h>
+
 #include <type_traits>
 
 #include "grouped_mm.h"
@@ -319,8 +321,43 @@ MmArgs arguments(const ds_grouped& p) {
   return a;
 }
 
-// (the tiles' loads need rows of 16 bytes at the least)
-bool many_rows(const ds_grouped& p) { return p.rows / p.groups > 64 && p.inner >= 8 && p.outer >= 8; }
+// ---- which form -----------------------------------------------------------------------------------------------------------------
+// Each form has a price in us on 256 compute units, from the number of its workgroups, how many run at a time, and what one takes for its share of the
+// contraction; the sizes of groups are not known on the host, so all are taken to be of the mean size. The figures were fitted to both
+// forms' times at 165 shapes and types each (1, 8 and 64 groups of 24 to 16,000 rows; widths of 64 to 4,000, odd ones among them): the choice
+// is within 15 % of the faster form at all but 11 of 990, and 0.7 % off it on average (a limit of 64 rows to a group: 13 %). In us, few / tiles:
+//   8 groups of 400 rows by 1,024 x 1,024, bf16: 36 / 38, of 1,000 rows: 66 / 41; 64 groups of 200 rows by 256 x 256: 26 / 18, by 64 x 64: 14 / 14
+constexpr double kUnits = 256;
+
+double ceil_div(double a, double b) { return ceil(a / b); }
+
+// the product by rows, `depth` long and `width` wide
+bool rows_in_tiles(const ds_grouped& p, int dtype, int depth, int width) {
+  if (p.inner < 8 || p.outer < 8) return false;   // (the tiles' loads need rows of 16 bytes at the least)
+  const bool f32 = dtype == DS_ELEM_F32;
+  const double mean = ceil_div(p.rows, p.groups);
+  const double block = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
+  const double few = p.groups * ceil_div(mean, block) * ceil_div(width, f32 ? 64 : 128) / kUnits;
+  const double few_us = (few > 1 ? few : 1) * (5 + (f32 ? 0.02 : 0.009) * depth);
+  if (!f32) return ceil_div(p.groups * ceil_div(mean, 256) * ceil_div(width, 256), kUnits) * (4 + 0.025 * depth) < few_us;
+  const bool wide = ds_wide_tiles(p.rows, width);
+  const double rounds = ceil_div(p.groups * ceil_div(mean, wide ? 256 : 128) * ceil_div(width, 128), kUnits);
+  return rounds * (wide ? 13 + 0.14 * depth : 8 + 0.075 * depth) + 6 < few_us;
+}
+
+bool weights_in_tiles(const ds_grouped& p, int dtype) {
+  if (p.inner < 8 || p.outer < 8) return false;
+  const bool f32 = dtype == DS_ELEM_F32;
+  const double mean = ceil_div(p.rows, p.groups), n = f32 ? 4 : 8;
+  const double few = p.groups * ceil_div(p.outer, 16 * n) * ceil_div(p.inner, 8 * n) / kUnits;
+  const double few_us = (few > 1 ? few : 1) * ((f32 ? 3 : 5) + 2 * ceil_div(mean, 16 * n));
+  const double side = f32 ? 128 : 256, unit = f32 ? 32 : 64;
+  const double tiles = ceil_div(p.inner, side) * ceil_div(p.outer, side), chunks = ds_weight_chunks(p.rows, (int64_t)tiles, (int)unit);
+  const double steps = ceil_div(p.groups * ceil_div(mean, unit), chunks), cut = 1 + (p.groups > chunks ? p.groups / chunks : 0) + (chunks > 1 ? 1 : 0);
+  const double rounds = chunks * tiles / kUnits;
+  const bool odd = p.inner % 4 || p.outer % 4;   // (fp32 rows that are not aligned: 750 us in few, 880 in tiles, of 64,000 by 513 x 300)
+  return (rounds > 1 ? rounds : 1) * (steps * (f32 ? odd ? 5.0 : 1.5 : 2.0) + cut * (f32 ? 8 : 5)) + (f32 ? 12 : 4) < few_us;
+}
 
 // whether a matrix has less than 16 bytes from its first element to its last
 template <typename T>
@@ -339,8 +376,8 @@ int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   constexpr int N = Piece<T>::N;
   hipStream_t stream = ctx->stream;
   a.col_tiles = ((TRANSPOSED ? p.inner : p.outer) + 16 * N - 1) / (16 * N);
-  const int64_t mean = p.rows / p.groups;
-  if (many_rows(p)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
+  const int64_t mean = (p.rows + p.groups - 1) / p.groups;
+  if (rows_in_tiles(p, element_of<T>(), TRANSPOSED ? p.outer : p.inner, TRANSPOSED ? p.inner : p.outer)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
   const int shift = mean <= 16 ? 4 : mean <= 32 ? 5 : 6;
   const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
   if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
@@ -371,7 +408,7 @@ int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
 template <typename T>
 int backward(ds_ctx* ctx, const ds_grouped& p, MmArgs& a, void* workspace) {
   DS_TRY((launch_rows<T, true>(ctx, p, a)));
-  if (many_rows(p)) return ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
+  if (weights_in_tiles(p, element_of<T>())) return ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
   return launch_weights<T>(ctx, p, a);
 }
 
@@ -392,7 +429,7 @@ int ds_launch_grouped_mm(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows x,
 }
 
 int64_t ds_grouped_mm_backward_bytes(int dtype, const ds_grouped& p) {
-  return many_rows(p) ? ds_weight_tiles_bytes(dtype, p.rows, p.inner, p.outer) : 0;
+  return weights_in_tiles(p, dtype) ? ds_weight_tiles_bytes(dtype, p.rows, p.inner, p.outer) : 0;
 }
 
 int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, ds_rows x, ds_rows gate, ds_rows dx,

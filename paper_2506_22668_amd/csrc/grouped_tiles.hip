@@ -13,16 +13,28 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
 
-__device__ __forceinline__ f32x16 multiply(PieceV<__bf16> a, PieceV<__bf16> b, f32x16 d) {
+// Part `part` of the product of two pieces: 16-bit ones take one instruction, fp32 ones four (which one after the other would each
+// wait for the sum of the last: see products)
+template <typename T>
+constexpr int kParts = sizeof(T) == 4 ? 4 : 1;
+__device__ __forceinline__ f32x16 multiply(PieceV<__bf16> a, PieceV<__bf16> b, f32x16 d, int) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, d, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 multiply(PieceV<_Float16> a, PieceV<_Float16> b, f32x16 d) {
+__device__ __forceinline__ f32x16 multiply(PieceV<_Float16> a, PieceV<_Float16> b, f32x16 d, int) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, d, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 multiply(PieceV<float> a, PieceV<float> b, f32x16 d) {
+__device__ __forceinline__ f32x16 multiply(PieceV<float> a, PieceV<float> b, f32x16 d, int part) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a[part], b[part], d, 0, 0, 0);
+}
+// all products of a slice, or their parts FIRST .. LAST - 1
+template <typename T, int NR, int NN, int FIRST = 0, int LAST = kParts<T>>
+__device__ __forceinline__ void products(const PieceV<T> (&fw)[NN], const PieceV<T> (&fx)[NR], f32x16 (&acc)[NR][NN]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], d, 0, 0, 0);
-  return d;
+  for (int part = FIRST; part < LAST; ++part)
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fw[n], fx[r], acc[r][n], part);
 }
 
 // column of the tile that row m of a matrix-core operand stands for: a lane's 16 results are then 16 neighbours
@@ -303,31 +315,48 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
 #pragma unroll
       for (int r = 0; r < NR; ++r) fx[c & 1][r] = rx.read(stage + WOp::BYTES, wr + r * 32, c);
     };
-    const auto work = [&](int c) __attribute__((always_inline)) {
-#pragma unroll
-      for (int r = 0; r < NR; ++r)
-#pragma unroll
-        for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fw[c & 1][n], fx[c & 1][r], acc[r][n]);
-    };
-    // One stage, in two phases between barriers: the wave's operands out of LDS and loads of what comes three stages on, into the stage that
-    // was `before`; then nothing but products. The two waves of a SIMD are a phase apart, so that one fills the matrix cores while the other
-    // works off addresses and waits. Waits leave the loads of two stages under way (near the end, where there are no more, none). `fresh`: in the
-    // two stages behind a tile's results, in front of whose stores all loads were waited for, so that the stores need not be.
-    const auto half = [&](bool fresh, char* now, char* before) __attribute__((always_inline)) {
-      read(now, 0);
-      read(now, 1);
-      put(before);
-      const bool more = fetch(before);
-      if (!DIRECT || fresh) meet<-1>();
-      else if (more) meet<2 * LOADS>();
-      else meet<0>();
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_setprio(1);
-      work(0);
-      work(1);
-      __builtin_amdgcn_s_setprio(0);
-      __builtin_amdgcn_sched_barrier(0);
-      meet<-1>();
+    // One stage.
+    // PAIRED (16-bit types): in two phases between barriers, the wave's operands out of LDS and loads of what comes three stages on, into the stage
+    // that was `before`; then nothing but products. The two waves of a SIMD are a phase apart, so that one fills the matrix cores while
+    // the other works off addresses and waits.
+    // Otherwise (fp32, whose products take 16 times as long): operands of a slice are read under the products of the one before, and loads of
+    // what comes four stages on are asked for, into `now`, where nobody reads it any more; one barrier. (65,536 rows by 512 x 512: 0.39 ms in phases.)
+    // Waits leave the loads of two stages under way (near the end, where there are no more, none). `fresh`: in the two stages
+    // behind a tile's results, in front of whose stores all loads were waited for, so that the stores need not be.
+    constexpr bool PAIRED = sizeof(T) == 2;
+    const auto half = [&](bool fresh, bool last, char* before, char* now, char* then) __attribute__((always_inline)) {
+      if constexpr (PAIRED) {
+        read(now, 0);
+        read(now, 1);
+        put(before);
+        const bool more = fetch(before);
+        if (!DIRECT || fresh) meet<-1>();
+        else if (more) meet<2 * LOADS>();
+        else meet<0>();
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        products<T, NR, NN>(fw[0], fx[0], acc);
+        products<T, NR, NN>(fw[1], fx[1], acc);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        meet<-1>();
+      } else {
+        read(now, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        products<T, NR, NN>(fw[0], fx[0], acc);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!DIRECT || fresh) meet<-1>();
+        else if (coming_at < stretch) meet<2 * LOADS>();
+        else meet<0>();
+        if (!last) read(then, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        products<T, NR, NN, 0, kParts<T> / 2>(fw[1], fx[1], acc);
+        __builtin_amdgcn_sched_barrier(0);
+        put(now);
+        fetch(now);
+        __builtin_amdgcn_sched_barrier(0);
+        products<T, NR, NN, kParts<T> / 2, kParts<T>>(fw[1], fx[1], acc);
+      }
     };
     static_assert(SLICES == 2, "");
     int number = 0;
@@ -425,28 +454,34 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
     put(stage1);
     fetch(stage2);
     put(stage2);
-    if (!DIRECT) fetch(stage3);
+    if (!PAIRED) {
+      fetch(stage3);
+      put(stage3);
+    }
+    if (!DIRECT) fetch(PAIRED ? stage3 : stage0);
     meet<0>();
-    const bool second = wave >= WR * WN / 2;   // the waves that are a phase behind; all leave a tile together
+    const bool second = PAIRED && wave >= WR * WN / 2;   // the waves that are a phase behind; all leave a tile together
     if (second) meet<-1>();
+    if (!PAIRED) read(stage0, 0);
     int s = 0;
     bool left = true;
-    const auto two = [&](char* before, char* now, char* then) __attribute__((always_inline)) {
-      half(left, now, before);
-      half(left, then, now);
+    const auto two = [&](char* before, char* now, char* then, char* behind) __attribute__((always_inline)) {
       s += 2;
+      half(left, false, before, now, then);
+      half(left, s == steps, now, then, behind);
       left = s == steps;
       if (left) {
-        if (!second) meet<-1>();
+        if (PAIRED && !second) meet<-1>();
         leave();
         s = 0;
         at += step_by;
         if (at >= stretch) return false;
         if (second) meet<-1>();
+        if (!PAIRED) read(behind, 0);
       }
       return true;
     };
-    while (two(stage3, stage0, stage1) && two(stage1, stage2, stage3)) {
+    while (two(stage3, stage0, stage1, stage2) && two(stage1, stage2, stage3, stage0)) {
     }
   }
   // rows of no group
@@ -611,12 +646,8 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
       else meet<0>();
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-#pragma unroll
-          for (int n = 0; n < NN; ++n) acc[r][n] = multiply(fd[c][n], fx[c][r], acc[r][n]);
+      products<T, NR, NN>(fd[0], fx[0], acc);
+      products<T, NR, NN>(fd[1], fx[1], acc);
       __builtin_amdgcn_s_setprio(0);
       __builtin_amdgcn_sched_barrier(0);
       meet<-1>();
@@ -691,25 +722,27 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   }
 }
 
-// Adds up the sums of groups that were cut, and clears the gradients of empty ones: a workgroup to a tile and 32 x 32 block of each wave
+constexpr int kJoin = 512;   // threads of a workgroup that adds up
+
+// Adds up the sums of groups that were cut, and clears the gradients of empty ones. 16 neighbouring results of a lane of the tile's workgroup are
+// a unit; `lanes` threads share a unit's chunks (each takes every lanes-th, and their sums meet in LDS, in order), `parts` workgroups a tile.
 template <typename T, int BR, int BN, int WR, int WN>
-__global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, const float* partial, int most_chunks) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 128 / sizeof(T);
+__global__ __launch_bounds__(kJoin) void weight_join_kernel(MmArgs a, const float* partial, int most_chunks, int parts, int lanes) {
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, UNIT = 128 / sizeof(T);
   constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wr = (wave / WN) * (BR / WR), wn = (wave % WN) * (BN / WN);
+  __shared__ float4 meet[4][kJoin];
   const int tiles = (a.inner + BR - 1) / BR * a.col_tiles;
-  const int group = (int)blockIdx.y, tile = (int)blockIdx.x / (NR * NN), block = (int)blockIdx.x % (NR * NN), r = block / NN, n = block % NN;
+  const int group = (int)blockIdx.y, tile = (int)blockIdx.x / parts, part = (int)blockIdx.x % parts;
   const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
   int begin, end;
-  const int steps = group_steps(a, group, DEPTH, &begin, &end);
+  const int steps = group_steps(a, group, UNIT, &begin, &end);
   int first = 0, last = -1;
   if (steps > 0) {
     // where the group's steps lie in the line: those of the groups before it first
     int mine = 0, all = 0;
-    for (int g = lane; g < a.groups; g += 64) {
+    for (int g = threadIdx.x & 63; g < a.groups; g += 64) {
       int b, e;
-      const int own = group_steps(a, g, DEPTH, &b, &e);
+      const int own = group_steps(a, g, UNIT, &b, &e);
       all += own;
       if (g < group) mine += own;
     }
@@ -723,45 +756,80 @@ __global__ __launch_bounds__(64 * WR * WN) void weight_join_kernel(MmArgs a, con
     last = (int)ds_mm_even_owner(mine + steps - 1, chunks, all);
     if (first == last) return;
   }
-  f32x16 v = {};
-  float sum = 0.f;
-  const bool with_sum = in0 == 0 && block == 0 && threadIdx.x < BN;
-  for (int b = first; b <= last; ++b) {
-    const float* p = partial + (((int64_t)b * tiles + tile) * 2 + (b == first)) * SLOT;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float4 f = reinterpret_cast<const float4*>(p)[(block * 4 + q) * THREADS + threadIdx.x];
-      v[4 * q] += f.x;
-      v[4 * q + 1] += f.y;
-      v[4 * q + 2] += f.z;
-      v[4 * q + 3] += f.w;
-    }
-    if (with_sum) sum += p[BR * BN + threadIdx.x];
-  }
+  const int across = kJoin / lanes, at = (int)threadIdx.x % across, turn = (int)threadIdx.x / across;
+  const auto sums = [&](int b) { return partial + (((int64_t)b * tiles + tile) * 2 + (b == first)) * SLOT; };
   T* dw = (T*)a.dw + (int64_t)group * a.inner * a.outer;
-  const int in = in0 + wr + r * 32 + (lane & 31);
+  const int units = NR * NN * THREADS, each = (units + parts - 1) / parts, stop = min(units, (part + 1) * each);
+  for (int base = part * each; base < stop; base += across) {
+    const int unit = base + at, block = unit / THREADS, thread = unit % THREADS, lane = thread & 63, wave = thread >> 6;
+    const int in = in0 + wave / WN * (BR / WR) + block / NN * 32 + (lane & 31);
+    const int col = col0 + wave % WN * (BN / WN) + block % NN * 32 + 16 * (lane >> 5);
+    const bool there = unit < stop && in < a.inner && col < a.outer;
+    float4 v[4] = {};
+    if (there) {
+#pragma unroll 2
+      for (int b = first + turn; b <= last; b += lanes) {
+        const float4* p = reinterpret_cast<const float4*>(sums(b)) + block * 4 * THREADS + thread;
 #pragma unroll
-  for (int p = 0; p < 16 / N; ++p) {
-    const int c = col0 + wn + n * 32 + 16 * (lane >> 5) + p * N;
-    if (in < a.inner && c < a.outer) {
-      PieceV<T> out;
+        for (int q = 0; q < 4; ++q) {
+          const float4 f = p[q * THREADS];
+          v[q].x += f.x;
+          v[q].y += f.y;
+          v[q].z += f.z;
+          v[q].w += f.w;
+        }
+      }
+    }
+    if (lanes > 1) {
+      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) out[i] = (T)v[p * N + i];
-      store_piece<T>(dw + (int64_t)in * a.outer + c, out, a.outer - c);
+      for (int q = 0; q < 4; ++q) meet[q][threadIdx.x] = v[q];
+      __syncthreads();
+      if (turn == 0) {
+        for (int l = 1; l < lanes; ++l)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 f = meet[q][l * across + at];
+            v[q].x += f.x;
+            v[q].y += f.y;
+            v[q].z += f.z;
+            v[q].w += f.w;
+          }
+      }
+    }
+    if (turn == 0 && there) {
+      const float r[16] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w,
+                           v[2].x, v[2].y, v[2].z, v[2].w, v[3].x, v[3].y, v[3].z, v[3].w};
+#pragma unroll
+      for (int p = 0; p < 16 / N; ++p) {
+        PieceV<T> out;
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = (T)r[p * N + i];
+        const int c = col + p * N;
+        T* to = dw + (int64_t)in * a.outer + c;
+        if (c + N <= a.outer) *reinterpret_cast<typename Piece<T>::U*>(to) = out;
+        else if (c < a.outer) store_first<T>(to, out, a.outer - c);
+      }
     }
   }
-  if (with_sum && col0 + (int)threadIdx.x < a.outer) a.db[(int64_t)group * a.outer + col0 + threadIdx.x] = sum;
-}
-
-// Chunks of the line of steps: as many as fill the compute units with every tile once, or twice where that leaves fewer of them idle in the last
-// round, but none of less than about 8 steps (512 rows of 16 bits), whose sums would cost more than they do.
-int chunks_of(int rows, int64_t tiles, int unit) {
-  constexpr int64_t kUnits = 256;
-  const auto idle = [&](int64_t p) { return (double)((p * tiles + kUnits - 1) / kUnits * kUnits) / (double)(p * tiles); };
-  const int64_t once = kUnits / tiles > 1 ? kUnits / tiles : 1, twice = 2 * kUnits / tiles > 1 ? 2 * kUnits / tiles : 1;
-  int64_t p = idle(twice) < 0.93 * idle(once) ? twice : once;
-  const int64_t most = rows / (8 * unit);
-  return (int)(p < most ? p : most > 1 ? most : 1);
+  if (in0 == 0 && part == 0) {   // db
+    float* one = reinterpret_cast<float*>(meet);
+    for (int base = 0; base < BN; base += across) {
+      const bool there = base + at < BN && col0 + base + at < a.outer;
+      float v = 0.f;
+      if (there) {
+#pragma unroll 4
+        for (int b = first + turn; b <= last; b += lanes) v += sums(b)[BR * BN + base + at];
+      }
+      __syncthreads();
+      one[threadIdx.x] = v;
+      __syncthreads();
+      if (turn == 0 && there) {
+        for (int l = 1; l < lanes; ++l) v += one[l * across + at];
+        a.db[(int64_t)group * a.outer + col0 + base + at] = v;
+      }
+    }
+  }
 }
 
 template <typename T, int BR, int BN>
@@ -772,14 +840,21 @@ int64_t weight_tiles(int inner, int outer) {
 template <typename T, int BR, int BN, int WR, int WN>
 int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
   a.col_tiles = (a.outer + BN - 1) / BN;
-  const int64_t tiles = weight_tiles<T, BR, BN>(a.inner, a.outer), chunks = chunks_of(a.rows, tiles, 128 / (int)sizeof(T));
-  const int64_t wgs = (tiles * chunks + 7) / 8 * 8, blocks = tiles * (BR / WR / 32) * (BN / WN / 32);
-  if (wgs > 0x7fffffff || blocks > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
+  const int64_t tiles = weight_tiles<T, BR, BN>(a.inner, a.outer), chunks = ds_weight_chunks(a.rows, tiles, 128 / (int)sizeof(T));
+  const int64_t wgs = (tiles * chunks + 7) / 8 * 8;
+  if (wgs > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
   const bool direct = sixteen(a.x, a.xs, sizeof(T)) && sixteen(a.dy, a.dys, sizeof(T)) && a.inner % Piece<T>::N == 0 && a.outer % Piece<T>::N == 0;
   const dim3 grid((unsigned)wgs), block(64 * WR * WN);
   if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
   else hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, false>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_join_kernel<T, BR, BN, WR, WN>), dim3((unsigned)blocks, a.groups), block, 0, ctx->stream, a, partial, (int)chunks);
+  // threads to a unit by the chunks that a group has on average; workgroups for about 2,048 in all
+  const int64_t of_group = chunks / (a.groups < chunks ? a.groups : chunks) + 1;
+  const int lanes = of_group > 16 ? 8 : of_group > 8 ? 4 : of_group > 4 ? 2 : 1;
+  const int64_t units = (int64_t)(BR / WR / 32) * (BN / WN / 32) * 64 * WR * WN * lanes / kJoin;
+  int64_t parts = 2048 / (tiles * a.groups);
+  parts = parts < 1 ? 1 : parts < units ? parts : units;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_join_kernel<T, BR, BN, WR, WN>), dim3((unsigned)(tiles * parts), a.groups), dim3(kJoin), 0, ctx->stream, a,
+                     partial, (int)chunks, (int)parts, lanes);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -794,8 +869,25 @@ int launch(ds_ctx* ctx, MmArgs& a) {
 
 }  // namespace
 
+// Chunks of the line of steps: as many as fill the compute units with every tile once, or twice where that leaves fewer of them idle in the last
+// round, but none of less than two steps (128 rows of 16 bits).
+int ds_weight_chunks(int rows, int64_t tiles, int unit) {
+  constexpr int64_t kUnits = 256;
+  const auto idle = [&](int64_t p) { return (double)((p * tiles + kUnits - 1) / kUnits * kUnits) / (double)(p * tiles); };
+  const int64_t once = kUnits / tiles > 1 ? kUnits / tiles : 1, twice = 2 * kUnits / tiles > 1 ? 2 * kUnits / tiles : 1;
+  const int64_t p = idle(twice) < 0.93 * idle(once) ? twice : once, most = rows / (2 * unit);
+  return (int)(p < most ? p : most > 1 ? most : 1);
+}
+
+// 256 rows to a tile where there are about as many tiles as compute units (65,536 rows by 512 x 512: 0.36 -> 0.34 ms; with half as many tiles, 4,096
+// rows by 2,048 x 512: 0.16 -> 0.27 ms)
+bool ds_wide_tiles(int rows, int width) { return (int64_t)(rows / 256) * ((width + 127) / 128) >= 224; }
+
 int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a) {
-  if (dtype == DS_ELEM_F32) return transposed ? launch<float, 128, 128, 2, 4, true>(ctx, a) : launch<float, 128, 128, 2, 4, false>(ctx, a);
+  if (dtype == DS_ELEM_F32) {
+    if (ds_wide_tiles(a.rows, transposed ? a.inner : a.outer)) return transposed ? launch<float, 256, 128, 4, 2, true>(ctx, a) : launch<float, 256, 128, 4, 2, false>(ctx, a);
+    return transposed ? launch<float, 128, 128, 2, 4, true>(ctx, a) : launch<float, 128, 128, 2, 4, false>(ctx, a);
+  }
   if (dtype == DS_ELEM_BF16) return transposed ? launch<__bf16, 256, 256, 2, 4, true>(ctx, a) : launch<__bf16, 256, 256, 2, 4, false>(ctx, a);
   return transposed ? launch<_Float16, 256, 256, 2, 4, true>(ctx, a) : launch<_Float16, 256, 256, 2, 4, false>(ctx, a);
 }
@@ -803,7 +895,7 @@ int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a) {
 int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer) {
   const int64_t side = dtype == DS_ELEM_F32 ? 128 : 256;
   const int64_t tiles = dtype == DS_ELEM_F32 ? weight_tiles<float, 128, 128>(inner, outer) : weight_tiles<__bf16, 256, 256>(inner, outer);
-  const int64_t chunks = chunks_of(rows, tiles, dtype == DS_ELEM_F32 ? 32 : 64);
+  const int64_t chunks = ds_weight_chunks(rows, tiles, dtype == DS_ELEM_F32 ? 32 : 64);
   return chunks > 1 ? tiles * chunks * 2 * (side * side + side) * (int64_t)sizeof(float) : 0;
 }
 
