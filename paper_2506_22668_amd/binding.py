@@ -193,6 +193,8 @@ class Context:
         self._keep = {}
         self._index = idx
         self._raw_stream = stream.cuda_stream if stream is not None else 0
+        # the handle of torch's current stream (a seventh of a small call's time as the attribute of a Stream object made for it)
+        self._current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self._elements = {torch.float32: DS_ELEM_F32, torch.bfloat16: DS_ELEM_BF16, torch.float16: DS_ELEM_F16}
 
     def close(self):
@@ -456,10 +458,10 @@ class Context:
     # does next; nothing waits on the host. Under graph capture the context has to be one made for the captured stream.
     def _queue(self, fn, *args):
         t = self.torch
-        current = t.cuda.current_stream(self._index)
-        if current.cuda_stream == self._raw_stream:
+        if self._current_stream(self._index) == self._raw_stream:
             self._check(fn(self.h, *args))
             return
+        current = t.cuda.current_stream(self._index)
         if t.cuda.is_current_stream_capturing():
             raise DistShapError(DS_EINVAL, "the stream being captured is not the context's")
         own = self._stream if self._stream is not None else t.cuda.default_stream(self._index)
@@ -515,7 +517,7 @@ class Context:
         rows, cols = x.shape
         weight, wp = self._values(weight, "weight", (cols,), t.float32)
         bias, bp = self._values(bias, "bias", (cols,), t.float32)
-        y = t.empty((rows, cols), dtype=x.dtype, device=x.device)
+        y = x.new_empty((rows, cols))
         mean = rstd = mp = rp = None
         if want_stats:
             mean, rstd = t.empty((2, rows), dtype=t.float32, device=x.device)
@@ -535,7 +537,7 @@ class Context:
         mean, mp = self._values(mean, "mean", (rows,), t.float32)
         rstd, rp = self._values(rstd, "rstd", (rows,), t.float32)
         weight, wp = self._values(weight, "weight", (cols,), t.float32)
-        dx = t.empty((rows, cols), dtype=x.dtype, device=x.device)
+        dx = x.new_empty((rows, cols))
         dweight, dbias = t.empty((2, cols), dtype=t.float32, device=x.device)
         ws, wsp, wsn = self._workspace(self.lib.ds_layer_norm_backward_workspace, rows, cols)
         self._queue(self.lib.ds_layer_norm_backward, self._elements[x.dtype], rows, cols, dy.data_ptr(), dys, x.data_ptr(), xs, mp,
@@ -552,7 +554,7 @@ class Context:
         if residual is not None:
             residual, rs = self._rows(residual, "residual", (rows, cols), x.dtype)
             rp = residual.data_ptr()
-        y = t.empty((rows, cols), dtype=x.dtype, device=x.device)
+        y = x.new_empty((rows, cols))
         self._queue(self.lib.ds_dropout, self._elements[x.dtype], rows, cols, x.data_ptr(), xs, rp, rs, p, int(seed),
                     int(tag) & 0xFFFFFFFF, y.data_ptr(), cols)
         return y
@@ -568,7 +570,7 @@ class Context:
         groups = int(groups)
         ws, wsp, wsn = self._workspace(self.lib.ds_group_rows_workspace, rows, groups)
         offsets = t.empty(groups + 1, dtype=t.int64, device=ids.device)
-        order = t.empty(rows, dtype=t.int32, device=ids.device)
+        order = ids.new_empty(rows)
         self._queue(self.lib.ds_group_rows, ip, rows, groups, offsets.data_ptr(), order.data_ptr(), wsp, wsn)
         return offsets, order
 
@@ -591,7 +593,7 @@ class Context:
         x, xs, w, wp, keep, op, rp = self._grouped(x, w, offsets, order)
         (rows, inner), (groups, _, outer) = x.shape, w.shape
         bias, bp = self._values(bias, "bias", (groups, outer), t.float32)
-        y = t.empty((rows, outer), dtype=x.dtype, device=x.device)
+        y = x.new_empty((rows, outer))
         self._queue(self.lib.ds_grouped_mm, self._elements[x.dtype], rows, inner, outer, groups, x.data_ptr(), xs, wp, op, rp, bp,
                     int(bool(relu)), y.data_ptr(), outer)
         return y
@@ -606,8 +608,8 @@ class Context:
         if gate is not None:
             gate, gs = self._rows(gate, "gate", (rows, inner), x.dtype)
             gp = gate.data_ptr()
-        dx = t.empty((rows, inner), dtype=x.dtype, device=x.device)
-        dw = t.empty((groups, inner, outer), dtype=x.dtype, device=x.device)
+        dx = x.new_empty((rows, inner))
+        dw = x.new_empty((groups, inner, outer))
         db = t.empty((groups, outer), dtype=t.float32, device=x.device)
         element = self._elements[x.dtype]
         ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_workspace, element, rows, inner, outer, groups)

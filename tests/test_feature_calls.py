@@ -134,7 +134,7 @@ def test_a_tensor_of_another_device_is_refused():
 
 def test_a_capture_of_a_stream_that_is_not_the_contexts_is_refused():
     c = _context()
-    c._raw_stream = 0
+    c._raw_stream, c._current_stream = 0, lambda i: 7
     c.torch = types.SimpleNamespace(cuda=types.SimpleNamespace(current_stream=lambda i: types.SimpleNamespace(cuda_stream=7),
                                                                is_current_stream_capturing=lambda: True))
     with pytest.raises(DistShapError):
