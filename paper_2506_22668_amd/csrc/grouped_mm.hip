@@ -323,10 +323,10 @@ MmArgs arguments(const ds_grouped& p) {
 
 // ---- which form -----------------------------------------------------------------------------------------------------------------
 // Each form has a price in us on 256 compute units, from the number of its workgroups, how many run at a time, and what one takes for its share of the
-// contraction; the sizes of groups are not known on the host, so all are taken to be of the mean size. The figures were fitted to both
-// forms' times at 165 shapes and types each (1, 8 and 64 groups of 24 to 16,000 rows; widths of 64 to 4,000, odd ones among them): the choice
-// is within 15 % of the faster form at all but 11 of 990, and 0.7 % off it on average (a limit of 64 rows to a group: 13 %). In us, few / tiles:
-//   8 groups of 400 rows by 1,024 x 1,024, bf16: 36 / 38, of 1,000 rows: 66 / 41; 64 groups of 200 rows by 256 x 256: 26 / 18, by 64 x 64: 14 / 14
+// contraction; the sizes of groups are not known on the host, so all are taken to be of the mean size. The figures were fitted to the forms' times at
+// 165 shapes of each type (1, 8 and 64 groups of 24 to 16,000 rows; widths of 64 to 4,000, odd ones among them), those of the small 16-bit tiles
+// to 315 more (1 to 64 groups, up to 900 tiles): the choice is 1.1 % off the fastest form there on average, and more than 12 % at 3. In us, few / tiles:
+//   8 groups of 400 rows by 1,024 x 1,024, bf16: 30 / 26, of 1,000 rows: 58 / 34; 64 groups of 200 rows by 256 x 256: 24 / 13, by 64 x 64: 12 / 13
 constexpr double kUnits = 256;
 
 double ceil_div(double a, double b) { return ceil(a / b); }
@@ -339,6 +339,8 @@ bool rows_in_tiles(const ds_grouped& p, int dtype, int depth, int width) {
   const double block = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
   const double few = p.groups * ceil_div(mean, block) * ceil_div(width, f32 ? 64 : 128) / kUnits;
   const double few_us = (few > 1 ? few : 1) * (5 + (f32 ? 0.02 : 0.009) * depth);
+  const double narrow = ds_narrow_tiles(p.rows, p.groups, width);
+  if (!f32 && narrow <= kNarrowTiles) return 1 + (narrow > kUnits ? 0.026 : 0.017) * depth < few_us;
   if (!f32) return ceil_div(p.groups * ceil_div(mean, 256) * ceil_div(width, 256), kUnits) * (4 + 0.025 * depth) < few_us;
   const bool wide = ds_wide_tiles(p.rows, width);
   const double rounds = ceil_div(p.groups * ceil_div(mean, wide ? 256 : 128) * ceil_div(width, 128), kUnits);

@@ -206,7 +206,7 @@ __device__ __forceinline__ int hidden(int v) {
   return v;
 }
 
-// Workgroups stay: one to a compute unit, which goes through tiles of BR rows and BN columns as through one line of steps of the
+// Workgroups stay: one to a compute unit (of 256 threads: two), which goes through tiles of BR rows and BN columns as through one line of steps of the
 // contraction (128 bytes of every row). A step is computed on from one half of the LDS, the next one is in the other half already, and
 // what comes behind that, of this tile or the next, is asked for as soon as the first half is through; a wave's operands for a slice of the
 // step are read while the matrix cores work on the slice before. Results leave through LDS of their own, while the next tile's steps come in.
@@ -223,8 +223,11 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
   __shared__ __attribute__((aligned(128))) char stage0[STAGE], stage1[STAGE], stage2[STAGE], stage3[STAGE], leaving[WR * WN * OUT_ROWS * OUT_ROW];
   __shared__ __attribute__((aligned(16))) float bias_of[WR * WN * TN];
   __shared__ GroupTable table;
-  // of the tiles under way, by their number: the rows, and the group (a tile comes in at most five stages before it is computed on, and has two at the least)
-  __shared__ int row_of[8][BR], group_of[8];
+  // of the tiles under way, by their number: the rows, and the group (a tile comes in at most four or, fp32, five stages before it is computed on,
+  // and has two at the least: three or four tiles are under way)
+  constexpr int HELD = sizeof(T) == 2 ? 4 : 8;
+  __shared__ int row_of[HELD][BR], group_of[HELD];
+  static_assert(sizeof(stage0) * 4 + sizeof(leaving) + sizeof(bias_of) + sizeof(table) + sizeof(row_of) + sizeof(group_of) <= (THREADS == 256 ? 80 : 160) * 1024, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = (wave / WN) * TR, wn = (wave % WN) * TN;
   const int width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
@@ -271,14 +274,14 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
       coming_col = coming_at % a.col_tiles * BN;
       from_w = (const T*)a.w + (int64_t)coming_group * a.inner * a.outer +
                (TRANSPOSED ? (int64_t)(coming_col + wline) * a.outer + wplace : (int64_t)wline * a.outer + coming_col + wplace);
-      int* rows = row_of[coming_number & 7];
+      int* rows = row_of[coming_number & (HELD - 1)];
       const int tid = hidden((int)threadIdx.x);
 #pragma unroll
       for (int u = 0; u < lx.PIECES; ++u) {
         from_x[u] = x + (row[u] < 0 ? 0 : row[u]) * xs + xk;   // (no row: any row, whose results go nowhere)
         if (tid % XOp::PER_ROW == 0) rows[u * XLINES + XOp::line(tid)] = row[u];
       }
-      group_of[coming_number & 7] = coming_group;
+      group_of[coming_number & (HELD - 1)] = coming_group;
       ++coming_number;
       if (coming_at + step_by < stretch) look_up(coming_at + step_by);
     }
@@ -365,14 +368,14 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
       char* mine = leaving + wave * (OUT_ROWS * OUT_ROW);
       float* bias = bias_of + wave * TN;
       if constexpr (!TRANSPOSED) {
-        const float* from = a.bias + (a.bias ? (int64_t)__builtin_amdgcn_readfirstlane(group_of[number & 7]) * width : 0);
+        const float* from = a.bias + (a.bias ? (int64_t)__builtin_amdgcn_readfirstlane(group_of[number & (HELD - 1)]) * width : 0);
 #pragma unroll
         for (int j = 0; j < TN; j += 64)
           if (TN % 64 == 0 || j + lane < TN) bias[j + lane] = a.bias ? from[min(col + j + lane, width - 1)] : 0.f;
       }
       const float least = !TRANSPOSED && a.relu ? 0.f : -INFINITY;
       const int chunk = lane % CHUNKS, c = col + chunk * N;
-      const int* rows = row_of[number & 7] + wr + lane / CHUNKS;
+      const int* rows = row_of[number & (HELD - 1)] + wr + lane / CHUNKS;
       // (a gate is asked for two blocks of rows ahead, in front of stores that its coming would otherwise wait for)
       PieceV<T> open[2 * NR][OUTS];
       const auto ask = [&](int r) __attribute__((always_inline)) {
@@ -499,7 +502,8 @@ int launch_one(ds_ctx* ctx, MmArgs& a) {
   a.col_tiles = ((TRANSPOSED ? a.inner : a.outer) + BN - 1) / BN;
   if (ds_most_tiles(a, BR == 256 ? 8 : 7) * a.col_tiles > 0x7fffffff)
     return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than are counted", a.rows, TRANSPOSED ? a.inner : a.outer);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(row_tiles_kernel<T, BR, BN, WR, WN, TRANSPOSED, DIRECT>), dim3((unsigned)(ctx->num_cus + 7) / 8 * 8),
+  constexpr int A_UNIT = WR * WN == 4 ? 2 : 1;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(row_tiles_kernel<T, BR, BN, WR, WN, TRANSPOSED, DIRECT>), dim3((unsigned)(A_UNIT * ctx->num_cus + 7) / 8 * 8),
                      dim3(64 * WR * WN), 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
@@ -884,13 +888,27 @@ int ds_weight_chunks(int rows, int64_t tiles, int unit) {
 // rows by 2,048 x 512: 0.16 -> 0.27 ms)
 bool ds_wide_tiles(int rows, int width) { return (int64_t)(rows / 256) * ((width + 127) / 128) >= 224; }
 
+// 16 bits: tiles of 128 by 128, of which a compute unit has two at a time, where there are no more than that: 256 by 256 would leave units idle
+// (8,192 rows in 8 groups by 512 x 512: 24 us in large, 17 in small; by 1,024 x 1,024: 39, 34). With more, the large ones' fewer loads from L2
+// count (131,072 rows by 512 x 512: 108, 144; by 1,024 x 1,024: 416, 520).
+double ds_narrow_tiles(int rows, int groups, int width) {
+  const double mean = ceil((double)rows / groups);
+  return groups * ceil(mean / 128) * ceil(width / 128.0);
+}
+
+template <typename T, bool TRANSPOSED>
+int launch_rows(ds_ctx* ctx, MmArgs& a) {
+  if (ds_narrow_tiles(a.rows, a.groups, TRANSPOSED ? a.inner : a.outer) <= kNarrowTiles) return launch<T, 128, 128, 2, 2, TRANSPOSED>(ctx, a);
+  return launch<T, 256, 256, 2, 4, TRANSPOSED>(ctx, a);
+}
+
 int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a) {
   if (dtype == DS_ELEM_F32) {
     if (ds_wide_tiles(a.rows, transposed ? a.inner : a.outer)) return transposed ? launch<float, 256, 128, 4, 2, true>(ctx, a) : launch<float, 256, 128, 4, 2, false>(ctx, a);
     return transposed ? launch<float, 128, 128, 2, 4, true>(ctx, a) : launch<float, 128, 128, 2, 4, false>(ctx, a);
   }
-  if (dtype == DS_ELEM_BF16) return transposed ? launch<__bf16, 256, 256, 2, 4, true>(ctx, a) : launch<__bf16, 256, 256, 2, 4, false>(ctx, a);
-  return transposed ? launch<_Float16, 256, 256, 2, 4, true>(ctx, a) : launch<_Float16, 256, 256, 2, 4, false>(ctx, a);
+  if (dtype == DS_ELEM_BF16) return transposed ? launch_rows<__bf16, true>(ctx, a) : launch_rows<__bf16, false>(ctx, a);
+  return transposed ? launch_rows<_Float16, true>(ctx, a) : launch_rows<_Float16, false>(ctx, a);
 }
 
 int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer) {

@@ -382,6 +382,14 @@ def test_grouped_mm_backward(ctx, t, rows, inner, outer, groups):
         assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), again))
 
 
+# many tiles: workgroups go through several, the shortest contraction among them
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", [(70001, 16, 129, 2), (66001, 264, 136, 3), (40003, 131, 259, 7), (33000, 72, 520, 20)])
+def test_grouped_mm_many_tiles(ctx, t, rows, inner, outer, groups):
+    test_grouped_mm(ctx, t, rows, inner, outer, groups)
+    test_grouped_mm_backward(ctx, t, rows, inner, outer, groups)
+
+
 # widths below a 16-byte piece, contractions that end right behind a step, matrices of less than 16 bytes
 NARROW = [(3, 1, 1, 1), (1, 1, 2, 1), (2, 3, 1, 2), (40, 33, 3, 2), (40, 3, 33, 2), (90, 65, 1, 1), (90, 1, 65, 1), (700, 40, 5, 3), (700, 5, 40, 3),
           (300, 34, 9, 1), (200, 129, 130, 2), (1, 33, 7, 1), (33, 128, 7, 1), (600, 8, 8, 2), (600, 9, 15, 2)]
