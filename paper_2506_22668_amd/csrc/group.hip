@@ -44,13 +44,24 @@ __device__ __forceinline__ void walk(const GroupArgs& a, int wave, Each each) {
   const int64_t first = ((int64_t)blockIdx.x * kWaves + wave) * a.per_wave;
   const int begin = first < a.rows ? (int)first : a.rows;
   const int end = a.rows - begin < a.per_wave ? a.rows : begin + a.per_wave;
-  int key = key_of(a, begin + lane, end);
-  for (int at = begin; at < end; at += 64) {
-    const int now = key;
-    if (end - at > 64) key = key_of(a, at + 64 + lane, end);
-    const unsigned long long same = same_key(now, bits);
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    each(at + lane, now, rank, __popcll(same));
+  // (the ids of four steps are on their way at a time, those of the next four while these are worked off)
+  int next[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) next[j] = key_of(a, begin + j * 64 + lane, end);
+  for (int at = begin; at < end; at += 256) {
+    int now[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      now[j] = next[j];
+      next[j] = end - at > 256 ? key_of(a, at + 256 + j * 64 + lane, end) : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (end - at <= j * 64) break;
+      const unsigned long long same = same_key(now[j], bits);
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      each(at + j * 64 + lane, now[j], rank, __popcll(same));
+    }
   }
 }
 
