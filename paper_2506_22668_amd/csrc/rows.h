@@ -43,17 +43,6 @@ __device__ __forceinline__ typename Piece<T>::V load_piece(const T* p, int have)
 }
 
 template <typename T>
-__device__ __forceinline__ void store_piece(T* p, typename Piece<T>::V v, int have) {
-  if (have >= Piece<T>::N) {
-    *reinterpret_cast<typename Piece<T>::U*>(p) = v;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < Piece<T>::N - 1; ++i)
-    if (i < have) p[i] = v[i];
-}
-
-template <typename T>
 using PieceV = typename Piece<T>::V;
 
 // without the first `by` (at most N) elements, zeros behind the others
@@ -104,6 +93,12 @@ __device__ __forceinline__ void store_first(T* p, PieceV<T> v, int have) {
     v[0] = v[2];
   }
   if (have & 1) *p = v[0];
+}
+
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, PieceV<T> v, int have) {
+  if (have >= Piece<T>::N) *reinterpret_cast<typename Piece<T>::U*>(p) = v;
+  else if (have > 0) store_first<T>(p, v, have);
 }
 
 template <int CTRL>
