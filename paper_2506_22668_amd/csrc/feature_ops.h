@@ -15,7 +15,7 @@ int ds_launch_layer_norm_backward(ds_ctx* ctx, int dtype, int64_t rows, int cols
                                   float* partial);
 int ds_launch_dropout(ds_ctx* ctx, int dtype, int64_t rows, int cols, ds_rows x, ds_rows residual, int threshold, uint64_t seed,
                       uint32_t tag, ds_rows y);
-int ds_group_blocks(int rows, int groups);
+int ds_group_blocks(int rows);
 int ds_launch_group_rows(ds_ctx* ctx, const int32_t* ids, int rows, int groups, int64_t* offsets, int32_t* order, int32_t* counts);
 
 struct ds_grouped {

@@ -5,7 +5,9 @@
 // steps of 64. Within a step the lanes of one group find each other by a ballot for every bit of the id, so that a row's rank is
 // a popcount and the lowest lane adds the step's count in LDS: no atomic decides an order, and the result is the
 // only one there is. Several workgroups: a first launch leaves every stretch's counts, a second adds up the ones before its own
-// (ids are read twice, from the caches the second time).
+// (ids are read twice, from the caches the second time). Its bytes are nothing (1,000,175 rows 1.6 us): what it takes is the latency of its steps.
+// 1,010 rows in 8 groups 8 us; 1,000,175 rows in 64 groups 19 us (counts 6, places 14: each workgroup reads all workgroups' counts, 5 us
+// there, and 50 of the 65 us of as many rows in 1,024 groups); 10,000,000 rows in 64 groups 137 us.
 #include "feature_ops.h"
 #include "rows.h"
 
@@ -158,15 +160,15 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a) {
 
 }  // namespace
 
-// One workgroup takes up to four stretches by itself: a second launch costs more than the rest of its walk does.
-int ds_group_blocks(int rows, int groups) {
-  (void)groups;
+// One workgroup takes up to four stretches by itself: a second launch costs more than the rest of its walk does (6,000 rows in 64 groups: 12.0 us in
+// one, 14.2 in two; 8,000: 15.1, 14.0, in 4 groups 11.3, 13.9).
+int ds_group_blocks(int rows) {
   const int blocks = (rows + kStretch - 1) / kStretch;
   return blocks <= 4 ? 1 : blocks < 256 ? blocks : 256;
 }
 
 int ds_launch_group_rows(ds_ctx* ctx, const int32_t* ids, int rows, int groups, int64_t* offsets, int32_t* order, int32_t* counts) {
-  const int blocks = ds_group_blocks(rows, groups);
+  const int blocks = ds_group_blocks(rows);
   GroupArgs a = {};
   a.ids = ids;
   a.rows = rows;
