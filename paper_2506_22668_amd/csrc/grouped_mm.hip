@@ -44,10 +44,10 @@ constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 // that there are not lead to results that nobody stores; where the contraction ends, the last step clears them. A piece that would reach over
 // the matrix' end, which it can in its last N rows alone, is read so that it ends there, and shifted. (TINY: matrices of less than 16 bytes, element by element.)
 // Bound by reading W, from memory once if a group has one tile of rows: 8 rows in 8 groups by 1,024 x 4,096 bf16 14.0 us, 4.8 TB/s.
-template <typename T, int RB, bool TRANSPOSED, bool TINY>
-__global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
-  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6, STEP = kWaves * 4 * N;
-  __shared__ float meet[kWaves][4][64][N];
+template <typename T, int RB, int WAVES, bool TRANSPOSED, bool TINY>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
+  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6, STEP = WAVES * 4 * N;
+  __shared__ float meet[WAVES][4][64][N];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
   const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N;
@@ -139,13 +139,13 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
   const T *gate = (const T*)a.gate, *gate_end = gate + (int64_t)(a.rows - 1) * a.gs + width;
   T* y = (T*)a.y;
   // wave w ends up with the four columns' quarter w of every row block: columns col + N (4 q + w) .. + N - 1
-  const int n = col + N * (4 * q + wave);
+  const int n = col + N * (4 * q + (wave & 3));
   float bias[N];
 #pragma unroll
   for (int j = 0; j < N; ++j)
     bias[j] = !TRANSPOSED && a.bias && gt.group < a.groups ? a.bias[(int64_t)gt.group * width + min(n + j, width - 1)] : 0.f;
   PieceV<T> open[RB];
-  if (TRANSPOSED && gate) {
+  if (TRANSPOSED && gate && wave < 4) {
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       if constexpr (TINY) open[r] = load_piece<T>(gate + row[r] * a.gs + n, row[r] >= 0 ? width - n : 0);
@@ -160,13 +160,13 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
 #pragma unroll
       for (int j = 0; j < N; ++j) meet[wave][i][lane][j] = acc[r][j][i];
     __syncthreads();
-    if (row[r] >= 0 && n < width) {
+    if (wave < 4 && row[r] >= 0 && n < width) {
       PieceV<T> out;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         float v = bias[j];
 #pragma unroll
-        for (int s = 0; s < kWaves; ++s) v += meet[s][wave][lane][j];
+        for (int s = 0; s < WAVES; ++s) v += meet[s][wave & 3][lane][j];
         if (!TRANSPOSED && a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
         if (TRANSPOSED && gate) v = (float)open[r][j] > 0.f ? v : 0.f;
         out[j] = (T)v;
@@ -178,18 +178,20 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(MmArgs a) {
   }
 }
 
-// dW and db of a group: 16 N outer by 8 N inner columns to a workgroup, the waves share the group's rows. Both operands
+// dW and db of a group: 16 N outer by 8 N inner columns to a workgroup, the waves share the group's rows; or (SHARED false, for groups of a few rows, which
+// would keep one wave of four busy) a quarter as many inner columns to a wave, whose results leave from its registers. Both operands
 // run across the contraction (the rows), so both are turned around in registers. db is one more product, with ones for x. The rows
 // of the next step are looked up, and those of this one's are on their way, while the products of the one before are formed. Bound by the latency of those loads.
-template <typename T, bool TINY>
+template <typename T, bool SHARED, bool TINY>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a) {
-  constexpr int N = Piece<T>::N, H = N / 2, STEP = kWaves * 4 * N;
+  constexpr int N = Piece<T>::N, H = SHARED ? N / 2 : N / 4, STEP = (SHARED ? kWaves : 1) * 4 * N;
   typedef T Half __attribute__((ext_vector_type(H)));
   typedef T HalfU __attribute__((ext_vector_type(H), aligned(sizeof(T))));
-  __shared__ float meet[kWaves][4][64][N];
+  __shared__ float meet[SHARED ? kWaves : 1][4][64][N];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int group = (int)blockIdx.y;
-  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N, in0 = ((int)blockIdx.x / a.col_tiles) * 16 * H;
+  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N, in0 = ((int)blockIdx.x / a.col_tiles * (SHARED ? 1 : kWaves) + (SHARED ? 0 : wave)) * 16 * H;
+  if (!SHARED && in0 >= a.inner) return;
   int begin, end;
   ds_group_range(a.offsets, a.groups, a.rows, group, &begin, &end);
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
       }
     }
   };
-  int at = begin + wave * 4 * N;
+  int at = begin + (SHARED ? wave * 4 * N : 0);
   if (at < end) {
     look_up(at);
     fetch();
@@ -275,6 +277,30 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
     }
   }
   T* dw = (T*)a.dw + (int64_t)group * a.inner * a.outer;
+  if constexpr (!SHARED) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int in = in0 + H * m + h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        PieceV<T> out;
+#pragma unroll
+        for (int j = 0; j < N; ++j) out[j] = (T)acc[h][j][i];
+        const int n = col + N * (4 * q + i);
+        if (in < a.inner && n < a.outer) store_piece<T>(dw + (int64_t)in * a.outer + n, out, a.outer - n);
+      }
+    }
+    if (with_sum && m == 0) {   // (every column of the product with ones is the sum)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const int n = col + N * (4 * q + i) + j;
+          if (n < a.outer) a.db[(int64_t)group * a.outer + n] = sum[j][i];
+        }
+    }
+    return;
+  }
   const int n = col + N * (4 * q + wave);
 #pragma unroll
   for (int h = 0; h <= H; ++h) {
@@ -302,7 +328,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
         if (n + N <= a.outer) *reinterpret_cast<typename Piece<T>::U*>(to) = out;
         else store_first<T>(to, out, a.outer - n);
       }
-    } else if (m == 0) {   // (every column of the product with ones is the sum)
+    } else if (m == 0) {
 #pragma unroll
       for (int j = 0; j < N; ++j)
         if (n + j < a.outer) a.db[(int64_t)group * a.outer + n + j] = v[j];
@@ -348,12 +374,19 @@ bool rows_in_tiles(const ds_grouped& p, int dtype, int depth, int width) {
   return rounds * (wide ? 13 + 0.14 * depth : 8 + 0.075 * depth) + 6 < few_us;
 }
 
+// Up to 32 rows to a group a wave of the few-rows form has columns of its own, a quarter as many, beyond that the waves of a workgroup share the
+// rows (both gradients, 8 groups by 1,024 x 1,024, alone / shared: 8 rows each bf16 25 / 40 us, fp32 32 / 44; 32 rows: 28 / 42, 41 / 47; 64 rows:
+// 36 / 46, 66 / 58; 128 rows: 44 / 48, 92 / 76)
+bool weights_shared(const ds_grouped& p) { return (int64_t)p.rows > 32 * (int64_t)p.groups; }
+
 bool weights_in_tiles(const ds_grouped& p, int dtype) {
   if (p.inner < 8 || p.outer < 8) return false;
   const bool f32 = dtype == DS_ELEM_F32;
   const double mean = ceil_div(p.rows, p.groups), n = f32 ? 4 : 8;
   const double few = p.groups * ceil_div(p.outer, 16 * n) * ceil_div(p.inner, 8 * n) / kUnits;
-  const double few_us = (few > 1 ? few : 1) * ((f32 ? 3 : 5) + 2 * ceil_div(mean, 16 * n));
+  const double alone = p.groups * ceil_div(p.outer, 16 * n) * ceil_div(p.inner, 4 * n) / (kUnits * (f32 ? 16 : 8));   // (waves at a time)
+  const double few_us = weights_shared(p) ? (few > 1 ? few : 1) * ((f32 ? 3 : 5) + 2 * ceil_div(mean, 16 * n))
+                                          : (alone > 1 ? alone : 1) * (6 + 2 * ceil_div(mean, 4 * n));
   const double side = f32 ? 128 : 256, unit = f32 ? 32 : 64;
   const double tiles = ceil_div(p.inner, side) * ceil_div(p.outer, side), chunks = ds_weight_chunks(p.rows, (int64_t)tiles, (int)unit);
   const double steps = ceil_div(p.groups * ceil_div(mean, unit), chunks), cut = 1 + (p.groups > chunks ? p.groups / chunks : 0) + (chunks > 1 ? 1 : 0);
@@ -373,6 +406,11 @@ int element_of() {
   return sizeof(T) == 4 ? DS_ELEM_F32 : std::is_same<T, __bf16>::value ? DS_ELEM_BF16 : DS_ELEM_F16;
 }
 
+// Twice the waves to a workgroup that takes up to 32 rows, where workgroups are few and the contraction is long (8 rows to a group, bf16 / fp32; 8 groups by
+// 4,096 x 1,024, 64 / 128 workgroups: 26.6 -> 19.7 us / 42 -> 33; 1 group by 1,024 x 1,024: 9.9 -> 11.8 / 12.1 -> 10.9; 8 groups by 1,024 x 4,096, 256 / 512
+// workgroups: 15.2 -> 15.0 / 23.6 -> 25.5; 64 rows to a group: no faster anywhere)
+bool eight_waves(double workgroups, int depth, int step) { return workgroups <= 128 && depth >= 16 * step; }
+
 template <typename T, bool TRANSPOSED>
 int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   if (p.rows == 0) return DS_OK;
@@ -385,13 +423,16 @@ int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
   if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
   const dim3 grid((unsigned)tiles), block(64 * kWaves);
+  const bool many = eight_waves(p.groups * ceil_div((double)mean, 1 << shift) * a.col_tiles, TRANSPOSED ? p.outer : p.inner, kWaves * 4 * N);
   // (rows of at least 16 bytes each would not be enough to ask for: an operand may have one row)
   const bool tiny = tiny_matrix<T>(TRANSPOSED ? a.dys : a.xs, p.rows, TRANSPOSED ? p.outer : p.inner) ||
                     tiny_matrix<T>((int64_t)p.inner * p.outer, p.groups, (int64_t)p.inner * p.outer) || (a.gate && tiny_matrix<T>(a.gs, p.rows, p.inner));
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, TRANSPOSED, true>), dim3((unsigned)(ds_most_tiles(a, 6) * a.col_tiles)), block, 0, stream, a);
-  else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, TRANSPOSED, false>), grid, block, 0, stream, a);
-  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, TRANSPOSED, false>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, TRANSPOSED, false>), grid, block, 0, stream, a);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, true>), dim3((unsigned)(ds_most_tiles(a, 6) * a.col_tiles)), block, 0, stream, a);
+  else if (shift == 4 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, false>), grid, dim3(512), 0, stream, a);
+  else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, false>), grid, block, 0, stream, a);
+  else if (shift == 5 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, false>), grid, dim3(512), 0, stream, a);
+  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, false>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false>), grid, block, 0, stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -400,10 +441,13 @@ template <typename T>
 int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   constexpr int N = Piece<T>::N;
   a.col_tiles = (p.outer + 16 * N - 1) / (16 * N);
-  const dim3 grid((unsigned)(((p.inner + 8 * N - 1) / (8 * N)) * a.col_tiles), p.groups), block(64 * kWaves);
+  const bool shared = weights_shared(p);
+  const int width = shared ? 8 * N : 16 * N;   // inner columns of a workgroup
+  const dim3 grid((unsigned)((p.inner + width - 1) / width * a.col_tiles), p.groups), block(64 * kWaves);
   const bool tiny = tiny_matrix<T>(a.xs, p.rows, p.inner) || tiny_matrix<T>(a.dys, p.rows, p.outer);
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true>), grid, block, 0, ctx->stream, a);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, false>), grid, block, 0, ctx->stream, a);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, true>), dim3((unsigned)((p.inner + 8 * N - 1) / (8 * N) * a.col_tiles), p.groups), block, 0, ctx->stream, a);
+  else if (shared) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, false>), grid, block, 0, ctx->stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, false, false>), grid, block, 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
