@@ -46,7 +46,7 @@ int check_groups(ds_ctx* ctx, int64_t rows, int64_t groups, const int64_t* offse
 int64_t norm_bytes(int64_t rows, int64_t cols) { return ds_layer_norm_partials(rows, (int)cols) * 2 * cols * (int64_t)sizeof(float); }
 int64_t group_bytes(int64_t rows, int64_t groups) {
   const int64_t blocks = ds_group_blocks((int)rows);
-  return blocks > 1 ? blocks * (groups + 1) * (int64_t)sizeof(int32_t) : 0;
+  return blocks > 1 ? (blocks + 1) * (groups + 1) * (int64_t)sizeof(int32_t) : 0;
 }
 
 }  // namespace

@@ -6,8 +6,8 @@
 // a popcount and the lowest lane adds the step's count in LDS: no atomic decides an order, and the result is the
 // only one there is. Several workgroups: a first launch leaves every stretch's counts, a second adds up the ones before its own
 // (ids are read twice, from the caches the second time). Its bytes are nothing (1,000,175 rows 1.6 us): what it takes is the latency of its steps.
-// 1,010 rows in 8 groups 8 us; 1,000,175 rows in 64 groups 19 us (counts 6, places 14: each workgroup reads all workgroups' counts, 5 us
-// there, and 50 of the 65 us of as many rows in 1,024 groups); 10,000,000 rows in 64 groups 137 us.
+// 1,010 rows in 8 groups 8 us; 1,000,175 rows in 64 groups 19 us (counts 6, places 14, of which every workgroup's reading of all counts is 5);
+// 10,000,000 rows in 64 groups 137 us. Where the counts are many, a launch between the two adds them up.
 #include "feature_ops.h"
 #include "rows.h"
 
@@ -16,11 +16,16 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kStretch = 2048;    // rows of a workgroup, at the least, where there are several (12,000 rows in 64 groups: 4,096 22.6 us, 2,048 11.7)
 
+constexpr int kMostBlocks = 256;   // workgroups (one to a compute unit: their counts in LDS)
+constexpr int kSummed = 28000;     // counts from which a launch of its own adds them up, below which every workgroup does (1,000,175 rows in 64 groups,
+                                   // 16,640 counts: 21.5 us with the launch, 19.3 without; 100,000 in 1,000, 49,049: 17.0, 22.2; 1,000,000 in 1,024: 29, 63)
+
 struct GroupArgs {
   const int32_t* ids;
   int rows, groups, per_wave;   // rows of a wave, a multiple of 64
   int64_t* offsets;
-  int32_t *order, *counts;      // counts: [block][groups + 1]
+  int32_t *order, *counts;      // counts: [block][groups + 1], and behind them the groups' rows
+  bool summed;                  // group_before_kernel has been over the counts
 };
 
 // the lanes whose key is this lane's
@@ -90,6 +95,35 @@ __global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a) {
   }
 }
 
+// Turns the workgroups' counts into the rows of the group before each of them, and leaves the groups' rows behind them: a lane a group, every wave a
+// sixteenth of the (at most 256) workgroups
+__global__ __launch_bounds__(kThreads) void group_before_kernel(GroupArgs a, int blocks) {
+  __shared__ int sum[kWaves][64];
+  const int keys = a.groups + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, key = (int)blockIdx.x * 64 + lane;
+  const int each = (blocks + kWaves - 1) / kWaves, first = wave * each;
+  int n[kMostBlocks / kWaves], all = 0;
+#pragma unroll
+  for (int j = 0; j < kMostBlocks / kWaves; ++j)
+    n[j] = j < each && first + j < blocks && key < keys ? a.counts[(int64_t)(first + j) * keys + key] : 0;
+#pragma unroll
+  for (int j = 0; j < kMostBlocks / kWaves; ++j) all += n[j];
+  sum[wave][lane] = all;
+  __syncthreads();
+  int before = 0, whole = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += sum[w][lane];
+    whole += sum[w][lane];
+  }
+  if (key >= keys) return;
+#pragma unroll
+  for (int j = 0; j < kMostBlocks / kWaves; ++j) {
+    if (j < each && first + j < blocks) a.counts[(int64_t)(first + j) * keys + key] = before;
+    before += n[j];
+  }
+  if (wave == 0) a.counts[(int64_t)blocks * keys + key] = whole;
+}
+
 __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a) {
   extern __shared__ int count[];   // [waves][keys], then the rows of a group in the whole and before this workgroup
   __shared__ int wave_sum[kWaves];
@@ -102,6 +136,12 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a) {
       for (int w = 0; w < kWaves; ++w) n += count[w * keys + g];
       whole[g] = n;
       before[g] = 0;
+    }
+  } else if (a.summed) {
+    const int mine = (int)blockIdx.x * keys, all = (int)gridDim.x * keys;
+    for (int g = threadIdx.x; g < keys; g += kThreads) {
+      before[g] = a.counts[mine + g];
+      whole[g] = a.counts[all + g];
     }
   } else {
     for (int g = threadIdx.x; g < keys; g += kThreads) whole[g] = before[g] = 0;
@@ -164,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a) {
 // one, 14.2 in two; 8,000: 15.1, 14.0, in 4 groups 11.3, 13.9).
 int ds_group_blocks(int rows) {
   const int blocks = (rows + kStretch - 1) / kStretch;
-  return blocks <= 4 ? 1 : blocks < 256 ? blocks : 256;
+  return blocks <= 4 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks;
 }
 
 int ds_launch_group_rows(ds_ctx* ctx, const int32_t* ids, int rows, int groups, int64_t* offsets, int32_t* order, int32_t* counts) {
@@ -184,6 +224,8 @@ int ds_launch_group_rows(ds_ctx* ctx, const int32_t* ids, int rows, int groups, 
     DS_HIP(ctx, hipFuncSetAttribute((const void*)group_place_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   }
   if (blocks > 1) hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kThreads), lds, ctx->stream, a);
+  a.summed = blocks > 1 && blocks * (groups + 1) >= kSummed;
+  if (a.summed) hipLaunchKernelGGL(group_before_kernel, dim3((groups + 64) / 64), dim3(kThreads), 0, ctx->stream, a, blocks);
   hipLaunchKernelGGL(group_place_kernel, dim3(blocks > 0 ? blocks : 1), dim3(kThreads), lds, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
