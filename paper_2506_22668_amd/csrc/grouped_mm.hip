@@ -39,41 +39,46 @@ constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 // wave has eight pieces of W a step in flight without a barrier. W is read in its own order: where its rows run along the
 // columns of the result (TRANSPOSED false: N steps of the contraction by 8 columns to a lane) the lane turns its square of
 // elements around in registers; column j of the squares of 16 lanes is an operand, so that a lane ends up with N neighbouring columns of a
-// row. TRANSPOSED: the product with W^T, whose pieces are operands as they are.
+// row. TRANSPOSED: the product with W^T, whose pieces are operands as they are (HALF: of half
+// the columns and twice the contraction: more workgroups, and a wave reads whole lines of 128 bytes of a row; see half_columns).
 // Loads have no branches, which they would be waited for at: a piece that reaches over its row's end brings the next row's elements along. Columns
 // that there are not lead to results that nobody stores; where the contraction ends, the last step clears them. A piece that would reach over
 // the matrix' end, which it can in its last N rows alone, is read so that it ends there, and shifted. (TINY: matrices of less than 16 bytes, element by element.)
 // Bound by reading W, from memory once if a group has one tile of rows: 8 rows in 8 groups by 1,024 x 4,096 bf16 14.0 us, 4.8 TB/s.
-template <typename T, int RB, int WAVES, bool TRANSPOSED, bool TINY>
+template <typename T, int RB, int WAVES, bool TRANSPOSED, bool HALF, bool TINY>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
-  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6, STEP = WAVES * 4 * N;
-  __shared__ float meet[WAVES][4][64][N];
+  constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
+  constexpr int COLS = HALF ? N / 2 : N, HALVES = N / COLS, STEP = WAVES * 4 * N * HALVES;   // of a lane's columns, and pieces of each
+  __shared__ float meet[WAVES][4][64][COLS];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
-  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * N;
+  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * COLS;
   GroupTiles all(a.offsets, a.groups, a.rows, SHIFT, true);
   if (tile >= all.count()) return;
   const GroupTile gt = all.find(tile);
   int row[RB];
 #pragma unroll
   for (int r = 0; r < RB; ++r) row[r] = gt.begin + 16 * r + m < gt.end ? ds_ordered_row(a.order, a.rows, gt.begin + 16 * r + m) : -1;
-  f32x4 acc[RB][N] = {};
+  f32x4 acc[RB][COLS] = {};
   const int64_t xs = TRANSPOSED ? a.dys : a.xs;
   const T* x = (const T*)(TRANSPOSED ? a.dy : a.x);
   if (gt.group < a.groups) {
     const T *w = (const T*)a.w + (int64_t)gt.group * a.inner * a.outer, *w_end = (const T*)a.w + (int64_t)a.groups * a.inner * a.outer;
     const T* x_end = x + (int64_t)(a.rows - 1) * xs + depth;
-    const int n0 = col + N * m;   // the lane's columns
-    PieceV<T> wp[N], xp[RB];
+    const int n0 = col + COLS * m;   // the lane's columns
+    PieceV<T> wp[N], xp[RB * HALVES];
     const auto over = [](const T* p, const T* end) -> unsigned {
       const int64_t by = p + N - end;
       return by <= 0 ? 0 : by < N ? (unsigned)by : N;
     };
     const auto w_at = [&](int k, int i) -> const T* {
-      if constexpr (TRANSPOSED) return w + (int64_t)min(n0 + i, width - 1) * a.outer + min(k, depth - 1);
+      if constexpr (TRANSPOSED) return w + (int64_t)min(n0 + i / HALVES, width - 1) * a.outer + min(k + i % HALVES * 4 * N, depth - 1);
       else return w + (int64_t)min(k + i, depth - 1) * a.outer + min(n0, width - 1);
     };
-    const auto x_at = [&](int k, int r) -> const T* { return x + (row[r] < 0 ? 0 : row[r]) * xs + min(k, depth - 1); };
+    const auto x_at = [&](int k, int i) -> const T* {
+      const int r = row[i / HALVES];
+      return x + (r < 0 ? 0 : r) * xs + min(k + i % HALVES * 4 * N, depth - 1);
+    };
     const auto fetch = [&](int k) {
       k += N * q;
 #pragma unroll
@@ -87,7 +92,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
         }
       }
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
+      for (int r = 0; r < RB * HALVES; ++r) {
         if constexpr (TINY) {
           xp[r] = load_piece<T>(x + row[r] * xs + k, row[r] >= 0 ? depth - k : 0);
         } else {
@@ -103,20 +108,20 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
       for (int i = 0; i < N; ++i) {
         const unsigned by = over(w_at(k, i), w_end);
         if (__any(by)) wp[i] = shifted<T>(wp[i], by);
-        wp[i] = first_elements<T>(wp[i], TRANSPOSED ? depth - k : k + i < depth ? N : 0);
+        wp[i] = first_elements<T>(wp[i], TRANSPOSED ? depth - k - i % HALVES * 4 * N : k + i < depth ? N : 0);
       }
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
+      for (int r = 0; r < RB * HALVES; ++r) {
         const unsigned by = over(x_at(k, r), x_end);
         if (__any(by)) xp[r] = shifted<T>(xp[r], by);
-        xp[r] = first_elements<T>(xp[r], depth - k);
+        xp[r] = first_elements<T>(xp[r], depth - k - r % HALVES * 4 * N);
       }
     };
-    int k = wave * 4 * N;
+    int k = wave * 4 * N * HALVES;
     if (k < depth) fetch(k);
     while (k < depth) {
-      if (!TINY && k + 5 * N > depth) clear(k);
-      PieceV<T> wn[N], xn[RB];
+      if (!TINY && k + 4 * N * HALVES + N > depth) clear(k);
+      PieceV<T> wn[N], xn[RB * HALVES];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         if constexpr (TRANSPOSED) {
@@ -127,22 +132,24 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
         }
       }
 #pragma unroll
-      for (int r = 0; r < RB; ++r) xn[r] = xp[r];
+      for (int r = 0; r < RB * HALVES; ++r) xn[r] = xp[r];
       k += STEP;
       if (k < depth) fetch(k);
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+      for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-        for (int r = 0; r < RB; ++r) acc[r][j] = multiply(wn[j], xn[r], acc[r][j]);
+        for (int j = 0; j < COLS; ++j)
+#pragma unroll
+          for (int r = 0; r < RB; ++r) acc[r][j] = multiply(wn[j * HALVES + h], xn[r * HALVES + h], acc[r][j]);
     }
   }
   const T *gate = (const T*)a.gate, *gate_end = gate + (int64_t)(a.rows - 1) * a.gs + width;
   T* y = (T*)a.y;
-  // wave w ends up with the four columns' quarter w of every row block: columns col + N (4 q + w) .. + N - 1
-  const int n = col + N * (4 * q + (wave & 3));
-  float bias[N];
+  // wave w ends up with the four columns' quarter w of every row block: columns col + COLS (4 q + w) .. + COLS - 1
+  const int n = col + COLS * (4 * q + (wave & 3));
+  float bias[COLS];
 #pragma unroll
-  for (int j = 0; j < N; ++j)
+  for (int j = 0; j < COLS; ++j)
     bias[j] = !TRANSPOSED && a.bias && gt.group < a.groups ? a.bias[(int64_t)gt.group * width + min(n + j, width - 1)] : 0.f;
   PieceV<T> open[RB];
   if (TRANSPOSED && gate && wave < 4) {
@@ -158,12 +165,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < N; ++j) meet[wave][i][lane][j] = acc[r][j][i];
+      for (int j = 0; j < COLS; ++j) meet[wave][i][lane][j] = acc[r][j][i];
     __syncthreads();
     if (wave < 4 && row[r] >= 0 && n < width) {
-      PieceV<T> out;
+      PieceV<T> out = {};
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
+      for (int j = 0; j < COLS; ++j) {
         float v = bias[j];
 #pragma unroll
         for (int s = 0; s < WAVES; ++s) v += meet[s][wave & 3][lane][j];
@@ -172,8 +179,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
         out[j] = (T)v;
       }
       T* to = y + row[r] * a.ys + n;
-      if (n + N <= width) *reinterpret_cast<typename Piece<T>::U*>(to) = out;
-      else store_first<T>(to, out, width - n);
+      if constexpr (COLS == N) store_piece<T>(to, out, width - n);
+      else store_first<T>(to, out, min(width - n, COLS));
     }
   }
 }
@@ -411,28 +418,44 @@ int element_of() {
 // workgroups: 15.2 -> 15.0 / 23.6 -> 25.5; 64 rows to a group: no faster anywhere)
 bool eight_waves(double workgroups, int depth, int step) { return workgroups <= 128 && depth >= 16 * step; }
 
+// The product with W^T of half the columns to a workgroup, where those of all would be at most 128 workgroups; with more, reading the rows twice as often
+// counts (both gradients in us, all / half columns; 8 groups by 1,024 x 4,096, 64 workgroups, bf16: 8 rows 73 / 59, 64 rows 80 / 65; 128 rows, 128 workgroups
+// 85 / 71; 256 rows, 256 workgroups 95 / 112; fp32, 4 groups by 1,024 x 4,096: 8 rows, 64 workgroups 68 / 55, 256 rows, 256 workgroups 211 / 227)
+bool half_columns(double workgroups) { return workgroups <= 128; }
+
+template <typename T, bool TRANSPOSED, bool HALF>
+void launch_few(int shift, bool many, unsigned grid, const MmArgs& a, hipStream_t stream) {
+  const dim3 block(64 * kWaves), twice(64 * 8);
+  if (shift == 4 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
+  else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
+  else if (shift == 5 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
+  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
+}
+
 template <typename T, bool TRANSPOSED>
 int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   if (p.rows == 0) return DS_OK;
   constexpr int N = Piece<T>::N;
   hipStream_t stream = ctx->stream;
-  a.col_tiles = ((TRANSPOSED ? p.inner : p.outer) + 16 * N - 1) / (16 * N);
-  const int64_t mean = (p.rows + p.groups - 1) / p.groups;
-  if (rows_in_tiles(p, element_of<T>(), TRANSPOSED ? p.outer : p.inner, TRANSPOSED ? p.inner : p.outer)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
-  const int shift = mean <= 16 ? 4 : mean <= 32 ? 5 : 6;
-  const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
-  if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, TRANSPOSED ? p.inner : p.outer);
-  const dim3 grid((unsigned)tiles), block(64 * kWaves);
-  const bool many = eight_waves(p.groups * ceil_div((double)mean, 1 << shift) * a.col_tiles, TRANSPOSED ? p.outer : p.inner, kWaves * 4 * N);
   // (rows of at least 16 bytes each would not be enough to ask for: an operand may have one row)
   const bool tiny = tiny_matrix<T>(TRANSPOSED ? a.dys : a.xs, p.rows, TRANSPOSED ? p.outer : p.inner) ||
                     tiny_matrix<T>((int64_t)p.inner * p.outer, p.groups, (int64_t)p.inner * p.outer) || (a.gate && tiny_matrix<T>(a.gs, p.rows, p.inner));
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, true>), dim3((unsigned)(ds_most_tiles(a, 6) * a.col_tiles)), block, 0, stream, a);
-  else if (shift == 4 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, false>), grid, dim3(512), 0, stream, a);
-  else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, false>), grid, block, 0, stream, a);
-  else if (shift == 5 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, false>), grid, dim3(512), 0, stream, a);
-  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, false>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false>), grid, block, 0, stream, a);
+  const int depth = TRANSPOSED ? p.outer : p.inner, width = TRANSPOSED ? p.inner : p.outer;
+  const int64_t mean = (p.rows + p.groups - 1) / p.groups;
+  if (rows_in_tiles(p, element_of<T>(), depth, width)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
+  const int shift = tiny || mean > 32 ? 6 : mean > 16 ? 5 : 4;
+  const double blocks = p.groups * ceil_div((double)mean, 1 << shift);   // (about: the sizes of groups are not known here)
+  const bool half = TRANSPOSED && !tiny && half_columns(blocks * ceil_div(width, 16 * N));
+  const int cols = half ? 8 * N : 16 * N;   // of a workgroup
+  a.col_tiles = (width + cols - 1) / cols;
+  const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
+  if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, width);
+  const bool many = eight_waves(blocks * a.col_tiles, depth, kWaves * 4 * N);
+  const unsigned grid = (unsigned)tiles;
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false, true>), dim3(grid), dim3(64 * kWaves), 0, stream, a);
+  else if (half) launch_few<T, TRANSPOSED, TRANSPOSED>(shift, many, grid, a, stream);
+  else launch_few<T, TRANSPOSED, false>(shift, many, grid, a, stream);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }

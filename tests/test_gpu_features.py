@@ -390,6 +390,15 @@ def test_grouped_mm_many_tiles(ctx, t, rows, inner, outer, groups):
     test_grouped_mm_backward(ctx, t, rows, inner, outer, groups)
 
 
+# few rows to a group: long contractions of few workgroups, and many workgroups
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", [(20, 2100, 136, 2), (50, 2101, 131, 2), (20, 136, 2100, 2), (50, 131, 2101, 2), (100, 72, 2056, 2),
+                                                        (300, 520, 264, 40), (1000, 515, 257, 40), (2000, 520, 1024, 40)])
+def test_grouped_mm_few_rows(ctx, t, rows, inner, outer, groups):
+    test_grouped_mm(ctx, t, rows, inner, outer, groups)
+    test_grouped_mm_backward(ctx, t, rows, inner, outer, groups)
+
+
 # widths below a 16-byte piece, contractions that end right behind a step, matrices of less than 16 bytes
 NARROW = [(3, 1, 1, 1), (1, 1, 2, 1), (2, 3, 1, 2), (40, 33, 3, 2), (40, 3, 33, 2), (90, 65, 1, 1), (90, 1, 65, 1), (700, 40, 5, 3), (700, 5, 40, 3),
           (300, 34, 9, 1), (200, 129, 130, 2), (1, 33, 7, 1), (33, 128, 7, 1), (600, 8, 8, 2), (600, 9, 15, 2)]
