@@ -405,7 +405,8 @@ int ds_grouped_mm(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64
 
 /* Gradients of ds_grouped_mm without its ReLU: dx[r] = dy[r] w[g]^T (zeros for rows of no group), dw[g] = sum over the
  * group's rows of x[r]^T dy[r], db: float[groups x outer] = sum of dy[r] (zeros for an empty group). gate: NULL, or rows like x:
- * dx is 0 where gate is not above 0 (the ReLU whose output x was). */
+ * dx is 0 where gate is not above 0 (the ReLU whose output x was). Where offsets do not ascend or order names a row twice or not at all, some
+ * gradients are left unwritten or belong to other rows, and nothing outside of the buffers is touched. */
 int ds_grouped_mm_backward_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups,
                                      int64_t* bytes /* [host] */);
 int ds_grouped_mm_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, const void* dy,

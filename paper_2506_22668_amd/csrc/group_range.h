@@ -21,3 +21,20 @@ DS_GROUP_FN int ds_ordered_row(const int32_t* order, int rows, int at) {
   const int r = order[at];
   return r >= 0 && r < rows ? r : -1;
 }
+
+// The rows cut into tiles (or steps) of `size`, group by group; `parts` counts the groups that can end inside one, the rows of no group among
+// them where they have tiles. As many as there can be if the offsets ascend: at most rows / 16 + 1,025.
+DS_GROUP_FN int ds_most_parts(int rows, int size, int parts) { return rows / size + (parts < rows ? parts : rows); }
+DS_GROUP_FN int ds_parts_of(int begin, int end, int size) { return (int)(((int64_t)(end - begin) + size - 1) / size); }
+
+// Sums of tiles stop at `most`. Offsets that do not ascend can give every group all rows, and 1,024 times 2^30 rows are more tiles than an int
+// counts. Sums of offsets that ascend never meet the end, and a capped sum is associative, so it can be formed in any order.
+DS_GROUP_FN int ds_add_parts(int a, int b, int most) { return a + b < most ? a + b : most; }
+
+// Workgroups [*first, *last] of `wgs` that share the `own` (> 0) steps of a group, in a line of `all` steps cut evenly, where `before` steps lie in
+// front of them (capped sums both). owner(x): the workgroup of step x.
+template <typename Owner>
+DS_GROUP_FN void ds_group_owners(int before, int own, int all, const Owner& owner, int* first, int* last) {
+  *first = owner(before < all ? before : all - 1);
+  *last = owner(ds_add_parts(before, own, all) - 1);
+}

@@ -1,6 +1,7 @@
 // What the two forms of the products by group share (no part of the ABI).
 #pragma once
 #include "feature_ops.h"
+#include "group_range.h"
 
 struct MmArgs {
   int rows, inner, outer, groups;
@@ -17,8 +18,7 @@ struct MmArgs {
 
 // tiles of 2^shift rows that the groups and the rows of none can have: every group may end inside one
 static inline int64_t ds_most_tiles(const MmArgs& a, int shift) {
-  const int64_t partial = a.groups + 1 < a.rows ? a.groups + 1 : a.rows;
-  return ((int64_t)a.rows >> shift) + partial;
+  return ds_most_parts(a.rows, 1 << shift, a.groups + 1);
 }
 
 // The product by rows in tiles through LDS (grouped_tiles.hip); transposed: dx = dy w^T

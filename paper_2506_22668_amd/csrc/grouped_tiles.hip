@@ -144,7 +144,7 @@ struct GroupTable {
 // Fills the table (all threads of the workgroup); the number of tiles
 template <int THREADS, int SHIFT>
 __device__ __forceinline__ int fill_table(GroupTable& t, const MmArgs& a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, most = ds_most_parts(a.rows, 1 << SHIFT, a.groups + 1);
   int before = 0;
   for (int base = 0; base < kMostGroups; base += THREADS) {
     const int g = base + (int)threadIdx.x;
@@ -154,22 +154,22 @@ __device__ __forceinline__ int fill_table(GroupTable& t, const MmArgs& a) {
     }
     int begin = 0, end = 0;
     if (g < a.groups) ds_group_range(a.offsets, a.groups, a.rows, g, &begin, &end);
-    int upto = (int)(((int64_t)(end - begin) + (1 << SHIFT) - 1) >> SHIFT);
+    int upto = ds_parts_of(begin, end, 1 << SHIFT);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += up;
+      if (lane >= o) upto = ds_add_parts(upto, up, most);
     }
     if (lane == 63) t.waves[wave] = upto;
     __syncthreads();
     int all = 0;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) {
-      if (w < wave) upto += t.waves[w];
-      all += t.waves[w];
+      if (w < wave) upto = ds_add_parts(upto, t.waves[w], most);
+      all = ds_add_parts(all, t.waves[w], most);
     }
-    t.upto[g] = before + upto;
-    before += all;
+    t.upto[g] = ds_add_parts(before, upto, most);
+    before = ds_add_parts(before, all, most);
     __syncthreads();
   }
   __syncthreads();
@@ -526,13 +526,13 @@ bool sixteen(const void* p, int64_t stride, size_t element) { return (uintptr_t)
 // the steps of a group's contraction
 __device__ __forceinline__ int group_steps(const MmArgs& a, int g, int depth, int* begin, int* end) {
   ds_group_range(a.offsets, a.groups, a.rows, g, begin, end);
-  return (*end - *begin + depth - 1) / depth;
+  return ds_parts_of(*begin, *end, depth);
 }
 
 // Steps of all groups, and where step `unit` of the line falls: its group (-1: behind the end) and the steps before it there. Called by whole
 // waves, the same answer in every lane.
 __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit, int* group, int* within) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, most = ds_most_parts(a.rows, depth, a.groups);
   int before = 0;
   *group = -1;
   for (int base = 0; base < a.groups; base += 64) {
@@ -542,15 +542,16 @@ __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit,
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += up;
+      if (lane >= o) upto = ds_add_parts(upto, up, most);
     }
-    const unsigned long long reach = __ballot(before + upto > unit);
+    upto = ds_add_parts(before, upto, most);
+    const unsigned long long reach = __ballot(upto > unit);
     if (reach && *group < 0) {
       const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)reach) - 1);
       *group = base + src;
-      *within = unit - __builtin_amdgcn_readlane(before + upto - own, src);
+      *within = unit - __builtin_amdgcn_readlane(upto - own, src);
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
+    before = __builtin_amdgcn_readlane(upto, 63);
   }
   return before;
 }
@@ -749,21 +750,21 @@ __global__ __launch_bounds__(kJoin) void weight_join_kernel(MmArgs a, const floa
   int first = 0, last = -1;
   if (steps > 0) {
     // where the group's steps lie in the line: those of the groups before it first
+    const int most = ds_most_parts(a.rows, UNIT, a.groups);
     int mine = 0, all = 0;
     for (int g = threadIdx.x & 63; g < a.groups; g += 64) {
       int b, e;
       const int own = group_steps(a, g, UNIT, &b, &e);
-      all += own;
-      if (g < group) mine += own;
+      all = ds_add_parts(all, own, most);
+      if (g < group) mine = ds_add_parts(mine, own, most);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
-      all += __shfl_xor(all, o, 64);
-      mine += __shfl_xor(mine, o, 64);
+      all = ds_add_parts(all, __shfl_xor(all, o, 64), most);
+      mine = ds_add_parts(mine, __shfl_xor(mine, o, 64), most);
     }
     const int chunks = min(all, most_chunks);
-    first = (int)ds_mm_even_owner(mine, chunks, all);
-    last = (int)ds_mm_even_owner(mine + steps - 1, chunks, all);
+    ds_group_owners(mine, steps, all, [&](int step) { return (int)ds_mm_even_owner(step, chunks, all); }, &first, &last);
     if (first == last) return;
   }
   const int across = kJoin / lanes, at = (int)threadIdx.x % across, turn = (int)threadIdx.x / across;

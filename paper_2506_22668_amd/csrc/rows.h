@@ -149,7 +149,7 @@ class GroupTiles {
     const unsigned long long reach = __ballot(upto_ > tile);
     const int src = reach ? __ffsll((long long)reach) - 1 : 63;
     const int g = __builtin_amdgcn_readfirstlane(src);
-    const int first = __builtin_amdgcn_readlane(upto_ - tiles_, g);
+    const int first = __builtin_amdgcn_readlane(upto_ - tiles_, g);   // (where the sum is capped, before its first tile: the tile lies in its rows all the same)
     const int b = __builtin_amdgcn_readlane(begin_, g), e = __builtin_amdgcn_readlane(end_, g);
     GroupTile t;
     t.group = base_ + g;
@@ -169,14 +169,15 @@ class GroupTiles {
     before_ = before;
     begin_ = end_ = 0;
     if (g < held_) ds_group_range(offsets_, groups_, rows_, g, &begin_, &end_);
-    tiles_ = (int)(((int64_t)(end_ - begin_) + (1 << shift_) - 1) >> shift_);
+    tiles_ = ds_parts_of(begin_, end_, 1 << shift_);
     upto_ = tiles_;
+    const int most = ds_most_parts(rows_, 1 << shift_, held_);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(upto_, o, 64);
-      if (lane >= o) upto_ += up;
+      if (lane >= o) upto_ = ds_add_parts(upto_, up, most);
     }
-    upto_ += before;
+    upto_ = ds_add_parts(upto_, before, most);
     last_ = __builtin_amdgcn_readlane(upto_, 63);
   }
 };

@@ -175,3 +175,74 @@ def test_rows_of_a_group_stay_inside_whatever_the_offsets_hold(tmp_path):
     src.write_text(MAIN)
     subprocess.run([cxx, "-std=c++17", "-I", os.path.join(ROOT, "paper_2506_22668_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout == "0\n"
+
+
+TILES = r"""
+#include <stdio.h>
+#include <stdlib.h>
+#include <vector>
+#include "group_range.h"
+#include "mm_split.h"
+static unsigned long long state = 88172645463325252ull;
+static unsigned long long draw() { state ^= state << 13; state ^= state >> 7; state ^= state << 17; return state; }
+int main() {
+  long bad = 0, capped = 0;
+  const int sizes[] = {16, 32, 64, 128, 256};
+  const int all_rows[] = {1, 5, 1000, 70001, 1 << 22, 1 << 28, 1 << 29, 1 << 30};
+  const int all_groups[] = {1, 2, 64, 65, 1000, 1024};
+  for (int rows : all_rows) for (int groups : all_groups) for (int size : sizes) for (int shape = 0; shape < 4; ++shape) {
+    std::vector<int64_t> offsets(groups + 1);
+    for (int g = 0; g <= groups; ++g)
+      offsets[g] = shape == 0 ? (int64_t)rows * g / groups                               // ascending: the tiles are exact
+                 : shape == 1 ? (g % 2 ? rows : 0)                                        // every other group has all rows
+                 : shape == 2 ? (int64_t)(draw() % (2ull * rows)) - rows / 2 : (g % 2 ? (int64_t)1 << 62 : -((int64_t)1 << 62));
+    for (int none = 0; none < 2; ++none) {   // with the tiles of the rows of no group (row products), or without (gradients of the weights)
+      const int most = ds_most_parts(rows, size, groups + none);
+      std::vector<int> upto(groups + none), begin(groups + none), end(groups + none);
+      long long exact = 0;
+      int sum = 0;
+      for (int g = 0; g < groups + none; ++g) {
+        ds_group_range(offsets.data(), groups, rows, g, &begin[g], &end[g]);
+        exact += ds_parts_of(begin[g], end[g], size);
+        upto[g] = sum = ds_add_parts(sum, ds_parts_of(begin[g], end[g], size), most);
+      }
+      bad += sum < 0 || sum > most || (shape == 0 && sum != exact);
+      capped += sum != exact;
+      for (int g = 0; g < groups + none; ++g) {
+        const int before = g ? upto[g - 1] : 0, own = ds_parts_of(begin[g], end[g], size);
+        if (upto[g] <= before) continue;
+        const int ends[] = {before, upto[g] - 1};
+        for (int tile : ends) {
+          // counted from the sum in front of the group, or from its own sum back
+          const int64_t one = begin[g] + (int64_t)(tile - before) * size, other = begin[g] + (int64_t)(tile - (upto[g] - own)) * size;
+          bad += one < begin[g] || one >= end[g] || other < begin[g] || other >= end[g] || (shape == 0 && one != other);
+        }
+      }
+      if (none) continue;
+      for (int wgs : {1, 3, 256, 512}) {
+        const int chunks = sum < wgs ? sum : wgs;
+        for (int g = 0; g < groups; ++g) {
+          const int before = g ? upto[g - 1] : 0, own = ds_parts_of(begin[g], end[g], size);
+          if (own == 0) continue;
+          int first = -1, last = -1;
+          ds_group_owners(before, own, sum, [&](int x) { return (int)ds_mm_even_owner(x, chunks, sum); }, &first, &last);
+          bad += first < 0 || last < first || last >= chunks;
+          if (shape == 0) bad += first != ds_mm_even_owner(before, chunks, sum) || last != ds_mm_even_owner(before + own - 1, chunks, sum);
+        }
+      }
+    }
+  }
+  printf("%ld %d\n", bad, capped > 0);
+}
+"""
+
+
+def test_tiles_of_offsets_that_do_not_ascend_are_counted_without_an_overflow(tmp_path):
+    """1,024 groups that all have up to 2^30 rows: tiles, steps and workgroups stay in range, and are exact where offsets ascend."""
+    cxx = shutil.which("g++")
+    assert cxx, "g++ is needed"
+    src, exe = tmp_path / "tiles.cpp", tmp_path / "tiles"
+    src.write_text(TILES)
+    subprocess.run([cxx, "-std=c++17", "-O1", "-fsanitize=signed-integer-overflow", "-fno-sanitize-recover", "-I",
+                    os.path.join(ROOT, "paper_2506_22668_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout == "0 1\n"
