@@ -1,0 +1,160 @@
+"""Forms of the operators on rows of features that the sizes alone do not reach: operands that lie as the direct loads of the tiles need
+them, more groups than a wave or a workgroup looks at in one go, orders with holes, outputs over inputs, and buffers of more than 2^31
+elements backwards. Tolerances are those of test_gpu_features.py."""
+import numpy as np
+import pytest
+
+from tests.gpu_common import say
+from tests.test_gpu_features import (BF16, EPS, F16, F32, TYPES, U, close, ctx, generator, grouping, mm_exact, norm_backward_exact,   # noqa: F401
+                                     normal, strided)
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+def check_backward(ctx, dy, x, w, offsets, perm, key, gate):   # noqa: F811
+    """Both gradients against 64 bits, and the same bits again."""
+    got = dx, dw, db = ctx.grouped_mm_backward(dy, x, w, offsets, order=perm, gate=gate)
+    e, size = mm_exact(dy, w.transpose(1, 2), key, None, False)
+    if gate is not None:
+        e, size = e.masked_fill(~(gate > 0), 0.0), size.masked_fill(~(gate > 0), 0.0)
+    close(dx, e, 2 * (w.shape[2] + 2) * U * size)
+    assert not dx[key >= w.shape[0]].any()
+    for k in range(w.shape[0]):
+        at = key == k
+        xk, dk, n = x[at].double(), dy[at].double(), int(at.sum())
+        close(dw[k], xk.t() @ dk, 2 * n * U * (xk.abs().t() @ dk.abs()))
+        close(db[k], dk.sum(0), 2 * n * U * dk.abs().sum(0))
+    again = ctx.grouped_mm_backward(dy, x, w, offsets, order=perm, gate=gate)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+# x and dy on 16 bytes, their rows whole pieces of 16 bytes apart: the gradient of the weights loads them into LDS directly. apart: 0 or a piece.
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", [(5000, 512, 768, 4), (3001, 256, 512, 7), (2049, 264, 136, 3), (1500, 1032, 40, 1),
+                                                        (40003, 136, 256, 7), (33000, 72, 520, 20), (66001, 264, 136, 3)])
+@pytest.mark.parametrize("apart", [0, 8])
+def test_gradients_of_aligned_rows(ctx, t, rows, inner, outer, groups, apart):   # noqa: F811
+    say(f"aligned {t} rows={rows} inner={inner} outer={outer} groups={groups} apart={apart}")
+    rng, g = np.random.default_rng(rows), generator(inner + apart)
+    for order in (True, False):
+        offsets, perm, key = grouping(ctx, rng, rows, groups, order)
+        x, dy = strided(normal(g, rows, inner, t=t), apart), strided(normal(g, rows, outer, t=t), apart)
+        assert x.data_ptr() % 16 == 0 and dy.data_ptr() % 16 == 0
+        w = normal(g, groups, inner, outer, t=t, scale=inner ** -0.5)
+        check_backward(ctx, dy, x, w, offsets, perm, key, x if order else None)
+
+
+def many_groups(ctx, seed, rows, groups, order):   # noqa: F811
+    """Ragged groups of which a third is empty, the first, the last and those next to multiples of 64 and 256 not among them; some rows in none."""
+    rng = np.random.default_rng(seed)
+    held = np.array([k for k in range(groups) if k % 3 != 1 or k % 64 in (0, 1, 63) or k == groups - 1])
+    ids = held[np.minimum(len(held) * rng.random(rows) ** 1.3, len(held) - 1).astype(np.int64)].astype(np.int32)
+    edge = [k for k in (0, 63, 64, 65, 255, 256, 257, 511, 512, 600, groups - 1) if k < groups and k in held]
+    ids[:2 * len(edge)] = edge * 2
+    ids[rng.random(rows) < 0.03] = -1
+    if not order:
+        ids = np.sort(np.where(ids < 0, groups, ids)).astype(np.int32)
+    offsets, perm = ctx.group_rows(torch.from_numpy(ids).cuda(), groups)
+    return offsets, (perm if order else None), torch.from_numpy(np.where(ids < 0, groups, ids)).cuda()
+
+
+# the first four: few rows to a group (rows that the waves share, and not); then tiles of rows, of weights, or both
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", [(900, 24, 40, 65), (6000, 40, 72, 130), (2000, 24, 16, 600), (9000, 16, 24, 1024),
+                                                        (30_000, 64, 264, 65), (60_000, 128, 136, 257), (150_000, 72, 256, 600),
+                                                        (200_000, 256, 64, 1024), (150_000, 131, 67, 513)])
+def test_products_of_many_groups(ctx, t, rows, inner, outer, groups):   # noqa: F811
+    say(f"many groups {t} rows={rows} inner={inner} outer={outer} groups={groups}")
+    g = generator(groups)
+    for order in (True, False):
+        offsets, perm, key = many_groups(ctx, groups, rows, groups, order)
+        x, dy = normal(g, rows, inner, t=t), normal(g, rows, outer, t=t)
+        w, bias = normal(g, groups, inner, outer, t=t, scale=inner ** -0.5), normal(g, groups, outer)
+        y = ctx.grouped_mm(x, w, offsets, order=perm, bias=bias, relu=order)
+        e, size = mm_exact(x, w, key, bias, order)
+        close(y, e, 2 * (inner + 2) * U * size)
+        assert not y[key == groups].any()
+        check_backward(ctx, dy, x, w, offsets, perm, key, x if order else None)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer", [(40, 48, 56), (100, 48, 56), (1500, 48, 56), (6000, 264, 256)])
+def test_orders_with_holes_add_no_other_row(ctx, t, rows, inner, outer):   # noqa: F811
+    """Positions of the order that name no row leave nothing in a gradient; row 0, which a kernel would read in their place, is large."""
+    say(f"order with holes {t} rows={rows} {inner} x {outer}")
+    g = generator(rows)
+    x, dy, w = normal(g, rows, inner, t=t), normal(g, rows, outer, t=t), normal(g, 2, inner, outer, t=t, scale=inner ** -0.5)
+    x[0], dy[0] = 100.0, 50.0
+    offsets = torch.tensor([0, rows // 2, rows], device="cuda")
+    order, key = torch.arange(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int64, device="cuda")
+    key[rows // 2:] = 1
+    holes = torch.tensor([3, rows // 2 - 1, rows // 2, rows - 6, rows - 1], device="cuda")
+    order[holes] = torch.tensor([-7, 2 ** 31 - 1, -2 ** 31, rows, -1], dtype=torch.int32, device="cuda")
+    named = torch.ones(rows, dtype=torch.bool, device="cuda")
+    named[holes] = False
+    y = ctx.grouped_mm(x, w, offsets, order=order)
+    e, size = mm_exact(x, w, key, None, False)
+    close(y[named], e[named], (2 * (inner + 2) * U * size)[named])
+    dx, dw, db = ctx.grouped_mm_backward(dy, x, w, offsets, order=order)
+    e, size = mm_exact(dy, w.transpose(1, 2), key, None, False)
+    close(dx[named], e[named], (2 * (outer + 2) * U * size)[named])
+    for k in range(2):
+        at = named & (key == k)
+        xk, dk, n = x[at].double(), dy[at].double(), int(at.sum())
+        close(dw[k], xk.t() @ dk, 2 * n * U * (xk.abs().t() @ dk.abs()))
+        close(db[k], dk.sum(0), 2 * n * U * dk.abs().sum(0))
+
+
+@pytest.mark.parametrize("t, element", [(F32, 0), (BF16, 1), (F16, 2)])
+@pytest.mark.parametrize("rows, cols, pad", [(67, 53, 5), (3, 4096, 0), (2000, 515, 0), (700, 2049, 3)])
+def test_norm_gradient_over_its_inputs(ctx, t, element, rows, cols, pad):   # noqa: F811
+    """dx in the buffer of dy, and in that of x, with equal strides."""
+    say(f"layer_norm_backward in place {t} {rows} x {cols}")
+    g = generator(cols)
+    x, dy, w = strided(normal(g, rows, cols, t=t), pad), strided(normal(g, rows, cols, t=t), pad), normal(g, cols)
+    _, mean, rstd = ctx.layer_norm(x, w, want_stats=True)
+    want = ctx.layer_norm_backward(dy, x, mean, rstd, w)
+    ex, ew, eb, size, sw, sb = norm_backward_exact(dy, x, mean, rstd, w)
+    close(want[0], ex, 48 * U * size)
+    ws, ptr, n = ctx._workspace(ctx.lib.ds_layer_norm_backward_workspace, rows, cols)
+    for over in ("dy", "x"):
+        a, b = strided(dy, pad), strided(x, pad)
+        dx = a if over == "dy" else b
+        dw, db = torch.full((2, cols), float("nan"), device="cuda")
+        assert ctx.lib.ds_layer_norm_backward(ctx.h, element, rows, cols, a.data_ptr(), cols + pad, b.data_ptr(), cols + pad, mean.data_ptr(),
+                                              rstd.data_ptr(), w.data_ptr(), dx.data_ptr(), cols + pad, dw.data_ptr(), db.data_ptr(), ptr, n) == 0
+        assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]) and torch.equal(db, want[2])
+    torch.cuda.synchronize()
+
+
+def test_gradients_of_rows_behind_the_first_two_to_the_31_elements(ctx):   # noqa: F811
+    """Offsets past 32 bits backwards: only the first and the last rows of a buffer of more than 2^31 elements are not zero."""
+    say("far rows backward")
+    rows, cols, outer = 540_001, 4096, 24
+    ends = torch.tensor([0, 1, 2, rows - 5, rows - 4, rows - 3, rows - 2, rows - 1], device="cuda")
+    g = generator(11)
+    x = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    x[ends] = normal(g, 8, cols, t=BF16)
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    e = x[ends].double()
+    mean[ends], rstd[ends] = e.mean(1).float(), (1 / torch.sqrt(e.var(1, unbiased=False) + EPS)).float()
+    near, w = normal(g, 8, cols, t=BF16), normal(g, cols)
+    dy = torch.zeros_like(x)
+    dy[ends] = near
+    dx, dw, db = ctx.layer_norm_backward(dy, x, mean, rstd, w)
+    ex, ew, eb, size, sw, sb = norm_backward_exact(near, x[ends], mean[ends], rstd[ends], w)
+    close(dx[ends], ex, 48 * U * size)
+    close(dw, ew, 48 * U * sw)
+    close(db, eb, 48 * U * sb)
+    assert not dx[1000:rows - 1000].any()
+    del dy, dx
+    m = normal(g, 1, cols, outer, t=BF16, scale=cols ** -0.5)
+    dy = torch.zeros(rows, outer, dtype=BF16, device="cuda")
+    dy[ends] = normal(g, 8, outer, t=BF16)
+    dx, dw, db = ctx.grouped_mm_backward(dy, x, m, torch.tensor([0, rows], device="cuda"), gate=x)
+    e, size = mm_exact(dy[ends], m.transpose(1, 2), torch.zeros(8, dtype=torch.int64, device="cuda"), None, False)
+    open_ = x[ends] > 0
+    close(dx[ends], e.masked_fill(~open_, 0.0), (2 * (outer + 2) * U * size).masked_fill(~open_, 0.0))
+    close(dw[0], x[ends].double().t() @ dy[ends].double(), 2 * 8 * U * (x[ends].double().abs().t() @ dy[ends].double().abs()))
+    close(db[0], dy[ends].double().sum(0), 2 * 8 * U * dy[ends].double().abs().sum(0))
