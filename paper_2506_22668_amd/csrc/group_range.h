@@ -38,3 +38,13 @@ DS_GROUP_FN void ds_group_owners(int before, int own, int all, const Owner& owne
   *first = owner(before < all ? before : all - 1);
   *last = owner(ds_add_parts(before, own, all) - 1);
 }
+
+// A launch counts its threads in 32 bits a dimension; of one with more, HIP leaves workgroups out without an error.
+inline int64_t ds_most_workgroups(int threads) { return 0xffffffffll / threads; }
+struct ds_lines {
+  unsigned x, y;   // workgroup number blockIdx.y * x + blockIdx.x; up to y - 1 of them are too many
+};
+inline ds_lines ds_launch_lines(int64_t workgroups, int threads) {
+  const int64_t most = ds_most_workgroups(threads), y = (workgroups + most - 1) / most, x = (workgroups + y - 1) / y;
+  return {(unsigned)x, (unsigned)y};
+}

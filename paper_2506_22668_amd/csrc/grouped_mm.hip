@@ -51,8 +51,9 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
   constexpr int COLS = HALF ? N / 2 : N, HALVES = N / COLS, STEP = WAVES * 4 * N * HALVES;   // of a lane's columns, and pieces of each
   __shared__ float meet[WAVES][4][64][COLS];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
-  const int tile = (int)blockIdx.x / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
-  const int col = ((int)blockIdx.x % a.col_tiles) * 16 * COLS;
+  const int at = (int)(blockIdx.y * gridDim.x + blockIdx.x);   // (see ds_launch_lines)
+  const int tile = at / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
+  const int col = (at % a.col_tiles) * 16 * COLS;
   GroupTiles all(a.offsets, a.groups, a.rows, SHIFT, true);
   if (tile >= all.count()) return;
   const GroupTile gt = all.find(tile);
@@ -424,8 +425,10 @@ bool eight_waves(double workgroups, int depth, int step) { return workgroups <= 
 bool half_columns(double workgroups) { return workgroups <= 128; }
 
 template <typename T, bool TRANSPOSED, bool HALF>
-void launch_few(int shift, bool many, unsigned grid, const MmArgs& a, hipStream_t stream) {
+void launch_few(int shift, bool many, int64_t workgroups, const MmArgs& a, hipStream_t stream) {
   const dim3 block(64 * kWaves), twice(64 * 8);
+  const ds_lines lines = ds_launch_lines(workgroups, 64 * (many ? 8 : kWaves));
+  const dim3 grid(lines.x, lines.y);
   if (shift == 4 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
   else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
   else if (shift == 5 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
@@ -450,12 +453,12 @@ int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   const int cols = half ? 8 * N : 16 * N;   // of a workgroup
   a.col_tiles = (width + cols - 1) / cols;
   const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
-  if (tiles > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, width);
+  if (tiles > 0x7fff0000) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, width);
   const bool many = eight_waves(blocks * a.col_tiles, depth, kWaves * 4 * N);
-  const unsigned grid = (unsigned)tiles;
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false, true>), dim3(grid), dim3(64 * kWaves), 0, stream, a);
-  else if (half) launch_few<T, TRANSPOSED, TRANSPOSED>(shift, many, grid, a, stream);
-  else launch_few<T, TRANSPOSED, false>(shift, many, grid, a, stream);
+  const ds_lines lines = ds_launch_lines(tiles, 64 * kWaves);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false, true>), dim3(lines.x, lines.y), dim3(64 * kWaves), 0, stream, a);
+  else if (half) launch_few<T, TRANSPOSED, TRANSPOSED>(shift, many, tiles, a, stream);
+  else launch_few<T, TRANSPOSED, false>(shift, many, tiles, a, stream);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -465,10 +468,13 @@ int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   constexpr int N = Piece<T>::N;
   a.col_tiles = (p.outer + 16 * N - 1) / (16 * N);
   const bool shared = weights_shared(p);
-  const int width = shared ? 8 * N : 16 * N;   // inner columns of a workgroup
-  const dim3 grid((unsigned)((p.inner + width - 1) / width * a.col_tiles), p.groups), block(64 * kWaves);
   const bool tiny = tiny_matrix<T>(a.xs, p.rows, p.inner) || tiny_matrix<T>(a.dys, p.rows, p.outer);
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, true>), dim3((unsigned)((p.inner + 8 * N - 1) / (8 * N) * a.col_tiles), p.groups), block, 0, ctx->stream, a);
+  const int width = shared || tiny ? 8 * N : 16 * N;   // inner columns of a workgroup
+  const int64_t tiles = (int64_t)((p.inner + width - 1) / width) * a.col_tiles;
+  if (tiles > ds_most_workgroups(64 * kWaves))
+    return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", p.inner, p.outer);
+  const dim3 grid((unsigned)tiles, p.groups), block(64 * kWaves);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, true>), grid, block, 0, ctx->stream, a);
   else if (shared) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, false>), grid, block, 0, ctx->stream, a);
   else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, false, false>), grid, block, 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());

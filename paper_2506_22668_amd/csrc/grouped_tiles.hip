@@ -853,7 +853,7 @@ int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
   a.col_tiles = (a.outer + BN - 1) / BN;
   const int64_t tiles = weight_tiles<T, BR, BN>(a.inner, a.outer), chunks = ds_weight_chunks(a.rows, tiles, 128 / (int)sizeof(T));
   const int64_t wgs = (tiles * chunks + 7) / 8 * 8;
-  if (wgs > 0x7fffffff) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
+  if (wgs > ds_most_workgroups(64 * WR * WN)) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
   const bool direct = sixteen(a.x, a.xs, sizeof(T)) && sixteen(a.dy, a.dys, sizeof(T)) && a.inner % Piece<T>::N == 0 && a.outer % Piece<T>::N == 0;
   const dim3 grid((unsigned)wgs), block(64 * WR * WN);
   if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true>), grid, block, 0, ctx->stream, a, partial, (int)chunks);

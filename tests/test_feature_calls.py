@@ -246,3 +246,29 @@ def test_tiles_of_offsets_that_do_not_ascend_are_counted_without_an_overflow(tmp
     subprocess.run([cxx, "-std=c++17", "-O1", "-fsanitize=signed-integer-overflow", "-fno-sanitize-recover", "-I",
                     os.path.join(ROOT, "paper_2506_22668_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout == "0 1\n"
+
+
+LINES = r"""
+#include <stdio.h>
+#include <initializer_list>
+#include "group_range.h"
+int main() {
+  long bad = 0;
+  const int64_t counts[] = {1, 2, 255, 65536, 16777215, 16777216, 16777217, 33554433, 1000000007, 0x7fff0000};
+  for (int64_t n : counts) for (int threads : {256, 512}) {
+    const ds_lines l = ds_launch_lines(n, threads);
+    const int64_t all = (int64_t)l.x * l.y;
+    bad += all < n || all - n >= l.y || all > 0x7fffffff || (int64_t)l.x * threads > 0xffffffffll || l.y > 65535 || (n * threads < 4294967296ll && l.y != 1);
+  }
+  printf("%ld\n", bad);
+}
+"""
+
+
+def test_a_launch_has_no_more_threads_in_a_line_than_are_counted(tmp_path):
+    cxx = shutil.which("g++")
+    assert cxx, "g++ is needed"
+    src, exe = tmp_path / "lines.cpp", tmp_path / "lines"
+    src.write_text(LINES)
+    subprocess.run([cxx, "-std=c++17", "-I", os.path.join(ROOT, "paper_2506_22668_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout == "0\n"

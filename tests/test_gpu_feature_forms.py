@@ -158,3 +158,20 @@ def test_gradients_of_rows_behind_the_first_two_to_the_31_elements(ctx):   # noq
     close(dx[ends], e.masked_fill(~open_, 0.0), (2 * (outer + 2) * U * size).masked_fill(~open_, 0.0))
     close(dw[0], x[ends].double().t() @ dy[ends].double(), 2 * 8 * U * (x[ends].double().abs().t() @ dy[ends].double().abs()))
     close(db[0], dy[ends].double().sum(0), 2 * 8 * U * dy[ends].double().abs().sum(0))
+
+
+def test_a_launch_of_more_workgroups_than_a_dimension_holds(ctx):   # noqa: F811
+    """2^30 rows of few columns: 2^24 workgroups of 256 threads, one more than 2^32 threads in a line. (Neighbouring rows overlap in all but one element.)"""
+    say("2^30 rows")
+    rows, inner = 2 ** 30, 4
+    g = generator(12)
+    line = torch.randn(rows + inner - 1, generator=g, device="cuda", dtype=BF16)
+    w = normal(g, 1, inner, 1, t=BF16)
+    y = ctx.grouped_mm(line.as_strided((rows, inner), (1, 1)), w, torch.tensor([0, rows], device="cuda"))
+    assert y.shape == (rows, 1)
+    part = 2 ** 26
+    for first in range(0, rows, part):
+        terms = [line[first + j:first + j + part].float() * w[0, j, 0].float() for j in range(inner)]   # (exact: 8 bits by 8)
+        size = sum(v.abs() for v in terms)
+        # four terms in two orders, a rounding of the kernel's result
+        assert ((y[first:first + part, 0].float() - sum(terms)).abs() <= (2 * (inner + 2) + inner) * U * size + 2.0 ** -8 * size).all(), first
