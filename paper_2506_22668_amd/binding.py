@@ -66,6 +66,29 @@ class DistShapError(RuntimeError):
         self.code = code
 
 
+_no_gradient_class = None
+
+
+def _no_gradient():
+    """The autograd function of a call whose gradient is a call of its own: its backward pass is an error."""
+    global _no_gradient_class
+    if _no_gradient_class is None:
+        import torch
+
+        class NoGradient(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, call, outputs, *inputs):
+                ctx.call = call
+                return outputs
+
+            @staticmethod
+            def backward(ctx, *grads):
+                raise DistShapError(DS_EINVAL, f"autograd cannot go through {ctx.call}: its gradient is a call of its own (*_backward; dropout of the gradient)")
+
+        _no_gradient_class = NoGradient
+    return _no_gradient_class
+
+
 def library_path():
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdistshap_hip.so")
 
@@ -455,7 +478,8 @@ class Context:
 
     # -- operators on rows of features ---------------------------------------------
     # Queued on the context's stream, which is ordered behind torch's current stream and in front of what that stream
-    # does next; nothing waits on the host. Under graph capture the context has to be one made for the captured stream.
+    # does next; nothing waits on the host. Under graph capture the context has to be one made for the captured stream. Gradients are calls of their own
+    # (`*_backward`; dropout is its own): autograd does not know them, and an error says so where it is asked to go through one.
     def _queue(self, fn, *args):
         t = self.torch
         if self._current_stream(self._index) == self._raw_stream:
@@ -473,6 +497,12 @@ class Context:
 
     def _refuse(self, message):
         raise DistShapError(DS_EINVAL, message)
+
+    def _outputs(self, call, outputs, a, b=None, c=None):
+        """The outputs; where autograd follows an input, they take part in its graph, so that its backward pass fails and leaves no gradient out."""
+        if (a.requires_grad or b is not None and b.requires_grad or c is not None and c.requires_grad) and self.torch.is_grad_enabled():
+            return _no_gradient().apply(call, outputs, *[i for i in (a, b, c) if i is not None])
+        return outputs
 
     def _rows(self, a, name, shape=None, dtype=None):
         """(tensor, its rows' distance): rows may lie apart, columns have to be neighbours (copied if they are not)."""
@@ -524,6 +554,7 @@ class Context:
             mp, rp = mean.data_ptr(), rstd.data_ptr()
         self._queue(self.lib.ds_layer_norm, self._elements[x.dtype], rows, cols, x.data_ptr(), xs, wp, bp, eps, y.data_ptr(),
                     cols, mp, rp)
+        y = self._outputs("layer_norm", y, x, weight, bias)
         return (y, mean, rstd) if want_stats else y
 
     def layer_norm_backward(self, dy, x, mean, rstd, weight=None):
@@ -542,7 +573,7 @@ class Context:
         ws, wsp, wsn = self._workspace(self.lib.ds_layer_norm_backward_workspace, rows, cols)
         self._queue(self.lib.ds_layer_norm_backward, self._elements[x.dtype], rows, cols, dy.data_ptr(), dys, x.data_ptr(), xs, mp,
                     rp, wp, dx.data_ptr(), cols, dweight.data_ptr(), dbias.data_ptr(), wsp, wsn)
-        return dx, dweight, dbias
+        return self._outputs("layer_norm_backward", (dx, dweight, dbias), dy, x, weight)
 
     def dropout(self, x, p, seed, tag=0, residual=None):
         """residual + dropout(x): the mask is a function of (row, column, seed, tag) and never stored, so the gradient is
@@ -557,7 +588,7 @@ class Context:
         y = x.new_empty((rows, cols))
         self._queue(self.lib.ds_dropout, self._elements[x.dtype], rows, cols, x.data_ptr(), xs, rp, rs, p, int(seed),
                     int(tag) & 0xFFFFFFFF, y.data_ptr(), cols)
-        return y
+        return self._outputs("dropout", y, x, residual)
 
     def group_rows(self, ids, groups):
         """(offsets int64[groups + 1], order int32[rows]): the rows by group, ascending within each, those whose id
@@ -596,7 +627,7 @@ class Context:
         y = x.new_empty((rows, outer))
         self._queue(self.lib.ds_grouped_mm, self._elements[x.dtype], rows, inner, outer, groups, x.data_ptr(), xs, wp, op, rp, bp,
                     int(bool(relu)), y.data_ptr(), outer)
-        return y
+        return self._outputs("grouped_mm", y, x, w, bias)
 
     def grouped_mm_backward(self, dy, x, w, offsets, order=None, gate=None):
         """(dx, dw, dbias fp32) of grouped_mm without its ReLU; dx is 0 where `gate` (rows like x) is not above 0."""
@@ -615,4 +646,4 @@ class Context:
         ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_workspace, element, rows, inner, outer, groups)
         self._queue(self.lib.ds_grouped_mm_backward, element, rows, inner, outer, groups, dy.data_ptr(), dys, x.data_ptr(), xs, wp, op,
                     rp, gp, gs, dx.data_ptr(), inner, dw.data_ptr(), db.data_ptr(), wsp, wsn)
-        return dx, dw, db
+        return self._outputs("grouped_mm_backward", (dx, dw, db), dy, x, w)

@@ -272,3 +272,38 @@ def test_a_launch_has_no_more_threads_in_a_line_than_are_counted(tmp_path):
     src.write_text(LINES)
     subprocess.run([cxx, "-std=c++17", "-I", os.path.join(ROOT, "paper_2506_22668_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout == "0\n"
+
+
+def _idle():
+    """A context whose calls do nothing: what the binding makes of arguments and outputs is left."""
+    c = _context()
+    c.lib, c._queue, c._workspace = types.SimpleNamespace(**{name: None for name in binding.EXPORTED_SYMBOLS}), lambda *a: None, lambda *a: (None, None, 0)
+    return c
+
+
+OFFSETS = torch.tensor([0, 2, 4])
+
+
+@pytest.mark.parametrize("call", [
+    lambda c, x, w: c.layer_norm(x, w[0, 0]),
+    lambda c, x, w: c.layer_norm(x, want_stats=True)[0],
+    lambda c, x, w: c.layer_norm(x.detach(), None, w[0, 0]),
+    lambda c, x, w: c.layer_norm_backward(x, x.detach(), torch.zeros(4), torch.zeros(4))[0],
+    lambda c, x, w: c.layer_norm_backward(x.detach(), x.detach(), torch.zeros(4), torch.zeros(4), w[0, 0])[2],
+    lambda c, x, w: c.dropout(x, 0.5, 1),
+    lambda c, x, w: c.dropout(x.detach(), 0.5, 1, residual=x),
+    lambda c, x, w: c.grouped_mm(x, w.detach(), OFFSETS),
+    lambda c, x, w: c.grouped_mm(x.detach(), w, OFFSETS),
+    lambda c, x, w: c.grouped_mm(x.detach(), w.detach(), OFFSETS, bias=w[:, 0]),
+    lambda c, x, w: c.grouped_mm_backward(x, x.detach(), w.detach(), OFFSETS)[1],
+    lambda c, x, w: c.grouped_mm_backward(x.detach(), x, w, OFFSETS)[2],
+])
+def test_a_gradient_is_not_lost_silently(call):
+    """The calls have gradients of their own and none for autograd: a backward pass through them says so, and does not leave them out."""
+    x, w = torch.zeros(4, 4, requires_grad=True), torch.zeros(2, 4, 4, requires_grad=True)
+    out = call(_idle(), x, w)
+    with pytest.raises(DistShapError, match="backward"):
+        (out.nan_to_num().sum() + x.sum() + w.sum()).backward()
+    with torch.no_grad():
+        assert not call(_idle(), x, w).requires_grad
+    assert not call(_idle(), x.detach(), w.detach()).requires_grad
