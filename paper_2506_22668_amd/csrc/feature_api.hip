@@ -36,10 +36,9 @@ int check_workspace(ds_ctx* ctx, const void* workspace, int64_t bytes, int64_t n
   return DS_OK;
 }
 
-int check_groups(ds_ctx* ctx, int64_t rows, int64_t groups, const int64_t* offsets) {
+int check_groups(ds_ctx* ctx, int64_t groups, const int64_t* offsets) {
   if (groups < 1 || groups > kMostGroups) return ds_fail(ctx, DS_EINVAL, "%lld groups out of range [1, %d]", (long long)groups, kMostGroups);
   if (!offsets) return ds_fail(ctx, DS_EINVAL, "offsets is null");
-  (void)rows;
   return DS_OK;
 }
 
@@ -109,7 +108,7 @@ int ds_group_rows(ds_ctx* ctx, const int32_t* ids, int64_t rows, int64_t groups,
                   int64_t workspace_bytes) {
   if (!ctx) return DS_EINVAL;
   if (rows < 0 || rows > kMostOrdered) return ds_fail(ctx, DS_EINVAL, "%lld rows out of range [0, %lld]", (long long)rows, (long long)kMostOrdered);
-  DS_TRY(check_groups(ctx, rows, groups, offsets));
+  DS_TRY(check_groups(ctx, groups, offsets));
   if (rows > 0 && (!ids || !order)) return ds_fail(ctx, DS_EINVAL, "%s is null", ids ? "order" : "ids");
   DS_TRY(check_workspace(ctx, workspace, workspace_bytes, group_bytes(rows, groups)));
   DS_HIP(ctx, hipSetDevice(ctx->device));
@@ -122,7 +121,7 @@ int ds_grouped_mm(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64
   if (!ctx) return DS_EINVAL;
   DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, inner, kMostCols));
   DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, outer, kMostCols));
-  DS_TRY(check_groups(ctx, rows, groups, offsets));
+  DS_TRY(check_groups(ctx, groups, offsets));
   DS_TRY(check_rows(ctx, "x", x, x_stride, rows, inner, dtype, false));
   DS_TRY(check_rows(ctx, "w", w, outer, groups, outer, dtype, false));
   DS_TRY(check_rows(ctx, "y", y, y_stride, rows, outer, dtype, true));
@@ -146,7 +145,7 @@ int ds_grouped_mm_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inn
   if (!ctx) return DS_EINVAL;
   DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, inner, kMostCols));
   DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, outer, kMostCols));
-  DS_TRY(check_groups(ctx, rows, groups, offsets));
+  DS_TRY(check_groups(ctx, groups, offsets));
   DS_TRY(check_rows(ctx, "dy", dy, dy_stride, rows, outer, dtype, false));
   DS_TRY(check_rows(ctx, "x", x, x_stride, rows, inner, dtype, false));
   DS_TRY(check_rows(ctx, "w", w, outer, groups, outer, dtype, false));

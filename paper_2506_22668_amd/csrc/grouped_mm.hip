@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
   const int at = (int)(blockIdx.y * gridDim.x + blockIdx.x);   // (see ds_launch_lines)
   const int tile = at / a.col_tiles, width = TRANSPOSED ? a.inner : a.outer, depth = TRANSPOSED ? a.outer : a.inner;
   const int col = (at % a.col_tiles) * 16 * COLS;
-  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT, true);
+  GroupTiles all(a.offsets, a.groups, a.rows, SHIFT);
   if (tile >= all.count()) return;
   const GroupTile gt = all.find(tile);
   int row[RB];

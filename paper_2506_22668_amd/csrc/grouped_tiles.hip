@@ -40,16 +40,17 @@ __device__ __forceinline__ void products(const PieceV<T> (&fw)[NN], const PieceV
 // column of the tile that row m of a matrix-core operand stands for: a lane's 16 results are then 16 neighbours
 __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
-// A stage of an operand in LDS: DEPTH elements of the contraction (64 or 128 bytes of them). ACROSS false: [COLS][DEPTH], the 16-byte pieces of
+// A stage of an operand in LDS: DEPTH elements of the contraction (64 bytes of them). ACROSS false: [COLS][DEPTH], the 16-byte pieces of
 // a column exchanged by bits of its number; true: [DEPTH][COLS], pieces exchanged by the step's last two bits (16-bit types). Either way
 // the lanes that read together meet all banks.
-template <typename T, int COLS, bool ACROSS, int DEPTH_BYTES>
+constexpr int kDepthBytes = 64;
+template <typename T, int COLS, bool ACROSS>
 struct Operand {
-  static constexpr int N = Piece<T>::N, DEPTH = DEPTH_BYTES / sizeof(T), BYTES = COLS * DEPTH_BYTES;
-  static constexpr int PER_ROW = ACROSS ? COLS / N : DEPTH_BYTES / 16;
+  static constexpr int N = Piece<T>::N, BYTES = COLS * kDepthBytes;
+  static constexpr int PER_ROW = ACROSS ? COLS / N : kDepthBytes / 16;
   static __device__ __forceinline__ int exchange(int line, int piece) {
     if constexpr (ACROSS) return sizeof(T) == 2 ? piece ^ ((line & 3) << 2) : piece;
-    else return DEPTH_BYTES == 64 ? piece ^ ((line >> 1) & 3) : piece ^ (line & 7);
+    else return piece ^ ((line >> 1) & 3);
   }
   // the place of piece number `at` of the stage: its column (or step) and which piece of that
   static __device__ __forceinline__ int line(int at) { return at / PER_ROW; }
@@ -57,9 +58,9 @@ struct Operand {
 };
 
 // A lane's operand pieces for 32 columns and 2 N steps of the contraction
-template <typename T, int COLS, bool ACROSS, bool ORDERED, int DEPTH_BYTES>
+template <typename T, int COLS, bool ACROSS, bool ORDERED>
 struct Reader {
-  using Op = Operand<T, COLS, ACROSS, DEPTH_BYTES>;
+  using Op = Operand<T, COLS, ACROSS>;
   int m, h, lane;
   __device__ __forceinline__ Reader(int lane_) : lane(lane_) {
     const int r = lane & 31;
@@ -70,7 +71,7 @@ struct Reader {
   __device__ __forceinline__ PieceV<T> read(const char* stage, int first, int slice) const {
     constexpr int N = Op::N;
     if constexpr (!ACROSS) {
-      return *reinterpret_cast<const PieceV<T>*>(stage + (first + m) * DEPTH_BYTES + (Op::exchange(m, 2 * slice + h) << 4));
+      return *reinterpret_cast<const PieceV<T>*>(stage + (first + m) * kDepthBytes + (Op::exchange(m, 2 * slice + h) << 4));
     } else if constexpr (sizeof(T) == 2) {
       const int i = lane & 15, four = ((lane >> 4) & 1) * 4 + (i & 3);
       const int col = first + (ORDERED ? 16 * (four & 1) + 4 * (four >> 1) : 4 * four);
@@ -216,11 +217,11 @@ __device__ __forceinline__ int hidden(int v) {
 // 460 TFLOP/s, 2.2 TB/s; fp32 30,011 rows by 512 x 256 76 us, 104 TFLOP/s (a large library product: 153).
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 64 / sizeof(T);
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
   constexpr int TR = BR / WR, TN = BN / WN, NR = TR / 32, NN = TN / 32, SLICES = DEPTH / (2 * N);
-  constexpr int SHIFT = BR == 256 ? 8 : BR == 128 ? 7 : 6;
-  using XOp = Operand<T, BR, false, 64>;
-  using WOp = Operand<T, BN, !TRANSPOSED, 64>;
+  constexpr int SHIFT = BR == 256 ? 8 : 7;
+  using XOp = Operand<T, BR, false>;
+  using WOp = Operand<T, BN, !TRANSPOSED>;
   constexpr int STAGE = XOp::BYTES + WOp::BYTES, LOADS = STAGE / 16 / THREADS;
   constexpr int OUT_ROW = TN * (int)sizeof(T), CHUNKS = OUT_ROW / 16, AT_ONCE = 64 / CHUNKS, OUT_ROWS = 16, OUTS = OUT_ROWS / AT_ONCE;
   // (arrays, not parts of one: only then does the compiler know that what is read of one does not wait for what comes into the other)
@@ -249,8 +250,8 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
   Loader<T, XOp::BYTES, THREADS, DIRECT> lx;
   Loader<T, WOp::BYTES, THREADS, DIRECT> lw;
   const T *x_end = x + (int64_t)(a.rows - 1) * xs + depth, *w_end = (const T*)a.w + (int64_t)a.groups * a.inner * a.outer;
-  const Reader<T, BR, false, false, 64> rx(lane);
-  const Reader<T, BN, !TRANSPOSED, true, 64> rw(lane);
+  const Reader<T, BR, false, false> rx(lane);
+  const Reader<T, BN, !TRANSPOSED, true> rw(lane);
   const int steps = (depth + 2 * DEPTH - 1) / (2 * DEPTH) * 2;   // stages of a tile, an even number (zeros behind the end)
   // A thread's pieces of a step lie in one place of lines that are a fixed number apart (the exchange of pieces goes by the last bits
   // of a line, which that number leaves alone)
@@ -558,10 +559,10 @@ __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit,
 
 template <typename T, int BR, int BN, int WR, int WN, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial, int most_chunks) {
-  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = 64 / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
+  constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
   constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
-  using XOp = Operand<T, BR, true, 64>;
-  using DOp = Operand<T, BN, true, 64>;
+  using XOp = Operand<T, BR, true>;
+  using DOp = Operand<T, BN, true>;
   constexpr int STAGE = XOp::BYTES + DOp::BYTES, LOADS = STAGE / 16 / THREADS;
   constexpr int LINES = THREADS / DOp::PER_ROW, EACH = DEPTH / LINES;   // of a thread's pieces of a stage: lines apart, and how many
   __shared__ __attribute__((aligned(128))) char stage0[STAGE], stage1[STAGE], stage2[STAGE], stage3[STAGE];
@@ -582,8 +583,8 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   const int in0 = tile / a.col_tiles * BR, col0 = tile % a.col_tiles * BN;
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
   const T *x_end = x + (int64_t)(a.rows - 1) * a.xs + a.inner, *dy_end = dy + (int64_t)(a.rows - 1) * a.dys + a.outer;
-  const Reader<T, BR, true, false, 64> rx(lane);
-  const Reader<T, BN, true, true, 64> rd(lane);
+  const Reader<T, BR, true, false> rx(lane);
+  const Reader<T, BN, true, true> rd(lane);
   static_assert(BR == BN && LINES % 4 == 0, "both operands' pieces of a thread lie in the same rows");
   const int line = DOp::line((int)threadIdx.x), place = DOp::piece((int)threadIdx.x) * N;
   while (unit < last && group < a.groups) {

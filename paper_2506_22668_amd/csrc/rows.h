@@ -129,23 +129,23 @@ struct GroupTile {
   int begin, end;       // positions in the order
 };
 
-// The rows cut into tiles of 2^shift, group by group; `with_none`: the rows of no group last. Used by whole waves, with the same answer in
+// The rows cut into tiles of 2^shift, group by group, the rows of no group last. Used by whole waves, with the same answer in
 // every lane: a lane holds one of 64 neighbouring groups, so that up to 64 groups are looked at once and a tile is found by a ballot.
 class GroupTiles {
  public:
-  __device__ __forceinline__ GroupTiles(const int64_t* offsets, int groups, int rows, int shift, bool with_none)
-      : offsets_(offsets), groups_(groups), rows_(rows), shift_(shift), held_(with_none ? groups + 1 : groups) {
+  __device__ __forceinline__ GroupTiles(const int64_t* offsets, int groups, int rows, int shift)
+      : offsets_(offsets), groups_(groups), rows_(rows), shift_(shift) {
     look(0, 0);
   }
   // number of tiles
   __device__ __forceinline__ int count() {
-    while (base_ + 64 < held_) look(base_ + 64, last_);
+    while (base_ + 64 <= groups_) look(base_ + 64, last_);
     return last_;
   }
   // tile 0 .. count() - 1
   __device__ __forceinline__ GroupTile find(int tile) {
     if (tile < before_) look(0, 0);
-    while (tile >= last_ && base_ + 64 < held_) look(base_ + 64, last_);
+    while (tile >= last_ && base_ + 64 <= groups_) look(base_ + 64, last_);
     const unsigned long long reach = __ballot(upto_ > tile);
     const int src = reach ? __ffsll((long long)reach) - 1 : 63;
     const int g = __builtin_amdgcn_readfirstlane(src);
@@ -160,7 +160,7 @@ class GroupTiles {
 
  private:
   const int64_t* offsets_;
-  int groups_, rows_, shift_, held_;
+  int groups_, rows_, shift_;
   int base_, before_, last_;           // the first of the 64 groups; tiles in front of them and up to their end
   int begin_, end_, tiles_, upto_;     // of the lane's group
   __device__ __forceinline__ void look(int base, int before) {
@@ -168,10 +168,10 @@ class GroupTiles {
     base_ = base;
     before_ = before;
     begin_ = end_ = 0;
-    if (g < held_) ds_group_range(offsets_, groups_, rows_, g, &begin_, &end_);
+    if (g <= groups_) ds_group_range(offsets_, groups_, rows_, g, &begin_, &end_);
     tiles_ = ds_parts_of(begin_, end_, 1 << shift_);
     upto_ = tiles_;
-    const int most = ds_most_parts(rows_, 1 << shift_, held_);
+    const int most = ds_most_parts(rows_, 1 << shift_, groups_ + 1);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(upto_, o, 64);
