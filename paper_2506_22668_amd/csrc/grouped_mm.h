@@ -2,6 +2,7 @@
 #pragma once
 #include "feature_ops.h"
 #include "group_range.h"
+#include "grouped_forms.h"
 
 struct MmArgs {
   int rows, inner, outer, groups;
@@ -26,8 +27,3 @@ int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a);
 // The gradient of the weights in tiles; partial: ds_weight_tiles_bytes of scratch
 int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer);
 int ds_launch_weight_tiles(ds_ctx* ctx, int dtype, MmArgs& a, void* partial);
-// what the choice between the forms has to know of the tiles
-bool ds_wide_tiles(int rows, int width);                           // fp32: 256 rows to a tile
-constexpr double kNarrowTiles = 512;                               // 16 bits: up to so many tiles are of 128 by 128 ..
-double ds_narrow_tiles(int rows, int groups, int width);           // .. if this many are needed
-int ds_weight_chunks(int rows, int64_t tiles, int unit);           // stretches that the rows are cut into, in units of `unit` rows

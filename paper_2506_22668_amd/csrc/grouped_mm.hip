@@ -6,8 +6,6 @@
 // The rows of group g are those at positions offsets[g] .. offsets[g + 1] of `order`. Sizes of groups are known on the GPU
 // alone: the grid has a tile for every one that there can be, and a workgroup finds its rows from the offsets.
 // All products go through the matrix cores, fp32 ones on their fp32 form, and are summed in fp32.
-#include <math.h>
-
 #include <type_traits>
 
 #include "grouped_mm.h"
@@ -356,52 +354,7 @@ MmArgs arguments(const ds_grouped& p) {
   return a;
 }
 
-// ---- which form -----------------------------------------------------------------------------------------------------------------
-// Each form has a price in us on 256 compute units, from the number of its workgroups, how many run at a time, and what one takes for its share of the
-// contraction; the sizes of groups are not known on the host, so all are taken to be of the mean size. The figures were fitted to the forms' times at
-// 165 shapes of each type (1, 8 and 64 groups of 24 to 16,000 rows; widths of 64 to 4,000, odd ones among them), those of the small 16-bit tiles
-// to 315 more (1 to 64 groups, up to 900 tiles): the choice is 1.1 % off the fastest form there on average, and more than 12 % at 3. In us, few / tiles:
-//   8 groups of 400 rows by 1,024 x 1,024, bf16: 30 / 26, of 1,000 rows: 58 / 34; 64 groups of 200 rows by 256 x 256: 24 / 13, by 64 x 64: 12 / 13
-constexpr double kUnits = 256;
-
-double ceil_div(double a, double b) { return ceil(a / b); }
-
-// the product by rows, `depth` long and `width` wide
-bool rows_in_tiles(const ds_grouped& p, int dtype, int depth, int width) {
-  if (p.inner < 8 || p.outer < 8) return false;   // (the tiles' loads need rows of 16 bytes at the least)
-  const bool f32 = dtype == DS_ELEM_F32;
-  const double mean = ceil_div(p.rows, p.groups);
-  const double block = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
-  const double few = p.groups * ceil_div(mean, block) * ceil_div(width, f32 ? 64 : 128) / kUnits;
-  const double few_us = (few > 1 ? few : 1) * (5 + (f32 ? 0.02 : 0.009) * depth);
-  const double narrow = ds_narrow_tiles(p.rows, p.groups, width);
-  if (!f32 && narrow <= kNarrowTiles) return 1 + (narrow > kUnits ? 0.026 : 0.017) * depth < few_us;
-  if (!f32) return ceil_div(p.groups * ceil_div(mean, 256) * ceil_div(width, 256), kUnits) * (4 + 0.025 * depth) < few_us;
-  const bool wide = ds_wide_tiles(p.rows, width);
-  const double rounds = ceil_div(p.groups * ceil_div(mean, wide ? 256 : 128) * ceil_div(width, 128), kUnits);
-  return rounds * (wide ? 13 + 0.14 * depth : 8 + 0.075 * depth) + 6 < few_us;
-}
-
-// Up to 32 rows to a group a wave of the few-rows form has columns of its own, a quarter as many, beyond that the waves of a workgroup share the
-// rows (both gradients, 8 groups by 1,024 x 1,024, alone / shared: 8 rows each bf16 25 / 40 us, fp32 32 / 44; 32 rows: 28 / 42, 41 / 47; 64 rows:
-// 36 / 46, 66 / 58; 128 rows: 44 / 48, 92 / 76)
-bool weights_shared(const ds_grouped& p) { return (int64_t)p.rows > 32 * (int64_t)p.groups; }
-
-bool weights_in_tiles(const ds_grouped& p, int dtype) {
-  if (p.inner < 8 || p.outer < 8) return false;
-  const bool f32 = dtype == DS_ELEM_F32;
-  const double mean = ceil_div(p.rows, p.groups), n = f32 ? 4 : 8;
-  const double few = p.groups * ceil_div(p.outer, 16 * n) * ceil_div(p.inner, 8 * n) / kUnits;
-  const double alone = p.groups * ceil_div(p.outer, 16 * n) * ceil_div(p.inner, 4 * n) / (kUnits * (f32 ? 16 : 8));   // (waves at a time)
-  const double few_us = weights_shared(p) ? (few > 1 ? few : 1) * ((f32 ? 3 : 5) + 2 * ceil_div(mean, 16 * n))
-                                          : (alone > 1 ? alone : 1) * (6 + 2 * ceil_div(mean, 4 * n));
-  const double side = f32 ? 128 : 256, unit = f32 ? 32 : 64;
-  const double tiles = ceil_div(p.inner, side) * ceil_div(p.outer, side), chunks = ds_weight_chunks(p.rows, (int64_t)tiles, (int)unit);
-  const double steps = ceil_div(p.groups * ceil_div(mean, unit), chunks), cut = 1 + (p.groups > chunks ? p.groups / chunks : 0) + (chunks > 1 ? 1 : 0);
-  const double rounds = chunks * tiles / kUnits;
-  const bool odd = p.inner % 4 || p.outer % 4;   // (fp32 rows that are not aligned: 750 us in few, 880 in tiles, of 64,000 by 513 x 300)
-  return (rounds > 1 ? rounds : 1) * (steps * (f32 ? odd ? 5.0 : 1.5 : 2.0) + cut * (f32 ? 8 : 5)) + (f32 ? 12 : 4) < few_us;
-}
+ds_mm_sizes sizes(const ds_grouped& p) { return {p.rows, p.inner, p.outer, p.groups}; }
 
 // whether a matrix has less than 16 bytes from its first element to its last
 template <typename T>
@@ -414,51 +367,35 @@ int element_of() {
   return sizeof(T) == 4 ? DS_ELEM_F32 : std::is_same<T, __bf16>::value ? DS_ELEM_BF16 : DS_ELEM_F16;
 }
 
-// Twice the waves to a workgroup that takes up to 32 rows, where workgroups are few and the contraction is long (8 rows to a group, bf16 / fp32; 8 groups by
-// 4,096 x 1,024, 64 / 128 workgroups: 26.6 -> 19.7 us / 42 -> 33; 1 group by 1,024 x 1,024: 9.9 -> 11.8 / 12.1 -> 10.9; 8 groups by 1,024 x 4,096, 256 / 512
-// workgroups: 15.2 -> 15.0 / 23.6 -> 25.5; 64 rows to a group: no faster anywhere)
-bool eight_waves(double workgroups, int depth, int step) { return workgroups <= 128 && depth >= 16 * step; }
-
-// The product with W^T of half the columns to a workgroup, where those of all would be at most 128 workgroups; with more, reading the rows twice as often
-// counts (both gradients in us, all / half columns; 8 groups by 1,024 x 4,096, 64 workgroups, bf16: 8 rows 73 / 59, 64 rows 80 / 65; 128 rows, 128 workgroups
-// 85 / 71; 256 rows, 256 workgroups 95 / 112; fp32, 4 groups by 1,024 x 4,096: 8 rows, 64 workgroups 68 / 55, 256 rows, 256 workgroups 211 / 227)
-bool half_columns(double workgroups) { return workgroups <= 128; }
-
 template <typename T, bool TRANSPOSED, bool HALF>
-void launch_few(int shift, bool many, int64_t workgroups, const MmArgs& a, hipStream_t stream) {
+void launch_few(const ds_few_form& form, int64_t workgroups, const MmArgs& a, hipStream_t stream) {
   const dim3 block(64 * kWaves), twice(64 * 8);
-  const ds_lines lines = ds_launch_lines(workgroups, 64 * (many ? 8 : kWaves));
+  const ds_lines lines = ds_launch_lines(workgroups, 64 * (form.eight_waves ? 8 : kWaves));
   const dim3 grid(lines.x, lines.y);
-  if (shift == 4 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
-  else if (shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
-  else if (shift == 5 && many) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
-  else if (shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
+  if (form.shift == 4 && form.eight_waves) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
+  else if (form.shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
+  else if (form.shift == 5 && form.eight_waves) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
+  else if (form.shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
   else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
 }
 
 template <typename T, bool TRANSPOSED>
 int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   if (p.rows == 0) return DS_OK;
-  constexpr int N = Piece<T>::N;
   hipStream_t stream = ctx->stream;
   // (rows of at least 16 bytes each would not be enough to ask for: an operand may have one row)
   const bool tiny = tiny_matrix<T>(TRANSPOSED ? a.dys : a.xs, p.rows, TRANSPOSED ? p.outer : p.inner) ||
                     tiny_matrix<T>((int64_t)p.inner * p.outer, p.groups, (int64_t)p.inner * p.outer) || (a.gate && tiny_matrix<T>(a.gs, p.rows, p.inner));
   const int depth = TRANSPOSED ? p.outer : p.inner, width = TRANSPOSED ? p.inner : p.outer;
-  const int64_t mean = (p.rows + p.groups - 1) / p.groups;
-  if (rows_in_tiles(p, element_of<T>(), depth, width)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
-  const int shift = tiny || mean > 32 ? 6 : mean > 16 ? 5 : 4;
-  const double blocks = p.groups * ceil_div((double)mean, 1 << shift);   // (about: the sizes of groups are not known here)
-  const bool half = TRANSPOSED && !tiny && half_columns(blocks * ceil_div(width, 16 * N));
-  const int cols = half ? 8 * N : 16 * N;   // of a workgroup
-  a.col_tiles = (width + cols - 1) / cols;
-  const int64_t tiles = ds_most_tiles(a, shift) * a.col_tiles;
+  if (ds_rows_in_tiles(sizes(p), element_of<T>(), depth, width)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
+  const ds_few_form form = ds_choose_few(sizes(p), element_of<T>(), TRANSPOSED, tiny);
+  a.col_tiles = (width + form.cols - 1) / form.cols;
+  const int64_t tiles = ds_most_tiles(a, form.shift) * a.col_tiles;
   if (tiles > 0x7fff0000) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, width);
-  const bool many = eight_waves(blocks * a.col_tiles, depth, kWaves * 4 * N);
   const ds_lines lines = ds_launch_lines(tiles, 64 * kWaves);
   if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false, true>), dim3(lines.x, lines.y), dim3(64 * kWaves), 0, stream, a);
-  else if (half) launch_few<T, TRANSPOSED, TRANSPOSED>(shift, many, tiles, a, stream);
-  else launch_few<T, TRANSPOSED, false>(shift, many, tiles, a, stream);
+  else if (form.half) launch_few<T, TRANSPOSED, TRANSPOSED>(form, tiles, a, stream);
+  else launch_few<T, TRANSPOSED, false>(form, tiles, a, stream);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -467,7 +404,7 @@ template <typename T>
 int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   constexpr int N = Piece<T>::N;
   a.col_tiles = (p.outer + 16 * N - 1) / (16 * N);
-  const bool shared = weights_shared(p);
+  const bool shared = ds_weights_shared(sizes(p));
   const bool tiny = tiny_matrix<T>(a.xs, p.rows, p.inner) || tiny_matrix<T>(a.dys, p.rows, p.outer);
   const int width = shared || tiny ? 8 * N : 16 * N;   // inner columns of a workgroup
   const int64_t tiles = (int64_t)((p.inner + width - 1) / width) * a.col_tiles;
@@ -484,7 +421,7 @@ int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
 template <typename T>
 int backward(ds_ctx* ctx, const ds_grouped& p, MmArgs& a, void* workspace) {
   DS_TRY((launch_rows<T, true>(ctx, p, a)));
-  if (weights_in_tiles(p, element_of<T>())) return ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
+  if (ds_weights_in_tiles(sizes(p), element_of<T>())) return ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
   return launch_weights<T>(ctx, p, a);
 }
 
@@ -505,7 +442,7 @@ int ds_launch_grouped_mm(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows x,
 }
 
 int64_t ds_grouped_mm_backward_bytes(int dtype, const ds_grouped& p) {
-  return weights_in_tiles(p, dtype) ? ds_weight_tiles_bytes(dtype, p.rows, p.inner, p.outer) : 0;
+  return ds_weights_in_tiles(sizes(p), dtype) ? ds_weight_tiles_bytes(dtype, p.rows, p.inner, p.outer) : 0;
 }
 
 int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, ds_rows x, ds_rows gate, ds_rows dx,

@@ -881,28 +881,6 @@ int launch(ds_ctx* ctx, MmArgs& a) {
 
 }  // namespace
 
-// Chunks of the line of steps: as many as fill the compute units with every tile once, or twice where that leaves fewer of them idle in the last
-// round, but none of less than two steps (128 rows of 16 bits).
-int ds_weight_chunks(int rows, int64_t tiles, int unit) {
-  constexpr int64_t kUnits = 256;
-  const auto idle = [&](int64_t p) { return (double)((p * tiles + kUnits - 1) / kUnits * kUnits) / (double)(p * tiles); };
-  const int64_t once = kUnits / tiles > 1 ? kUnits / tiles : 1, twice = 2 * kUnits / tiles > 1 ? 2 * kUnits / tiles : 1;
-  const int64_t p = idle(twice) < 0.93 * idle(once) ? twice : once, most = rows / (2 * unit);
-  return (int)(p < most ? p : most > 1 ? most : 1);
-}
-
-// 256 rows to a tile where there are about as many tiles as compute units (65,536 rows by 512 x 512: 0.36 -> 0.34 ms; with half as many tiles, 4,096
-// rows by 2,048 x 512: 0.16 -> 0.27 ms)
-bool ds_wide_tiles(int rows, int width) { return (int64_t)(rows / 256) * ((width + 127) / 128) >= 224; }
-
-// 16 bits: tiles of 128 by 128, of which a compute unit has two at a time, where there are no more than that: 256 by 256 would leave units idle
-// (8,192 rows in 8 groups by 512 x 512: 24 us in large, 17 in small; by 1,024 x 1,024: 39, 34). With more, the large ones' fewer loads from L2
-// count (131,072 rows by 512 x 512: 108, 144; by 1,024 x 1,024: 416, 520).
-double ds_narrow_tiles(int rows, int groups, int width) {
-  const double mean = ceil((double)rows / groups);
-  return groups * ceil(mean / 128) * ceil(width / 128.0);
-}
-
 template <typename T, bool TRANSPOSED>
 int launch_rows(ds_ctx* ctx, MmArgs& a) {
   if (ds_narrow_tiles(a.rows, a.groups, TRANSPOSED ? a.inner : a.outer) <= kNarrowTiles) return launch<T, 128, 128, 2, 2, TRANSPOSED>(ctx, a);

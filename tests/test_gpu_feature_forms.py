@@ -4,6 +4,7 @@ elements backwards. Tolerances are those of test_gpu_features.py."""
 import numpy as np
 import pytest
 
+from tests import test_gpu_features as features
 from tests.gpu_common import say
 from tests.test_gpu_features import (BF16, EPS, F16, F32, TYPES, U, close, ctx, generator, grouping, mm_exact, norm_backward_exact,   # noqa: F401
                                      normal, strided)
@@ -43,6 +44,16 @@ def test_gradients_of_aligned_rows(ctx, t, rows, inner, outer, groups, apart):  
         assert x.data_ptr() % 16 == 0 and dy.data_ptr() % 16 == 0
         w = normal(g, groups, inner, outer, t=t, scale=inner ** -0.5)
         check_backward(ctx, dy, x, w, offsets, perm, key, x if order else None)
+
+
+# the tiles that test_gpu_features.py does not come to: fp32 of 128 rows, rows of whole pieces and odd ones, and dx of 256; 17 to 32 rows to a group
+# whose dx has many workgroups (tests/test_grouped_forms.py says which form a shape takes)
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", [(6000, 131, 515, 2), (6000, 515, 130, 2), (3000, 1024, 64, 2), (4000, 2048, 128, 1), (40_003, 388, 133, 3),
+                                                        (600, 1032, 1032, 20)])
+def test_products_of_further_forms(ctx, t, rows, inner, outer, groups):   # noqa: F811
+    features.test_grouped_mm(ctx, t, rows, inner, outer, groups)
+    features.test_grouped_mm_backward(ctx, t, rows, inner, outer, groups)
 
 
 def many_groups(ctx, seed, rows, groups, order):   # noqa: F811
