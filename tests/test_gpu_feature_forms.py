@@ -186,3 +186,54 @@ def test_a_launch_of_more_workgroups_than_a_dimension_holds(ctx):   # noqa: F811
         size = sum(v.abs() for v in terms)
         # four terms in two orders, a rounding of the kernel's result
         assert ((y[first:first + part, 0].float() - sum(terms)).abs() <= (2 * (inner + 2) + inner) * U * size + 2.0 ** -8 * size).all(), first
+
+
+def test_the_most_rows_by_group(ctx):   # noqa: F811
+    """2^30 rows in 1,000 groups, the limits of the call but for 24 groups."""
+    say("2^30 rows by group")
+    rows, groups = 2 ** 30, 1000
+    ids = torch.randint(-1, groups, (rows,), generator=generator(13), device="cuda", dtype=torch.int32)
+    offsets, order = ctx.group_rows(ids, groups)
+    of = torch.bincount(ids + 1, minlength=groups + 1)
+    assert offsets.tolist() == [0] + torch.cumsum(of[1:], 0).tolist()
+    part = 2 ** 26
+    for first in range(0, rows, part):
+        at = order[max(first - 1, 0):first + part].long()
+        key = ids[at]
+        key = torch.where(key < 0, groups, key)
+        step = key[1:] - key[:-1]
+        # by group, and ascending within a group: with the sizes of the groups, every row once
+        assert (step >= 0).all() and (at[1:] > at[:-1])[step == 0].all() and at.min() >= 0 and at.max() < rows, first
+
+
+def test_many_groups_captured_into_a_graph():
+    """Groups whose counts need more LDS than a kernel has by itself, and the gradient of the weights in two launches."""
+    say("graph of many groups")
+    from paper_2506_22668_amd import Context
+    stream = torch.cuda.Stream()
+    mine, plain = Context("cuda:0", stream=stream), Context("cuda:0")
+    rows, inner, outer, groups = 60_000, 128, 136, 1000
+
+    def inputs(seed):
+        g = generator(seed)
+        return [torch.randint(-1, groups, (rows,), generator=g, device="cuda").int(), normal(g, rows, inner, t=BF16), normal(g, rows, outer, t=BF16),
+                normal(g, groups, inner, outer, t=BF16, scale=0.1)]
+
+    def run(c, ids, x, dy, w):
+        offsets, order = c.group_rows(ids, groups)
+        return [offsets, order, c.grouped_mm(x, w, offsets, order=order), *c.grouped_mm_backward(dy, x, w, offsets, order=order, gate=x)]
+
+    held = inputs(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = run(mine, *held)
+    for seed in (2, 3, 4):
+        for to, new in zip(held, inputs(seed)):
+            to.copy_(new)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, run(plain, *held))), seed
+    mine.close()
+    plain.close()
