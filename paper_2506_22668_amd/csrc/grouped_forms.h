@@ -1,7 +1,8 @@
 // Which form of the products by group a call takes. Host functions of its sizes alone (tests/test_grouped_forms.py compiles them by themselves).
 //
 // Each form has a price in us on 256 compute units, from the number of its workgroups, how many run at a time, and what one takes for its share of the
-// contraction; the sizes of groups are not known on the host, so all are taken to be of the mean size.
+// contraction; the sizes of groups are not known on the host, so all are taken to be of the mean size. What that costs where they are not, both gradients
+// in bf16 by 256 x 256, rows spread evenly / all in one group: 65,536 rows, 1,024 groups 151 / 575 us; 4,096 rows, 256 groups 37 / 357 us.
 //
 // Measured, each form forced, at 323 shapes (1, 8 and 64 equal groups of 8 to 16,000 rows, eight pairs of widths of 64 to 4,096, 513 x 300 among them, bf16 and
 // fp32; profiles/operators_forms.md): forward the choice is 0.8 % off the faster form on average and more than 12 % at 3 shapes, both gradients 2.5 % and 19,
@@ -66,7 +67,7 @@ inline bool ds_rows_in_tiles(const ds_mm_sizes& p, int dtype, int depth, int wid
 inline bool ds_weights_shared(const ds_mm_sizes& p) { return (int64_t)p.rows > 32 * (int64_t)p.groups; }
 
 inline bool ds_weights_in_tiles(const ds_mm_sizes& p, int dtype) {
-  if (p.inner < 8 || p.outer < 8) return false;
+  if (p.inner < 8 || p.outer < 8) return false;   // (as above, and long groups pay for it: both gradients, 100,000 rows in 3 groups, bf16, by 256 x 5 900 us, by 256 x 8 63)
   const bool f32 = dtype == DS_ELEM_F32;
   const double mean = ds_ceil_div(p.rows, p.groups), n = f32 ? 4 : 8;
   const double few = p.groups * ds_ceil_div(p.outer, 16 * n) * ds_ceil_div(p.inner, 8 * n) / kFormUnits;
@@ -77,7 +78,7 @@ inline bool ds_weights_in_tiles(const ds_mm_sizes& p, int dtype) {
   const double tiles = ds_ceil_div(p.inner, side) * ds_ceil_div(p.outer, side), chunks = ds_weight_chunks(p.rows, (int64_t)tiles, (int)unit);
   const double steps = ds_ceil_div(p.groups * ds_ceil_div(mean, unit), chunks), cut = 1 + (p.groups > chunks ? p.groups / chunks : 0) + (chunks > 1 ? 1 : 0);
   const double rounds = chunks * tiles / kFormUnits;
-  const bool odd = p.inner % 4 || p.outer % 4;   // (fp32 rows that are not aligned: 750 us in few, 880 in tiles, of 64,000 by 513 x 300)
+  const bool odd = p.inner % 4 || p.outer % 4;   // (fp32 rows that are not aligned: both gradients of 64 groups of 1,000 rows by 513 x 300, dW in few 749 us, in tiles 831)
   return (rounds > 1 ? rounds : 1) * (steps * (f32 ? odd ? 5.0 : 1.5 : 2.0) + cut * (f32 ? 8 : 5)) + (f32 ? 12 : 4) < few_us;
 }
 

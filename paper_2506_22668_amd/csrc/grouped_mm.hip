@@ -42,7 +42,8 @@ constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 // Loads have no branches, which they would be waited for at: a piece that reaches over its row's end brings the next row's elements along. Columns
 // that there are not lead to results that nobody stores; where the contraction ends, the last step clears them. A piece that would reach over
 // the matrix' end, which it can in its last N rows alone, is read so that it ends there, and shifted. (TINY: matrices of less than 16 bytes, element by element.)
-// Bound by reading W, from memory once if a group has one tile of rows: 8 rows in 8 groups by 1,024 x 4,096 bf16 14.0 us, 4.8 TB/s.
+// Bound by reading W, from memory once if a group has one tile of rows: 8 rows in 8 groups by 1,024 x 4,096 bf16 14.1 us, 4.8 TB/s. (64 rows of 16 bits
+// to a workgroup take 130 + 128 registers, dx 136 + 128 or 196 + 68: one wave to a SIMD.)
 template <typename T, int RB, int WAVES, bool TRANSPOSED, bool HALF, bool TINY>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
   constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
@@ -187,7 +188,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
 // dW and db of a group: 16 N outer by 8 N inner columns to a workgroup, the waves share the group's rows; or (SHARED false, for groups of a few rows, which
 // would keep one wave of four busy) a quarter as many inner columns to a wave, whose results leave from its registers. Both operands
 // run across the contraction (the rows), so both are turned around in registers. db is one more product, with ones for x. The rows
-// of the next step are looked up, and those of this one's are on their way, while the products of the one before are formed. Bound by the latency of those loads.
+// of the next step are looked up, and those of this one's are on their way, while the products of the one before are formed. Bound by the latency of those loads,
+// about 2 us a step, and a group's rows are never cut over workgroups: long groups belong to the tiles.
 template <typename T, bool SHARED, bool TINY>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a) {
   constexpr int N = Piece<T>::N, H = SHARED ? N / 2 : N / 4, STEP = (SHARED ? kWaves : 1) * 4 * N;

@@ -156,7 +156,8 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
 // dw and db: a thread adds up its columns over its rows in registers, the workgroup's rows meet in LDS, and every workgroup
 // leaves one pair of partial rows: no atomics, so the same inputs give the same bits. Bound by memory (x and dy read, dx written): 100,003 rows of 1,000
 // bf16 126 us, 4.8 TB/s, 30,011 rows of 515 fp32 49 us, 3.8 TB/s, of which the second launch and the gap before
-// it take 12. 16-bit rows are kept to 128 registers, for four waves to a SIMD (133, three waves: 134 us; 400,000 rows of 130: 90 -> 71).
+// it take 12. 16-bit rows are kept to 128 registers, for four waves to a SIMD, though 3 to 13 of their values
+// then go through scratch memory (133, three waves: 134 us; 400,000 rows of 130: 90 -> 71).
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) void layer_norm_backward_kernel(NormArgs a) {
   constexpr int N = Piece<T>::N, PIECES = kPer / N, ROWS = kThreads / TPR;
