@@ -237,3 +237,38 @@ def test_many_groups_captured_into_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(out, run(plain, *held))), seed
     mine.close()
     plain.close()
+
+
+@pytest.mark.parametrize("t, element", [(F32, 0), (BF16, 1), (F16, 2)])
+@pytest.mark.parametrize("rows, inner, outer, groups", [(90, 24, 40, 65), (2000, 24, 16, 600), (20_000, 64, 264, 65), (60_000, 64, 72, 1000)])
+def test_offsets_that_do_not_ascend_stay_inside(ctx, t, element, rows, inner, outer, groups):   # noqa: F811
+    """Every other group has all rows, and all have the same weights: a row of the product is right or left as it was, and nothing around the outputs changes."""
+    say(f"offsets up and down {t} rows={rows} groups={groups}")
+    lib, g = ctx.lib, generator(rows)
+    x, dy = normal(g, rows, inner, t=t), normal(g, rows, outer, t=t)
+    w = normal(g, 1, inner, outer, t=t, scale=inner ** -0.5).repeat(groups, 1, 1)
+    offsets = torch.tensor([0 if k % 2 == 0 else rows for k in range(groups + 1)], device="cuda")
+    want = ctx.grouped_mm(x, w[:1], torch.tensor([0, rows], device="cuda"))
+    e, size = mm_exact(x, w[:1], torch.zeros(rows, dtype=torch.int64, device="cuda"), None, False)
+    before, guard = 2 * (inner + 2) * U * size, 64
+
+    def guarded(*shape, of=t):
+        n = int(np.prod(shape))
+        buf = torch.full((n + 2 * guard,), 3.0, dtype=of, device="cuda")
+        return buf, buf[guard:guard + n].view(*shape)
+
+    def untouched(buf):
+        return (buf[:guard] == 3).all() and (buf[-guard:] == 3).all()
+
+    outer_y, y = guarded(rows, outer)
+    assert lib.ds_grouped_mm(ctx.h, element, rows, inner, outer, groups, x.data_ptr(), inner, w.data_ptr(), offsets.data_ptr(), None, None, 0,
+                             y.data_ptr(), outer) == 0
+    left = (y == 3).all(1) | (y == 0).all(1)   # (rows that some group's end leaves to no group are zeros)
+    close(torch.where(left[:, None], want, y), e, before)
+    assert untouched(outer_y)
+    buffers = [guarded(rows, inner), guarded(groups, inner, outer), guarded(groups, outer, of=F32)]
+    ws, ptr, n = ctx._workspace(lib.ds_grouped_mm_backward_workspace, element, rows, inner, outer, groups)
+    assert lib.ds_grouped_mm_backward(ctx.h, element, rows, inner, outer, groups, dy.data_ptr(), outer, x.data_ptr(), inner, w.data_ptr(), offsets.data_ptr(),
+                                      None, None, 0, buffers[0][1].data_ptr(), inner, buffers[1][1].data_ptr(), buffers[2][1].data_ptr(), ptr, n) == 0
+    assert all(untouched(buf) for buf, _ in buffers)
+    assert torch.equal(ctx.grouped_mm(x, w[:1], torch.tensor([0, rows], device="cuda")), want)
