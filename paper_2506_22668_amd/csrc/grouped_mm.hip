@@ -38,7 +38,7 @@ constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 // columns of the result (TRANSPOSED false: N steps of the contraction by 8 columns to a lane) the lane turns its square of
 // elements around in registers; column j of the squares of 16 lanes is an operand, so that a lane ends up with N neighbouring columns of a
 // row. TRANSPOSED: the product with W^T, whose pieces are operands as they are (HALF: of half
-// the columns and twice the contraction: more workgroups, and a wave reads whole lines of 128 bytes of a row; see half_columns).
+// the columns and twice the contraction: more workgroups, and a wave reads whole lines of 128 bytes of a row; see ds_half_columns).
 // Loads have no branches, which they would be waited for at: a piece that reaches over its row's end brings the next row's elements along. Columns
 // that there are not lead to results that nobody stores; where the contraction ends, the last step clears them. A piece that would reach over
 // the matrix' end, which it can in its last N rows alone, is read so that it ends there, and shifted. (TINY: matrices of less than 16 bytes, element by element.)
