@@ -358,10 +358,10 @@ int ds_fidelity(ds_ctx* ctx, const ds_cgraph* cg, const float* phi, const int64_
 /* ---- operators on rows of features ------------------------------------------------
  *
  * What a learned encoder of node features computes and trains on: layer norm, dropout with a residual sum, rows grouped
- * by a type (or by the expert that a router chose), and products with the weights of a row's group. Rows are of ds_element
+ * by a type (or by the expert that a router chose), products with the weights of a row's group, rows of a table by id, the router, and rows held in 8 bits. Rows are of ds_element
  * `dtype`, `*_stride` elements apart (at least a row's width for outputs; 0 repeats one row of an input), at any alignment that the
  * element itself has; parameters of a norm, biases, their gradients and statistics are fp32. Sums are held in fp32 and every result is rounded once.
- * An output may be the same buffer as an input of the same rows for ds_layer_norm (x), ds_dropout (x, residual) and
+ * An output may be the same buffer as an input of the same rows for ds_layer_norm (x), ds_dropout (x, residual), ds_route_backward (x) and
  * ds_layer_norm_backward (dy, x), with equal strides; otherwise outputs overlap nothing. The calls queue their kernels on the context's
  * stream and return: they allocate nothing, copy nothing to the host and wait for nothing, so they may be
  * captured into a HIP graph. A call that needs scratch memory says how much (`*_workspace`, pure host functions); the
@@ -413,6 +413,51 @@ int ds_grouped_mm_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inn
                            int64_t dy_stride, const void* x, int64_t x_stride, const void* w, const int64_t* offsets,
                            const int32_t* order, const void* gate, int64_t gate_stride, void* dx, int64_t dx_stride, void* dw,
                            float* db, void* workspace, int64_t workspace_bytes);
+
+/* Rows of a table by id: y[r] = scale * table[ids[r]], zeros where ids[r] is outside of [0, vocab). table: vocab rows of `table_dtype`, which is `dtype` or
+ * DS_ELEM_F32; ids: int32[rows]. 1 <= vocab <= 2^30, rows <= 2^30; scale is finite. */
+int ds_embed(ds_ctx* ctx, int32_t dtype, int32_t table_dtype, int64_t rows, int64_t cols, int64_t vocab, const void* table, int64_t table_stride,
+             const int32_t* ids, float scale, void* y, int64_t y_stride);
+
+/* Gradient of ds_embed: dtable[v] = scale * sum of dy[r] over the rows with ids[r] = v (zeros where there is none), of `table_dtype`, all vocab rows
+ * written. */
+int ds_embed_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int64_t* bytes /* [host] */);
+int ds_embed_backward(ds_ctx* ctx, int32_t dtype, int32_t table_dtype, int64_t rows, int64_t cols, int64_t vocab, const void* dy, int64_t dy_stride,
+                      const int32_t* ids, float scale, void* dtable, int64_t dtable_stride, void* workspace, int64_t workspace_bytes);
+
+/* The experts of every row from a router's scores x [rows x experts]: with p = softmax(x) over a row, ids: int32[k x rows] out, the experts of its k highest
+ * scores, highest first, ties to the lowest expert, -1 in the place of a score of -inf (an expert that is closed to the row); weights: float[k x rows] out,
+ * their p, or with renorm != 0 each's share of the chosen p, 0 where ids is -1; counts: int64[experts + 1] out, how often each expert was chosen, then N, the
+ * rows that have one; loss: float out = experts * sum over e of (counts[e] / sum of counts) (sum over rows of p[e] / N), which is 1 where all are used alike;
+ * lse: float[rows] out or NULL, the logarithm of a row's sum of exp(x), what the backward pass needs. Slot j's ids (ids + j * rows) are what ds_group_rows
+ * takes. A row that is -inf throughout has no expert (lse -inf) and is not in N; one with a NaN or +inf has none either, and its weights, its lse and the
+ * loss are NaN. 1 <= experts <= 1024, 1 <= k <= min(8, experts), rows <= 2^30. */
+int ds_route_workspace(int64_t rows, int64_t experts, int64_t* bytes /* [host] */);
+int ds_route(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t experts, int64_t k, int32_t renorm, const void* x, int64_t x_stride, int32_t* ids,
+             float* weights, int64_t* counts, float* loss, float* lse, void* workspace, int64_t workspace_bytes);
+
+/* Gradient of ds_route: dx of `dtype` from dweights (float[k x rows] or NULL) and dloss (float, on the device, or NULL; one of the two at least). lse, ids,
+ * counts: what the forward pass left (ids may be NULL without dweights, counts without dloss); the choice itself and the counts have no gradient. dx may be
+ * the same buffer as x, with equal strides. */
+int ds_route_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t experts, int64_t k, int32_t renorm, const void* x, int64_t x_stride, const float* lse,
+                      const int32_t* ids, const int64_t* counts, const float* dweights, const float* dloss, void* dx, int64_t dx_stride);
+
+/* Rows held in 8 bits for a backward pass: x ~ code * 2^(scale - 127). codes: e4m3 numbers (OCP: 4 bits of exponent, 3 of fraction, 448 the largest, no infinities),
+ * one byte a column; scales: one byte for every 32 columns, ceil(cols / 32) to a row; both strides in bytes. ds_pack_rows takes the smallest power of two that
+ * leaves the block's finite values at or below 448 (2^0 for zeros, 2^-126 at the least) and the nearest code, to even, except that no value but 0 becomes 0 (the
+ * smallest code of its sign instead), that no code passes what x's type holds, and that infinities become NaN. ds_unpack_rows rounds once. */
+int ds_pack_rows(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, uint8_t* codes, int64_t codes_stride,
+                 uint8_t* scales, int64_t scales_stride);
+int ds_unpack_rows(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes, int64_t codes_stride, const uint8_t* scales,
+                   int64_t scales_stride, void* y, int64_t y_stride);
+
+/* ds_grouped_mm_backward with x held in 8 bits. gate: NULL, or codes of rows like x: dx is 0 where the code is not above 0. */
+int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, int32_t gate,
+                                            int64_t* bytes /* [host] */);
+int ds_grouped_mm_backward_packed(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, const void* dy, int64_t dy_stride,
+                                  const uint8_t* codes, int64_t codes_stride, const uint8_t* scales, int64_t scales_stride, const void* w,
+                                  const int64_t* offsets, const int32_t* order, const uint8_t* gate, int64_t gate_stride, void* dx, int64_t dx_stride,
+                                  void* dw, float* db, void* workspace, int64_t workspace_bytes);
 
 /* Measurement aid: a plain device-to-device copy of `bytes` bytes (multiple of 16) by a simple
  * streaming kernel on the context's stream. Profilers' HBM byte counters are calibrated against it

@@ -7,6 +7,7 @@ There is no fallback: without the built library every call raises.
 """
 import ctypes as C
 import os
+from typing import Any, NamedTuple
 
 DS_OK, DS_EINVAL, DS_ECAPACITY, DS_ENOMEM, DS_ENOTCONV, DS_EDEVICE, DS_ESINGULAR, DS_EINTERNAL = range(8)
 DS_F32, DS_BF16_IN_F32_ACC = 0, 1
@@ -22,6 +23,8 @@ EXPORTED_SYMBOLS = [
     "ds_plan_tables", "ds_plan_tables_ex", "ds_sample_ex", "ds_sample_range", "ds_eval", "ds_eval_pairs", "ds_eval_noalloc", "ds_solve", "ds_fidelity", "ds_copy_probe", "ds_version",
     "ds_layer_norm", "ds_layer_norm_backward_workspace", "ds_layer_norm_backward", "ds_dropout", "ds_group_rows_workspace",
     "ds_group_rows", "ds_grouped_mm", "ds_grouped_mm_backward_workspace", "ds_grouped_mm_backward",
+    "ds_embed", "ds_embed_backward_workspace", "ds_embed_backward", "ds_route_workspace", "ds_route", "ds_route_backward",
+    "ds_pack_rows", "ds_unpack_rows", "ds_grouped_mm_backward_packed_workspace", "ds_grouped_mm_backward_packed",
 ]
 
 
@@ -58,6 +61,12 @@ class CGraphInfo(C.Structure):
     _fields_ = [("num_players", C.c_int64), ("num_nodes", C.c_int64), ("num_entries", C.c_int64),
                 ("target", C.c_int64), ("hops", C.c_int32), ("directed", C.c_int32),
                 ("ball", C.c_int64 * 8)]
+
+
+class Packed(NamedTuple):
+    """Rows held in 8 bits: x ~ codes * 2^(scales - 127), one scale for 32 neighbouring columns (`Context.pack_rows`)."""
+    codes: Any    # float8_e4m3fn[rows, cols]
+    scales: Any   # uint8[rows, ceil(cols / 32)]
 
 
 class DistShapError(RuntimeError):
@@ -149,6 +158,16 @@ def load_library():
         "ds_grouped_mm": [p, i32, i64, i64, i64, i64, p, i64, p, p, p, p, i32, p, i64],
         "ds_grouped_mm_backward_workspace": [i32, i64, i64, i64, i64, C.POINTER(i64)],
         "ds_grouped_mm_backward": [p, i32, i64, i64, i64, i64, p, i64, p, i64, p, p, p, p, i64, p, i64, p, p, p, i64],
+        "ds_embed": [p, i32, i32, i64, i64, i64, p, i64, p, C.c_float, p, i64],
+        "ds_embed_backward_workspace": [i64, i64, i64, C.POINTER(i64)],
+        "ds_embed_backward": [p, i32, i32, i64, i64, i64, p, i64, p, C.c_float, p, i64, p, i64],
+        "ds_route_workspace": [i64, i64, C.POINTER(i64)],
+        "ds_route": [p, i32, i64, i64, i64, i32, p, i64, p, p, p, p, p, p, i64],
+        "ds_route_backward": [p, i32, i64, i64, i64, i32, p, i64, p, p, p, p, p, p, i64],
+        "ds_pack_rows": [p, i32, i64, i64, p, i64, p, i64, p, i64],
+        "ds_unpack_rows": [p, i32, i64, i64, p, i64, p, i64, p, i64],
+        "ds_grouped_mm_backward_packed_workspace": [i32, i64, i64, i64, i64, i32, C.POINTER(i64)],
+        "ds_grouped_mm_backward_packed": [p, i32, i64, i64, i64, i64, p, i64, p, i64, p, i64, p, p, p, p, i64, p, i64, p, p, p, i64],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -630,8 +649,13 @@ class Context:
         return self._outputs("grouped_mm", y, x, w, bias)
 
     def grouped_mm_backward(self, dy, x, w, offsets, order=None, gate=None):
-        """(dx, dw, dbias fp32) of grouped_mm without its ReLU; dx is 0 where `gate` (rows like x) is not above 0."""
+        """(dx, dw, dbias fp32) of grouped_mm without its ReLU; dx is 0 where `gate` (rows like x) is not above 0. x may be rows that
+        pack_rows holds in 8 bits; a gate is then one too."""
         t = self.torch
+        if isinstance(x, Packed):
+            return self._grouped_backward_packed(dy, x, w, offsets, order, gate)
+        if isinstance(gate, Packed):
+            self._refuse("a gate that is held in 8 bits is one of rows that are")
         x, xs, w, wp, keep, op, rp = self._grouped(x, w, offsets, order)
         (rows, inner), (groups, _, outer) = x.shape, w.shape
         dy, dys = self._rows(dy, "dy", (rows, outer), x.dtype)
@@ -647,3 +671,151 @@ class Context:
         self._queue(self.lib.ds_grouped_mm_backward, element, rows, inner, outer, groups, dy.data_ptr(), dys, x.data_ptr(), xs, wp, op,
                     rp, gp, gs, dx.data_ptr(), inner, dw.data_ptr(), db.data_ptr(), wsp, wsn)
         return self._outputs("grouped_mm_backward", (dx, dw, db), dy, x, w)
+
+    def _packed(self, a, name, shape=None):
+        """The codes and scales of rows held in 8 bits, and for both the distance of rows."""
+        t = self.torch
+        if not isinstance(a, Packed):
+            self._refuse(f"{name} is not held in 8 bits (pack_rows)")
+        codes, scales = a
+        if codes.dtype != t.float8_e4m3fn or scales.dtype != t.uint8:
+            self._refuse(f"{name} is {codes.dtype} with scales of {scales.dtype}, float8_e4m3fn and uint8 are needed")
+        if codes.dim() != 2 or (shape is not None and tuple(codes.shape) != shape):
+            self._refuse(f"{name} has shape {tuple(codes.shape)}, {'two dimensions are' if shape is None else f'{shape} is'} needed")
+        if tuple(scales.shape) != (codes.shape[0], (codes.shape[1] + 31) // 32):
+            self._refuse(f"{name}: scales of shape {tuple(scales.shape)} for codes of shape {tuple(codes.shape)}")
+        if codes.get_device() != self._index or scales.get_device() != self._index:
+            self._refuse(f"{name} is not on {self.device}")
+        if codes.stride(1) != 1 and codes.shape[1] > 1:
+            codes = codes.contiguous()
+        if scales.stride(1) != 1 and scales.shape[1] > 1:
+            scales = scales.contiguous()
+        return codes, codes.stride(0), scales, scales.stride(0)
+
+    def _grouped_backward_packed(self, dy, x, w, offsets, order, gate):
+        t = self.torch
+        codes, cs, scales, ss = self._packed(x, "x")
+        rows, inner = codes.shape
+        if w is None or w.dim() != 3 or w.shape[1] != inner:
+            self._refuse(f"w is [groups, {inner}, outer] for rows of {inner} columns")
+        groups, _, outer = w.shape
+        if w.dtype not in self._elements:
+            self._refuse(f"w is {w.dtype}, float32, bfloat16 or float16 is needed")
+        w, wp = self._values(w, "w", tuple(w.shape), w.dtype)
+        if offsets is None:
+            self._refuse("offsets are needed")
+        offsets, op = self._values(offsets, "offsets", (groups + 1,), t.int64)
+        order, rp = self._values(order, "order", (rows,), t.int32)
+        dy, dys = self._rows(dy, "dy", (rows, outer), w.dtype)
+        gp, gs = None, 0
+        if gate is not None:
+            gate, gs, _, _ = self._packed(gate, "gate", (rows, inner))
+            gp = gate.data_ptr()
+        dx = w.new_empty((rows, inner))
+        dw = w.new_empty((groups, inner, outer))
+        db = t.empty((groups, outer), dtype=t.float32, device=w.device)
+        element = self._elements[w.dtype]
+        ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_packed_workspace, element, rows, inner, outer, groups, int(gp is not None))
+        self._queue(self.lib.ds_grouped_mm_backward_packed, element, rows, inner, outer, groups, dy.data_ptr(), dys, codes.data_ptr(), cs, scales.data_ptr(), ss,
+                    wp, op, rp, gp, gs, dx.data_ptr(), inner, dw.data_ptr(), db.data_ptr(), wsp, wsn)
+        return self._outputs("grouped_mm_backward", (dx, dw, db), dy, w)
+
+    def pack_rows(self, x):
+        """The rows of x in 8 bits, as `Packed`: what a training step keeps of an activation, half of 16 bits. Zeros stay zeros, and nothing else becomes
+        one; an infinity becomes NaN."""
+        t = self.torch
+        given, (x, xs) = x, self._rows(x, "x")
+        rows, cols = x.shape
+        codes = t.empty((rows, cols), dtype=t.float8_e4m3fn, device=x.device)
+        scales = t.empty((rows, (cols + 31) // 32), dtype=t.uint8, device=x.device)
+        self._queue(self.lib.ds_pack_rows, self._elements[x.dtype], rows, cols, x.data_ptr(), xs, codes.data_ptr(), cols, scales.data_ptr(), scales.shape[1])
+        return Packed(*self._outputs("pack_rows", (codes, scales), given))
+
+    def unpack_rows(self, packed, dtype=None):
+        """The rows that `packed` stands for, in `dtype` (float32 if none is given)."""
+        t = self.torch
+        codes, cs, scales, ss = self._packed(packed, "packed")
+        dtype = t.float32 if dtype is None else dtype
+        if dtype not in self._elements:
+            self._refuse(f"rows are float32, bfloat16 or float16, not {dtype}")
+        y = t.empty(tuple(codes.shape), dtype=dtype, device=codes.device)
+        self._queue(self.lib.ds_unpack_rows, self._elements[dtype], *y.shape, codes.data_ptr(), cs, scales.data_ptr(), ss, y.data_ptr(), y.shape[1])
+        return self._outputs("unpack_rows", y, codes)
+
+    def _ids(self, ids):
+        if ids is None or ids.dim() != 1:
+            self._refuse("ids: one for every row")
+        return self._values(ids, "ids", (ids.shape[0],), self.torch.int32)
+
+    def embed(self, table, ids, scale=1.0, dtype=None):
+        """y[r] = scale * table[ids[r]], zeros where the id (int32[rows]) is outside of the table. table: [vocab, cols]; y is of `dtype`: the
+        table's (if none is given), or any where the table is fp32."""
+        given, (table, ts) = table, self._rows(table, "table")
+        vocab, cols = table.shape
+        ids, ip = self._ids(ids)
+        dtype = table.dtype if dtype is None else dtype
+        if dtype not in self._elements:
+            self._refuse(f"rows are float32, bfloat16 or float16, not {dtype}")
+        y = table.new_empty((ids.shape[0], cols), dtype=dtype)
+        self._queue(self.lib.ds_embed, self._elements[dtype], self._elements[table.dtype], ids.shape[0], cols, vocab, table.data_ptr(), ts, ip, scale,
+                    y.data_ptr(), cols)
+        return self._outputs("embed", y, given)
+
+    def embed_backward(self, dy, ids, vocab, scale=1.0, dtype=None):
+        """dtable [vocab, cols] of embed, in `dtype`: dy's (if none is given), or fp32. Its rows are summed by sorted ids, in fp32."""
+        t = self.torch
+        ids, ip = self._ids(ids)
+        given = dy
+        if dy.dim() != 2:
+            self._refuse(f"dy has shape {tuple(dy.shape)}, two dimensions are needed")
+        dy, dys = self._rows(dy, "dy", (ids.shape[0], dy.shape[1]))
+        (rows, cols), vocab = dy.shape, int(vocab)
+        dtype = dy.dtype if dtype is None else dtype
+        if dtype not in self._elements:
+            self._refuse(f"a table is float32, bfloat16 or float16, not {dtype}")
+        ws, wsp, wsn = self._workspace(self.lib.ds_embed_backward_workspace, rows, cols, vocab)
+        dtable = dy.new_empty((vocab, cols), dtype=dtype)
+        self._queue(self.lib.ds_embed_backward, self._elements[dy.dtype], self._elements[dtype], rows, cols, vocab, dy.data_ptr(), dys, ip, scale,
+                    dtable.data_ptr(), cols, wsp, wsn)
+        return self._outputs("embed_backward", dtable, given)
+
+    def route(self, scores, k=1, renorm=False):
+        """(ids int32[k, rows], weights fp32[k, rows], counts int64[experts + 1], loss, lse fp32[rows]): every row's experts of the k highest scores, ties to
+        the lowest (ids[j] is what group_rows takes; -1: none, a score of -inf closes an expert to a row); their softmax, or with `renorm` each's share of the
+        chosen; how often each was chosen, then the rows that have one; a balance loss, 1 where all are used alike; and what route_backward needs. scores:
+        [rows, experts], at most 1,024 experts and k of 8."""
+        t = self.torch
+        given, (x, xs) = scores, self._rows(scores, "scores")
+        (rows, experts), k = x.shape, int(k)
+        ws, wsp, wsn = self._workspace(self.lib.ds_route_workspace, rows, experts)
+        if not 1 <= k <= min(8, experts):
+            self._refuse(f"{k} experts to a row out of range [1, {min(8, experts)}]")
+        ids = t.empty((k, rows), dtype=t.int32, device=x.device)
+        weights = t.empty((k, rows), dtype=t.float32, device=x.device)
+        counts = t.empty(experts + 1, dtype=t.int64, device=x.device)
+        lse = t.empty(rows, dtype=t.float32, device=x.device)
+        loss = t.empty((), dtype=t.float32, device=x.device)
+        self._queue(self.lib.ds_route, self._elements[x.dtype], rows, experts, k, int(bool(renorm)), x.data_ptr(), xs, ids.data_ptr(), weights.data_ptr(),
+                    counts.data_ptr(), loss.data_ptr(), lse.data_ptr(), wsp, wsn)
+        return self._outputs("route", (ids, weights, counts, loss, lse), given)
+
+    def route_backward(self, scores, lse, ids, counts, dweights=None, dloss=None, renorm=False):
+        """The scores' gradient, of their type, from the weights' (fp32[k, rows]) and the loss' (a fp32 tensor of one element), one of them at
+        least. lse, ids and counts are what route gave for the scores, `renorm` what it was called with."""
+        t = self.torch
+        given, (x, xs) = scores, self._rows(scores, "scores")
+        rows, experts = x.shape
+        if ids is None or ids.dim() != 2 or lse is None or counts is None:
+            self._refuse("lse, ids and counts of the forward pass are needed")
+        k = ids.shape[0]
+        lse, lp = self._values(lse, "lse", (rows,), t.float32)
+        ids, ip = self._values(ids, "ids", (k, rows), t.int32)
+        counts, cp = self._values(counts, "counts", (experts + 1,), t.int64)
+        dweights, wp = self._values(dweights, "dweights", (k, rows), t.float32)
+        if dloss is not None and dloss.numel() != 1:
+            self._refuse(f"dloss has shape {tuple(dloss.shape)}, one element is needed")
+        dloss, dp = self._values(dloss, "dloss", () if dloss is None else tuple(dloss.shape), t.float32)
+        dx = x.new_empty((rows, experts))
+        self._queue(self.lib.ds_route_backward, self._elements[x.dtype], rows, experts, k, int(bool(renorm)), x.data_ptr(), xs, lp, ip, cp, wp, dp,
+                    dx.data_ptr(), experts)
+        return self._outputs("route_backward", dx, given, dweights, dloss)

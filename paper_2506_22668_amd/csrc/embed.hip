@@ -1,0 +1,537 @@
+// Rows of a table by id, and the table's gradient.
+//
+//   forward:   y[r] = s T[id_r],                          zeros where id_r is outside of [0, V)
+//   backward:  dT[v] = s sum over r with id_r = v of dy[r],   zeros where there is none
+//
+// The gradient is summed by sorted ids: a stable radix sort of the pairs (id, r) on digits of up to 10 bits, then sums over stretches of equally many sorted
+// rows, whatever ids they hold, so that an id with a large share of the rows costs as much as as many ids with one row. Where a stretch
+// ends inside an id's rows it leaves a partial sum in fp32, and a last launch adds those up in order and clears the rows of ids that did not come up.
+// No atomic decides an order of floating-point sums: the same inputs give the same bits.
+#include "feature_ops.h"
+#include "group_range.h"
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---- the rows -------------------------------------------------------------------------------------------------------------------------
+
+struct LookArgs {
+  int64_t rows;
+  int cols, calls;      // pieces to a row
+  int64_t rows_step;    // how far a thread's next piece is
+  int calls_step, vocab;
+  const int32_t* ids;
+  const void* table;
+  void* y;
+  int64_t ts, ys;
+  float scale;
+};
+
+constexpr int kAhead = 4;   // pieces of a thread on their way at a time: each waits for an id, and then for a row of the table
+
+template <typename T, typename Y, bool TINY>
+__global__ __launch_bounds__(kThreads) void look_up_kernel(LookArgs a) {
+  constexpr int N = Piece<Y>::N;
+  const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int64_t row = first / a.calls;
+  int call = (int)(first % a.calls);
+  while (row < a.rows) {
+    int64_t at[kAhead];
+    int col[kAhead], id[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      at[j] = row;
+      col[j] = call * N;
+      id[j] = row < a.rows ? a.ids[row] : -1;
+      row += a.rows_step;
+      call += a.calls_step;
+      if (call >= a.calls) {
+        call -= a.calls;
+        ++row;
+      }
+    }
+    typename Elements<T, N>::V v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if ((uint32_t)id[j] >= (uint32_t)a.vocab) id[j] = -1;
+      v[j] = load_elements<T, N, TINY>((const T*)a.table + (int64_t)(id[j] < 0 ? 0 : id[j]) * a.ts, col[j], a.cols);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (at[j] >= a.rows) break;
+      settle_elements<T, N, TINY>(v[j], col[j], a.cols);
+      PieceV<Y> out;
+#pragma unroll
+      for (int i = 0; i < N; ++i) out[i] = id[j] < 0 ? (Y)0.f : (Y)((float)v[j][i] * a.scale);
+      store_piece<Y>((Y*)a.y + at[j] * a.ys + col[j], out, a.cols - col[j]);
+    }
+  }
+}
+
+template <typename T, typename Y>
+void launch_look_up(ds_ctx* ctx, LookArgs& a) {
+  constexpr int N = Piece<Y>::N;
+  a.calls = (a.cols + N - 1) / N;
+  const int64_t pieces = a.rows * a.calls, want = (pieces + kThreads - 1) / kThreads, most = 8 * (int64_t)ctx->num_cus;
+  const int64_t blocks = want < most ? want : most, step = blocks * kThreads;
+  a.rows_step = step / a.calls;
+  a.calls_step = (int)(step % a.calls);
+  const dim3 grid((unsigned)blocks), block(kThreads);
+  if (a.cols < N) hipLaunchKernelGGL(HIP_KERNEL_NAME(look_up_kernel<T, Y, true>), grid, block, 0, ctx->stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(look_up_kernel<T, Y, false>), grid, block, 0, ctx->stream, a);
+}
+
+// ---- the sorted pairs -------------------------------------------------------------------------------------------------------------------
+
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kMostBits = 10;      // of a digit: counts of 16 waves in 64 KB of LDS
+constexpr int kStretch = 2048;     // rows of a workgroup, at the least, where there are several
+constexpr int kMostBlocks = 256;
+
+struct SortArgs {
+  const int32_t* ids;       // the first pass: the keys come from here, and rows are counted
+  const int2* from;         // later ones: (key, row)
+  int2* to;
+  int rows, vocab, shift, bits, per_wave;
+  int32_t* counts;          // [block][digits], and behind them the digits' rows
+  uint8_t* seen;            // [vocab], cleared by the first launch
+};
+
+__device__ __forceinline__ int2 pair_at(const SortArgs& a, int at) {
+  if (!a.ids) return a.from[at];
+  const int id = a.ids[at];
+  return {(uint32_t)id < (uint32_t)a.vocab ? id : a.vocab, at};
+}
+
+// the pairs of one wave: a stretch of the rows
+struct Stretch {
+  int begin, end;
+};
+__device__ __forceinline__ Stretch stretch_of(const SortArgs& a, int block) {
+  const int64_t first = ((int64_t)block * kSortWaves + (threadIdx.x >> 6)) * a.per_wave;
+  Stretch s;
+  s.begin = first < a.rows ? (int)first : a.rows;
+  s.end = a.rows - s.begin < a.per_wave ? a.rows : s.begin + a.per_wave;
+  return s;
+}
+
+// counts of the workgroup's rows by wave and digit
+__device__ __forceinline__ void count_digits(const SortArgs& a, int block, int* count) {
+  const int digits = 1 << a.bits, lane = threadIdx.x & 63;
+  for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortThreads) count[i] = 0;
+  __syncthreads();
+  int* mine = count + (threadIdx.x >> 6) * digits;
+  const Stretch s = stretch_of(a, block);
+  for (int at = s.begin + lane; at < s.end; at += 64) atomicAdd(&mine[pair_at(a, at).x >> a.shift & (digits - 1)], 1);   // (whole numbers: any order)
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs a, bool clear) {
+  extern __shared__ int count[];
+  if (clear)
+    for (int64_t i = ((int64_t)blockIdx.x * kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)gridDim.x * kSortThreads * 16)
+      *reinterpret_cast<uint4*>(a.seen + i) = uint4{0, 0, 0, 0};   // (its end is rounded up to 16 bytes)
+  const int digits = 1 << a.bits;
+  count_digits(a, (int)blockIdx.x, count);
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+    int n = 0;
+    for (int w = 0; w < kSortWaves; ++w) n += count[w * digits + d];
+    a.counts[(int)blockIdx.x * digits + d] = n;
+  }
+}
+
+// Turns the workgroups' counts into the rows of the digit before each of them, and leaves the digits' rows behind them
+__global__ __launch_bounds__(kSortThreads) void sort_before_kernel(SortArgs a, int blocks) {
+  __shared__ int sum[kSortWaves][64];
+  const int digits = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = (int)blockIdx.x * 64 + lane;
+  const int each = (blocks + kSortWaves - 1) / kSortWaves, first = wave * each;
+  int n[kMostBlocks / kSortWaves], all = 0;
+#pragma unroll
+  for (int j = 0; j < kMostBlocks / kSortWaves; ++j) n[j] = j < each && first + j < blocks && d < digits ? a.counts[(first + j) * digits + d] : 0;
+#pragma unroll
+  for (int j = 0; j < kMostBlocks / kSortWaves; ++j) all += n[j];
+  sum[wave][lane] = all;
+  __syncthreads();
+  int before = 0, whole = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    if (w < wave) before += sum[w][lane];
+    whole += sum[w][lane];
+  }
+  if (d >= digits) return;
+#pragma unroll
+  for (int j = 0; j < kMostBlocks / kSortWaves; ++j) {
+    if (j < each && first + j < blocks) a.counts[(first + j) * digits + d] = before;
+    before += n[j];
+  }
+  if (wave == 0) a.counts[blocks * digits + d] = whole;
+}
+
+// One pass: each workgroup's pairs to their places. Lanes of one digit find each other by a ballot for each of its bits, so that a
+// pair's rank is a popcount, and pairs of one digit keep their order.
+__device__ __forceinline__ void place_pairs(const SortArgs& a, int block, int blocks, int* count, int* wave_sum) {
+  const int digits = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  count_digits(a, block, count);
+  // (digits <= threads: thread d has digit d)
+  const int d = (int)threadIdx.x;
+  int whole = 0, before = 0;
+  if (d < digits) {
+    if (blocks == 1) {
+      for (int w = 0; w < kSortWaves; ++w) whole += count[w * digits + d];
+    } else {
+      before = a.counts[block * digits + d];
+      whole = a.counts[blocks * digits + d];
+    }
+  }
+  int upto = whole;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += up;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  if (d < digits) {
+    int at = upto - whole + before;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w)
+      if (w < wave) at += wave_sum[w];
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = count[w * digits + d];
+      count[w * digits + d] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  volatile int* mine = count + wave * digits;
+  const Stretch s = stretch_of(a, block);
+  int2 next = s.begin + lane < s.end ? pair_at(a, s.begin + lane) : int2{0, 0};
+  for (int base = s.begin; base < s.end; base += 64) {
+    const int2 now = next;
+    const bool there = base + lane < s.end;
+    if (base + 64 + lane < s.end) next = pair_at(a, base + 64 + lane);
+    const int digit = now.x >> a.shift & (digits - 1);
+    unsigned long long same = __ballot(there);
+    for (int b = 0; b < a.bits; ++b) {
+      const unsigned long long set = __ballot(digit >> b & 1);
+      same &= digit >> b & 1 ? set : ~set;
+    }
+    if (there) {
+      const int rank = __popcll(same & ((1ull << lane) - 1)), at = mine[digit];
+      a.to[at + rank] = now;
+      if (rank == 0) mine[digit] = at + __popcll(same);   // (a wave's LDS accesses keep their order)
+    }
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a) {
+  extern __shared__ int count[];
+  __shared__ int wave_sum[kSortWaves];
+  place_pairs(a, (int)blockIdx.x, (int)gridDim.x, count, wave_sum);
+}
+
+// All passes of few rows in one workgroup; the others clear what is to be cleared
+__global__ __launch_bounds__(kSortThreads) void sort_few_kernel(SortArgs a, int2* other, int passes) {
+  extern __shared__ int count[];
+  __shared__ int wave_sum[kSortWaves];
+  if (blockIdx.x > 0) {
+    for (int64_t i = ((int64_t)(blockIdx.x - 1) * kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)(gridDim.x - 1) * kSortThreads * 16)
+      *reinterpret_cast<uint4*>(a.seen + i) = uint4{0, 0, 0, 0};
+    return;
+  }
+  int2* to = a.to;
+  for (int p = 0; p < passes; ++p) {
+    a.to = (passes - 1 - p) & 1 ? other : to;
+    place_pairs(a, 0, 1, count, wave_sum);
+    a.ids = nullptr;
+    a.from = a.to;
+    a.shift += a.bits;
+    __syncthreads();
+  }
+}
+
+// ---- the sums -----------------------------------------------------------------------------------------------------------------------------
+
+struct SumArgs {
+  int rows, cols, vocab, chunk, chunks, calls;
+  const int2* pairs;
+  const void* dy;
+  void* dtable;
+  int64_t dys, dts;
+  float scale;
+  uint8_t* seen;
+  float* partial;       // [chunk][2][cols]: of the id that began before the chunk; of the one that goes on behind it
+  int64_t rows_step;    // the pass over the table: how far a thread's next piece is
+  int calls_step, zero_blocks;
+};
+
+constexpr int kRowsAhead = 8;
+
+// N elements as the table has them, in pieces of 16 bytes
+template <typename T, int N>
+__device__ __forceinline__ void store_sums(T* to, const float (&v)[N], float scale, int have) {
+  constexpr int P = Piece<T>::N;
+#pragma unroll
+  for (int p = 0; p < N / P; ++p) {
+    PieceV<T> out;
+#pragma unroll
+    for (int i = 0; i < P; ++i) out[i] = (T)(v[p * P + i] * scale);
+    store_piece<T>(to + p * P, out, have - p * P);
+  }
+}
+
+// LANES threads take a stretch of `chunk` sorted rows, N columns to a thread
+template <typename D, typename T, int LANES, bool TINY>
+__global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
+  constexpr int N = Piece<D>::N;
+  const int chunk = (int)blockIdx.x * (kThreads / LANES) + (int)threadIdx.x / LANES, col = ((int)blockIdx.y * LANES + (int)threadIdx.x % LANES) * N;
+  const int begin = (int)min((int64_t)chunk * a.chunk, (int64_t)a.rows), end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
+  if (begin >= end || col >= a.cols) return;
+  const int have = a.cols - col;
+  const D* dy = (const D*)a.dy;
+  T* dtable = (T*)a.dtable + col;
+  float* partial = a.partial + (int64_t)chunk * 2 * a.cols + col;
+  int key = a.pairs[begin].x;
+  bool before = begin > 0 && a.pairs[begin - 1].x == key;   // the id began before the chunk
+  const bool after = end < a.rows && a.pairs[end].x == a.pairs[end - 1].x;
+  float sum[N] = {};
+  const auto leave = [&](bool last) __attribute__((always_inline)) {
+    if (key >= a.vocab) return;
+    if (before || last) {
+      store_sums<float, N>(partial + (last ? a.cols : 0), sum, 1.f, have);
+    } else {
+      store_sums<T, N>(dtable + (int64_t)key * a.dts, sum, a.scale, have);
+    }
+    if (!before && col == 0) a.seen[key] = 1;
+  };
+  int2 now[kRowsAhead], next[kRowsAhead];
+  typename Elements<D, N>::V v[kRowsAhead];
+  const auto ask = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) next[j] = a.pairs[min(at + j, end - 1)];
+  };
+  ask(begin);
+  for (int at = begin; at < end; at += kRowsAhead) {
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      now[j] = next[j];
+      v[j] = load_elements<D, N, TINY>(dy + now[j].y * a.dys, col, a.cols);
+    }
+    if (at + kRowsAhead < end) ask(at + kRowsAhead);
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      if (at + j >= end) break;
+      if (now[j].x != key) {
+        leave(false);
+        before = false;
+        key = now[j].x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.f;
+      }
+      if (key >= a.vocab) return;   // (the rows of no id are the last ones)
+      settle_elements<D, N, TINY>(v[j], col, a.cols);
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += (float)v[j][i];
+    }
+  }
+  leave(after);
+}
+
+// Adds up what the chunks left of ids that reach over a chunk's end, and clears the rows of ids that did not come up (the workgroups behind `join_blocks`).
+template <typename T>
+__global__ __launch_bounds__(kThreads) void finish_kernel(SumArgs a, int join_blocks) {
+  constexpr int N = Piece<T>::N;
+  if ((int)blockIdx.x >= join_blocks) {
+    const int64_t first = (int64_t)((int)blockIdx.x - join_blocks) * kThreads + threadIdx.x;
+    int64_t row = first / a.calls;
+    int call = (int)(first % a.calls);
+    while (row < a.vocab) {
+      if (!a.seen[row]) store_piece<T>((T*)a.dtable + row * a.dts + call * N, PieceV<T>{}, a.cols - call * N);
+      row += a.rows_step;
+      call += a.calls_step;
+      if (call >= a.calls) {
+        call -= a.calls;
+        ++row;
+      }
+    }
+    return;
+  }
+  // the id that begins in this chunk and goes on behind it
+  const int chunk = (int)blockIdx.x, begin = chunk * a.chunk, end = begin + a.chunk;
+  if (end >= a.rows) return;
+  const int key = a.pairs[end - 1].x;
+  if (key >= a.vocab || a.pairs[end].x != key || (begin > 0 && a.pairs[begin - 1].x == key)) return;
+  // the last chunk that it has rows in
+  __shared__ int last_of[kThreads];
+  int last = chunk + 1;
+  for (int c = chunk + 1 + (int)threadIdx.x; c < a.chunks && a.pairs[c * a.chunk].x == key; c += kThreads) last = c;
+  last_of[threadIdx.x] = last;
+  __syncthreads();
+  for (int o = kThreads / 2; o > 0; o >>= 1) {
+    if ((int)threadIdx.x < o) last_of[threadIdx.x] = max(last_of[threadIdx.x], last_of[threadIdx.x + o]);
+    __syncthreads();
+  }
+  last = last_of[0];
+  for (int col = threadIdx.x; col < a.cols; col += kThreads) {
+    float sum = 0.f;
+#pragma unroll 8
+    for (int c = chunk; c < last; ++c) sum += a.partial[((int64_t)c * 2 + 1) * a.cols + col];
+    sum += a.partial[(int64_t)last * 2 * a.cols + col];
+    ((T*)a.dtable)[(int64_t)key * a.dts + col] = (T)(sum * a.scale);
+  }
+}
+
+// rows of a chunk: enough chunks for the card, each long enough to be worth its partial sums
+int chunk_of(int rows) {
+  int c = 16;
+  while (c < 256 && (rows + c - 1) / c > 16384) c *= 2;
+  return c;
+}
+int digits_of(int vocab, int* passes) {
+  const int bits = 32 - __builtin_clz((unsigned)vocab);   // of 0 .. vocab
+  *passes = (bits + kMostBits - 1) / kMostBits;
+  return (bits + *passes - 1) / *passes;
+}
+int sort_blocks(int rows) {
+  const int blocks = (rows + kStretch - 1) / kStretch;
+  return blocks <= 4 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks;
+}
+
+struct Layout {
+  int64_t pairs, other, counts, seen, partial, bytes;
+};
+Layout layout_of(int rows, int cols, int vocab) {
+  int passes;
+  const int bits = digits_of(vocab, &passes), blocks = sort_blocks(rows);
+  const int64_t chunks = (rows + chunk_of(rows) - 1) / chunk_of(rows);
+  Layout l = {};
+  int64_t at = 0;
+  const auto place = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += (bytes + 15) / 16 * 16;
+    return here;
+  };
+  l.pairs = place((int64_t)rows * 8);
+  l.other = place(passes > 1 ? (int64_t)rows * 8 : 0);
+  l.counts = place(blocks > 1 ? (int64_t)(blocks + 1) * (1 << bits) * 4 : 0);
+  l.seen = place(vocab);
+  l.partial = place(chunks * 2 * cols * 4);
+  l.bytes = at;
+  return l;
+}
+
+int sort_ids(ds_ctx* ctx, const int32_t* ids, int rows, int vocab, int2* pairs, int2* other, int32_t* counts, uint8_t* seen) {
+  int passes;
+  SortArgs a = {};
+  a.ids = ids;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.bits = digits_of(vocab, &passes);
+  a.counts = counts;
+  a.seen = seen;
+  const int blocks = sort_blocks(rows), lds = kSortWaves * (1 << a.bits) * (int)sizeof(int);
+  const int64_t waves = (int64_t)blocks * kSortWaves, each = (rows + waves - 1) / waves;
+  a.per_wave = (int)((each + 63) / 64 * 64);
+  if (lds > 48 * 1024) {
+    DS_HIP(ctx, hipFuncSetAttribute((const void*)sort_count_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    DS_HIP(ctx, hipFuncSetAttribute((const void*)sort_place_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    DS_HIP(ctx, hipFuncSetAttribute((const void*)sort_few_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  }
+  if (blocks == 1) {
+    const int64_t clear = ((int64_t)vocab + 16 * kSortThreads - 1) / (16 * kSortThreads);
+    a.to = pairs;
+    hipLaunchKernelGGL(sort_few_kernel, dim3(1 + (unsigned)(clear < 2 * ctx->num_cus ? clear : 2 * ctx->num_cus)), dim3(kSortThreads), lds, ctx->stream, a, other, passes);
+  } else {
+    for (int p = 0; p < passes; ++p) {
+      a.to = (passes - 1 - p) & 1 ? other : pairs;
+      hipLaunchKernelGGL(sort_count_kernel, dim3(blocks), dim3(kSortThreads), lds, ctx->stream, a, p == 0);
+      hipLaunchKernelGGL(sort_before_kernel, dim3(((1 << a.bits) + 63) / 64), dim3(kSortThreads), 0, ctx->stream, a, blocks);
+      hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(kSortThreads), lds, ctx->stream, a);
+      a.ids = nullptr;
+      a.from = a.to;
+      a.shift += a.bits;
+    }
+  }
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+template <typename D, typename T, int LANES>
+void launch_sum(const SumArgs& a, hipStream_t stream) {
+  constexpr int N = Piece<D>::N, WORKERS = kThreads / LANES;
+  const dim3 grid((a.chunks + WORKERS - 1) / WORKERS, (a.cols + LANES * N - 1) / (LANES * N)), block(kThreads);
+  if (a.cols < N) hipLaunchKernelGGL(HIP_KERNEL_NAME(sum_kernel<D, T, LANES, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(sum_kernel<D, T, LANES, false>), grid, block, 0, stream, a);
+}
+
+template <typename D, typename T>
+int launch_sums(ds_ctx* ctx, SumArgs& a) {
+  const int pieces = (a.cols + Piece<D>::N - 1) / Piece<D>::N;
+  if (a.rows > 0) {
+    if (pieces <= 8) launch_sum<D, T, 8>(a, ctx->stream);
+    else if (pieces <= 16) launch_sum<D, T, 16>(a, ctx->stream);
+    else if (pieces <= 32) launch_sum<D, T, 32>(a, ctx->stream);
+    else launch_sum<D, T, 64>(a, ctx->stream);
+  }
+  a.calls = (a.cols + Piece<T>::N - 1) / Piece<T>::N;
+  const int64_t all = (int64_t)a.vocab * a.calls, want = (all + kThreads - 1) / kThreads, most = 8 * (int64_t)ctx->num_cus;
+  a.zero_blocks = (int)(want < most ? want : most);
+  const int64_t step = (int64_t)a.zero_blocks * kThreads;
+  a.rows_step = step / a.calls;
+  a.calls_step = (int)(step % a.calls);
+  const int joins = a.rows > 0 ? a.chunks : 0;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(finish_kernel<T>), dim3(joins + a.zero_blocks), dim3(kThreads), 0, ctx->stream, a, joins);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+}  // namespace
+
+int ds_launch_embed(ds_ctx* ctx, int dtype, int table_dtype, int64_t rows, int cols, int vocab, ds_rows table, const int32_t* ids, float scale, ds_rows y) {
+  if (rows == 0) return DS_OK;
+  LookArgs a = {};
+  a.rows = rows;
+  a.cols = cols;
+  a.vocab = vocab;
+  a.ids = ids;
+  a.table = table.data;
+  a.ts = table.stride;
+  a.y = (void*)y.data;
+  a.ys = y.stride;
+  a.scale = scale;
+  if (dtype == DS_ELEM_F32) launch_look_up<float, float>(ctx, a);
+  else if (dtype == DS_ELEM_BF16) table_dtype == DS_ELEM_F32 ? launch_look_up<float, __bf16>(ctx, a) : launch_look_up<__bf16, __bf16>(ctx, a);
+  else table_dtype == DS_ELEM_F32 ? launch_look_up<float, _Float16>(ctx, a) : launch_look_up<_Float16, _Float16>(ctx, a);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+int64_t ds_embed_backward_bytes(int rows, int cols, int vocab) { return layout_of(rows, cols, vocab).bytes; }
+
+int ds_launch_embed_backward(ds_ctx* ctx, int dtype, int table_dtype, int rows, int cols, int vocab, ds_rows dy, const int32_t* ids, float scale,
+                             ds_rows dtable, void* workspace) {
+  const Layout l = layout_of(rows, cols, vocab);
+  char* base = (char*)workspace;
+  int2* pairs = (int2*)(base + l.pairs);
+  uint8_t* seen = (uint8_t*)(base + l.seen);
+  DS_TRY(sort_ids(ctx, ids, rows, vocab, pairs, (int2*)(base + l.other), (int32_t*)(base + l.counts), seen));
+  SumArgs a = {};
+  a.rows = rows;
+  a.cols = cols;
+  a.vocab = vocab;
+  a.chunk = chunk_of(rows);
+  a.chunks = (rows + a.chunk - 1) / a.chunk;
+  a.pairs = pairs;
+  a.dy = dy.data;
+  a.dys = dy.stride;
+  a.dtable = (void*)dtable.data;
+  a.dts = dtable.stride;
+  a.scale = scale;
+  a.seen = seen;
+  a.partial = (float*)(base + l.partial);
+  if (dtype == DS_ELEM_F32) return launch_sums<float, float>(ctx, a);
+  if (dtype == DS_ELEM_BF16) return table_dtype == DS_ELEM_F32 ? launch_sums<__bf16, float>(ctx, a) : launch_sums<__bf16, __bf16>(ctx, a);
+  return table_dtype == DS_ELEM_F32 ? launch_sums<_Float16, float>(ctx, a) : launch_sums<_Float16, _Float16>(ctx, a);
+}

@@ -5,7 +5,7 @@
 
 namespace {
 
-constexpr int kMostCols = 1 << 20, kMostNormCols = 4096, kMostGroups = 1024;
+constexpr int kMostCols = 1 << 20, kMostNormCols = 4096, kMostGroups = 1024, kMostChosen = 8;
 constexpr int64_t kMostRows = 1ll << 40, kMostOrdered = 1ll << 30;
 
 bool known(int dtype) { return dtype == DS_ELEM_F32 || dtype == DS_ELEM_BF16 || dtype == DS_ELEM_F16; }
@@ -39,6 +39,33 @@ int check_workspace(ds_ctx* ctx, const void* workspace, int64_t bytes, int64_t n
 int check_groups(ds_ctx* ctx, int64_t groups, const int64_t* offsets) {
   if (groups < 1 || groups > kMostGroups) return ds_fail(ctx, DS_EINVAL, "%lld groups out of range [1, %d]", (long long)groups, kMostGroups);
   if (!offsets) return ds_fail(ctx, DS_EINVAL, "offsets is null");
+  return DS_OK;
+}
+
+// the same of rows held in 8 bits
+int check_bytes(ds_ctx* ctx, const char* name, const void* p, int64_t stride, int64_t rows, int64_t cols, bool out) {
+  if (rows == 0) return DS_OK;
+  if (!p) return ds_fail(ctx, DS_EINVAL, "%s is null", name);
+  if (stride < 0 || (out && rows > 1 && stride < cols))
+    return ds_fail(ctx, DS_EINVAL, "%s: rows of %lld bytes cannot lie %lld apart", name, (long long)cols, (long long)stride);
+  if (stride > (1ll << 40)) return ds_fail(ctx, DS_EINVAL, "%s: rows lie too far apart", name);
+  return DS_OK;
+}
+
+int check_embed(ds_ctx* ctx, int dtype, int table_dtype, int64_t rows, int64_t cols, int64_t vocab, const int32_t* ids, float scale) {
+  DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, cols, kMostCols));
+  if (table_dtype != dtype && table_dtype != DS_ELEM_F32)
+    return ds_fail(ctx, DS_EINVAL, "the table is of element type %d: it has to be of the rows' type %d, or fp32", table_dtype, dtype);
+  if (vocab < 1 || vocab > kMostOrdered) return ds_fail(ctx, DS_EINVAL, "a table of %lld rows: out of range [1, %lld]", (long long)vocab, (long long)kMostOrdered);
+  if (rows > 0 && !ids) return ds_fail(ctx, DS_EINVAL, "ids is null");
+  if (!isfinite(scale)) return ds_fail(ctx, DS_EINVAL, "scale must be a finite number");
+  return DS_OK;
+}
+
+int check_route(ds_ctx* ctx, int dtype, int64_t rows, int64_t experts, int64_t k) {
+  DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, experts, kMostGroups));
+  if (k < 1 || k > kMostChosen || k > experts)
+    return ds_fail(ctx, DS_EINVAL, "%lld experts to a row out of range [1, %lld]", (long long)k, (long long)(experts < kMostChosen ? experts : kMostChosen));
   return DS_OK;
 }
 
@@ -158,6 +185,118 @@ int ds_grouped_mm_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inn
   DS_HIP(ctx, hipSetDevice(ctx->device));
   return ds_launch_grouped_mm_backward(ctx, dtype, p, {dy, dy_stride}, {x, x_stride}, {gate, gate_stride}, {dx, dx_stride}, dw, db,
                                        workspace);
+}
+
+int ds_embed(ds_ctx* ctx, int32_t dtype, int32_t table_dtype, int64_t rows, int64_t cols, int64_t vocab, const void* table, int64_t table_stride,
+             const int32_t* ids, float scale, void* y, int64_t y_stride) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_embed(ctx, dtype, table_dtype, rows, cols, vocab, ids, scale));
+  DS_TRY(check_rows(ctx, "table", table, table_stride, vocab, cols, table_dtype, false));
+  DS_TRY(check_rows(ctx, "y", y, y_stride, rows, cols, dtype, true));
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_embed(ctx, dtype, table_dtype, rows, (int)cols, (int)vocab, {table, table_stride}, ids, scale, {y, y_stride});
+}
+
+int ds_embed_backward_workspace(int64_t rows, int64_t cols, int64_t vocab, int64_t* bytes) {
+  if (!bytes || rows < 0 || rows > kMostOrdered || cols < 1 || cols > kMostCols || vocab < 1 || vocab > kMostOrdered) return DS_EINVAL;
+  *bytes = ds_embed_backward_bytes((int)rows, (int)cols, (int)vocab);
+  return DS_OK;
+}
+
+int ds_embed_backward(ds_ctx* ctx, int32_t dtype, int32_t table_dtype, int64_t rows, int64_t cols, int64_t vocab, const void* dy, int64_t dy_stride,
+                      const int32_t* ids, float scale, void* dtable, int64_t dtable_stride, void* workspace, int64_t workspace_bytes) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_embed(ctx, dtype, table_dtype, rows, cols, vocab, ids, scale));
+  DS_TRY(check_rows(ctx, "dy", dy, dy_stride, rows, cols, dtype, false));
+  DS_TRY(check_rows(ctx, "dtable", dtable, dtable_stride, vocab, cols, table_dtype, true));
+  DS_TRY(check_workspace(ctx, workspace, workspace_bytes, ds_embed_backward_bytes((int)rows, (int)cols, (int)vocab)));
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_embed_backward(ctx, dtype, table_dtype, (int)rows, (int)cols, (int)vocab, {dy, dy_stride}, ids, scale, {dtable, dtable_stride}, workspace);
+}
+
+int ds_route_workspace(int64_t rows, int64_t experts, int64_t* bytes) {
+  if (!bytes || rows < 0 || rows > kMostOrdered || experts < 1 || experts > kMostGroups) return DS_EINVAL;
+  *bytes = ds_route_bytes(rows, (int)experts);
+  return DS_OK;
+}
+
+int ds_route(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t experts, int64_t k, int32_t renorm, const void* x, int64_t x_stride, int32_t* ids,
+             float* weights, int64_t* counts, float* loss, float* lse, void* workspace, int64_t workspace_bytes) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_route(ctx, dtype, rows, experts, k));
+  DS_TRY(check_rows(ctx, "x", x, x_stride, rows, experts, dtype, false));
+  if (rows > 0 && (!ids || !weights)) return ds_fail(ctx, DS_EINVAL, "%s is null", ids ? "weights" : "ids");
+  if (!counts || !loss) return ds_fail(ctx, DS_EINVAL, "%s is null", counts ? "loss" : "counts");
+  DS_TRY(check_workspace(ctx, workspace, workspace_bytes, ds_route_bytes(rows, (int)experts)));
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_route(ctx, dtype, rows, (int)experts, (int)k, renorm, {x, x_stride}, ids, weights, counts, loss, lse, workspace);
+}
+
+int ds_route_backward(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t experts, int64_t k, int32_t renorm, const void* x, int64_t x_stride, const float* lse,
+                      const int32_t* ids, const int64_t* counts, const float* dweights, const float* dloss, void* dx, int64_t dx_stride) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_route(ctx, dtype, rows, experts, k));
+  DS_TRY(check_rows(ctx, "x", x, x_stride, rows, experts, dtype, false));
+  DS_TRY(check_rows(ctx, "dx", dx, dx_stride, rows, experts, dtype, true));
+  if (rows > 0 && !dweights && !dloss) return ds_fail(ctx, DS_EINVAL, "dweights or dloss is needed");
+  if (rows > 0 && !lse) return ds_fail(ctx, DS_EINVAL, "lse of the forward pass is needed");
+  if (rows > 0 && dweights && !ids) return ds_fail(ctx, DS_EINVAL, "ids of the forward pass are needed for the weights' gradient");
+  if (dloss && !counts) return ds_fail(ctx, DS_EINVAL, "counts of the forward pass are needed for the loss' gradient");
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_route_backward(ctx, dtype, rows, (int)experts, (int)k, renorm, {x, x_stride}, lse, ids, counts, dweights, dloss, {dx, dx_stride});
+}
+
+int ds_pack_rows(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, uint8_t* codes, int64_t codes_stride,
+                 uint8_t* scales, int64_t scales_stride) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_shape(ctx, dtype, rows, kMostRows, cols, kMostCols));
+  DS_TRY(check_rows(ctx, "x", x, x_stride, rows, cols, dtype, false));
+  DS_TRY(check_bytes(ctx, "codes", codes, codes_stride, rows, cols, true));
+  DS_TRY(check_bytes(ctx, "scales", scales, scales_stride, rows, (cols + 31) / 32, true));
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_pack(ctx, dtype, rows, (int)cols, {x, x_stride}, {codes, codes_stride, scales, scales_stride});
+}
+
+int ds_unpack_rows(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes, int64_t codes_stride, const uint8_t* scales,
+                   int64_t scales_stride, void* y, int64_t y_stride) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_shape(ctx, dtype, rows, kMostRows, cols, kMostCols));
+  DS_TRY(check_bytes(ctx, "codes", codes, codes_stride, rows, cols, false));
+  DS_TRY(check_bytes(ctx, "scales", scales, scales_stride, rows, (cols + 31) / 32, false));
+  DS_TRY(check_rows(ctx, "y", y, y_stride, rows, cols, dtype, true));
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_unpack(ctx, dtype, rows, (int)cols, {codes, codes_stride, scales, scales_stride}, {y, y_stride});
+}
+
+int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, int32_t gate, int64_t* bytes) {
+  if (!bytes || !known(dtype) || rows < 0 || rows > kMostOrdered || inner < 1 || inner > kMostCols || outer < 1 || outer > kMostCols ||
+      groups < 1 || groups > kMostGroups)
+    return DS_EINVAL;
+  *bytes = ds_grouped_mm_backward_packed_bytes(dtype, {(int)rows, (int)inner, (int)outer, (int)groups, nullptr, nullptr, nullptr}, gate != 0);
+  return DS_OK;
+}
+
+int ds_grouped_mm_backward_packed(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, const void* dy, int64_t dy_stride,
+                                  const uint8_t* codes, int64_t codes_stride, const uint8_t* scales, int64_t scales_stride, const void* w,
+                                  const int64_t* offsets, const int32_t* order, const uint8_t* gate, int64_t gate_stride, void* dx, int64_t dx_stride,
+                                  void* dw, float* db, void* workspace, int64_t workspace_bytes) {
+  if (!ctx) return DS_EINVAL;
+  DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, inner, kMostCols));
+  DS_TRY(check_shape(ctx, dtype, rows, kMostOrdered, outer, kMostCols));
+  DS_TRY(check_groups(ctx, groups, offsets));
+  DS_TRY(check_rows(ctx, "dy", dy, dy_stride, rows, outer, dtype, false));
+  DS_TRY(check_bytes(ctx, "codes", codes, codes_stride, rows, inner, false));
+  DS_TRY(check_bytes(ctx, "scales", scales, scales_stride, rows, (inner + 31) / 32, false));
+  DS_TRY(check_rows(ctx, "w", w, outer, groups, outer, dtype, false));
+  if (gate) DS_TRY(check_bytes(ctx, "gate", gate, gate_stride, rows, inner, false));
+  DS_TRY(check_rows(ctx, "dx", dx, dx_stride, rows, inner, dtype, true));
+  DS_TRY(check_rows(ctx, "dw", dw, outer, groups, outer, dtype, true));
+  if (!db) return ds_fail(ctx, DS_EINVAL, "db is null");
+  const ds_grouped p = {(int)rows, (int)inner, (int)outer, (int)groups, w, offsets, order};
+  DS_TRY(check_workspace(ctx, workspace, workspace_bytes, ds_grouped_mm_backward_packed_bytes(dtype, p, gate != nullptr)));
+  DS_HIP(ctx, hipSetDevice(ctx->device));
+  return ds_launch_grouped_mm_backward_packed(ctx, dtype, p, {dy, dy_stride}, {codes, codes_stride, scales, scales_stride}, gate, gate_stride, {dx, dx_stride}, dw,
+                                              db, workspace);
 }
 
 }  // extern "C"

@@ -464,3 +464,18 @@ int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, d
   if (dtype == DS_ELEM_BF16) return backward<__bf16>(ctx, p, a, workspace);
   return backward<_Float16>(ctx, p, a, workspace);
 }
+
+// Packed rows are unpacked in front of the products
+int64_t ds_grouped_mm_backward_packed_bytes(int dtype, const ds_grouped& p, bool gate) {
+  const int64_t rows = ((int64_t)p.rows * p.inner * (dtype == DS_ELEM_F32 ? 4 : 2) + 15) / 16 * 16;
+  return (gate ? 2 : 1) * rows + ds_grouped_mm_backward_bytes(dtype, p);
+}
+
+int ds_launch_grouped_mm_backward_packed(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, const ds_packed& x, const uint8_t* gate, int64_t gate_stride,
+                                         ds_rows dx, void* dw, float* db, void* workspace) {
+  const int64_t rows = ((int64_t)p.rows * p.inner * (dtype == DS_ELEM_F32 ? 4 : 2) + 15) / 16 * 16;
+  const ds_rows whole = {workspace, p.inner}, open = {(char*)workspace + rows, p.inner};
+  DS_TRY(ds_launch_unpack(ctx, dtype, p.rows, p.inner, x, whole));
+  if (gate) DS_TRY(ds_launch_unpack(ctx, dtype, p.rows, p.inner, {gate, gate_stride, nullptr, 0}, open));
+  return ds_launch_grouped_mm_backward(ctx, dtype, p, dy, whole, gate ? open : ds_rows{nullptr, 0}, dx, dw, db, (char*)workspace + (gate ? 2 : 1) * rows);
+}

@@ -1,0 +1,186 @@
+// Rows into 8 bits and back: e4m3 codes with a power of two for every 32 columns (packed.h).
+//
+// The power is the smallest that leaves the block's finite values at or below 448, so a value is off by at most 2^-4 of itself, or by 2^-10 of that power where it
+// is smaller than 2^-6 of it. Two things are kept exactly: which values are 0, since a ReLU's gate is read from the codes (what would round to 0
+// becomes the smallest code of its sign), and what is finite: no value comes back larger than its type holds, infinities and NaN come back as NaN.
+#include <type_traits>
+
+#include "feature_ops.h"
+#include "packed.h"
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 256, kCols = 8;   // columns of a thread: four threads to a block
+
+struct PackArgs {
+  int64_t rows;
+  int cols, calls, blocks;      // pieces of eight columns to a row, the last block's four filled up; blocks of a row
+  int64_t rows_step;            // how far a thread's next piece is
+  int calls_step;
+  const void* x;                // pack: in; unpack: out
+  uint8_t *codes, *scales;
+  int64_t xs, cs, ss;
+};
+
+__device__ __forceinline__ uint32_t max_of_four(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
+}
+
+typedef uint32_t Eight __attribute__((ext_vector_type(2)));
+typedef uint32_t EightU __attribute__((ext_vector_type(2), aligned(1)));
+
+template <typename T, bool TINY>
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
+  constexpr uint32_t kMostExponent = std::is_same<T, _Float16>::value ? 142 : 254;
+  const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int64_t row = first / a.calls;
+  int call = (int)(first % a.calls);
+  while (row < a.rows) {   // (the four threads of a block go on together)
+    const int col = call * kCols, have = a.cols - col;
+    float x[kCols] = {};
+    if (have > 0) {
+      auto v = load_elements<T, kCols, TINY>((const T*)a.x + row * a.xs, col, a.cols);
+      settle_elements<T, kCols, TINY>(v, col, a.cols);
+#pragma unroll
+      for (int i = 0; i < kCols; ++i) x[i] = i < have ? (float)v[i] : 0.f;
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) {
+      const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
+      most = max(most, bits < 0x7f800000u ? bits : 0);
+    }
+    most = max_of_four(most);
+    const uint32_t exponent = most >> 23;
+    const bool wide = (most & 0x7fffffu) > 0x600000u;   // above 448 of the power below
+    const uint32_t scale = most == 0 ? 127 : max((int)exponent - 8 + (int)wide, 1);
+    const float top = wide && exponent == kMostExponent ? 240.f : 448.f, inv = __uint_as_float((254 - scale) << 23);
+    uint32_t word[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kCols; i += 2) {
+      float q[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float v = x[i + j], s = v * inv;
+        q[j] = fabsf(s) < 0x1p-9f && v != 0.f ? copysignf(0x1p-9f, v) : fminf(fmaxf(s, -top), top);
+        if (!(fabsf(v) < INFINITY)) q[j] = NAN;
+      }
+      word[i / 4] = i % 4 ? __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], word[i / 4], true) : __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], word[i / 4], false);
+    }
+    uint8_t* to = a.codes + row * a.cs + col;
+    if (have >= kCols) {
+      *reinterpret_cast<EightU*>(to) = Eight{word[0], word[1]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCols - 1; ++i)
+        if (i < have) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
+    }
+    if (call % 4 == 0) a.scales[row * a.ss + call / 4] = (uint8_t)scale;
+    row += a.rows_step;
+    call += a.calls_step;
+    if (call >= a.calls) {
+      call -= a.calls;
+      ++row;
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void unpack_kernel(PackArgs a) {
+  constexpr int N = Piece<T>::N;
+  const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int64_t row = first / a.calls;
+  int call = (int)(first % a.calls);
+  while (row < a.rows) {
+    const int col = call * kCols, have = a.cols - col;
+    const uint8_t* from = a.codes + row * a.cs + col;
+    uint32_t word[2] = {0, 0};
+    if (have >= kCols) {
+      const Eight v = *reinterpret_cast<const EightU*>(from);
+      word[0] = v[0];
+      word[1] = v[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCols - 1; ++i)
+        if (i < have) word[i / 4] |= (uint32_t)from[i] << (8 * (i % 4));
+    }
+    const float power = a.scales ? power_of_scale(a.scales[row * a.ss + col / kPackBlock]) : 1.f;
+    float x[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; i += 2) {
+      const auto two = i % 4 ? __builtin_amdgcn_cvt_pk_f32_fp8(word[i / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8(word[i / 4], false);
+      x[i] = two[0] * power;
+      x[i + 1] = two[1] * power;
+    }
+#pragma unroll
+    for (int p = 0; p < kCols / N; ++p) {
+      PieceV<T> out;
+#pragma unroll
+      for (int i = 0; i < N; ++i) out[i] = (T)x[p * N + i];
+      store_piece<T>((T*)a.x + row * a.xs + col + p * N, out, have - p * N);
+    }
+    row += a.rows_step;
+    call += a.calls_step;
+    if (call >= a.calls) {
+      call -= a.calls;
+      ++row;
+    }
+  }
+}
+
+unsigned spread(ds_ctx* ctx, PackArgs& a, int calls) {
+  a.calls = calls;
+  const int64_t pieces = a.rows * a.calls, want = (pieces + kThreads - 1) / kThreads, most = 8 * (int64_t)ctx->num_cus;
+  const int64_t blocks = want < most ? want : most, step = blocks * kThreads;
+  a.rows_step = step / a.calls;
+  a.calls_step = (int)(step % a.calls);
+  return (unsigned)blocks;
+}
+
+template <typename T>
+void launch_pack(const PackArgs& a, unsigned blocks, hipStream_t stream) {
+  if (a.cols < kCols) hipLaunchKernelGGL(HIP_KERNEL_NAME(pack_kernel<T, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(pack_kernel<T, false>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+
+}  // namespace
+
+int ds_launch_pack(ds_ctx* ctx, int dtype, int64_t rows, int cols, ds_rows x, const ds_packed& to) {
+  if (rows == 0) return DS_OK;
+  PackArgs a = {};
+  a.rows = rows;
+  a.cols = cols;
+  a.x = x.data;
+  a.xs = x.stride;
+  a.codes = (uint8_t*)to.codes;
+  a.cs = to.codes_stride;
+  a.scales = (uint8_t*)to.scales;
+  a.ss = to.scales_stride;
+  const unsigned blocks = spread(ctx, a, (cols + kPackBlock - 1) / kPackBlock * (kPackBlock / kCols));
+  if (dtype == DS_ELEM_F32) launch_pack<float>(a, blocks, ctx->stream);
+  else if (dtype == DS_ELEM_BF16) launch_pack<__bf16>(a, blocks, ctx->stream);
+  else launch_pack<_Float16>(a, blocks, ctx->stream);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+int ds_launch_unpack(ds_ctx* ctx, int dtype, int64_t rows, int cols, const ds_packed& from, ds_rows y) {
+  if (rows == 0) return DS_OK;
+  PackArgs a = {};
+  a.rows = rows;
+  a.cols = cols;
+  a.x = y.data;
+  a.xs = y.stride;
+  a.codes = (uint8_t*)from.codes;
+  a.cs = from.codes_stride;
+  a.scales = (uint8_t*)from.scales;
+  a.ss = from.scales_stride;
+  const unsigned blocks = spread(ctx, a, (cols + kCols - 1) / kCols);
+  if (dtype == DS_ELEM_F32) hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<float>), dim3(blocks), dim3(kThreads), 0, ctx->stream, a);
+  else if (dtype == DS_ELEM_BF16) hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<__bf16>), dim3(blocks), dim3(kThreads), 0, ctx->stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<_Float16>), dim3(blocks), dim3(kThreads), 0, ctx->stream, a);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}

@@ -101,6 +101,40 @@ __device__ __forceinline__ void store_piece(T* p, PieceV<T> v, int have) {
   else if (have > 0) store_first<T>(p, v, have);
 }
 
+// N neighbouring elements of a row
+template <typename T, int N>
+struct Elements {
+  typedef T V __attribute__((ext_vector_type(N)));
+  typedef T U __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// Those from `col` (< cols) on; of rows of N or more, where fewer are left, the row's last N, which settle moves to their place (TINY: rows of fewer, one by one)
+template <typename T, int N, bool TINY>
+__device__ __forceinline__ typename Elements<T, N>::V load_elements(const T* row, int col, int cols) {
+  if constexpr (TINY) {
+    typename Elements<T, N>::V v = {};
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i)
+      if (col + i < cols) v[i] = row[col + i];
+    return v;
+  } else {
+    return *reinterpret_cast<const typename Elements<T, N>::U*>(row + min(col, cols - N));
+  }
+}
+template <typename T, int N, bool TINY>
+__device__ __forceinline__ void settle_elements(typename Elements<T, N>::V& v, int col, int cols) {
+  if constexpr (!TINY) {
+    const int by = col + N - cols;
+    if (by <= 0) return;
+#pragma unroll
+    for (int s = 1; s < N; ++s)
+      if (by >= s) {
+#pragma unroll
+        for (int i = 0; i + 1 < N; ++i) v[i] = v[i + 1];
+      }
+  }
+}
+
 template <int CTRL>
 __device__ __forceinline__ float add_across(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));

@@ -1,0 +1,278 @@
+"""Rows in 8 bits on the GPU: bit by bit against the definition on the CPU, and the gradients of the products by group that read them.
+
+Codes and scales are whole numbers and equal (any NaN code stands for a NaN). Gradients: the operands are what the codes stand for, so the tolerances are
+those of the same products of 16-bit or fp32 rows: n terms within 2 n 2^-24 of the sum of their magnitudes, one rounding of the result."""
+import numpy as np
+import pytest
+
+from tests.gpu_common import say
+from tests.test_gpu_features import BF16, F16, F32, TYPES, U, close, generator, grouping, mm_exact, normal, strided
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2506_22668_amd import Context
+    c = Context("cuda:0")
+    yield c
+    c.close()
+
+
+def code_values():
+    """What the 256 codes stand for, from the format's definition."""
+    out = np.empty(256)
+    for c in range(256):
+        e, m = c >> 3 & 15, c & 7
+        v = m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10)
+        out[c] = np.nan if c & 127 == 127 else -v if c & 128 else v
+    return out
+
+
+def defined(x):
+    """(codes, scales) of rows, in 64 bits on the CPU, each code the nearest of all."""
+    t, x = x.dtype, x.double().cpu().numpy()
+    rows, cols = x.shape
+    grid = code_values()
+    level = grid[:127]                       # 0 .. 448, ascending
+    most = float(torch.finfo(t).max)
+    codes, scales = np.zeros((rows, cols), np.uint8), np.zeros((rows, -(-cols // 32)), np.uint8)
+    for r in range(rows):
+        for b in range(scales.shape[1]):
+            v = x[r, 32 * b:32 * b + 32]
+            fine = np.isfinite(v)
+            top = np.abs(v[fine]).max(initial=0.0)
+            s = 127
+            if top > 0:
+                s = 1
+                while top > 448 * 2.0 ** (s - 127):
+                    s += 1
+            unit = 2.0 ** (s - 127)
+            q = np.abs(np.where(fine, v, 0.0)) / unit
+            hi = np.searchsorted(level, q, side="left").clip(0, 126)       # the first level that is not below
+            lo = np.maximum(hi - 1, 0)
+            up = level[hi] - q < q - level[lo]
+            tie = level[hi] - q == q - level[lo]
+            c = np.where(q == level[hi], hi, np.where(up | (tie & (hi % 2 == 0)), hi, lo))
+            c = np.where((c == 0) & (q > 0), 1, c)
+            while (level[c] * unit > most).any():
+                c = np.where(level[c] * unit > most, c - 1, c)
+            c = np.where(np.signbit(v) & fine, c | 128, c)
+            codes[r, 32 * b:32 * b + 32] = np.where(fine, c, 127)
+            scales[r, b] = s
+    return codes, scales
+
+
+def values(codes, scales):
+    return code_values()[codes] * np.repeat(2.0 ** (scales.astype(np.float64) - 127), 32, 1)[:, :codes.shape[1]]
+
+
+def same(got, want):
+    codes, scales = got.codes.view(torch.uint8).cpu().numpy(), got.scales.cpu().numpy()
+    nan = want[0] & 127 == 127
+    assert np.array_equal(scales, want[1])
+    assert np.array_equal(codes[~nan], want[0][~nan]) and (codes[nan] & 127 == 127).all()
+
+
+WIDTHS = [1, 2, 3, 7, 8, 9, 15, 16, 31, 32, 33, 40, 63, 64, 65, 100, 129, 257]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_pack_equals_its_definition(ctx, t, cols):
+    say(f"pack {t} cols={cols}")
+    g = generator(cols)
+    for rows, pad, shift, relu in [(1, 0, 0, False), (37, 3, 1, True), (50, 0, 0, False)]:
+        x = normal(g, rows, cols) * torch.exp2(torch.randint(-9, 9, (rows, cols), generator=g, device="cuda"))
+        x = strided((x.clamp(min=0) if relu else x).to(t), pad, shift)
+        p = ctx.pack_rows(x)
+        want = defined(x)
+        same(p, want)
+        exact = torch.from_numpy(values(*want)).cuda()
+        for to in TYPES:   # (one rounding; back to the rows' own type none)
+            assert torch.equal(ctx.unpack_rows(p, to), exact.to(to) if to == F32 else exact.float().to(to))
+        assert torch.equal(ctx.unpack_rows(p, t).double(), exact)
+        assert torch.equal(ctx.unpack_rows(p, t) > 0, x > 0) and torch.equal(ctx.unpack_rows(p, t) == 0, x == 0)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_pack_at_the_ends_of_the_types(ctx, t):
+    """Largest and smallest values, borders between two codes and between two scales, zeros of both signs, infinities and NaN."""
+    say(f"pack ends {t}")
+    f = torch.finfo(t)
+    least = f.smallest_normal * f.eps
+    rows = [[f.max, -f.max, 1.0, 0.0], [f.max / 2, f.max / 4, 3.0, least], [least, -least, 0.0, 2 * least], [0.0, -0.0, 0.0, 0.0],
+            [float("inf"), 1.0, -2.0, 3.0], [float("nan"), float("-inf"), 0.0, 0.0], [f.smallest_normal, least, -f.smallest_normal, 5 * least],
+            [448.0, 1.0, 2.0 ** -10, 2.0 ** -12], [449.0, 464.0, 1.0, -1.0], [1.75, 1.76, -1.8, 2.0 ** -14], [1.0625, 1.1875, -1.0625, 448.0],
+            [17.0, 18.0, 19.0, 448.0], [2.0 ** -9 * 1.5, 2.0 ** -9 * 2.5, 2.0 ** -10, 448.0], [f.max, 2.0 ** -9, 1e-3, -1e-4]]
+    for cols in (4, 33, 71):
+        x = torch.zeros(len(rows), cols, dtype=t, device="cuda")
+        x[:, :4] = torch.tensor(rows, dtype=torch.float64).to(t).cuda()
+        x[:, cols - 1] += torch.tensor([r[2] for r in rows], dtype=torch.float64).to(t).cuda()
+        p = ctx.pack_rows(x)
+        same(p, defined(x))
+        y = ctx.unpack_rows(p, t)
+        assert torch.equal(torch.isfinite(y), torch.isfinite(x)) and torch.equal(y == 0, x == 0)
+
+
+def test_every_code_and_scale_comes_back(ctx):
+    say("unpack every code and scale")
+    from paper_2506_22668_amd import Packed
+    codes = torch.arange(256, device="cuda").to(torch.uint8).repeat(255, 1)
+    scales = torch.arange(255, device="cuda").to(torch.uint8)[:, None].repeat(1, 8)
+    y = ctx.unpack_rows(Packed(codes.view(torch.float8_e4m3fn), scales))
+    want = torch.from_numpy(values(codes.cpu().numpy(), scales.cpu().numpy())).float()
+    y = y.cpu()
+    assert torch.equal(torch.isnan(y), torch.isnan(want)) and torch.equal(y[~torch.isnan(y)], want[~torch.isnan(want)])
+
+
+@pytest.mark.parametrize("t, element", [(F32, 0), (BF16, 1), (F16, 2)])
+def test_pack_beyond_the_ordinary(ctx, t, element):
+    say(f"pack no rows, many, transposed, strided outputs {t}")
+    g = generator(3)
+    p = ctx.pack_rows(torch.empty(0, 40, dtype=t, device="cuda"))
+    assert p.codes.shape == (0, 40) and p.scales.shape == (0, 2) and ctx.unpack_rows(p, t).shape == (0, 40)
+    x = normal(g, 60, 70, t=t)
+    p = ctx.pack_rows(x)
+    same(ctx.pack_rows(x.t().contiguous().t()), defined(x))
+    same(ctx.pack_rows(x[:1].expand(60, 70)), defined(x[:1].repeat(60, 1)))
+    apart = type(p)(p.codes.t().contiguous().t(), p.scales.t().contiguous().t())
+    assert torch.equal(ctx.unpack_rows(apart, t), ctx.unpack_rows(p, t))
+    codes, scales = torch.full((60, 77), 5, dtype=torch.uint8, device="cuda"), torch.full((60, 5), 6, dtype=torch.uint8, device="cuda")
+    y = torch.full((60, 75), 3.0, dtype=t, device="cuda")
+    assert ctx.lib.ds_pack_rows(ctx.h, element, 60, 70, x.data_ptr(), 70, codes.data_ptr(), 77, scales.data_ptr(), 5) == 0
+    assert ctx.lib.ds_unpack_rows(ctx.h, element, 60, 70, codes.data_ptr(), 77, scales.data_ptr(), 5, y.data_ptr(), 75) == 0
+    assert torch.equal(codes[:, :70], p.codes.view(torch.uint8)) and (codes[:, 70:] == 5).all()
+    assert torch.equal(scales[:, :3], p.scales) and (scales[:, 3:] == 6).all()
+    assert torch.equal(y[:, :70], ctx.unpack_rows(p, t)) and (y[:, 70:] == 3).all()
+    x = normal(g, 70_001, 48, t=t)
+    many = ctx.pack_rows(x)
+    few = ctx.pack_rows(x[-500:].clone())
+    assert torch.equal(many.codes[-500:].view(torch.uint8), few.codes.view(torch.uint8)) and torch.equal(many.scales[-500:], few.scales)
+    assert (ctx.unpack_rows(many).sub(x.float()).abs() <= torch.maximum(x.float().abs() / 16, x.float().abs().amax(1, keepdim=True) * 2.0 ** -16)).all()   # (the smallest code stands for 2^-9 / 224 of a block's largest value at the most)
+
+
+def test_pack_behind_the_first_two_to_the_31_elements(ctx):
+    say("pack far rows")
+    rows, cols = 540_001, 4096
+    x = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    x[-5:] = normal(generator(9), 5, cols, t=BF16)
+    p, tail = ctx.pack_rows(x), ctx.pack_rows(x[-5:].clone())
+    assert torch.equal(p.codes[-5:].view(torch.uint8), tail.codes.view(torch.uint8)) and torch.equal(p.scales[-5:], tail.scales)
+    assert torch.equal(ctx.unpack_rows(p, BF16)[-5:], ctx.unpack_rows(tail, BF16))
+
+
+# ---- gradients from packed rows -------------------------------------------------------------------------------------------------------
+
+def both(ctx, t, rows, inner, outer, groups):
+    rng, g = np.random.default_rng(rows + 1), generator(outer)
+    for order, pad, shift, gated in [(True, 0, 0, True), (False, 3, 1, False), (False, 8, 0, True)]:
+        offsets, perm, key = grouping(ctx, rng, rows, groups, order)
+        x, dy = normal(g, rows, inner, t=t), strided(normal(g, rows, outer, t=t), pad, shift)
+        p = ctx.pack_rows(x.clamp(min=0) if gated else x)
+        if pad:   # rows of codes and scales that lie apart, at odd places
+            wide = torch.full((rows, inner + pad), 0x7f, dtype=torch.uint8, device="cuda")
+            wide[:, shift:shift + inner] = p.codes.view(torch.uint8)
+            over = torch.full((rows, p.scales.shape[1] + pad), 250, dtype=torch.uint8, device="cuda")
+            over[:, shift:shift + p.scales.shape[1]] = p.scales
+            p = type(p)(wide.view(torch.float8_e4m3fn)[:, shift:shift + inner], over[:, shift:shift + p.scales.shape[1]])
+        x = ctx.unpack_rows(p, t)
+        w = normal(g, groups, inner, outer, t=t, scale=inner ** -0.5)
+        dx, dw, db = ctx.grouped_mm_backward(dy, p, w, offsets, order=perm, gate=p if gated else None)
+        e, size = mm_exact(dy, w.transpose(1, 2), key, None, False)
+        if gated:
+            e, size = e.masked_fill(x <= 0, 0.0), size.masked_fill(x <= 0, 0.0)
+        close(dx, e, 2 * (outer + 2) * U * size)
+        assert not dx[key == groups].any()
+        for k in range(groups):
+            at = key == k
+            xk, dk = x[at].double(), dy[at].double()
+            n = int(at.sum())
+            close(dw[k], xk.t() @ dk, 2 * n * U * (xk.abs().t() @ dk.abs()))
+            close(db[k], dk.sum(0), 2 * n * U * dk.abs().sum(0))
+        again = ctx.grouped_mm_backward(dy, p, w, offsets, order=perm, gate=p if gated else None)
+        assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), again))
+
+
+SHAPES = [(1, 1, 1, 1), (1, 16, 16, 3), (5, 40, 24, 4), (8, 256, 1000, 8), (33, 129, 65, 2), (64, 64, 128, 1), (70, 17, 300, 64),
+          (200, 100, 36, 3), (300, 513, 130, 2), (1000, 128, 256, 5), (1111, 72, 520, 20), (2049, 264, 136, 3), (3001, 259, 515, 7),
+          (5000, 512, 768, 4), (777, 1032, 40, 1),
+          # many tiles
+          (70001, 16, 129, 2), (66001, 264, 136, 3), (40003, 131, 259, 7), (33000, 72, 520, 20), (20000, 512, 512, 2),
+          # few rows to a group
+          (20, 2100, 136, 2), (50, 2101, 131, 2), (20, 136, 2100, 2), (100, 72, 2056, 2), (1000, 515, 257, 40), (2000, 520, 1024, 40),
+          # narrow
+          (2, 3, 1, 2), (40, 33, 3, 2), (40, 3, 33, 2), (90, 65, 1, 1), (90, 1, 65, 1), (700, 5, 40, 3), (300, 34, 9, 1), (600, 8, 8, 2), (600, 9, 15, 2), (1, 33, 7, 1)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows, inner, outer, groups", SHAPES)
+def test_gradients_from_packed_rows(ctx, t, rows, inner, outer, groups):
+    say(f"packed gradients {t} rows={rows} inner={inner} outer={outer} groups={groups}")
+    both(ctx, t, rows, inner, outer, groups)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows", [40, 3000])
+def test_gradients_from_packed_rows_beyond_the_ordinary(ctx, t, rows):
+    say(f"packed gradients: no rows, one for all, non-finite, bad orders {t} rows={rows}")
+    g = generator(rows)
+    w, offsets = normal(g, 2, 40, 24, t=t), torch.tensor([0, rows // 2, rows], device="cuda")
+    x, dy = normal(g, rows, 40, t=t), normal(g, rows, 24, t=t)
+    p = ctx.pack_rows(x)
+    none = ctx.pack_rows(x[:0])
+    dx, dw, db = ctx.grouped_mm_backward(dy[:0], none, w, torch.zeros(3, dtype=torch.int64, device="cuda"))
+    assert dx.shape == (0, 40) and not dw.any() and not db.any()
+    dx, dw, db = ctx.grouped_mm_backward(dy, p, w, torch.zeros(3, dtype=torch.int64, device="cuda"), gate=p)
+    assert not dx.any() and not dw.any() and not db.any()
+    one = type(p)(p.codes[:1].expand(rows, 40), p.scales[:1].expand(rows, 2))
+    long = type(p)(one.codes.contiguous(), one.scales.contiguous())
+    for a, b in zip(ctx.grouped_mm_backward(dy, one, w, offsets, gate=one), ctx.grouped_mm_backward(dy, long, w, offsets, gate=long)):
+        assert torch.equal(a, b)
+    # a row that is not finite stays in its group; its gate is shut
+    x[0, 5], x[rows - 1, 7] = float("inf"), float("nan")
+    q = ctx.pack_rows(x)
+    dx, dw, db = ctx.grouped_mm_backward(dy, q, w, offsets, gate=q)
+    want = ctx.grouped_mm_backward(dy, p, w, offsets, gate=p)
+    assert dx[0, 5] == 0 and dx[rows - 1, 7] == 0 and torch.isfinite(dx).all() and torch.equal(db, want[2])
+    assert torch.isnan(dw[0, 5]).all() and torch.isnan(dw[1, 7]).all() and torch.isfinite(dw).sum() == dw.numel() - 48
+    # an order that names no row, offsets that hold anything
+    order = torch.arange(rows, device="cuda").int()
+    order[3], order[rows - 1] = -5, rows
+    named = torch.ones(rows, dtype=torch.bool, device="cuda")
+    named[3] = named[rows - 1] = False
+    assert torch.equal(ctx.grouped_mm_backward(dy, p, w, offsets, order=order)[0][named], ctx.grouped_mm_backward(dy, p, w, offsets)[0][named])
+    wild, tame = torch.tensor([-2 ** 62, 2 ** 40, 2 ** 62], device="cuda"), torch.tensor([0, rows, rows], device="cuda")
+    assert torch.equal(ctx.grouped_mm_backward(dy, p, w, wild)[1], ctx.grouped_mm_backward(dy, p, w, tame)[1])
+
+
+def test_a_gate_of_other_rows(ctx):
+    say("packed gate of other rows")
+    g = generator(21)
+    for rows in (30, 4000):
+        x, gate, dy, w = normal(g, rows, 72, t=BF16), normal(g, rows, 72, t=BF16), normal(g, rows, 40, t=BF16), normal(g, 1, 72, 40, t=BF16)
+        offsets = torch.tensor([0, rows], device="cuda")
+        p = ctx.pack_rows(x)
+        shut = ctx.grouped_mm_backward(dy, p, w, offsets, gate=ctx.pack_rows(gate))
+        open_ = ctx.grouped_mm_backward(dy, p, w, offsets)
+        assert torch.equal(shut[0], torch.where(gate > 0, open_[0], 0)) and torch.equal(shut[1], open_[1]) and torch.equal(shut[2], open_[2])
+
+
+def test_gradients_from_packed_rows_behind_two_to_the_31_elements(ctx):
+    say("packed gradients far rows")
+    rows, inner, outer = 540_001, 4096, 24
+    from paper_2506_22668_amd import Packed
+    codes = torch.zeros(rows, inner, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, inner // 32), 127, dtype=torch.uint8, device="cuda")
+    tail = ctx.pack_rows(normal(generator(9), 5, inner, t=BF16))
+    codes[-5:], scales[-5:] = tail.codes.view(torch.uint8), tail.scales
+    dy, w = normal(generator(10), rows, outer, t=BF16), normal(generator(11), 1, inner, outer, t=BF16, scale=0.02)
+    offsets = torch.tensor([0, rows], device="cuda")
+    p = Packed(codes.view(torch.float8_e4m3fn), scales)
+    dx, dw, db = ctx.grouped_mm_backward(dy, p, w, offsets, gate=p)
+    x = ctx.unpack_rows(tail, BF16)
+    e, size = mm_exact(dy[-5:], w.transpose(1, 2), torch.zeros(5, dtype=torch.int64, device="cuda"), None, False)
+    close(dx[-5:], e.masked_fill(x <= 0, 0.0), 2 * (outer + 2) * U * size)
+    assert not dx[:-5].any()
+    close(dw[0], x.double().t() @ dy[-5:].double(), 2 * 5 * U * (x.double().abs().t() @ dy[-5:].double().abs()))
