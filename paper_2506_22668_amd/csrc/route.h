@@ -1,0 +1,489 @@
+// The experts of every row from a router's scores, how evenly they are used, and the scores' gradient.
+//
+//   forward:   p = softmax(x) over a row's experts; ids: those of the k highest scores, ties to the lowest, -inf never; w_j = p at id_j, or its share of
+//              the k; counts_e = how often e was chosen, N = rows with an expert; loss = E sum_e (counts_e / sum of counts) (sum_r p_re / N)
+//   backward:  dx = p (g - sum_e p g), g_e = dloss E counts_e / (N sum of counts) + [e = id_j] dp_j,
+//              dp_j = dw_j, or (dw_j - sum_i dw_i w_i) / sum of the chosen p
+//
+// A row of up to 1,024 scores stays in the registers of TPR threads, PER to a thread. A row that is -inf throughout has no expert: ids -1, weights 0, and it takes no
+// part in N. One with NaN or +inf has none either, but its weights, and so the loss, are NaN. All sums are fp32, over rows first in a thread, then in
+// a workgroup, and the workgroups' in 64 bits in a fixed order: the same inputs give the same bits.
+//
+// Vector instructions, not memory, are what such a kernel runs out of first (a wave's take four cycles: 1,000,175 rows of 64 bf16 in 29 us leave 18 a score), so:
+//  - a score and its expert are one integer, ordered as scores are and, of equal ones, the lowest expert first: a thread's k highest are a list that each
+//    score passes through in one median and one maximum of three a place, and the row's are the threads' heads, highest first. A 16-bit score
+//    leaves 13 bits of 32 free for the expert. Of an fp32 one the last bits give way to it, which orders all scores but those that differ in these bits alone:
+//    a list of k + 1 shows where that is so, and these rows are gone through again, k times, in full.
+//  - e^(x - top) is one exponential of base 2, with the difference formed first (a fused x log2(e) - top log2(e) would be off by what the second term is rounded by, more
+//    than the exponential's range for scores of 2^31). It knows no subnormal results; where they matter, it is the square of the one of half the power.
+#pragma once
+#include <math.h>
+
+#include "feature_ops.h"
+#include "rows.h"
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+struct RouteArgs {
+  int64_t rows;
+  int experts, k;
+  bool renorm;
+  uint32_t low;         // the bits of a key that hold the expert
+  const void* x;
+  int64_t xs;
+  int32_t* ids;
+  float *weights, *loss, *lse;
+  int64_t* counts;
+  // what workgroups leave, where there are several: sums of p [block][experts], counts [block][experts], rows [block]; and of the workgroups that add these up,
+  // their part of the loss and of the counts, and how many are through
+  float* sums;
+  int32_t *chosen, *with, *through;
+  double* losses;
+  int64_t* numbers;
+};
+
+template <int CTRL>
+__device__ __forceinline__ int across(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+}
+// The highest of LANES neighbouring lanes, in each of them
+template <int LANES>
+__device__ __forceinline__ int max_lanes(int v) {
+  if constexpr (LANES >= 2) v = max(v, across<0xB1>(v));
+  if constexpr (LANES >= 4) v = max(v, across<0x4E>(v));
+  if constexpr (LANES >= 8) v = max(v, across<0x141>(v));
+  if constexpr (LANES >= 16) v = max(v, across<0x140>(v));
+  if constexpr (LANES >= 32) v = max(v, __shfl_xor(v, 16, 64));
+  if constexpr (LANES >= 64) v = max(v, __shfl_xor(v, 32, 64));
+  return v;
+}
+
+template <int LANES>
+__device__ __forceinline__ float highest_lane(float v) {
+  if constexpr (LANES >= 2) v = fmaxf(v, __int_as_float(across<0xB1>(__float_as_int(v))));
+  if constexpr (LANES >= 4) v = fmaxf(v, __int_as_float(across<0x4E>(__float_as_int(v))));
+  if constexpr (LANES >= 8) v = fmaxf(v, __int_as_float(across<0x141>(__float_as_int(v))));
+  if constexpr (LANES >= 16) v = fmaxf(v, __int_as_float(across<0x140>(__float_as_int(v))));
+  if constexpr (LANES >= 32) v = fmaxf(v, __shfl_xor(v, 16, 64));
+  if constexpr (LANES >= 64) v = fmaxf(v, __shfl_xor(v, 32, 64));
+  return v;
+}
+
+// e^d; 0 below 2^-126
+__device__ __forceinline__ float power_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// e^d with subnormal results
+__device__ __forceinline__ float whole_power_of(float d) {
+  const float e = __builtin_amdgcn_exp2f(d * (0.5f * kLog2e));
+  return e * e;
+}
+
+// A thread's scores: pieces of 16 bytes, a row's threads side by side; `absent` where the row has ended
+template <typename T, int TPR, int PER>
+struct Scores {
+  static constexpr int N = Piece<T>::N, PIECES = PER / N;
+  PieceV<T> v[PIECES];
+  __device__ __forceinline__ void load(const T* row, int t, int experts) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int at = (p * TPR + t) * N;
+      if (experts < N) v[p] = load_piece<T>(row + at, experts - at);
+      else v[p] = *reinterpret_cast<const typename Piece<T>::U*>(row + min(at, experts - N));
+    }
+  }
+  __device__ __forceinline__ void read(int t, int experts, float absent, float (&to)[PER]) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int at = (p * TPR + t) * N, have = experts - at;
+      if (have >= N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[p * N + i] = (float)v[p][i];
+      } else {
+        if (experts >= N && have > 0) v[p] = shifted<T>(v[p], (unsigned)(N - have));
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[p * N + i] = i < have ? (float)v[p][i] : absent;
+      }
+    }
+  }
+};
+// the expert of a thread's score i
+template <typename T, int TPR>
+__device__ __forceinline__ int expert_of(int t, int i) {
+  constexpr int N = Piece<T>::N;
+  return (i / N * TPR + t) * N + i % N;
+}
+
+// A score's key, less the expert: ordered as whole numbers as the scores are (-0 as 0), `low` bits cleared
+__device__ __forceinline__ uint32_t key_of(float v, uint32_t low) {
+  const uint32_t bits = __float_as_uint(v + 0.f);
+  return (bits ^ ((uint32_t)((int)bits >> 31) & (0x7fffffffu & ~low))) & ~low;
+}
+__device__ __forceinline__ float score_of(int key, uint32_t low) {
+  const uint32_t t = (uint32_t)key & ~low;
+  return __uint_as_float(t ^ ((uint32_t)((int)t >> 31) & (0x7fffffffu & ~low)));
+}
+
+// The highest K of a thread's keys, highest first
+template <int K, int PER>
+__device__ __forceinline__ void highest(const int (&key)[PER], int (&list)[K]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+#pragma unroll
+    for (int j = K - 1; j > 0; --j) list[j] = max(min(list[j - 1], key[i]), list[j]);   // (list[j - 1] >= list[j]: the middle one of three)
+    list[0] = max(list[0], key[i]);
+  }
+}
+
+// Counts of a row's experts are added up in LDS (whole numbers: in any order). 1,000,175 rows of 64 bf16, 2 of them each: see the table of times in front of launch_of.
+template <typename T, int TPR, int PER, int K, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
+  constexpr int ROWS = THREADS / TPR, WAVES = THREADS / 64, WIDE = TPR * PER, LIST = sizeof(T) == 4 ? K + 1 : K;
+  __shared__ float meet[WAVES][WIDE];
+  __shared__ int count[WIDE], with_of[WAVES];
+  const int t = threadIdx.x % TPR;
+  const float none = -INFINITY;
+  const int lowest = (int)(0x80000000u), shut = (int)(key_of(none, a.low) | a.low);   // at or below: -inf, or no score
+  for (int e = threadIdx.x; e < WIDE; e += THREADS) count[e] = 0;
+  __syncthreads();
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  float sum[PER] = {};
+  int with = 0;
+  Scores<T, TPR, PER> next = {};
+  if (row < a.rows) next.load((const T*)a.x + row * a.xs, t, a.experts);
+  for (; row < a.rows; row += step) {
+    Scores<T, TPR, PER> now = next;
+    if (row + step < a.rows) next.load((const T*)a.x + (row + step) * a.xs, t, a.experts);
+    float x[PER];
+    now.read(t, a.experts, none, x);
+    int list[LIST];
+    {
+      int key[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int e = expert_of<T, TPR>(t, i);
+        key[i] = e < a.experts ? (int)(key_of(x[i], a.low) | (a.low - (uint32_t)e)) : lowest;
+      }
+#pragma unroll
+      for (int j = 0; j < LIST; ++j) list[j] = lowest;
+      highest(key, list);
+    }
+    int id[K], high[K];
+    bool again = false;   // fp32: scores that are told apart by their last bits alone
+    int last = lowest;
+#pragma unroll
+    for (int j = 0; j < LIST; ++j) {
+      if (j >= a.k + (LIST - K)) break;
+      const int best = max_lanes<TPR>(list[0]);
+      if constexpr (sizeof(T) == 4) again |= j > 0 && best > shut && ((best ^ last) & ~a.low) == 0;
+      last = best;
+      if (j < K) {
+        high[j < K ? j : 0] = best;
+        id[j < K ? j : 0] = best > shut ? (int)(a.low - ((uint32_t)best & a.low)) : -1;
+      }
+      if (list[0] == best) {
+#pragma unroll
+        for (int i = 0; i + 1 < LIST; ++i) list[i] = list[i + 1];
+        list[LIST - 1] = lowest;
+      }
+    }
+    float top = high[0] > shut ? score_of(high[0], a.low) : 0.f;
+    if constexpr (sizeof(T) == 4) {   // (a key's bits alone may be far from a large score)
+      top = none;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) top = fmaxf(top, x[i]);
+      top = highest_lane<TPR>(top);
+      if (top == none) top = 0.f;
+    }
+    float q[PER], total = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      q[i] = power_of(x[i] - top);
+      total += q[i];
+    }
+    total = sum_lanes<TPR>(total);
+    const bool fine = total > 0.f && total < INFINITY;   // (a NaN is neither; a row without an open expert sums up to 0)
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum[i] = fmaf(q[i], inv, sum[i]);
+    with += fine && t == 0;
+    if (sizeof(T) == 4 && __any(again)) {
+      int taken[K];
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j >= a.k) break;
+        float best = none;
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int e = expert_of<T, TPR>(t, i);
+          bool open = x[i] > best;
+#pragma unroll
+          for (int l = 0; l < j; ++l) open &= taken[l] != e;
+          best = open ? x[i] : best;
+          at = open ? e : at;
+        }
+        const float most = highest_lane<TPR>(best);
+        const int first = -max_lanes<TPR>(best == most ? -at : -0x7fffffff);
+        taken[j] = most > none ? first : -1;
+        if (again) id[j] = taken[j];
+      }
+    }
+    float weight[K], shares = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if (j >= a.k) break;
+      if (!fine) id[j] = -1;
+      float score;
+      if constexpr (sizeof(T) == 4) score = id[j] < 0 ? none : ((const float*)a.x)[row * a.xs + id[j]];
+      else score = score_of(high[j], a.low);
+      weight[j] = id[j] >= 0 ? whole_power_of(score - top) * inv : fine || total == 0.f ? 0.f : NAN;
+      shares += weight[j];
+    }
+    const float by = a.renorm && shares > 0.f ? 1.f / shares : 1.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if (j >= a.k) break;
+      if (t == j % TPR) {
+        a.ids[j * a.rows + row] = id[j];
+        a.weights[j * a.rows + row] = weight[j] * by;
+        if (id[j] >= 0) atomicAdd(&count[id[j]], 1);
+      }
+    }
+    if (t == 0 && a.lse) a.lse[row] = total == 0.f ? none : fmaf(__log2f(total), kLn2, top);
+  }
+  // the workgroup's rows: those of a wave first (lanes TPR apart)
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+#pragma unroll
+    for (int o = TPR; o < 64; o <<= 1) sum[i] += __shfl_xor(sum[i], o, 64);
+    if (lane < TPR) meet[wave][expert_of<T, TPR>(t, i)] = sum[i];
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) with += __shfl_xor(with, o, 64);
+  if (lane == 0) with_of[wave] = with;
+  __syncthreads();
+  const bool alone = gridDim.x == 1;
+  double loss = 0.0;
+  int number = 0;
+  for (int e = threadIdx.x; e < a.experts; e += THREADS) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) s += meet[w][e];
+    if (alone) {
+      a.counts[e] = count[e];
+      loss += (double)s * count[e];
+      number += count[e];
+    } else {
+      a.sums[(int64_t)blockIdx.x * a.experts + e] = s;
+      a.chosen[(int64_t)blockIdx.x * a.experts + e] = count[e];
+    }
+  }
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) all += with_of[w];
+  if (!alone) {
+    if (threadIdx.x == 0) {
+      a.with[blockIdx.x] = all;
+      if (blockIdx.x == 0) *a.through = 0;
+    }
+    return;
+  }
+  __syncthreads();
+  double* part = reinterpret_cast<double*>(&meet[0][0]);
+  static_assert(sizeof(meet) >= 16 * WAVES, "");
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    loss += __shfl_xor(loss, o, 64);
+    number += __shfl_xor(number, o, 64);
+  }
+  if (lane == 0) {
+    part[wave] = loss;
+    part[WAVES + wave] = (double)number;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double sum_loss = 0.0, chosen = 0.0;
+    for (int w = 0; w < WAVES; ++w) {
+      sum_loss += part[w];
+      chosen += part[WAVES + w];
+    }
+    a.counts[a.experts] = all;
+    // (a sum that is NaN stays one, where nothing was chosen too)
+    *a.loss = (float)(sum_loss * a.experts / (fmax(chosen, 1.0) * (double)(all > 0 ? all : 1)));
+  }
+}
+
+struct RouteGradArgs {
+  int64_t rows;
+  int experts, k;
+  bool renorm;
+  const void* x;
+  int64_t xs, ys;
+  const float *lse, *dweights, *dloss;
+  const int32_t* ids;
+  const int64_t* counts;
+  void* dx;
+};
+
+// The scores that were chosen are read once more, each by its address: a row's sum takes their gradients from there, and the threads that hold them add
+// them by comparing experts (two instructions a score and choice, where looking the probabilities up in the registers was as many again).
+template <typename T, int TPR, int PER, int K, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
+  constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N;
+  __shared__ int64_t part[THREADS];
+  const int t = threadIdx.x % TPR;
+  const float none = -INFINITY;
+  // the loss' part of g: the same for all rows
+  float share[PER] = {};
+  double by = 0.0;
+  if (a.dloss) {
+    int64_t n = 0;
+    for (int e = threadIdx.x; e < a.experts; e += THREADS) n += a.counts[e];
+    part[threadIdx.x] = n;
+    __syncthreads();
+    for (int o = THREADS / 2; o > 0; o >>= 1) {
+      if ((int)threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
+      __syncthreads();
+    }
+    const int64_t chosen = part[0], with = a.counts[a.experts];
+    by = (double)*a.dloss * a.experts / ((double)(chosen > 0 ? chosen : 1) * (double)(with > 0 ? with : 1));
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = expert_of<T, TPR>(t, i);
+      share[i] = e < a.experts ? (float)(by * (double)a.counts[e]) : 0.f;
+    }
+  }
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  Scores<T, TPR, PER> next = {};
+  if (row < a.rows) next.load((const T*)a.x + row * a.xs, t, a.experts);
+  for (; row < a.rows; row += step) {
+    Scores<T, TPR, PER> now = next;
+    int id[K];
+    float dp[K], of[K];
+    const T* from = (const T*)a.x + row * a.xs;
+    const float lse = a.lse[row], base = lse == none ? 0.f : lse;
+    if (a.dweights) {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j >= a.k) break;
+        id[j] = a.ids[j * a.rows + row];
+        dp[j] = a.dweights[j * a.rows + row];
+        if ((uint32_t)id[j] >= (uint32_t)a.experts) id[j] = -1;
+      }
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j >= a.k) break;
+        of[j] = (float)from[id[j] < 0 ? 0 : id[j]];
+      }
+    }
+    if (row + step < a.rows) next.load((const T*)a.x + (row + step) * a.xs, t, a.experts);
+    float p[PER], s = 0.f, own = 0.f;
+    now.read(t, a.experts, none, p);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      p[i] = whole_power_of(p[i] - base);   // (a row that is closed throughout: 0)
+      s = fmaf(p[i], share[i], s);
+    }
+    s = sum_lanes<TPR>(s);
+    float g[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) g[i] = share[i];
+    if (a.dweights) {
+      float dot = 0.f, total = 0.f;
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j >= a.k) break;
+        of[j] = id[j] < 0 ? 0.f : whole_power_of(of[j] - base);
+        total += of[j];
+        if (id[j] >= 0) dot = fmaf(dp[j], of[j], dot);
+      }
+      const float inv = a.renorm ? total > 0.f ? 1.f / total : 0.f : 1.f;
+      dot = a.renorm ? dot * inv : 0.f;
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j >= a.k) break;
+        dp[j] = id[j] < 0 ? 0.f : (dp[j] - dot) * inv;
+        own = fmaf(dp[j], of[j], own);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) g[i] = id[j] == expert_of<T, TPR>(t, i) ? share[i] + dp[j] : g[i];
+      }
+    }
+    s += own;
+    T* dx = (T*)a.dx + row * a.ys;
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+      const int at = (q * TPR + t) * N;
+      PieceV<T> out;
+#pragma unroll
+      for (int i = 0; i < N; ++i) out[i] = (T)(p[q * N + i] * (g[q * N + i] - s));
+      store_piece<T>(dx + at, out, a.experts - at);
+    }
+  }
+}
+
+// Scores of a thread and threads of a row: the fewest places that hold it, and of those the fewest threads
+struct Form {
+  int per, threads;
+};
+Form form_of(int experts) {
+  if (experts <= 8) return {8, 1};
+  int t = 1;
+  while (t * 16 < experts) t *= 2;
+  return t >= 2 && t / 2 * 24 >= experts ? Form{24, t / 2} : Form{16, t};
+}
+constexpr int kThreads = 512;
+
+int64_t blocks_for(int64_t rows, int experts, int64_t most) {
+  const int64_t per = kThreads / form_of(experts).threads, blocks = (rows + per - 1) / per;
+  return blocks < most ? blocks : most;
+}
+
+template <typename T, int TPR, int PER, int K>
+void launch(const RouteArgs& a, unsigned blocks, hipStream_t stream) {
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_kernel<T, TPR, PER, K, kThreads>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+template <typename T, int TPR, int PER, int K>
+void launch(const RouteGradArgs& a, unsigned blocks, hipStream_t stream) {
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_grad_kernel<T, TPR, PER, K, kThreads>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+template <typename T, int TPR, int PER, typename Args>
+void launch_k(const Args& a, unsigned blocks, hipStream_t stream) {
+  if (a.k == 1) launch<T, TPR, PER, 1>(a, blocks, stream);
+  else if (a.k == 2) launch<T, TPR, PER, 2>(a, blocks, stream);
+  else if (a.k <= 4) launch<T, TPR, PER, 4>(a, blocks, stream);
+  else launch<T, TPR, PER, 8>(a, blocks, stream);
+}
+template <typename T, typename Args>
+void launch_for(const Args& a, unsigned blocks, hipStream_t stream) {
+  const Form f = form_of(a.experts);
+  if (f.per == 8) return launch_k<T, 1, 8>(a, blocks, stream);
+  if (f.per == 16) switch (f.threads) {
+      case 1: return launch_k<T, 1, 16>(a, blocks, stream);
+      case 2: return launch_k<T, 2, 16>(a, blocks, stream);
+      case 4: return launch_k<T, 4, 16>(a, blocks, stream);
+      case 8: return launch_k<T, 8, 16>(a, blocks, stream);
+      case 16: return launch_k<T, 16, 16>(a, blocks, stream);
+      case 32: return launch_k<T, 32, 16>(a, blocks, stream);
+      default: return launch_k<T, 64, 16>(a, blocks, stream);
+    }
+  switch (f.threads) {
+    case 1: return launch_k<T, 1, 24>(a, blocks, stream);
+    case 2: return launch_k<T, 2, 24>(a, blocks, stream);
+    case 4: return launch_k<T, 4, 24>(a, blocks, stream);
+    case 8: return launch_k<T, 8, 24>(a, blocks, stream);
+    case 16: return launch_k<T, 16, 24>(a, blocks, stream);
+    default: return launch_k<T, 32, 24>(a, blocks, stream);
+  }
+}
+
+}  // namespace
+
+// The launches of a type: route_f32.hip, route_bf16.hip, route_f16.hip
+template <typename T>
+void ds_route_rows(const void* args, unsigned blocks, hipStream_t stream);
+template <typename T>
+void ds_route_rows_backward(const void* args, unsigned blocks, hipStream_t stream);
