@@ -14,10 +14,12 @@
 //    score passes through in one median and one maximum of three a place, and the row's are the threads' heads, highest first. A 16-bit score
 //    leaves 13 bits of 32 free for the expert. Of an fp32 one the last bits give way to it, which orders all scores but those that differ in these bits alone:
 //    a list of k + 1 shows where that is so, and these rows are gone through again, k times, in full.
-//  - e^(x - top) is one exponential of base 2, with the difference formed first (a fused x log2(e) - top log2(e) would be off by what the second term is rounded by, more
-//    than the exponential's range for scores of 2^31). It knows no subnormal results; where they matter, it is the square of the one of half the power.
+//  - e^(x - top) is one exponential of base 2, of x log2(e) - top log2(e) in one fused product where a row's highest score is below 2^16 (beyond, what the second term
+//    is rounded by would count: there the difference is formed first). It knows no subnormal results; where they matter, it is squared from half the power.
 #pragma once
 #include <math.h>
+
+#include <type_traits>
 
 #include "feature_ops.h"
 #include "rows.h"
@@ -36,10 +38,10 @@ struct RouteArgs {
   int32_t* ids;
   float *weights, *loss, *lse;
   int64_t* counts;
-  // what workgroups leave, where there are several: sums of p [block][experts], counts [block][experts], rows [block]; and of the workgroups that add these up,
+  // what workgroups leave, where there are several: sums of p and counts [block][experts], rows [block]; and of the workgroups that add these up,
   // their part of the loss and of the counts, and how many are through
-  float* sums;
-  int32_t *chosen, *with, *through;
+  float2* sums;
+  int32_t *with, *through;
   double* losses;
   int64_t* numbers;
 };
@@ -55,8 +57,14 @@ __device__ __forceinline__ int max_lanes(int v) {
   if constexpr (LANES >= 4) v = max(v, across<0x4E>(v));
   if constexpr (LANES >= 8) v = max(v, across<0x141>(v));
   if constexpr (LANES >= 16) v = max(v, across<0x140>(v));
-  if constexpr (LANES >= 32) v = max(v, __shfl_xor(v, 16, 64));
-  if constexpr (LANES >= 64) v = max(v, __shfl_xor(v, 32, 64));
+  if constexpr (LANES >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = max((int)p[0], (int)p[1]);
+  }
+  if constexpr (LANES >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = max((int)p[0], (int)p[1]);
+  }
   return v;
 }
 
@@ -66,17 +74,29 @@ __device__ __forceinline__ float highest_lane(float v) {
   if constexpr (LANES >= 4) v = fmaxf(v, __int_as_float(across<0x4E>(__float_as_int(v))));
   if constexpr (LANES >= 8) v = fmaxf(v, __int_as_float(across<0x141>(__float_as_int(v))));
   if constexpr (LANES >= 16) v = fmaxf(v, __int_as_float(across<0x140>(__float_as_int(v))));
-  if constexpr (LANES >= 32) v = fmaxf(v, __shfl_xor(v, 16, 64));
-  if constexpr (LANES >= 64) v = fmaxf(v, __shfl_xor(v, 32, 64));
+  if constexpr (LANES >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  if constexpr (LANES >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
   return v;
 }
 
 // e^d; 0 below 2^-126
 __device__ __forceinline__ float power_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
-// e^d with subnormal results
-__device__ __forceinline__ float whole_power_of(float d) {
-  const float e = __builtin_amdgcn_exp2f(d * (0.5f * kLog2e));
+// 2^d with subnormal results
+__device__ __forceinline__ float whole_power(float d) {
+  const float e = __builtin_amdgcn_exp2f(0.5f * d);
   return e * e;
+}
+
+// Element `row` (of up to 2^30, each of four bytes) behind an address that all lanes share
+template <typename V>
+__device__ __forceinline__ V& at_row(V* base, uint32_t row) {
+  return *reinterpret_cast<V*>(reinterpret_cast<char*>(const_cast<typename std::remove_const<V>::type*>(base)) + row * 4u);
 }
 
 // A thread's scores: pieces of 16 bytes, a row's threads side by side; `absent` where the row has ended
@@ -130,7 +150,7 @@ __device__ __forceinline__ void highest(const int (&key)[PER], int (&list)[K]) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
 #pragma unroll
-    for (int j = K - 1; j > 0; --j) list[j] = max(min(list[j - 1], key[i]), list[j]);   // (list[j - 1] >= list[j]: the middle one of three)
+    for (int j = K - 1; j > 0; --j) asm("v_med3_i32 %0, %1, %2, %0" : "+v"(list[j]) : "v"(list[j - 1]), "v"(key[i]));   // (the compiler makes two of it)
     list[0] = max(list[0], key[i]);
   }
 }
@@ -139,22 +159,24 @@ __device__ __forceinline__ void highest(const int (&key)[PER], int (&list)[K]) {
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
   constexpr int ROWS = THREADS / TPR, WAVES = THREADS / 64, WIDE = TPR * PER, LIST = sizeof(T) == 4 ? K + 1 : K;
-  __shared__ float meet[WAVES][WIDE];
+  // the waves' sums, at the end; until then, fp32: the scores of the rows under way, from which those that were chosen are read
+  __shared__ __attribute__((aligned(16))) float room[sizeof(T) == 4 ? THREADS * PER : WAVES * WIDE];
+  float* mine = room + (int)threadIdx.x / TPR * WIDE;
   __shared__ int count[WIDE], with_of[WAVES];
   const int t = threadIdx.x % TPR;
   const float none = -INFINITY;
   const int lowest = (int)(0x80000000u), shut = (int)(key_of(none, a.low) | a.low);   // at or below: -inf, or no score
   for (int e = threadIdx.x; e < WIDE; e += THREADS) count[e] = 0;
   __syncthreads();
-  const int64_t step = (int64_t)gridDim.x * ROWS;
-  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const uint32_t step = gridDim.x * ROWS, rows = (uint32_t)a.rows;   // (at most 2^30)
+  uint32_t row = blockIdx.x * ROWS + threadIdx.x / TPR;
   float sum[PER] = {};
   int with = 0;
   Scores<T, TPR, PER> next = {};
-  if (row < a.rows) next.load((const T*)a.x + row * a.xs, t, a.experts);
-  for (; row < a.rows; row += step) {
+  if (row < rows) next.load((const T*)a.x + row * a.xs, t, a.experts);
+  for (; row < rows; row += step) {
     Scores<T, TPR, PER> now = next;
-    if (row + step < a.rows) next.load((const T*)a.x + (row + step) * a.xs, t, a.experts);
+    if (row + step < rows) next.load((const T*)a.x + (row + step) * a.xs, t, a.experts);
     float x[PER];
     now.read(t, a.experts, none, x);
     int list[LIST];
@@ -162,8 +184,8 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
       int key[PER];
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int e = expert_of<T, TPR>(t, i);
-        key[i] = e < a.experts ? (int)(key_of(x[i], a.low) | (a.low - (uint32_t)e)) : lowest;
+        // (where the row has ended the score is -inf, and which expert its key names does not matter)
+        key[i] = (int)(key_of(x[i], a.low) | ((a.low - (uint32_t)expert_of<T, TPR>(t, i)) & a.low));
       }
 #pragma unroll
       for (int j = 0; j < LIST; ++j) list[j] = lowest;
@@ -191,20 +213,31 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
     float top = high[0] > shut ? score_of(high[0], a.low) : 0.f;
     if constexpr (sizeof(T) == 4) {   // (a key's bits alone may be far from a large score)
       top = none;
+      __builtin_amdgcn_wave_barrier();   // (a row's threads are of one wave, whose LDS accesses keep their order)
+#pragma unroll
+      for (int p = 0; p < PER / 4; ++p) *reinterpret_cast<float4*>(mine + (p * TPR + t) * 4) = float4{x[4 * p], x[4 * p + 1], x[4 * p + 2], x[4 * p + 3]};
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int i = 0; i < PER; ++i) top = fmaxf(top, x[i]);
       top = highest_lane<TPR>(top);
       if (top == none) top = 0.f;
     }
     float q[PER], total = 0.f;
+    // (the second term's rounding is the same for a whole row, so it cancels in p; lse takes the term as it is)
+    const bool near = fabsf(top) < 65536.f;
+    const float base = top * kLog2e;
+    if (near) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      q[i] = power_of(x[i] - top);
-      total += q[i];
+      for (int i = 0; i < PER; ++i) q[i] = __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -base));
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) q[i] = power_of(x[i] - top);
     }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) total += q[i];
     total = sum_lanes<TPR>(total);
     const bool fine = total > 0.f && total < INFINITY;   // (a NaN is neither; a row without an open expert sums up to 0)
-    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float inv = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum[i] = fmaf(q[i], inv, sum[i]);
     with += fine && t == 0;
@@ -236,30 +269,31 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
       if (j >= a.k) break;
       if (!fine) id[j] = -1;
       float score;
-      if constexpr (sizeof(T) == 4) score = id[j] < 0 ? none : ((const float*)a.x)[row * a.xs + id[j]];
+      if constexpr (sizeof(T) == 4) score = id[j] < 0 ? none : mine[id[j]];
       else score = score_of(high[j], a.low);
-      weight[j] = id[j] >= 0 ? whole_power_of(score - top) * inv : fine || total == 0.f ? 0.f : NAN;
+      weight[j] = id[j] >= 0 ? whole_power(near ? fmaf(score, kLog2e, -base) : (score - top) * kLog2e) * inv : fine || total == 0.f ? 0.f : NAN;
       shares += weight[j];
     }
-    const float by = a.renorm && shares > 0.f ? 1.f / shares : 1.f;
+    const float by = a.renorm && shares > 0.f ? __builtin_amdgcn_rcpf(shares) : 1.f;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
       if (j >= a.k) break;
       if (t == j % TPR) {
-        a.ids[j * a.rows + row] = id[j];
-        a.weights[j * a.rows + row] = weight[j] * by;
+        at_row(a.ids + j * a.rows, row) = id[j];
+        at_row(a.weights + j * a.rows, row) = weight[j] * by;
         if (id[j] >= 0) atomicAdd(&count[id[j]], 1);
       }
     }
-    if (t == 0 && a.lse) a.lse[row] = total == 0.f ? none : fmaf(__log2f(total), kLn2, top);
+    if (t == 0 && a.lse) at_row(a.lse, row) = total == 0.f ? none : near ? (base + __log2f(total)) * kLn2 : fmaf(__log2f(total), kLn2, top);
   }
+  if constexpr (sizeof(T) == 4) __syncthreads();
   // the workgroup's rows: those of a wave first (lanes TPR apart)
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
 #pragma unroll
     for (int o = TPR; o < 64; o <<= 1) sum[i] += __shfl_xor(sum[i], o, 64);
-    if (lane < TPR) meet[wave][expert_of<T, TPR>(t, i)] = sum[i];
+    if (lane < TPR) room[wave * WIDE + expert_of<T, TPR>(t, i)] = sum[i];
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) with += __shfl_xor(with, o, 64);
@@ -271,14 +305,13 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
   for (int e = threadIdx.x; e < a.experts; e += THREADS) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) s += meet[w][e];
+    for (int w = 0; w < WAVES; ++w) s += room[w * WIDE + e];
     if (alone) {
       a.counts[e] = count[e];
       loss += (double)s * count[e];
       number += count[e];
     } else {
-      a.sums[(int64_t)blockIdx.x * a.experts + e] = s;
-      a.chosen[(int64_t)blockIdx.x * a.experts + e] = count[e];
+      a.sums[(int64_t)blockIdx.x * a.experts + e] = float2{s, __int_as_float(count[e])};
     }
   }
   int all = 0;
@@ -292,8 +325,8 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
     return;
   }
   __syncthreads();
-  double* part = reinterpret_cast<double*>(&meet[0][0]);
-  static_assert(sizeof(meet) >= 16 * WAVES, "");
+  double* part = reinterpret_cast<double*>(room);
+  static_assert(sizeof(room) >= 16 * WAVES, "");
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     loss += __shfl_xor(loss, o, 64);
@@ -328,64 +361,87 @@ struct RouteGradArgs {
   void* dx;
 };
 
-// The scores that were chosen are read once more, each by its address: a row's sum takes their gradients from there, and the threads that hold them add
-// them by comparing experts (two instructions a score and choice, where looking the probabilities up in the registers was as many again).
+// The scores that were chosen are read once more, each by its address: a row's sum takes their gradients from there, and the threads that hold them take them from a row
+// in LDS, which is zero but for them (comparing experts in the registers takes four instructions a score and choice). Only the row's own threads, of one
+// wave, touch it, and a wave's LDS accesses keep their order.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
   constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N;
-  __shared__ int64_t part[THREADS];
+  __shared__ __attribute__((aligned(16))) float added[ROWS][TPR * PER];
   const int t = threadIdx.x % TPR;
   const float none = -INFINITY;
+  float* mine = added[threadIdx.x / TPR];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine[expert_of<T, TPR>(t, i)] = 0.f;
   // the loss' part of g: the same for all rows
   float share[PER] = {};
-  double by = 0.0;
   if (a.dloss) {
-    int64_t n = 0;
-    for (int e = threadIdx.x; e < a.experts; e += THREADS) n += a.counts[e];
-    part[threadIdx.x] = n;
-    __syncthreads();
-    for (int o = THREADS / 2; o > 0; o >>= 1) {
-      if ((int)threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
-      __syncthreads();
-    }
-    const int64_t chosen = part[0], with = a.counts[a.experts];
-    by = (double)*a.dloss * a.experts / ((double)(chosen > 0 ? chosen : 1) * (double)(with > 0 ? with : 1));
+    // (every wave for itself: whole numbers below 2^53)
+    double chosen = 0.0;
+    for (int e = threadIdx.x & 63; e < a.experts; e += 64) chosen += (double)a.counts[e];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) chosen += __shfl_xor(chosen, o, 64);
+    const int64_t with = a.counts[a.experts];
+    const double by = (double)*a.dloss * a.experts / ((chosen > 0.0 ? chosen : 1.0) * (double)(with > 0 ? with : 1));
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int e = expert_of<T, TPR>(t, i);
       share[i] = e < a.experts ? (float)(by * (double)a.counts[e]) : 0.f;
     }
   }
-  const int64_t step = (int64_t)gridDim.x * ROWS;
-  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const uint32_t step = gridDim.x * ROWS, rows = (uint32_t)a.rows;   // (at most 2^30)
+  uint32_t row = blockIdx.x * ROWS + threadIdx.x / TPR;
+  // A row's scores, those that were chosen among them, come in while the row before is worked off; which ones were chosen, while the one before that is.
   Scores<T, TPR, PER> next = {};
-  if (row < a.rows) next.load((const T*)a.x + row * a.xs, t, a.experts);
-  for (; row < a.rows; row += step) {
+  int late_id[K], next_id[K];
+  float late_dw[K], next_dw[K], late_lse = none, next_lse = none;
+  T next_of[K];
+  const auto look_up = [&](uint32_t r) __attribute__((always_inline)) {
+    if (r >= rows) return;
+    late_lse = at_row(a.lse, r);
+    if (!a.dweights) return;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if (j >= a.k) break;
+      late_id[j] = at_row(a.ids + j * a.rows, r);
+      late_dw[j] = at_row(a.dweights + j * a.rows, r);
+    }
+  };
+  const auto fetch = [&](uint32_t r) __attribute__((always_inline)) {
+    if (r >= rows) return;
+    const T* from = (const T*)a.x + r * a.xs;
+    next.load(from, t, a.experts);
+    next_lse = late_lse;
+    if (!a.dweights) return;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if (j >= a.k) break;
+      next_dw[j] = late_dw[j];
+      next_id[j] = (uint32_t)late_id[j] < (uint32_t)a.experts ? late_id[j] : -1;
+      next_of[j] = from[next_id[j] < 0 ? 0 : next_id[j]];
+    }
+  };
+  look_up(row);
+  fetch(row);
+  look_up(row + step);
+  for (; row < rows; row += step) {
     Scores<T, TPR, PER> now = next;
     int id[K];
     float dp[K], of[K];
-    const T* from = (const T*)a.x + row * a.xs;
-    const float lse = a.lse[row], base = lse == none ? 0.f : lse;
-    if (a.dweights) {
+    const float base = next_lse == none ? 0.f : next_lse;
 #pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j >= a.k) break;
-        id[j] = a.ids[j * a.rows + row];
-        dp[j] = a.dweights[j * a.rows + row];
-        if ((uint32_t)id[j] >= (uint32_t)a.experts) id[j] = -1;
-      }
-#pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j >= a.k) break;
-        of[j] = (float)from[id[j] < 0 ? 0 : id[j]];
-      }
+    for (int j = 0; j < K; ++j) {
+      id[j] = next_id[j];
+      dp[j] = next_dw[j];
+      of[j] = (float)next_of[j];
     }
-    if (row + step < a.rows) next.load((const T*)a.x + (row + step) * a.xs, t, a.experts);
+    fetch(row + step);
+    look_up(row + 2 * step);
     float p[PER], s = 0.f, own = 0.f;
     now.read(t, a.experts, none, p);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      p[i] = whole_power_of(p[i] - base);   // (a row that is closed throughout: 0)
+      p[i] = whole_power((p[i] - base) * kLog2e);   // (a row that is closed throughout: 0)
       s = fmaf(p[i], share[i], s);
     }
     s = sum_lanes<TPR>(s);
@@ -397,20 +453,37 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
 #pragma unroll
       for (int j = 0; j < K; ++j) {
         if (j >= a.k) break;
-        of[j] = id[j] < 0 ? 0.f : whole_power_of(of[j] - base);
+        of[j] = id[j] < 0 ? 0.f : whole_power((of[j] - base) * kLog2e);
         total += of[j];
         if (id[j] >= 0) dot = fmaf(dp[j], of[j], dot);
       }
-      const float inv = a.renorm ? total > 0.f ? 1.f / total : 0.f : 1.f;
+      const float inv = a.renorm ? total > 0.f ? __builtin_amdgcn_rcpf(total) : 0.f : 1.f;
       dot = a.renorm ? dot * inv : 0.f;
 #pragma unroll
       for (int j = 0; j < K; ++j) {
         if (j >= a.k) break;
         dp[j] = id[j] < 0 ? 0.f : (dp[j] - dot) * inv;
         own = fmaf(dp[j], of[j], own);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) g[i] = id[j] == expert_of<T, TPR>(t, i) ? share[i] + dp[j] : g[i];
+        if (t == j % TPR && id[j] >= 0) mine[id[j]] += dp[j];   // (the same expert twice, which route never leaves: by one thread, or by neighbours one after the other)
+        __builtin_amdgcn_wave_barrier();
       }
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q)
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(mine + (q * TPR + t) * N + i);
+          g[q * N + i] += v.x;
+          g[q * N + i + 1] += v.y;
+          g[q * N + i + 2] += v.z;
+          g[q * N + i + 3] += v.w;
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j >= a.k) break;
+        if (t == j % TPR && id[j] >= 0) mine[id[j]] = 0.f;
+      }
+      __builtin_amdgcn_wave_barrier();
     }
     s += own;
     T* dx = (T*)a.dx + row * a.ys;
@@ -425,30 +498,33 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
   }
 }
 
-// Scores of a thread and threads of a row: the fewest places that hold it, and of those the fewest threads
+// Scores of a thread and threads of a row: 16, or 24 of 16 bits (12 of fp32) where that takes fewer places
 struct Form {
   int per, threads;
 };
-Form form_of(int experts) {
+inline Form form_of(int experts, bool f32) {
   if (experts <= 8) return {8, 1};
   int t = 1;
   while (t * 16 < experts) t *= 2;
+  if (f32) return t * 12 >= experts ? Form{12, t} : Form{16, t};
   return t >= 2 && t / 2 * 24 >= experts ? Form{24, t / 2} : Form{16, t};
 }
-constexpr int kThreads = 512;
 
-int64_t blocks_for(int64_t rows, int experts, int64_t most) {
-  const int64_t per = kThreads / form_of(experts).threads, blocks = (rows + per - 1) / per;
+// Threads of a workgroup that adds up probabilities: fewer workgroups leave fewer sums, but beyond two experts to a row a thread has too many registers for two of 512
+constexpr int threads_of(int k) { return k <= 2 ? 512 : 256; }
+constexpr int kGradThreads = 256;
+inline int64_t blocks_for(int64_t rows, int experts, bool f32, int threads, int64_t most) {
+  const int64_t per = threads / form_of(experts, f32).threads, blocks = (rows + per - 1) / per;
   return blocks < most ? blocks : most;
 }
 
 template <typename T, int TPR, int PER, int K>
 void launch(const RouteArgs& a, unsigned blocks, hipStream_t stream) {
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_kernel<T, TPR, PER, K, kThreads>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_kernel<T, TPR, PER, K, threads_of(K)>), dim3(blocks), dim3(threads_of(K)), 0, stream, a);
 }
 template <typename T, int TPR, int PER, int K>
 void launch(const RouteGradArgs& a, unsigned blocks, hipStream_t stream) {
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_grad_kernel<T, TPR, PER, K, kThreads>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_grad_kernel<T, TPR, PER, K, kGradThreads>), dim3(blocks), dim3(kGradThreads), 0, stream, a);
 }
 template <typename T, int TPR, int PER, typename Args>
 void launch_k(const Args& a, unsigned blocks, hipStream_t stream) {
@@ -459,7 +535,9 @@ void launch_k(const Args& a, unsigned blocks, hipStream_t stream) {
 }
 template <typename T, typename Args>
 void launch_for(const Args& a, unsigned blocks, hipStream_t stream) {
-  const Form f = form_of(a.experts);
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int OTHER = F32 ? 12 : 24;
+  const Form f = form_of(a.experts, F32);
   if (f.per == 8) return launch_k<T, 1, 8>(a, blocks, stream);
   if (f.per == 16) switch (f.threads) {
       case 1: return launch_k<T, 1, 16>(a, blocks, stream);
@@ -471,12 +549,14 @@ void launch_for(const Args& a, unsigned blocks, hipStream_t stream) {
       default: return launch_k<T, 64, 16>(a, blocks, stream);
     }
   switch (f.threads) {
-    case 1: return launch_k<T, 1, 24>(a, blocks, stream);
-    case 2: return launch_k<T, 2, 24>(a, blocks, stream);
-    case 4: return launch_k<T, 4, 24>(a, blocks, stream);
-    case 8: return launch_k<T, 8, 24>(a, blocks, stream);
-    case 16: return launch_k<T, 16, 24>(a, blocks, stream);
-    default: return launch_k<T, 32, 24>(a, blocks, stream);
+    case 1: return launch_k<T, 1, OTHER>(a, blocks, stream);
+    case 2: return launch_k<T, 2, OTHER>(a, blocks, stream);
+    case 4: return launch_k<T, 4, OTHER>(a, blocks, stream);
+    case 8: return launch_k<T, 8, OTHER>(a, blocks, stream);
+    case 16: return launch_k<T, 16, OTHER>(a, blocks, stream);
+    case 32: return launch_k<T, 32, OTHER>(a, blocks, stream);
+    default:
+      if constexpr (F32) return launch_k<T, 64, OTHER>(a, blocks, stream);
   }
 }
 

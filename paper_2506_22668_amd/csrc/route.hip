@@ -13,10 +13,11 @@ __global__ __launch_bounds__(kJoinThreads) void route_join_kernel(RouteArgs a, i
   double s = 0.0;
   int64_t n = 0;
   if (e < a.experts) {
-#pragma unroll 8
+#pragma unroll 16
     for (int b = part; b < blocks; b += kJoinParts) {
-      s += a.sums[(int64_t)b * a.experts + e];
-      n += a.chosen[(int64_t)b * a.experts + e];
+      const float2 v = a.sums[(int64_t)b * a.experts + e];
+      s += v.x;
+      n += __float_as_int(v.y);
     }
   }
   sum_of[part][lane] = s;
@@ -60,24 +61,31 @@ __global__ __launch_bounds__(kJoinThreads) void route_join_kernel(RouteArgs a, i
   }
 }
 
-// Workgroups that leave sums. One takes up to two rounds of rows by itself, and nothing is left to add up.
-constexpr int64_t kMostBlocks = 512, kAlone = 2;
-int64_t sum_blocks(int64_t rows, int experts) {
-  const int64_t b = blocks_for(rows, experts, kMostBlocks);
+// Workgroups that leave sums: 16 waves to a compute unit, or 12 of more than two experts to a row. One takes up to two rounds of rows by itself, and nothing is
+// left to add up.
+constexpr int64_t kAlone = 2;
+int64_t sum_blocks(int64_t rows, int experts, bool f32, int k) {
+  const int64_t b = blocks_for(rows, experts, f32, threads_of(k), k <= 2 ? 512 : 768);
   return b <= kAlone ? 1 : b;
 }
 int join_blocks(int experts) { return (experts + 63) / 64; }
 
 }  // namespace
 
+// (of the type and number of experts to a row that have the most workgroups)
 int64_t ds_route_bytes(int64_t rows, int experts) {
-  const int64_t blocks = sum_blocks(rows, experts);
+  int64_t blocks = 1;
+  for (int f32 = 0; f32 < 2; ++f32)
+    for (int k = 2; k < 4; ++k) {
+      const int64_t b = sum_blocks(rows, experts, f32, k);
+      blocks = b > blocks ? b : blocks;
+    }
   return blocks > 1 ? join_blocks(experts) * 16 + blocks * (2 * (int64_t)experts + 1) * 4 + 4 : 0;
 }
 
 int ds_launch_route(ds_ctx* ctx, int dtype, int64_t rows, int experts, int k, int renorm, ds_rows x, int32_t* ids, float* weights, int64_t* counts, float* loss,
                     float* lse, void* workspace) {
-  const int64_t blocks = sum_blocks(rows, experts);
+  const int64_t blocks = sum_blocks(rows, experts, dtype == DS_ELEM_F32, k);
   const int joins = join_blocks(experts);
   RouteArgs a = {};
   a.rows = rows;
@@ -94,9 +102,8 @@ int ds_launch_route(ds_ctx* ctx, int dtype, int64_t rows, int experts, int k, in
   a.lse = lse;
   a.losses = (double*)workspace;
   a.numbers = (int64_t*)workspace + joins;
-  a.sums = (float*)workspace + 4 * joins;
-  a.chosen = (int32_t*)a.sums + blocks * experts;
-  a.with = a.chosen + blocks * experts;
+  a.sums = (float2*)workspace + 2 * joins;
+  a.with = (int32_t*)(a.sums + blocks * experts);
   a.through = a.with + blocks;
   const unsigned grid = (unsigned)blocks;
   if (dtype == DS_ELEM_F32) ds_route_rows<float>(&a, grid, ctx->stream);
@@ -124,7 +131,7 @@ int ds_launch_route_backward(ds_ctx* ctx, int dtype, int64_t rows, int experts, 
   a.dloss = dloss;
   a.dx = (void*)dx.data;
   a.ys = dx.stride;
-  const unsigned grid = (unsigned)blocks_for(rows, experts, 4 * (int64_t)ctx->num_cus);
+  const unsigned grid = (unsigned)blocks_for(rows, experts, dtype == DS_ELEM_F32, kGradThreads, 4 * (int64_t)ctx->num_cus);
   if (dtype == DS_ELEM_F32) ds_route_rows_backward<float>(&a, grid, ctx->stream);
   else if (dtype == DS_ELEM_BF16) ds_route_rows_backward<__bf16>(&a, grid, ctx->stream);
   else ds_route_rows_backward<_Float16>(&a, grid, ctx->stream);
