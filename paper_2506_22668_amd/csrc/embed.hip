@@ -257,6 +257,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_few_kernel(SortArgs a, int2
 struct SumArgs {
   int rows, cols, vocab, chunk, chunks, calls;
   const int2* pairs;
+  const int32_t* ids;   // few rows: not sorted yet
+  int range;            //   and the ids of a workgroup
   const void* dy;
   void* dtable;
   int64_t dys, dts;
@@ -264,7 +266,7 @@ struct SumArgs {
   uint8_t* seen;
   float* partial;       // [chunk][2][cols]: of the id that began before the chunk; of the one that goes on behind it
   int64_t rows_step;    // the pass over the table: how far a thread's next piece is
-  int calls_step, zero_blocks;
+  int calls_step;
 };
 
 constexpr int kRowsAhead = 8;
@@ -282,7 +284,48 @@ __device__ __forceinline__ void store_sums(T* to, const float (&v)[N], float sca
   }
 }
 
-// LANES threads take a stretch of `chunk` sorted rows, N columns to a thread
+// A thread's columns col .. of the sorted rows [begin, end): pair(i) is row i's (id, row), leave(id, sum, first, last) takes the sum of an id's rows, the first
+// id's with `first` set, the last one's with `last`. Ids of `none` and beyond come last and are passed over.
+template <typename D, bool TINY, typename Pair, typename Leave>
+__device__ __forceinline__ void sum_rows(int begin, int end, int col, int cols, const D* dy, int64_t dys, int none, const Pair& pair, const Leave& leave) {
+  constexpr int N = Piece<D>::N;
+  float sum[N] = {};
+  int2 now[kRowsAhead], next[kRowsAhead];
+  typename Elements<D, N>::V v[kRowsAhead];
+  int key = pair(begin).x;
+  bool first = true;
+#pragma unroll
+  for (int j = 0; j < kRowsAhead; ++j) next[j] = pair(min(begin + j, end - 1));
+  for (int at = begin; at < end; at += kRowsAhead) {
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      now[j] = next[j];
+      v[j] = load_elements<D, N, TINY>(dy + now[j].y * dys, col, cols);
+    }
+    if (at + kRowsAhead < end) {
+#pragma unroll
+      for (int j = 0; j < kRowsAhead; ++j) next[j] = pair(min(at + kRowsAhead + j, end - 1));
+    }
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      if (at + j >= end) break;
+      if (now[j].x != key) {
+        leave(key, sum, first, false);
+        first = false;
+        key = now[j].x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.f;
+      }
+      if (key >= none) return;
+      settle_elements<D, N, TINY>(v[j], col, cols);
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += (float)v[j][i];
+    }
+  }
+  leave(key, sum, first, true);
+}
+
+// LANES threads take a stretch of `chunk` sorted rows, a piece of 16 bytes of their columns to a thread
 template <typename D, typename T, int LANES, bool TINY>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   constexpr int N = Piece<D>::N;
@@ -290,61 +333,28 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   const int begin = (int)min((int64_t)chunk * a.chunk, (int64_t)a.rows), end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
   if (begin >= end || col >= a.cols) return;
   const int have = a.cols - col;
-  const D* dy = (const D*)a.dy;
   T* dtable = (T*)a.dtable + col;
   float* partial = a.partial + (int64_t)chunk * 2 * a.cols + col;
-  int key = a.pairs[begin].x;
-  bool before = begin > 0 && a.pairs[begin - 1].x == key;   // the id began before the chunk
-  const bool after = end < a.rows && a.pairs[end].x == a.pairs[end - 1].x;
-  float sum[N] = {};
-  const auto leave = [&](bool last) __attribute__((always_inline)) {
-    if (key >= a.vocab) return;
-    if (before || last) {
-      store_sums<float, N>(partial + (last ? a.cols : 0), sum, 1.f, have);
-    } else {
-      store_sums<T, N>(dtable + (int64_t)key * a.dts, sum, a.scale, have);
-    }
-    if (!before && col == 0) a.seen[key] = 1;
-  };
-  int2 now[kRowsAhead], next[kRowsAhead];
-  typename Elements<D, N>::V v[kRowsAhead];
-  const auto ask = [&](int at) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) next[j] = a.pairs[min(at + j, end - 1)];
-  };
-  ask(begin);
-  for (int at = begin; at < end; at += kRowsAhead) {
-#pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) {
-      now[j] = next[j];
-      v[j] = load_elements<D, N, TINY>(dy + now[j].y * a.dys, col, a.cols);
-    }
-    if (at + kRowsAhead < end) ask(at + kRowsAhead);
-#pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j) {
-      if (at + j >= end) break;
-      if (now[j].x != key) {
-        leave(false);
-        before = false;
-        key = now[j].x;
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] = 0.f;
-      }
-      if (key >= a.vocab) return;   // (the rows of no id are the last ones)
-      settle_elements<D, N, TINY>(v[j], col, a.cols);
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] += (float)v[j][i];
-    }
-  }
-  leave(after);
+  const bool before = begin > 0 && a.pairs[begin - 1].x == a.pairs[begin].x;   // the first id began before the chunk
+  const bool after = end < a.rows && a.pairs[end].x == a.pairs[end - 1].x;     // the last one goes on behind it
+  sum_rows<D, TINY>(begin, end, col, a.cols, (const D*)a.dy, a.dys, a.vocab, [&](int i) { return a.pairs[i]; },
+                    [&](int key, const float(&sum)[N], bool first, bool last) {
+                      const bool goes_on = last && after, began = first && before;
+                      if (key >= a.vocab) return;
+                      if (goes_on || began) store_sums<float, N>(partial + (goes_on ? a.cols : 0), sum, 1.f, have);
+                      else store_sums<T, N>(dtable + (int64_t)key * a.dts, sum, a.scale, have);
+                      if (!began && col == 0) a.seen[key] = 1;
+                    });
 }
 
-// Adds up what the chunks left of ids that reach over a chunk's end, and clears the rows of ids that did not come up (the workgroups behind `join_blocks`).
+// Adds up what the chunks left of ids that reach over a chunk's end: a workgroup looks at kJoinChunks chunks, 64 columns, 16 threads to an id of up to kShort
+// chunks, all of them to a longer one. The workgroups behind `joins` clear the rows of ids that did not come up.
+constexpr int kJoinThreads = 512, kJoinChunks = 64, kJoinCols = 64, kJoinLanes = kJoinCols / 4, kJoinWorkers = kJoinThreads / kJoinLanes, kShort = 8;
 template <typename T>
-__global__ __launch_bounds__(kThreads) void finish_kernel(SumArgs a, int join_blocks) {
+__global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int joins, int col_tiles) {
   constexpr int N = Piece<T>::N;
-  if ((int)blockIdx.x >= join_blocks) {
-    const int64_t first = (int64_t)((int)blockIdx.x - join_blocks) * kThreads + threadIdx.x;
+  if ((int)blockIdx.x >= joins) {
+    const int64_t first = (int64_t)((int)blockIdx.x - joins) * kJoinThreads + threadIdx.x;
     int64_t row = first / a.calls;
     int call = (int)(first % a.calls);
     while (row < a.vocab) {
@@ -358,28 +368,182 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(SumArgs a, int join_bl
     }
     return;
   }
-  // the id that begins in this chunk and goes on behind it
-  const int chunk = (int)blockIdx.x, begin = chunk * a.chunk, end = begin + a.chunk;
-  if (end >= a.rows) return;
-  const int key = a.pairs[end - 1].x;
-  if (key >= a.vocab || a.pairs[end].x != key || (begin > 0 && a.pairs[begin - 1].x == key)) return;
-  // the last chunk that it has rows in
-  __shared__ int last_of[kThreads];
-  int last = chunk + 1;
-  for (int c = chunk + 1 + (int)threadIdx.x; c < a.chunks && a.pairs[c * a.chunk].x == key; c += kThreads) last = c;
-  last_of[threadIdx.x] = last;
+  __shared__ int of_short[kJoinChunks], of_long[kJoinChunks], last_of[kJoinChunks], shorts, longs, last;
+  __shared__ float meet[kJoinWorkers][kJoinCols];
+  const int base = (int)blockIdx.x / col_tiles * kJoinChunks, col = (int)blockIdx.x % col_tiles * kJoinCols + (int)threadIdx.x % kJoinLanes * 4;
+  const int worker = (int)threadIdx.x / kJoinLanes, have = a.cols - col;
+  if (threadIdx.x == 0) shorts = longs = 0;
   __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) last_of[threadIdx.x] = max(last_of[threadIdx.x], last_of[threadIdx.x + o]);
+  if ((int)threadIdx.x < kJoinChunks) {
+    // the id that begins in this chunk and goes on behind it
+    const int chunk = base + (int)threadIdx.x, begin = chunk < a.chunks ? chunk * a.chunk : a.rows;
+    if (a.rows - begin > a.chunk) {
+      const int end = begin + a.chunk, key = a.pairs[end - 1].x;
+      if (key < a.vocab && a.pairs[end].x == key && !(begin > 0 && a.pairs[begin - 1].x == key)) {
+        int c = chunk + 1;   // the last chunk that it has rows in, as far as kShort
+        while (c - chunk < kShort && c + 1 < a.chunks && a.pairs[(c + 1) * a.chunk].x == key) ++c;
+        if (c - chunk < kShort) {
+          last_of[threadIdx.x] = c;
+          of_short[atomicAdd(&shorts, 1)] = (int)threadIdx.x;   // (in any order: each has a result of its own)
+        } else {
+          of_long[atomicAdd(&longs, 1)] = (int)threadIdx.x;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const auto add = [&](float (&sum)[4], int chunk, int slot) __attribute__((always_inline)) {
+    const float* p = a.partial + ((int64_t)chunk * 2 + slot) * a.cols + col;
+    if (have >= 4) {
+      const Elements<float, 4>::V v = *reinterpret_cast<const Elements<float, 4>::U*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) sum[i] += i < have ? p[i] : 0.f;
+    }
+  };
+  const auto leave = [&](const float (&sum)[4], int key) __attribute__((always_inline)) {
+    T* to = (T*)a.dtable + (int64_t)key * a.dts + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < have) to[i] = (T)(sum[i] * a.scale);
+  };
+  for (int s = worker; s < shorts; s += kJoinWorkers) {
+    const int chunk = base + of_short[s], upto = last_of[of_short[s]];
+    float sum[4] = {};
+#pragma unroll 4
+    for (int c = chunk; c < upto; ++c) add(sum, c, 1);
+    add(sum, upto, 0);
+    leave(sum, a.pairs[(chunk + 1) * a.chunk].x);
+  }
+  for (int l = 0; l < longs; ++l) {
+    const int chunk = base + of_long[l], key = a.pairs[(chunk + 1) * a.chunk].x;
+    if (threadIdx.x == 0) last = 0;
+    __syncthreads();
+    int upto = chunk + 1;
+    for (int c = chunk + 1 + (int)threadIdx.x; c < a.chunks && a.pairs[c * a.chunk].x == key; c += kJoinThreads) upto = c;
+    atomicMax(&last, upto);
+    __syncthreads();
+    upto = last;
+    float sum[4] = {};
+#pragma unroll 8
+    for (int c = chunk + worker; c <= upto; c += kJoinWorkers) add(sum, c, c < upto);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) meet[worker][(int)threadIdx.x % kJoinLanes * 4 + i] = sum[i];
+    __syncthreads();
+    if (worker == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sum[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kJoinWorkers; ++w) sum[i] += meet[w][(int)threadIdx.x * 4 + i];
+      }
+      leave(sum, key);
+    }
     __syncthreads();
   }
-  last = last_of[0];
-  for (int col = threadIdx.x; col < a.cols; col += kThreads) {
-    float sum = 0.f;
-#pragma unroll 8
-    for (int c = chunk; c < last; ++c) sum += a.partial[((int64_t)c * 2 + 1) * a.cols + col];
-    sum += a.partial[(int64_t)last * 2 * a.cols + col];
-    ((T*)a.dtable)[(int64_t)key * a.dts + col] = (T)(sum * a.scale);
+}
+
+// Few rows, in one launch: a workgroup has the ids [first, first + range) and the columns of its threads, finds its rows among all and sorts them in LDS, and its
+// workers take equal shares of them. What ids that reach over a share's end leave meets in LDS.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRange = 256;
+constexpr int kFewRows = 4096;
+template <typename D, typename T, int LANES, bool TINY>
+__global__ __launch_bounds__(kFewThreads) void few_sums_kernel(SumArgs a) {
+  constexpr int N = Piece<D>::N, WORKERS = kFewThreads / LANES, P = Piece<T>::N;
+  __shared__ int count[kFewWaves][kFewRange], start[kFewRange + 1], wave_sum[kFewWaves];
+  __shared__ int2 held[kFewRows];
+  __shared__ float meet[WORKERS][2][LANES * N];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first_id = (int)blockIdx.x * a.range, range = min(a.range, a.vocab - first_id);
+  for (int i = threadIdx.x; i < kFewWaves * kFewRange; i += kFewThreads) (&count[0][0])[i] = 0;
+  __syncthreads();
+  const int each = ((a.rows + kFewWaves - 1) / kFewWaves + 63) / 64 * 64, begin = min(wave * each, a.rows), end = min(begin + each, a.rows);
+  const auto digit_of = [&](int row) { return row < end ? (uint32_t)a.ids[row] - (uint32_t)first_id : ~0u; };
+  for (int row = begin + lane; row < end; row += 64) {
+    const uint32_t digit = digit_of(row);
+    if (digit < (uint32_t)range) atomicAdd(&count[wave][digit], 1);   // (whole numbers: any order)
+  }
+  __syncthreads();
+  int own = 0, upto;
+  if ((int)threadIdx.x < kFewRange)
+    for (int w = 0; w < kFewWaves; ++w) own += count[w][threadIdx.x];
+  upto = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += up;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  if ((int)threadIdx.x < kFewRange) {
+    int at = upto - own;
+    for (int w = 0; w < wave; ++w) at += wave_sum[w];
+    start[threadIdx.x] = at;
+    if (threadIdx.x == kFewRange - 1) start[kFewRange] = at + own;
+    for (int w = 0; w < kFewWaves; ++w) {
+      const int c = count[w][threadIdx.x];
+      count[w][threadIdx.x] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  const int all = start[kFewRange];
+  if (all > 0) {
+    volatile int* mine = count[wave];
+    for (int base = begin; base < end; base += 64) {
+      const uint32_t digit = digit_of(base + lane);
+      const bool there = digit < (uint32_t)range;
+      unsigned long long same = __ballot(there);
+      if (same == 0) continue;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const unsigned long long set = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? set : ~set;
+      }
+      if (there) {
+        const int rank = __popcll(same & ((1ull << lane) - 1)), at = mine[digit];
+        held[at + rank] = int2{(int)digit, base + lane};
+        if (rank == 0) mine[digit] = at + __popcll(same);   // (a wave's LDS accesses keep their order)
+      }
+    }
+  }
+  __syncthreads();
+  T* dtable = (T*)a.dtable + (int64_t)first_id * a.dts;
+  const int worker = (int)threadIdx.x / LANES, place = (int)threadIdx.x % LANES * N, col = (int)blockIdx.y * LANES * N + place, have = a.cols - col;
+  const int share = (all + WORKERS - 1) / WORKERS, from = min(worker * share, all), to = min(from + share, all);
+  const bool before = from > 0 && from < to && held[from - 1].x == held[from].x, after = to < all && from < to && held[to].x == held[to - 1].x;
+  if (have > 0) {
+    for (int v = worker; v < range; v += WORKERS)
+      if (start[v] == start[v + 1])
+#pragma unroll
+        for (int p = 0; p < N / P; ++p) store_piece<T>(dtable + (int64_t)v * a.dts + col + p * P, PieceV<T>{}, have - p * P);
+    if (from < to)
+      sum_rows<D, TINY>(from, to, col, a.cols, (const D*)a.dy, a.dys, a.range, [&](int i) { return held[i]; },
+                        [&](int key, const float(&sum)[N], bool first, bool last) {
+                          const bool goes_on = last && after, began = first && before;
+                          if (goes_on || began) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) meet[worker][goes_on][place + i] = sum[i];
+                          } else {
+                            store_sums<T, N>(dtable + (int64_t)key * a.dts + col, sum, a.scale, have);
+                          }
+                        });
+  }
+  __syncthreads();
+  // an id that begins in this share and goes on behind it
+  if (have > 0 && after && !(before && held[from].x == held[to - 1].x)) {
+    const int key = held[to - 1].x;
+    float sum[N] = {};
+    int w = worker;
+    do {
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += meet[w][1][place + i];
+      ++w;
+    } while ((w + 1) * share < all && held[(w + 1) * share].x == key);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += meet[w][0][place + i];
+    store_sums<T, N>(dtable + (int64_t)key * a.dts + col, sum, a.scale, have);
   }
 }
 
@@ -399,6 +563,13 @@ int sort_blocks(int rows) {
   return blocks <= 4 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks;
 }
 
+// Few rows: ids of a workgroup, so that there are about 512 workgroups (of 64 columns or more); 0: another form
+int few_range(int rows, int cols, int vocab) {
+  if (rows > kFewRows) return 0;
+  const int64_t range = ((int64_t)vocab * ((cols + 63) / 64) + 511) / 512;
+  return range > kFewRange ? 0 : range < 8 ? 8 : (int)range;
+}
+
 struct Layout {
   int64_t pairs, other, counts, seen, partial, bytes;
 };
@@ -407,6 +578,7 @@ Layout layout_of(int rows, int cols, int vocab) {
   const int bits = digits_of(vocab, &passes), blocks = sort_blocks(rows);
   const int64_t chunks = (rows + chunk_of(rows) - 1) / chunk_of(rows);
   Layout l = {};
+  if (few_range(rows, cols, vocab)) return l;
   int64_t at = 0;
   const auto place = [&](int64_t bytes) {
     const int64_t here = at;
@@ -476,13 +648,30 @@ int launch_sums(ds_ctx* ctx, SumArgs& a) {
     else launch_sum<D, T, 64>(a, ctx->stream);
   }
   a.calls = (a.cols + Piece<T>::N - 1) / Piece<T>::N;
-  const int64_t all = (int64_t)a.vocab * a.calls, want = (all + kThreads - 1) / kThreads, most = 8 * (int64_t)ctx->num_cus;
-  a.zero_blocks = (int)(want < most ? want : most);
-  const int64_t step = (int64_t)a.zero_blocks * kThreads;
+  const int64_t all = (int64_t)a.vocab * a.calls, want = (all + kJoinThreads - 1) / kJoinThreads, most = 4 * (int64_t)ctx->num_cus;
+  const int64_t clears = want < most ? want : most, step = clears * kJoinThreads;
   a.rows_step = step / a.calls;
   a.calls_step = (int)(step % a.calls);
-  const int joins = a.rows > 0 ? a.chunks : 0;
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(finish_kernel<T>), dim3(joins + a.zero_blocks), dim3(kThreads), 0, ctx->stream, a, joins);
+  const int col_tiles = (a.cols + kJoinCols - 1) / kJoinCols;
+  const int64_t joins = (int64_t)((a.chunks + kJoinChunks - 1) / kJoinChunks) * col_tiles;
+  if (joins + clears > ds_most_workgroups(kJoinThreads)) return ds_fail(ctx, DS_EINVAL, "%d rows of %d columns are more than a launch has", a.rows, a.cols);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(finish_kernel<T>), dim3((unsigned)(joins + clears)), dim3(kJoinThreads), 0, ctx->stream, a, (int)joins, col_tiles);
+  DS_HIP(ctx, hipGetLastError());
+  return DS_OK;
+}
+
+template <typename D, typename T, int LANES>
+void launch_few(const SumArgs& a, hipStream_t stream) {
+  const dim3 grid((a.vocab + a.range - 1) / a.range, (a.cols + LANES * Piece<D>::N - 1) / (LANES * Piece<D>::N)), block(kFewThreads);
+  if (a.cols < Piece<D>::N) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_sums_kernel<D, T, LANES, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_sums_kernel<D, T, LANES, false>), grid, block, 0, stream, a);
+}
+
+template <typename D, typename T>
+int launch_backward(ds_ctx* ctx, SumArgs& a) {
+  if (a.range == 0) return launch_sums<D, T>(ctx, a);
+  if (a.cols <= 8 * Piece<D>::N) launch_few<D, T, 8>(a, ctx->stream);
+  else launch_few<D, T, 16>(a, ctx->stream);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -516,7 +705,6 @@ int ds_launch_embed_backward(ds_ctx* ctx, int dtype, int table_dtype, int rows, 
   char* base = (char*)workspace;
   int2* pairs = (int2*)(base + l.pairs);
   uint8_t* seen = (uint8_t*)(base + l.seen);
-  DS_TRY(sort_ids(ctx, ids, rows, vocab, pairs, (int2*)(base + l.other), (int32_t*)(base + l.counts), seen));
   SumArgs a = {};
   a.rows = rows;
   a.cols = cols;
@@ -531,7 +719,10 @@ int ds_launch_embed_backward(ds_ctx* ctx, int dtype, int table_dtype, int rows, 
   a.scale = scale;
   a.seen = seen;
   a.partial = (float*)(base + l.partial);
-  if (dtype == DS_ELEM_F32) return launch_sums<float, float>(ctx, a);
-  if (dtype == DS_ELEM_BF16) return table_dtype == DS_ELEM_F32 ? launch_sums<__bf16, float>(ctx, a) : launch_sums<__bf16, __bf16>(ctx, a);
-  return table_dtype == DS_ELEM_F32 ? launch_sums<_Float16, float>(ctx, a) : launch_sums<_Float16, _Float16>(ctx, a);
+  a.ids = ids;
+  a.range = few_range(rows, cols, vocab);
+  if (a.range == 0) DS_TRY(sort_ids(ctx, ids, rows, vocab, pairs, (int2*)(base + l.other), (int32_t*)(base + l.counts), seen));
+  if (dtype == DS_ELEM_F32) return launch_backward<float, float>(ctx, a);
+  if (dtype == DS_ELEM_BF16) return table_dtype == DS_ELEM_F32 ? launch_backward<__bf16, float>(ctx, a) : launch_backward<__bf16, __bf16>(ctx, a);
+  return table_dtype == DS_ELEM_F32 ? launch_backward<_Float16, float>(ctx, a) : launch_backward<_Float16, _Float16>(ctx, a);
 }

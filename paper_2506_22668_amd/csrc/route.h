@@ -158,7 +158,7 @@ __device__ __forceinline__ void highest(const int (&key)[PER], int (&list)[K]) {
 // Counts of a row's experts are added up in LDS (whole numbers: in any order). 1,000,175 rows of 64 bf16, 2 of them each: see the table of times in front of launch_of.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
-  constexpr int ROWS = THREADS / TPR, WAVES = THREADS / 64, WIDE = TPR * PER, LIST = sizeof(T) == 4 ? K + 1 : K;
+  constexpr int ROWS = THREADS / TPR, WAVES = THREADS / 64, WIDE = TPR * PER, LIST = sizeof(T) == 4 ? K + 1 : K, OWN = (K + TPR - 1) / TPR;
   // the waves' sums, at the end; until then, fp32: the scores of the rows under way, from which those that were chosen are read
   __shared__ __attribute__((aligned(16))) float room[sizeof(T) == 4 ? THREADS * PER : WAVES * WIDE];
   float* mine = room + (int)threadIdx.x / TPR * WIDE;
@@ -191,26 +191,25 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
       for (int j = 0; j < LIST; ++j) list[j] = lowest;
       highest(key, list);
     }
-    int id[K], high[K];
+    // (thread t of the row has its choices t, t + TPR, ..)
+    int own[OWN], first = lowest, last = lowest;
     bool again = false;   // fp32: scores that are told apart by their last bits alone
-    int last = lowest;
+#pragma unroll
+    for (int c = 0; c < OWN; ++c) own[c] = lowest;
 #pragma unroll
     for (int j = 0; j < LIST; ++j) {
-      if (j >= a.k + (LIST - K)) break;
+      if (j >= a.k + (LIST - K)) continue;
       const int best = max_lanes<TPR>(list[0]);
       if constexpr (sizeof(T) == 4) again |= j > 0 && best > shut && ((best ^ last) & ~a.low) == 0;
       last = best;
-      if (j < K) {
-        high[j < K ? j : 0] = best;
-        id[j < K ? j : 0] = best > shut ? (int)(a.low - ((uint32_t)best & a.low)) : -1;
-      }
-      if (list[0] == best) {
+      if (j == 0) first = best;
+      if (j < K && j < a.k) own[j < K ? j / TPR : 0] = t == j % TPR ? best : own[j < K ? j / TPR : 0];
+      if (list[0] == best) {   // (of what comes behind the last K - j nothing is asked for any more)
 #pragma unroll
-        for (int i = 0; i + 1 < LIST; ++i) list[i] = list[i + 1];
-        list[LIST - 1] = lowest;
+        for (int i = 0; i + 1 < LIST - j; ++i) list[i] = list[i + 1];
       }
     }
-    float top = high[0] > shut ? score_of(high[0], a.low) : 0.f;
+    float top = first > shut ? score_of(first, a.low) : 0.f;
     if constexpr (sizeof(T) == 4) {   // (a key's bits alone may be far from a large score)
       top = none;
       __builtin_amdgcn_wave_barrier();   // (a row's threads are of one wave, whose LDS accesses keep their order)
@@ -241,47 +240,47 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum[i] = fmaf(q[i], inv, sum[i]);
     with += fine && t == 0;
+    int exact[OWN] = {};
     if (sizeof(T) == 4 && __any(again)) {
-      int taken[K];
-#pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j >= a.k) break;
+#pragma clang loop unroll(disable)
+      for (int j = 0; j < a.k; ++j) {
         float best = none;
         int at = 0x7fffffff;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          const int e = expert_of<T, TPR>(t, i);
-          bool open = x[i] > best;
-#pragma unroll
-          for (int l = 0; l < j; ++l) open &= taken[l] != e;
-          best = open ? x[i] : best;
-          at = open ? e : at;
+          const bool above = x[i] > best;
+          best = above ? x[i] : best;
+          at = above ? expert_of<T, TPR>(t, i) : at;
         }
         const float most = highest_lane<TPR>(best);
-        const int first = -max_lanes<TPR>(best == most ? -at : -0x7fffffff);
-        taken[j] = most > none ? first : -1;
-        if (again) id[j] = taken[j];
+        const int lowest_expert = -max_lanes<TPR>(best == most ? -at : -0x7fffffff), found = most > none ? lowest_expert : -1;
+#pragma unroll
+        for (int c = 0; c < OWN; ++c) exact[c] = j == c * TPR + t ? found : exact[c];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = expert_of<T, TPR>(t, i) == found ? none : x[i];
       }
     }
-    float weight[K], shares = 0.f;
+    int id[OWN];
+    float weight[OWN], shares = 0.f;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if (j >= a.k) break;
-      if (!fine) id[j] = -1;
+    for (int c = 0; c < OWN; ++c) {
+      id[c] = fine && own[c] > shut ? (int)(a.low - ((uint32_t)own[c] & a.low)) : -1;
+      if (sizeof(T) == 4 && again && fine) id[c] = exact[c];
       float score;
-      if constexpr (sizeof(T) == 4) score = id[j] < 0 ? none : mine[id[j]];
-      else score = score_of(high[j], a.low);
-      weight[j] = id[j] >= 0 ? whole_power(near ? fmaf(score, kLog2e, -base) : (score - top) * kLog2e) * inv : fine || total == 0.f ? 0.f : NAN;
-      shares += weight[j];
+      if constexpr (sizeof(T) == 4) score = id[c] < 0 ? none : mine[id[c]];
+      else score = score_of(own[c], a.low);
+      weight[c] = id[c] >= 0 ? whole_power(near ? fmaf(score, kLog2e, -base) : (score - top) * kLog2e) * inv : fine || total == 0.f ? 0.f : NAN;
+      shares += sum_lanes<TPR>(c * TPR + t < a.k ? weight[c] : 0.f);
     }
     const float by = a.renorm && shares > 0.f ? __builtin_amdgcn_rcpf(shares) : 1.f;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if (j >= a.k) break;
-      if (t == j % TPR) {
-        at_row(a.ids + j * a.rows, row) = id[j];
-        at_row(a.weights + j * a.rows, row) = weight[j] * by;
-        if (id[j] >= 0) atomicAdd(&count[id[j]], 1);
+    for (int c = 0; c < OWN; ++c) {
+      const int j = c * TPR + t;
+      if (j < a.k) {
+        const int64_t at = j * a.rows + row;
+        a.ids[at] = id[c];
+        a.weights[at] = weight[c] * by;
+        if (id[c] >= 0) atomicAdd(&count[id[c]], 1);
       }
     }
     if (t == 0 && a.lse) at_row(a.lse, row) = total == 0.f ? none : near ? (base + __log2f(total)) * kLn2 : fmaf(__log2f(total), kLn2, top);
@@ -366,13 +365,11 @@ struct RouteGradArgs {
 // wave, touch it, and a wave's LDS accesses keep their order.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
-  constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N;
+  constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N, OWN = (K + TPR - 1) / TPR;
   __shared__ __attribute__((aligned(16))) float added[ROWS][TPR * PER];
   const int t = threadIdx.x % TPR;
   const float none = -INFINITY;
   float* mine = added[threadIdx.x / TPR];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) mine[expert_of<T, TPR>(t, i)] = 0.f;
   // the loss' part of g: the same for all rows
   float share[PER] = {};
   if (a.dloss) {
@@ -383,28 +380,36 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
     for (int o = 1; o < 64; o <<= 1) chosen += __shfl_xor(chosen, o, 64);
     const int64_t with = a.counts[a.experts];
     const double by = (double)*a.dloss * a.experts / ((chosen > 0.0 ? chosen : 1.0) * (double)(with > 0 ? with : 1));
+    static_assert(THREADS >= TPR, "a row of `added` holds every expert");
+    float* all = &added[0][0];
+    for (int e = threadIdx.x; e < TPR * PER; e += THREADS) all[e] = e < a.experts ? (float)(by * (double)a.counts[e]) : 0.f;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = expert_of<T, TPR>(t, i);
-      share[i] = e < a.experts ? (float)(by * (double)a.counts[e]) : 0.f;
-    }
+    for (int i = 0; i < PER; ++i) share[i] = all[expert_of<T, TPR>(t, i)];
+    __syncthreads();
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine[expert_of<T, TPR>(t, i)] = 0.f;
   const uint32_t step = gridDim.x * ROWS, rows = (uint32_t)a.rows;   // (at most 2^30)
   uint32_t row = blockIdx.x * ROWS + threadIdx.x / TPR;
   // A row's scores, those that were chosen among them, come in while the row before is worked off; which ones were chosen, while the one before that is.
   Scores<T, TPR, PER> next = {};
-  int late_id[K], next_id[K];
-  float late_dw[K], next_dw[K], late_lse = none, next_lse = none;
-  T next_of[K];
+  // (thread t of the row has its choices t, t + TPR, ..)
+  int late_id[OWN] = {}, next_id[OWN];
+  float late_dw[OWN] = {}, next_dw[OWN], late_lse = none, next_lse = none;
+  T next_of[OWN];
   const auto look_up = [&](uint32_t r) __attribute__((always_inline)) {
     if (r >= rows) return;
     late_lse = at_row(a.lse, r);
     if (!a.dweights) return;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if (j >= a.k) break;
-      late_id[j] = at_row(a.ids + j * a.rows, r);
-      late_dw[j] = at_row(a.dweights + j * a.rows, r);
+    for (int c = 0; c < OWN; ++c) {
+      const int j = c * TPR + t;
+      late_id[c] = -1;
+      if (j < a.k) {
+        late_id[c] = a.ids[j * a.rows + r];
+        late_dw[c] = a.dweights[j * a.rows + r];
+      }
     }
   };
   const auto fetch = [&](uint32_t r) __attribute__((always_inline)) {
@@ -414,11 +419,10 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
     next_lse = late_lse;
     if (!a.dweights) return;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      if (j >= a.k) break;
-      next_dw[j] = late_dw[j];
-      next_id[j] = (uint32_t)late_id[j] < (uint32_t)a.experts ? late_id[j] : -1;
-      next_of[j] = from[next_id[j] < 0 ? 0 : next_id[j]];
+    for (int c = 0; c < OWN; ++c) {
+      next_dw[c] = late_dw[c];
+      next_id[c] = (uint32_t)late_id[c] < (uint32_t)a.experts ? late_id[c] : -1;
+      next_of[c] = from[next_id[c] < 0 ? 0 : next_id[c]];
     }
   };
   look_up(row);
@@ -426,14 +430,14 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
   look_up(row + step);
   for (; row < rows; row += step) {
     Scores<T, TPR, PER> now = next;
-    int id[K];
-    float dp[K], of[K];
+    int id[OWN];
+    float dp[OWN], of[OWN];
     const float base = next_lse == none ? 0.f : next_lse;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      id[j] = next_id[j];
-      dp[j] = next_dw[j];
-      of[j] = (float)next_of[j];
+    for (int c = 0; c < OWN; ++c) {
+      id[c] = next_id[c];
+      dp[c] = next_dw[c];
+      of[c] = (float)next_of[c];
     }
     fetch(row + step);
     look_up(row + 2 * step);
@@ -451,22 +455,24 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
     if (a.dweights) {
       float dot = 0.f, total = 0.f;
 #pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j >= a.k) break;
-        of[j] = id[j] < 0 ? 0.f : whole_power((of[j] - base) * kLog2e);
-        total += of[j];
-        if (id[j] >= 0) dot = fmaf(dp[j], of[j], dot);
+      for (int c = 0; c < OWN; ++c) {
+        of[c] = id[c] < 0 ? 0.f : whole_power((of[c] - base) * kLog2e);
+        dp[c] = id[c] < 0 ? 0.f : dp[c];
+        total += of[c];
+        dot = fmaf(dp[c], of[c], dot);
       }
+      total = sum_lanes<TPR>(total);
+      dot = sum_lanes<TPR>(dot);
       const float inv = a.renorm ? total > 0.f ? __builtin_amdgcn_rcpf(total) : 0.f : 1.f;
       dot = a.renorm ? dot * inv : 0.f;
 #pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j >= a.k) break;
-        dp[j] = id[j] < 0 ? 0.f : (dp[j] - dot) * inv;
-        own = fmaf(dp[j], of[j], own);
-        if (t == j % TPR && id[j] >= 0) mine[id[j]] += dp[j];   // (the same expert twice, which route never leaves: by one thread, or by neighbours one after the other)
-        __builtin_amdgcn_wave_barrier();
+      for (int c = 0; c < OWN; ++c) {
+        dp[c] = id[c] < 0 ? 0.f : (dp[c] - dot) * inv;
+        own = fmaf(dp[c], of[c], own);
+        if (id[c] >= 0) mine[id[c]] = dp[c];
       }
+      own = sum_lanes<TPR>(own);
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int q = 0; q < PIECES; ++q)
 #pragma unroll
@@ -479,10 +485,8 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
         }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j >= a.k) break;
-        if (t == j % TPR && id[j] >= 0) mine[id[j]] = 0.f;
-      }
+      for (int c = 0; c < OWN; ++c)
+        if (id[c] >= 0) mine[id[c]] = 0.f;
       __builtin_amdgcn_wave_barrier();
     }
     s += own;
@@ -510,9 +514,7 @@ inline Form form_of(int experts, bool f32) {
   return t >= 2 && t / 2 * 24 >= experts ? Form{24, t / 2} : Form{16, t};
 }
 
-// Threads of a workgroup that adds up probabilities: fewer workgroups leave fewer sums, but beyond two experts to a row a thread has too many registers for two of 512
-constexpr int threads_of(int k) { return k <= 2 ? 512 : 256; }
-constexpr int kGradThreads = 256;
+constexpr int kThreads = 512, kGradThreads = 256;
 inline int64_t blocks_for(int64_t rows, int experts, bool f32, int threads, int64_t most) {
   const int64_t per = threads / form_of(experts, f32).threads, blocks = (rows + per - 1) / per;
   return blocks < most ? blocks : most;
@@ -520,7 +522,7 @@ inline int64_t blocks_for(int64_t rows, int experts, bool f32, int threads, int6
 
 template <typename T, int TPR, int PER, int K>
 void launch(const RouteArgs& a, unsigned blocks, hipStream_t stream) {
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_kernel<T, TPR, PER, K, threads_of(K)>), dim3(blocks), dim3(threads_of(K)), 0, stream, a);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(route_kernel<T, TPR, PER, K, kThreads>), dim3(blocks), dim3(kThreads), 0, stream, a);
 }
 template <typename T, int TPR, int PER, int K>
 void launch(const RouteGradArgs& a, unsigned blocks, hipStream_t stream) {

@@ -3,40 +3,59 @@
 
 namespace {
 
-// What the workgroups left, in order: 64 experts to a workgroup, 16 threads to an expert; the last one that is through adds up their parts of the loss.
-constexpr int kJoinThreads = 1024, kJoinParts = kJoinThreads / 64;
+// What the workgroups left, in order: 16 experts to a workgroup, 64 threads to an expert; the last workgroup that is through adds up their parts of the loss.
+constexpr int kJoinThreads = 1024, kJoinExperts = 16, kJoinParts = kJoinThreads / kJoinExperts;
 __global__ __launch_bounds__(kJoinThreads) void route_join_kernel(RouteArgs a, int blocks) {
-  __shared__ double sum_of[kJoinParts][64];
-  __shared__ int64_t number_of[kJoinParts][64];
+  __shared__ double sum_of[kJoinParts / 4][kJoinExperts];
+  __shared__ int64_t number_of[kJoinParts / 4][kJoinExperts];
   __shared__ int turn;
-  const int lane = threadIdx.x & 63, part = threadIdx.x >> 6, e = (int)blockIdx.x * 64 + lane;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = threadIdx.x / kJoinExperts, e = (int)blockIdx.x * kJoinExperts + lane % kJoinExperts;
   double s = 0.0;
   int64_t n = 0;
   if (e < a.experts) {
-#pragma unroll 16
+#pragma unroll 8
     for (int b = part; b < blocks; b += kJoinParts) {
       const float2 v = a.sums[(int64_t)b * a.experts + e];
       s += v.x;
       n += __float_as_int(v.y);
     }
   }
-  sum_of[part][lane] = s;
-  number_of[part][lane] = n;
-  __syncthreads();
-  if (part > 0) return;
-  for (int p = 1; p < kJoinParts; ++p) {
-    s += sum_of[p][lane];
-    n += number_of[p][lane];
-  }
-  if (e < a.experts) a.counts[e] = n;
-  double loss = s * (double)n;
-  int64_t with = 0;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    loss += __shfl_xor(loss, o, 64);
+  for (int o = kJoinExperts; o < 64; o <<= 1) {
+    s += __shfl_xor(s, o, 64);
     n += __shfl_xor(n, o, 64);
   }
-  if (gridDim.x > 1) {
+  if (lane < kJoinExperts) {
+    sum_of[wave][lane] = s;
+    number_of[wave][lane] = n;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  s = 0.0;
+  n = 0;
+  if (lane < kJoinExperts) {
+#pragma unroll
+    for (int p = 0; p < kJoinParts / 4; ++p) {
+      s += sum_of[p][lane];
+      n += number_of[p][lane];
+    }
+  }
+  if (lane < kJoinExperts && e < a.experts) a.counts[e] = n;
+  double loss = s * (double)n;
+  int64_t with = 0;
+#pragma unroll 4
+  for (int b = lane; b < blocks; b += 64) with += a.with[b];
+  const auto add_up = [&]() {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      loss += __shfl_xor(loss, o, 64);
+      n += __shfl_xor(n, o, 64);
+    }
+  };
+  add_up();
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) with += __shfl_xor(with, o, 64);
+  if (gridDim.x > 1) {   // (at most 64 workgroups: 1,024 experts)
     if (lane == 0) {
       a.losses[blockIdx.x] = loss;
       a.numbers[blockIdx.x] = n;
@@ -45,47 +64,36 @@ __global__ __launch_bounds__(kJoinThreads) void route_join_kernel(RouteArgs a, i
     }
     if (__builtin_amdgcn_readfirstlane(turn) != (int)gridDim.x - 1) return;
     __threadfence();
-    loss = 0.0;
-    n = 0;
-    for (int g = 0; g < (int)gridDim.x; ++g) {
-      loss += __hip_atomic_load(&a.losses[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      n += __hip_atomic_load(&a.numbers[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    const bool there = lane < (int)gridDim.x;
+    loss = there ? __hip_atomic_load(&a.losses[lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+    n = there ? __hip_atomic_load(&a.numbers[lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+    add_up();
   }
-  for (int b = lane; b < blocks; b += 64) with += a.with[b];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) with += __shfl_xor(with, o, 64);
   if (lane == 0) {
     a.counts[a.experts] = with;
     *a.loss = (float)(loss * a.experts / ((double)(n > 0 ? n : 1) * (double)(with > 0 ? with : 1)));
   }
 }
 
-// Workgroups that leave sums: 16 waves to a compute unit, or 12 of more than two experts to a row. One takes up to two rounds of rows by itself, and nothing is
-// left to add up.
-constexpr int64_t kAlone = 2;
-int64_t sum_blocks(int64_t rows, int experts, bool f32, int k) {
-  const int64_t b = blocks_for(rows, experts, f32, threads_of(k), k <= 2 ? 512 : 768);
+// Workgroups that leave sums: two to a compute unit. One takes up to two rounds of rows by itself, and nothing is left to add up.
+constexpr int64_t kMostBlocks = 512, kAlone = 2;
+int64_t sum_blocks(int64_t rows, int experts, bool f32) {
+  const int64_t b = blocks_for(rows, experts, f32, kThreads, kMostBlocks);
   return b <= kAlone ? 1 : b;
 }
-int join_blocks(int experts) { return (experts + 63) / 64; }
+int join_blocks(int experts) { return (experts + kJoinExperts - 1) / kJoinExperts; }
 
 }  // namespace
 
-// (of the type and number of experts to a row that have the most workgroups)
+// (of the type that has more workgroups)
 int64_t ds_route_bytes(int64_t rows, int experts) {
-  int64_t blocks = 1;
-  for (int f32 = 0; f32 < 2; ++f32)
-    for (int k = 2; k < 4; ++k) {
-      const int64_t b = sum_blocks(rows, experts, f32, k);
-      blocks = b > blocks ? b : blocks;
-    }
+  const int64_t a = sum_blocks(rows, experts, true), b = sum_blocks(rows, experts, false), blocks = a > b ? a : b;
   return blocks > 1 ? join_blocks(experts) * 16 + blocks * (2 * (int64_t)experts + 1) * 4 + 4 : 0;
 }
 
 int ds_launch_route(ds_ctx* ctx, int dtype, int64_t rows, int experts, int k, int renorm, ds_rows x, int32_t* ids, float* weights, int64_t* counts, float* loss,
                     float* lse, void* workspace) {
-  const int64_t blocks = sum_blocks(rows, experts, dtype == DS_ELEM_F32, k);
+  const int64_t blocks = sum_blocks(rows, experts, dtype == DS_ELEM_F32);
   const int joins = join_blocks(experts);
   RouteArgs a = {};
   a.rows = rows;

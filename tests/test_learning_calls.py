@@ -10,7 +10,7 @@ from tests.test_feature_calls import P, _context, ctx  # noqa: F401
 torch = pytest.importorskip("torch")
 
 EMBED = dict(dtype=1, table_dtype=0, rows=5, cols=8, vocab=7, table=P, ts=8, ids=P, scale=1.0, y=P, ys=8)
-EMBED_BACKWARD = dict(dtype=1, table_dtype=0, rows=5, cols=8, vocab=7, dy=P, dys=8, ids=P, scale=1.0, dtable=P, dts=8, ws=P, wsn=1 << 20)
+EMBED_BACKWARD = dict(dtype=1, table_dtype=0, rows=100_000, cols=8, vocab=7, dy=P, dys=8, ids=P, scale=1.0, dtable=P, dts=8, ws=P, wsn=1 << 30)
 ROUTE = dict(dtype=1, rows=100_000, experts=9, k=2, renorm=0, x=P, xs=9, ids=P, weights=P, counts=P, loss=P, lse=None, ws=P, wsn=1 << 20)
 ROUTE_BACKWARD = dict(dtype=1, rows=5, experts=9, k=2, renorm=1, x=P, xs=9, lse=P, ids=P, counts=P, dweights=P, dloss=P, dx=P, dxs=9)
 PACK = dict(dtype=0, rows=5, cols=40, x=P, xs=40, codes=P, cs=40, scales=P, ss=2)
@@ -51,7 +51,7 @@ def test_bad_arguments_are_refused_before_any_work(ctx, name, good, bad):  # noq
 
 
 @pytest.mark.parametrize("name, good, sizes", [
-    ("ds_embed_backward", EMBED_BACKWARD, (5, 8, 7)), ("ds_route", ROUTE, (100_000, 9)),
+    ("ds_embed_backward", EMBED_BACKWARD, (100_000, 8, 7)), ("ds_route", ROUTE, (100_000, 9)),
 ])
 def test_a_workspace_that_is_too_small_is_refused(ctx, name, good, sizes):  # noqa: F811
     lib = binding.load_library()
