@@ -96,7 +96,8 @@ struct SortArgs {
   int2* to;
   int rows, vocab, shift, bits, per_wave;
   int32_t* counts;          // [block][digits], and behind them the digits' rows
-  uint8_t* seen;            // [vocab], cleared by the first launch
+  uint8_t* seen;            // [vocab], cleared by the first launch, set by the last pass where an id comes up
+  bool mark;                // this is the last pass
 };
 
 __device__ __forceinline__ int2 pair_at(const SortArgs& a, int at) {
@@ -221,6 +222,7 @@ __device__ __forceinline__ void place_pairs(const SortArgs& a, int block, int bl
     if (there) {
       const int rank = __popcll(same & ((1ull << lane) - 1)), at = mine[digit];
       a.to[at + rank] = now;
+      if (a.mark && now.x < a.vocab) a.seen[now.x] = 1;
       if (rank == 0) mine[digit] = at + __popcll(same);   // (a wave's LDS accesses keep their order)
     }
   }
@@ -232,30 +234,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a) {
   place_pairs(a, (int)blockIdx.x, (int)gridDim.x, count, wave_sum);
 }
 
-// All passes of few rows in one workgroup; the others clear what is to be cleared
-__global__ __launch_bounds__(kSortThreads) void sort_few_kernel(SortArgs a, int2* other, int passes) {
-  extern __shared__ int count[];
-  __shared__ int wave_sum[kSortWaves];
-  if (blockIdx.x > 0) {
-    for (int64_t i = ((int64_t)(blockIdx.x - 1) * kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)(gridDim.x - 1) * kSortThreads * 16)
-      *reinterpret_cast<uint4*>(a.seen + i) = uint4{0, 0, 0, 0};
-    return;
-  }
-  int2* to = a.to;
-  for (int p = 0; p < passes; ++p) {
-    a.to = (passes - 1 - p) & 1 ? other : to;
-    place_pairs(a, 0, 1, count, wave_sum);
-    a.ids = nullptr;
-    a.from = a.to;
-    a.shift += a.bits;
-    __syncthreads();
-  }
+__global__ __launch_bounds__(kThreads) void clear_kernel(uint8_t* seen, int vocab) {
+  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 16; i < vocab; i += (int64_t)gridDim.x * kThreads * 16)
+    *reinterpret_cast<uint4*>(seen + i) = uint4{0, 0, 0, 0};   // (its end is rounded up to 16 bytes)
 }
 
 // ---- the sums -----------------------------------------------------------------------------------------------------------------------------
 
 struct SumArgs {
-  int rows, cols, vocab, chunk, chunks, calls;
+  int rows, cols, vocab, share, chunk, chunks, calls;   // rows of a worker, and of a workgroup
   const int2* pairs;
   const int32_t* ids;   // few rows: not sorted yet
   int range;            //   and the ids of a workgroup
@@ -266,7 +253,7 @@ struct SumArgs {
   uint8_t* seen;
   float* partial;       // [chunk][2][cols]: of the id that began before the chunk; of the one that goes on behind it
   int64_t rows_step;    // the pass over the table: how far a thread's next piece is
-  int calls_step;
+  int calls_step, clears;   // and its workgroups
 };
 
 constexpr int kRowsAhead = 8;
@@ -325,40 +312,22 @@ __device__ __forceinline__ void sum_rows(int begin, int end, int col, int cols, 
   leave(key, sum, first, true);
 }
 
-// LANES threads take a stretch of `chunk` sorted rows, a piece of 16 bytes of their columns to a thread
-template <typename D, typename T, int LANES, bool TINY>
-__global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
-  constexpr int N = Piece<D>::N;
-  const int chunk = (int)blockIdx.x * (kThreads / LANES) + (int)threadIdx.x / LANES, col = ((int)blockIdx.y * LANES + (int)threadIdx.x % LANES) * N;
-  const int begin = (int)min((int64_t)chunk * a.chunk, (int64_t)a.rows), end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
-  if (begin >= end || col >= a.cols) return;
-  const int have = a.cols - col;
-  T* dtable = (T*)a.dtable + col;
-  float* partial = a.partial + (int64_t)chunk * 2 * a.cols + col;
-  const bool before = begin > 0 && a.pairs[begin - 1].x == a.pairs[begin].x;   // the first id began before the chunk
-  const bool after = end < a.rows && a.pairs[end].x == a.pairs[end - 1].x;     // the last one goes on behind it
-  sum_rows<D, TINY>(begin, end, col, a.cols, (const D*)a.dy, a.dys, a.vocab, [&](int i) { return a.pairs[i]; },
-                    [&](int key, const float(&sum)[N], bool first, bool last) {
-                      const bool goes_on = last && after, began = first && before;
-                      if (key >= a.vocab) return;
-                      if (goes_on || began) store_sums<float, N>(partial + (goes_on ? a.cols : 0), sum, 1.f, have);
-                      else store_sums<T, N>(dtable + (int64_t)key * a.dts, sum, a.scale, have);
-                      if (!began && col == 0) a.seen[key] = 1;
-                    });
-}
-
-// Adds up what the chunks left of ids that reach over a chunk's end: a workgroup looks at kJoinChunks chunks, 64 columns, 16 threads to an id of up to kShort
-// chunks, all of them to a longer one. The workgroups behind `joins` clear the rows of ids that did not come up.
-constexpr int kJoinThreads = 512, kJoinChunks = 64, kJoinCols = 64, kJoinLanes = kJoinCols / 4, kJoinWorkers = kJoinThreads / kJoinLanes, kShort = 8;
+// Clears the rows of ids that did not come up
 template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int joins, int col_tiles) {
-  constexpr int N = Piece<T>::N;
-  if ((int)blockIdx.x >= joins) {
-    const int64_t first = (int64_t)((int)blockIdx.x - joins) * kJoinThreads + threadIdx.x;
-    int64_t row = first / a.calls;
-    int call = (int)(first % a.calls);
-    while (row < a.vocab) {
-      if (!a.seen[row]) store_piece<T>((T*)a.dtable + row * a.dts + call * N, PieceV<T>{}, a.cols - call * N);
+__device__ __forceinline__ void clear_rows(const SumArgs& a, int block) {
+  constexpr int N = Piece<T>::N, AHEAD = 4;
+  const int64_t first = (int64_t)block * kThreads + threadIdx.x;
+  int64_t row = first / a.calls;
+  int call = (int)(first % a.calls);
+  while (row < a.vocab) {
+    int64_t at[AHEAD];
+    int col[AHEAD];
+    bool empty[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      at[j] = row;
+      col[j] = call * N;
+      empty[j] = row < a.vocab && !a.seen[row];
       row += a.rows_step;
       call += a.calls_step;
       if (call >= a.calls) {
@@ -366,41 +335,153 @@ __global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int joi
         ++row;
       }
     }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (empty[j]) store_piece<T>((T*)a.dtable + at[j] * a.dts + col[j], PieceV<T>{}, a.cols - col[j]);
+  }
+}
+
+// LANES threads take a.share sorted rows, a piece of 16 bytes of their columns to a thread, and a workgroup a chunk: sums of ids that reach over a share's end meet in
+// LDS, those of ids that reach over the chunk's go to memory. The first workgroups of the launch clear the rows of ids that did not come up beside it.
+// Bound by memory: 1,000,175 rows of 128 bf16 into 50,021 of fp32 59 us, 4.9 TB/s.
+template <typename D, typename T, int LANES, bool TINY>
+__global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
+  constexpr int N = Piece<D>::N, WORKERS = kThreads / LANES;
+  __shared__ float meet[WORKERS][2][LANES * N];
+  __shared__ bool through[WORKERS];   // one id has all of a worker's rows, and more on both sides
+  if ((int)blockIdx.x < a.clears) {
+    if (blockIdx.y == 0) clear_rows<T>(a, (int)blockIdx.x);
     return;
   }
-  __shared__ int of_short[kJoinChunks], of_long[kJoinChunks], last_of[kJoinChunks], shorts, longs, last;
+  const int chunk = (int)blockIdx.x - a.clears, worker = (int)threadIdx.x / LANES, place = (int)threadIdx.x % LANES * N;
+  const int col = (int)blockIdx.y * LANES * N + place, have = a.cols - col;
+  const int64_t first_row = (int64_t)chunk * a.chunk + worker * a.share;
+  const int begin = (int)min(first_row, (int64_t)a.rows), end = a.rows - begin < a.share ? a.rows : begin + a.share;
+  T* dtable = (T*)a.dtable + col;
+  bool before = false, after = false, whole = false;
+  int key = 0;
+  if (begin < end) {
+    const int first_key = a.pairs[begin].x;
+    key = a.pairs[end - 1].x;
+    before = begin > 0 && a.pairs[begin - 1].x == first_key && first_key < a.vocab;   // the first id began before the share
+    after = end < a.rows && a.pairs[end].x == key && key < a.vocab;                   // the last one goes on behind it
+    whole = before && after && first_key == key;
+    if (have > 0)
+      sum_rows<D, TINY>(begin, end, col, a.cols, (const D*)a.dy, a.dys, a.vocab, [&](int i) { return a.pairs[i]; },
+                        [&](int id, const float(&sum)[N], bool first, bool last) {
+                          const bool goes_on = last && after, began = first && before;
+                          if (goes_on || began) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) meet[worker][goes_on][place + i] = sum[i];
+                          } else {
+                            store_sums<T, N>(dtable + (int64_t)id * a.dts, sum, a.scale, have);
+                          }
+                        });
+  }
+  if (place == 0) through[worker] = whole;
+  __syncthreads();
+  if (have <= 0) return;
+  float* partial = a.partial + (int64_t)chunk * 2 * a.cols + col;
+  float sum[N];
+  const auto take = [&](int w, int slot, bool more) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = more ? sum[i] + meet[w][slot][place + i] : meet[w][slot][place + i];
+  };
+  // the chunk's first id, where it began before and ends in the first share
+  if (worker == 0 && before && !whole) {
+    take(0, 0, false);
+    store_sums<float, N>(partial, sum, 1.f, have);
+  }
+  // an id that goes on behind a share: its first worker here adds it up
+  if (after && (worker == 0 || !whole)) {
+    take(worker, 1, false);
+    int w = worker + 1;
+    while (w < WORKERS && through[w]) take(w++, 1, true);
+    // (in the last share it goes on behind the chunk; else it ends in share w)
+    if (w < WORKERS) {
+      take(w, 0, true);
+      if (whole) store_sums<float, N>(partial, sum, 1.f, have);
+      else store_sums<T, N>(dtable + (int64_t)key * a.dts, sum, a.scale, have);
+    } else {
+      store_sums<float, N>(partial + a.cols, sum, 1.f, have);
+    }
+  }
+}
+
+// Adds up what the chunks left of ids that reach over a chunk's end: a workgroup looks at kJoinChunks chunks, kJoinCols columns, kJoinLanes threads to an id of up to kShort
+// chunks, all of them to a longer one.
+constexpr int kJoinThreads = 512, kJoinChunks = 64, kJoinCols = 32, kJoinLanes = kJoinCols / 4, kJoinWorkers = kJoinThreads / kJoinLanes, kShort = 32;
+template <typename T>
+__global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int col_tiles) {
+  __shared__ int of_short[kJoinChunks], of_long[kJoinChunks], last_of[kJoinChunks], key_of[kJoinChunks], shorts, longs, last;
   __shared__ float meet[kJoinWorkers][kJoinCols];
   const int base = (int)blockIdx.x / col_tiles * kJoinChunks, col = (int)blockIdx.x % col_tiles * kJoinCols + (int)threadIdx.x % kJoinLanes * 4;
   const int worker = (int)threadIdx.x / kJoinLanes, have = a.cols - col;
   if (threadIdx.x == 0) shorts = longs = 0;
-  __syncthreads();
   if ((int)threadIdx.x < kJoinChunks) {
-    // the id that begins in this chunk and goes on behind it
+    // the id that begins in this chunk and goes on behind it; -1: none
     const int chunk = base + (int)threadIdx.x, begin = chunk < a.chunks ? chunk * a.chunk : a.rows;
+    int found = -1;
     if (a.rows - begin > a.chunk) {
-      const int end = begin + a.chunk, key = a.pairs[end - 1].x;
-      if (key < a.vocab && a.pairs[end].x == key && !(begin > 0 && a.pairs[begin - 1].x == key)) {
-        int c = chunk + 1;   // the last chunk that it has rows in, as far as kShort
-        while (c - chunk < kShort && c + 1 < a.chunks && a.pairs[(c + 1) * a.chunk].x == key) ++c;
-        if (c - chunk < kShort) {
-          last_of[threadIdx.x] = c;
-          of_short[atomicAdd(&shorts, 1)] = (int)threadIdx.x;   // (in any order: each has a result of its own)
-        } else {
-          of_long[atomicAdd(&longs, 1)] = (int)threadIdx.x;
-        }
+      const int end = begin + a.chunk, key = a.pairs[end - 1].x, behind = a.pairs[end].x, before = begin > 0 ? a.pairs[begin - 1].x : -1;
+      if (key < a.vocab && behind == key && before != key) found = key;
+    }
+    key_of[threadIdx.x] = found;
+  }
+  __syncthreads();
+  {
+    // how far it goes, as far as kShort chunks: a wave looks at eight of the workgroup's chunks
+    constexpr int EACH = kJoinChunks / (kJoinThreads / 64);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int start[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int chunk = base + wave * EACH + j + 1 + lane;
+      start[j] = key_of[wave * EACH + j] >= 0 && chunk < a.chunks ? a.pairs[chunk * a.chunk].x : -2;
+    }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int c = wave * EACH + j;
+      const unsigned long long other = __ballot(start[j] != key_of[c]);
+      const int chunks = other ? __ffsll((long long)other) - 1 : 64;
+      if (lane == 0 && key_of[c] >= 0) {
+        last_of[c] = base + c + chunks;
+        if (chunks < kShort) of_short[atomicAdd(&shorts, 1)] = c;   // (in any order: each has a result of its own)
+        else of_long[atomicAdd(&longs, 1)] = c;
       }
     }
   }
   __syncthreads();
-  const auto add = [&](float (&sum)[4], int chunk, int slot) __attribute__((always_inline)) {
-    const float* p = a.partial + ((int64_t)chunk * 2 + slot) * a.cols + col;
-    if (have >= 4) {
-      const Elements<float, 4>::V v = *reinterpret_cast<const Elements<float, 4>::U*>(p);
+  // the sums of chunks from, from + step, .. upto, eight on their way at a time; a row's last columns are read where four end, and moved to their place
+  const int at = have >= 4 ? col : max(a.cols - 4, 0), by = col - at;
+  const auto add = [&](float (&sum)[4], int from, int upto, int step) __attribute__((always_inline)) {
+    for (int c = from; c <= upto; c += 8 * step) {
+      Elements<float, 4>::V v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] += v[i];
-    } else {
+      for (int j = 0; j < 8; ++j) {
+        const int chunk = min(c + j * step, upto);
+        const float* p = a.partial + ((int64_t)chunk * 2 + (chunk < upto)) * a.cols + at;
+        if (a.cols >= 4) {
+          v[j] = *reinterpret_cast<const Elements<float, 4>::U*>(p);
+        } else {
 #pragma unroll
-      for (int i = 0; i < 3; ++i) sum[i] += i < have ? p[i] : 0.f;
+          for (int i = 0; i < 3; ++i) v[j][i] = i < a.cols ? p[i] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j * step <= upto) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] += v[j][i];
+        }
+    }
+    if (have > 0 && have < 4 && a.cols >= 4) {
+#pragma unroll
+      for (int s = 1; s < 4; ++s)
+        if (by >= s) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) sum[i] = sum[i + 1];
+        }
     }
   };
   const auto leave = [&](const float (&sum)[4], int key) __attribute__((always_inline)) {
@@ -410,25 +491,30 @@ __global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int joi
       if (i < have) to[i] = (T)(sum[i] * a.scale);
   };
   for (int s = worker; s < shorts; s += kJoinWorkers) {
-    const int chunk = base + of_short[s], upto = last_of[of_short[s]];
+    const int c = of_short[s];
     float sum[4] = {};
-#pragma unroll 4
-    for (int c = chunk; c < upto; ++c) add(sum, c, 1);
-    add(sum, upto, 0);
-    leave(sum, a.pairs[(chunk + 1) * a.chunk].x);
+    add(sum, base + c, last_of[c], 1);
+    leave(sum, key_of[c]);
   }
   for (int l = 0; l < longs; ++l) {
-    const int chunk = base + of_long[l], key = a.pairs[(chunk + 1) * a.chunk].x;
+    const int chunk = base + of_long[l], key = key_of[of_long[l]];
     if (threadIdx.x == 0) last = 0;
     __syncthreads();
-    int upto = chunk + 1;
-    for (int c = chunk + 1 + (int)threadIdx.x; c < a.chunks && a.pairs[c * a.chunk].x == key; c += kJoinThreads) upto = c;
+    int upto = last_of[of_long[l]];
+    for (int c = upto + 1 + (int)threadIdx.x; c < a.chunks; c += 4 * kJoinThreads) {
+      int start[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) start[j] = c + j * kJoinThreads < a.chunks ? a.pairs[(c + j * kJoinThreads) * a.chunk].x : -2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (start[j] == key) upto = c + j * kJoinThreads;
+      if (start[3] != key) break;
+    }
     atomicMax(&last, upto);
     __syncthreads();
     upto = last;
     float sum[4] = {};
-#pragma unroll 8
-    for (int c = chunk + worker; c <= upto; c += kJoinWorkers) add(sum, c, c < upto);
+    add(sum, chunk + worker, upto, kJoinWorkers);
 #pragma unroll
     for (int i = 0; i < 4; ++i) meet[worker][(int)threadIdx.x % kJoinLanes * 4 + i] = sum[i];
     __syncthreads();
@@ -547,8 +633,8 @@ __global__ __launch_bounds__(kFewThreads) void few_sums_kernel(SumArgs a) {
   }
 }
 
-// rows of a chunk: enough chunks for the card, each long enough to be worth its partial sums
-int chunk_of(int rows) {
+// rows of a worker: enough workers for the card
+int share_of(int rows) {
   int c = 16;
   while (c < 256 && (rows + c - 1) / c > 16384) c *= 2;
   return c;
@@ -576,7 +662,7 @@ struct Layout {
 Layout layout_of(int rows, int cols, int vocab) {
   int passes;
   const int bits = digits_of(vocab, &passes), blocks = sort_blocks(rows);
-  const int64_t chunks = (rows + chunk_of(rows) - 1) / chunk_of(rows);
+  const int64_t least = 4 * share_of(rows), chunks = (rows + least - 1) / least;   // (four workers to a workgroup at the least)
   Layout l = {};
   if (few_range(rows, cols, vocab)) return l;
   int64_t at = 0;
@@ -609,53 +695,52 @@ int sort_ids(ds_ctx* ctx, const int32_t* ids, int rows, int vocab, int2* pairs, 
   if (lds > 48 * 1024) {
     DS_HIP(ctx, hipFuncSetAttribute((const void*)sort_count_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     DS_HIP(ctx, hipFuncSetAttribute((const void*)sort_place_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    DS_HIP(ctx, hipFuncSetAttribute((const void*)sort_few_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   }
-  if (blocks == 1) {
-    const int64_t clear = ((int64_t)vocab + 16 * kSortThreads - 1) / (16 * kSortThreads);
-    a.to = pairs;
-    hipLaunchKernelGGL(sort_few_kernel, dim3(1 + (unsigned)(clear < 2 * ctx->num_cus ? clear : 2 * ctx->num_cus)), dim3(kSortThreads), lds, ctx->stream, a, other, passes);
-  } else {
-    for (int p = 0; p < passes; ++p) {
-      a.to = (passes - 1 - p) & 1 ? other : pairs;
+  for (int p = 0; p < passes; ++p) {
+    a.to = (passes - 1 - p) & 1 ? other : pairs;
+    a.mark = p == passes - 1;
+    if (blocks > 1) {
       hipLaunchKernelGGL(sort_count_kernel, dim3(blocks), dim3(kSortThreads), lds, ctx->stream, a, p == 0);
       hipLaunchKernelGGL(sort_before_kernel, dim3(((1 << a.bits) + 63) / 64), dim3(kSortThreads), 0, ctx->stream, a, blocks);
-      hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(kSortThreads), lds, ctx->stream, a);
-      a.ids = nullptr;
-      a.from = a.to;
-      a.shift += a.bits;
+    } else if (p == 0) {
+      const int64_t clear = ((int64_t)vocab + 16 * kThreads - 1) / (16 * kThreads), most = 8 * (int64_t)ctx->num_cus;
+      hipLaunchKernelGGL(clear_kernel, dim3((unsigned)(clear < most ? clear : most)), dim3(kThreads), 0, ctx->stream, seen, vocab);
     }
+    hipLaunchKernelGGL(sort_place_kernel, dim3(blocks), dim3(kSortThreads), lds, ctx->stream, a);
+    a.ids = nullptr;
+    a.from = a.to;
+    a.shift += a.bits;
   }
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
 
 template <typename D, typename T, int LANES>
-void launch_sum(const SumArgs& a, hipStream_t stream) {
-  constexpr int N = Piece<D>::N, WORKERS = kThreads / LANES;
-  const dim3 grid((a.chunks + WORKERS - 1) / WORKERS, (a.cols + LANES * N - 1) / (LANES * N)), block(kThreads);
+void launch_sum(SumArgs& a, hipStream_t stream) {
+  constexpr int N = Piece<D>::N;
+  a.chunk = a.share * (kThreads / LANES);
+  a.chunks = (a.rows + a.chunk - 1) / a.chunk;
+  const dim3 grid(a.clears + a.chunks, (a.cols + LANES * N - 1) / (LANES * N)), block(kThreads);
   if (a.cols < N) hipLaunchKernelGGL(HIP_KERNEL_NAME(sum_kernel<D, T, LANES, true>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL(HIP_KERNEL_NAME(sum_kernel<D, T, LANES, false>), grid, block, 0, stream, a);
 }
 
 template <typename D, typename T>
 int launch_sums(ds_ctx* ctx, SumArgs& a) {
-  const int pieces = (a.cols + Piece<D>::N - 1) / Piece<D>::N;
-  if (a.rows > 0) {
-    if (pieces <= 8) launch_sum<D, T, 8>(a, ctx->stream);
-    else if (pieces <= 16) launch_sum<D, T, 16>(a, ctx->stream);
-    else if (pieces <= 32) launch_sum<D, T, 32>(a, ctx->stream);
-    else launch_sum<D, T, 64>(a, ctx->stream);
-  }
   a.calls = (a.cols + Piece<T>::N - 1) / Piece<T>::N;
-  const int64_t all = (int64_t)a.vocab * a.calls, want = (all + kJoinThreads - 1) / kJoinThreads, most = 4 * (int64_t)ctx->num_cus;
-  const int64_t clears = want < most ? want : most, step = clears * kJoinThreads;
+  const int64_t all = (int64_t)a.vocab * a.calls, want = (all + kThreads - 1) / kThreads, most = 4 * (int64_t)ctx->num_cus;
+  a.clears = (int)(want < most ? want : most);
+  const int64_t step = (int64_t)a.clears * kThreads;
   a.rows_step = step / a.calls;
   a.calls_step = (int)(step % a.calls);
-  const int col_tiles = (a.cols + kJoinCols - 1) / kJoinCols;
+  const int pieces = (a.cols + Piece<D>::N - 1) / Piece<D>::N, col_tiles = (a.cols + kJoinCols - 1) / kJoinCols;
+  if (pieces <= 8) launch_sum<D, T, 8>(a, ctx->stream);
+  else if (pieces <= 16) launch_sum<D, T, 16>(a, ctx->stream);
+  else if (pieces <= 32) launch_sum<D, T, 32>(a, ctx->stream);
+  else launch_sum<D, T, 64>(a, ctx->stream);
   const int64_t joins = (int64_t)((a.chunks + kJoinChunks - 1) / kJoinChunks) * col_tiles;
-  if (joins + clears > ds_most_workgroups(kJoinThreads)) return ds_fail(ctx, DS_EINVAL, "%d rows of %d columns are more than a launch has", a.rows, a.cols);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(finish_kernel<T>), dim3((unsigned)(joins + clears)), dim3(kJoinThreads), 0, ctx->stream, a, (int)joins, col_tiles);
+  if (joins > ds_most_workgroups(kJoinThreads)) return ds_fail(ctx, DS_EINVAL, "%d rows of %d columns are more than a launch has", a.rows, a.cols);
+  if (a.chunks > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(finish_kernel<T>), dim3((unsigned)joins), dim3(kJoinThreads), 0, ctx->stream, a, col_tiles);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
@@ -709,8 +794,7 @@ int ds_launch_embed_backward(ds_ctx* ctx, int dtype, int table_dtype, int rows, 
   a.rows = rows;
   a.cols = cols;
   a.vocab = vocab;
-  a.chunk = chunk_of(rows);
-  a.chunks = (rows + a.chunk - 1) / a.chunk;
+  a.share = share_of(rows);
   a.pairs = pairs;
   a.dy = dy.data;
   a.dys = dy.stride;
