@@ -118,14 +118,21 @@ __device__ __forceinline__ Stretch stretch_of(const SortArgs& a, int block) {
   return s;
 }
 
-// counts of the workgroup's rows by wave and digit
-__device__ __forceinline__ void count_digits(const SortArgs& a, int block, int* count) {
+constexpr int kHeld = 4;   // pairs of a thread that stay in its registers between counting and placing: all of them up to about a million rows
+
+// counts of the workgroup's rows by wave and digit; the first kHeld pairs of a thread are left in `held`
+__device__ __forceinline__ void count_digits(const SortArgs& a, const Stretch& s, int* count, int2 (&held)[kHeld]) {
   const int digits = 1 << a.bits, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) held[j] = s.begin + j * 64 + lane < s.end ? pair_at(a, s.begin + j * 64 + lane) : int2{0, 0};
   for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortThreads) count[i] = 0;
   __syncthreads();
   int* mine = count + (threadIdx.x >> 6) * digits;
-  const Stretch s = stretch_of(a, block);
-  for (int at = s.begin + lane; at < s.end; at += 64) atomicAdd(&mine[pair_at(a, at).x >> a.shift & (digits - 1)], 1);   // (whole numbers: any order)
+  const auto add = [&](int key) { atomicAdd(&mine[key >> a.shift & (digits - 1)], 1); };   // (whole numbers: any order)
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (s.begin + j * 64 + lane < s.end) add(held[j].x);
+  for (int at = s.begin + kHeld * 64 + lane; at < s.end; at += 64) add(pair_at(a, at).x);
   __syncthreads();
 }
 
@@ -135,7 +142,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs a, bo
     for (int64_t i = ((int64_t)blockIdx.x * kSortThreads + threadIdx.x) * 16; i < a.vocab; i += (int64_t)gridDim.x * kSortThreads * 16)
       *reinterpret_cast<uint4*>(a.seen + i) = uint4{0, 0, 0, 0};   // (its end is rounded up to 16 bytes)
   const int digits = 1 << a.bits;
-  count_digits(a, (int)blockIdx.x, count);
+  int2 held[kHeld];
+  count_digits(a, stretch_of(a, (int)blockIdx.x), count, held);
   for (int d = threadIdx.x; d < digits; d += kSortThreads) {
     int n = 0;
     for (int w = 0; w < kSortWaves; ++w) n += count[w * digits + d];
@@ -174,18 +182,18 @@ __global__ __launch_bounds__(kSortThreads) void sort_before_kernel(SortArgs a, i
 // pair's rank is a popcount, and pairs of one digit keep their order.
 __device__ __forceinline__ void place_pairs(const SortArgs& a, int block, int blocks, int* count, int* wave_sum) {
   const int digits = 1 << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  count_digits(a, block, count);
   // (digits <= threads: thread d has digit d)
   const int d = (int)threadIdx.x;
   int whole = 0, before = 0;
-  if (d < digits) {
-    if (blocks == 1) {
-      for (int w = 0; w < kSortWaves; ++w) whole += count[w * digits + d];
-    } else {
-      before = a.counts[block * digits + d];
-      whole = a.counts[blocks * digits + d];
-    }
+  if (d < digits && blocks > 1) {
+    before = a.counts[block * digits + d];
+    whole = a.counts[blocks * digits + d];
   }
+  const Stretch s = stretch_of(a, block);
+  int2 held[kHeld];
+  count_digits(a, s, count, held);
+  if (d < digits && blocks == 1)
+    for (int w = 0; w < kSortWaves; ++w) whole += count[w * digits + d];
   int upto = whole;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -207,12 +215,7 @@ __device__ __forceinline__ void place_pairs(const SortArgs& a, int block, int bl
   }
   __syncthreads();
   volatile int* mine = count + wave * digits;
-  const Stretch s = stretch_of(a, block);
-  int2 next = s.begin + lane < s.end ? pair_at(a, s.begin + lane) : int2{0, 0};
-  for (int base = s.begin; base < s.end; base += 64) {
-    const int2 now = next;
-    const bool there = base + lane < s.end;
-    if (base + 64 + lane < s.end) next = pair_at(a, base + 64 + lane);
+  const auto place = [&](int2 now, bool there) __attribute__((always_inline)) {
     const int digit = now.x >> a.shift & (digits - 1);
     unsigned long long same = __ballot(there);
     for (int b = 0; b < a.bits; ++b) {
@@ -225,6 +228,18 @@ __device__ __forceinline__ void place_pairs(const SortArgs& a, int block, int bl
       if (a.mark && now.x < a.vocab) a.seen[now.x] = 1;
       if (rank == 0) mine[digit] = at + __popcll(same);   // (a wave's LDS accesses keep their order)
     }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    if (s.begin + j * 64 >= s.end) return;
+    place(held[j], s.begin + j * 64 + lane < s.end);
+  }
+  const int more = s.begin + kHeld * 64;
+  int2 next = more + lane < s.end ? pair_at(a, more + lane) : int2{0, 0};
+  for (int base = more; base < s.end; base += 64) {
+    const int2 now = next;
+    if (base + 64 + lane < s.end) next = pair_at(a, base + 64 + lane);
+    place(now, base + lane < s.end);
   }
 }
 
