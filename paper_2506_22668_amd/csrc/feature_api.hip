@@ -272,7 +272,7 @@ int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t
   if (!bytes || !known(dtype) || rows < 0 || rows > kMostOrdered || inner < 1 || inner > kMostCols || outer < 1 || outer > kMostCols ||
       groups < 1 || groups > kMostGroups)
     return DS_EINVAL;
-  *bytes = ds_grouped_mm_backward_packed_bytes(dtype, {(int)rows, (int)inner, (int)outer, (int)groups, nullptr, nullptr, nullptr}, gate != 0);
+  *bytes = ds_grouped_mm_backward_bytes(dtype, {(int)rows, (int)inner, (int)outer, (int)groups, nullptr, nullptr, nullptr});
   return DS_OK;
 }
 
@@ -293,7 +293,7 @@ int ds_grouped_mm_backward_packed(ds_ctx* ctx, int32_t dtype, int64_t rows, int6
   DS_TRY(check_rows(ctx, "dw", dw, outer, groups, outer, dtype, true));
   if (!db) return ds_fail(ctx, DS_EINVAL, "db is null");
   const ds_grouped p = {(int)rows, (int)inner, (int)outer, (int)groups, w, offsets, order};
-  DS_TRY(check_workspace(ctx, workspace, workspace_bytes, ds_grouped_mm_backward_packed_bytes(dtype, p, gate != nullptr)));
+  DS_TRY(check_workspace(ctx, workspace, workspace_bytes, ds_grouped_mm_backward_bytes(dtype, p)));
   DS_HIP(ctx, hipSetDevice(ctx->device));
   return ds_launch_grouped_mm_backward_packed(ctx, dtype, p, {dy, dy_stride}, {codes, codes_stride, scales, scales_stride}, gate, gate_stride, {dx, dx_stride}, dw,
                                               db, workspace);

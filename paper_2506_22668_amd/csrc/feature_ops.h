@@ -48,6 +48,5 @@ struct ds_packed {          // rows in 8 bits (packed.h); strides in bytes
 };
 int ds_launch_pack(ds_ctx* ctx, int dtype, int64_t rows, int cols, ds_rows x, const ds_packed& to);
 int ds_launch_unpack(ds_ctx* ctx, int dtype, int64_t rows, int cols, const ds_packed& from, ds_rows y);
-int64_t ds_grouped_mm_backward_packed_bytes(int dtype, const ds_grouped& p, bool gate);
 int ds_launch_grouped_mm_backward_packed(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, const ds_packed& x, const uint8_t* gate, int64_t gate_stride,
                                          ds_rows dx, void* dw, float* db, void* workspace);

@@ -15,6 +15,9 @@ struct MmArgs {
   void* y;            // the product by rows (y, or dx)
   void* dw;
   float* db;
+  // x held in 8 bits (xs: the distance of its rows of codes; the gate is codes too)
+  const uint8_t *codes, *scales;
+  int64_t scales_stride;
 };
 
 // tiles of 2^shift rows that the groups and the rows of none can have: every group may end inside one
@@ -27,3 +30,6 @@ int ds_launch_row_tiles(ds_ctx* ctx, int dtype, bool transposed, MmArgs& a);
 // The gradient of the weights in tiles; partial: ds_weight_tiles_bytes of scratch
 int64_t ds_weight_tiles_bytes(int dtype, int rows, int inner, int outer);
 int ds_launch_weight_tiles(ds_ctx* ctx, int dtype, MmArgs& a, void* partial);
+// The same where x, and the gate, are held in 8 bits (packed_tiles.hip)
+int ds_launch_row_tiles_packed(ds_ctx* ctx, int dtype, MmArgs& a);
+int ds_launch_weight_tiles_packed(ds_ctx* ctx, int dtype, MmArgs& a, void* partial);

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "grouped_mm.h"
+#include "packed.h"
 #include "rows.h"
 
 namespace {
@@ -44,7 +45,7 @@ constexpr int kWaves = 4;   // of a workgroup: they share the contraction
 // the matrix' end, which it can in its last N rows alone, is read so that it ends there, and shifted. (TINY: matrices of less than 16 bytes, element by element.)
 // Bound by reading W, from memory once if a group has one tile of rows: 8 rows in 8 groups by 1,024 x 4,096 bf16 14.1 us, 4.8 TB/s. (64 rows of 16 bits
 // to a workgroup take 130 + 128 registers, dx 136 + 128 or 196 + 68: one wave to a SIMD.)
-template <typename T, int RB, int WAVES, bool TRANSPOSED, bool HALF, bool TINY>
+template <typename T, int RB, int WAVES, bool TRANSPOSED, bool HALF, bool TINY, bool PACKED = false>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
   constexpr int N = Piece<T>::N, SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
   constexpr int COLS = HALF ? N / 2 : N, HALVES = N / COLS, STEP = WAVES * 4 * N * HALVES;   // of a lane's columns, and pieces of each
@@ -143,7 +144,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
           for (int r = 0; r < RB; ++r) acc[r][j] = multiply(wn[j * HALVES + h], xn[r * HALVES + h], acc[r][j]);
     }
   }
-  const T *gate = (const T*)a.gate, *gate_end = gate + (int64_t)(a.rows - 1) * a.gs + width;
+  using Gate = RowGate<T, PACKED>;   // (of dx alone)
+  const typename Gate::E *gate = (const typename Gate::E*)a.gate, *gate_end = gate + (int64_t)(a.rows - 1) * a.gs + width;
   T* y = (T*)a.y;
   // wave w ends up with the four columns' quarter w of every row block: columns col + COLS (4 q + w) .. + COLS - 1
   const int n = col + COLS * (4 * q + (wave & 3));
@@ -151,12 +153,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
 #pragma unroll
   for (int j = 0; j < COLS; ++j)
     bias[j] = !TRANSPOSED && a.bias && gt.group < a.groups ? a.bias[(int64_t)gt.group * width + min(n + j, width - 1)] : 0.f;
-  PieceV<T> open[RB];
+  typename Gate::V open[RB];
   if (TRANSPOSED && gate && wave < 4) {
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-      if constexpr (TINY) open[r] = load_piece<T>(gate + row[r] * a.gs + n, row[r] >= 0 ? width - n : 0);
-      else open[r] = load_within<T>(gate + (row[r] < 0 ? 0 : row[r]) * a.gs + min(n, width - 1), gate_end);
+      if constexpr (TINY) open[r] = Gate::load_first(gate + row[r] * a.gs + n, row[r] >= 0 ? width - n : 0);
+      else open[r] = Gate::load(gate + (row[r] < 0 ? 0 : row[r]) * a.gs + min(n, width - 1), gate_end);
     }
   }
 #pragma unroll
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
 #pragma unroll
         for (int s = 0; s < WAVES; ++s) v += meet[s][wave & 3][lane][j];
         if (!TRANSPOSED && a.relu) v = v < 0.f ? 0.f : v;   // (a NaN stays one)
-        if (TRANSPOSED && gate) v = (float)open[r][j] > 0.f ? v : 0.f;
+        if (TRANSPOSED && gate) v = Gate::is_open(open[r], j) ? v : 0.f;
         out[j] = (T)v;
       }
       T* to = y + row[r] * a.ys + n;
@@ -190,7 +192,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(MmArgs a) {
 // run across the contraction (the rows), so both are turned around in registers. db is one more product, with ones for x. The rows
 // of the next step are looked up, and those of this one's are on their way, while the products of the one before are formed. Bound by the latency of those loads,
 // about 2 us a step, and a group's rows are never cut over workgroups: long groups belong to the tiles.
-template <typename T, bool SHARED, bool TINY>
+template <typename T, bool SHARED, bool TINY, bool PACKED = false>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a) {
   constexpr int N = Piece<T>::N, H = SHARED ? N / 2 : N / 4, STEP = (SHARED ? kWaves : 1) * 4 * N;
   typedef T Half __attribute__((ext_vector_type(H)));
@@ -204,6 +206,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
   ds_group_range(a.offsets, a.groups, a.rows, group, &begin, &end);
   const T *x = (const T*)a.x, *dy = (const T*)a.dy;
   const T *x_end = x + (int64_t)(a.rows - 1) * a.xs + a.inner, *dy_end = dy + (int64_t)(a.rows - 1) * a.dys + a.outer;
+  const uint8_t* codes_end = a.codes + (int64_t)(a.rows - 1) * a.xs + a.inner;
   const int n0 = min(col + N * m, a.outer - 1), c0 = min(in0 + H * m, a.inner - 1);   // the lane's columns
   f32x4 acc[H][N] = {}, sum[N] = {};
   PieceV<T> ones;
@@ -212,7 +215,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
   const bool with_sum = in0 == 0;
   int row[N], late[N];   // of the pieces under way, and of the next ones
   PieceV<T> dp[N];
-  Half xp[N];
+  Half xp[PACKED ? 1 : N];
+  PackedPiece<H> cp[PACKED ? N : 1];   // x held in 8 bits, and its powers
+  uint32_t sp[PACKED ? N : 1];
   const auto look_up = [&](int at) {
 #pragma unroll
     for (int i = 0; i < N; ++i) late[i] = at + N * q + i < end ? ds_ordered_row(a.order, a.rows, at + N * q + i) : -1;
@@ -224,13 +229,25 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
       if constexpr (TINY) {
         dp[i] = load_piece<T>(dy + row[i] * a.dys + col + N * m, row[i] >= 0 ? a.outer - col - N * m : 0);
         const int have = row[i] >= 0 ? a.inner - in0 - H * m : 0;
+        if constexpr (PACKED) {
+          cp[i] = load_first_codes<H>(a.codes + row[i] * a.xs + in0 + H * m, have);
+          sp[i] = have > 0 ? a.scales[row[i] * a.scales_stride + (in0 + H * m) / kPackBlock] : 0;
+        } else {
 #pragma unroll
-        for (int j = 0; j < H; ++j) xp[i][j] = j < have ? x[row[i] * a.xs + in0 + H * m + j] : (T)0.f;
+          for (int j = 0; j < H; ++j) xp[i][j] = j < have ? x[row[i] * a.xs + in0 + H * m + j] : (T)0.f;
+        }
       } else {
         const int r = row[i] < 0 ? 0 : row[i];
-        const T *pd = dy + r * a.dys + n0, *px = x + r * a.xs + c0;
+        const T* pd = dy + r * a.dys + n0;
         dp[i] = *reinterpret_cast<const typename Piece<T>::U*>(pd + N <= dy_end ? pd : dy_end - N);
-        xp[i] = *reinterpret_cast<const HalfU*>(px + H <= x_end ? px : x_end - H);
+        if constexpr (PACKED) {
+          const uint8_t* pc = a.codes + r * a.xs + c0;
+          cp[i] = load_codes<H>(pc + H <= codes_end ? pc : codes_end - H);
+          sp[i] = a.scales[r * a.scales_stride + c0 / kPackBlock];
+        } else {
+          const T* px = x + r * a.xs + c0;
+          xp[i] = *reinterpret_cast<const HalfU*>(px + H <= x_end ? px : x_end - H);
+        }
       }
     }
   };
@@ -247,9 +264,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
       for (int i = 0; i < N; ++i) {
         // (rows that there are not are cleared; pieces that would reach over the end have been read so that they end there)
         const int r = row[i] < 0 ? 0 : row[i];
-        const int64_t by = dy + r * a.dys + n0 + N - dy_end, bx = x + r * a.xs + c0 + H - x_end;
+        const int64_t by = dy + r * a.dys + n0 + N - dy_end;
+        const int64_t bx = PACKED ? a.codes + r * a.xs + c0 + H - codes_end : x + r * a.xs + c0 + H - x_end;
         if (__any(by > 0)) dp[i] = shifted<T>(dp[i], by <= 0 ? 0 : by < N ? (unsigned)by : N);
-        if (__any(bx > 0)) {
+        if constexpr (PACKED) {
+          if (__any(bx > 0)) cp[i] = shifted_codes<H>(cp[i], bx <= 0 ? 0 : bx < H ? (unsigned)bx : H);
+        } else if (__any(bx > 0)) {
           Half moved = xp[i];
 #pragma unroll
           for (int s = 1; s <= H; ++s)
@@ -262,7 +282,8 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
         }
         if (row[i] < 0) {
           dp[i] = PieceV<T>{};
-          xp[i] = Half{};
+          if constexpr (PACKED) cp[i] = 0;
+          else xp[i] = Half{};
         }
       }
     }
@@ -270,8 +291,15 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_weights_kernel(MmArgs a)
     for (int i = 0; i < N; ++i) {
 #pragma unroll
       for (int j = 0; j < N; ++j) dn[j][i] = dp[i][j];
+      if constexpr (PACKED) {
+        T four[4];
+        four_of((uint32_t)cp[i], __uint_as_float(sp[i] << 23), four);
 #pragma unroll
-      for (int j = 0; j < H; ++j) xn[j][i] = xp[i][j];
+        for (int j = 0; j < H; ++j) xn[j][i] = four[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < H; ++j) xn[j][i] = xp[i][j];
+      }
     }
     if (at + STEP < end) {
       fetch();
@@ -369,40 +397,41 @@ int element_of() {
   return sizeof(T) == 4 ? DS_ELEM_F32 : std::is_same<T, __bf16>::value ? DS_ELEM_BF16 : DS_ELEM_F16;
 }
 
-template <typename T, bool TRANSPOSED, bool HALF>
+template <typename T, bool TRANSPOSED, bool HALF, bool PACKED>
 void launch_few(const ds_few_form& form, int64_t workgroups, const MmArgs& a, hipStream_t stream) {
   const dim3 block(64 * kWaves), twice(64 * 8);
   const ds_lines lines = ds_launch_lines(workgroups, 64 * (form.eight_waves ? 8 : kWaves));
   const dim3 grid(lines.x, lines.y);
-  if (form.shift == 4 && form.eight_waves) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
-  else if (form.shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
-  else if (form.shift == 5 && form.eight_waves) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, HALF, false>), dim3(grid), twice, 0, stream, a);
-  else if (form.shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, HALF, false>), dim3(grid), block, 0, stream, a);
+  if (form.shift == 4 && form.eight_waves) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, 8, TRANSPOSED, HALF, false, PACKED>), dim3(grid), twice, 0, stream, a);
+  else if (form.shift == 4) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 1, kWaves, TRANSPOSED, HALF, false, PACKED>), dim3(grid), block, 0, stream, a);
+  else if (form.shift == 5 && form.eight_waves) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, 8, TRANSPOSED, HALF, false, PACKED>), dim3(grid), twice, 0, stream, a);
+  else if (form.shift == 5) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 2, kWaves, TRANSPOSED, HALF, false, PACKED>), dim3(grid), block, 0, stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, HALF, false, PACKED>), dim3(grid), block, 0, stream, a);
 }
 
-template <typename T, bool TRANSPOSED>
+template <typename T, bool TRANSPOSED, bool PACKED = false>
 int launch_rows(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   if (p.rows == 0) return DS_OK;
   hipStream_t stream = ctx->stream;
   // (rows of at least 16 bytes each would not be enough to ask for: an operand may have one row)
   const bool tiny = tiny_matrix<T>(TRANSPOSED ? a.dys : a.xs, p.rows, TRANSPOSED ? p.outer : p.inner) ||
-                    tiny_matrix<T>((int64_t)p.inner * p.outer, p.groups, (int64_t)p.inner * p.outer) || (a.gate && tiny_matrix<T>(a.gs, p.rows, p.inner));
+                    tiny_matrix<T>((int64_t)p.inner * p.outer, p.groups, (int64_t)p.inner * p.outer) || (a.gate && tiny_matrix<T>(a.gs, p.rows, p.inner));   // (codes: the same number of them)
   const int depth = TRANSPOSED ? p.outer : p.inner, width = TRANSPOSED ? p.inner : p.outer;
-  if (ds_rows_in_tiles(sizes(p), element_of<T>(), depth, width)) return ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
+  if (ds_rows_in_tiles(sizes(p), element_of<T>(), depth, width))
+    return PACKED ? ds_launch_row_tiles_packed(ctx, element_of<T>(), a) : ds_launch_row_tiles(ctx, element_of<T>(), TRANSPOSED, a);
   const ds_few_form form = ds_choose_few(sizes(p), element_of<T>(), TRANSPOSED, tiny);
   a.col_tiles = (width + form.cols - 1) / form.cols;
   const int64_t tiles = ds_most_tiles(a, form.shift) * a.col_tiles;
   if (tiles > 0x7fff0000) return ds_fail(ctx, DS_EINVAL, "%d rows by %d columns are more tiles than a launch has", p.rows, width);
   const ds_lines lines = ds_launch_lines(tiles, 64 * kWaves);
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false, true>), dim3(lines.x, lines.y), dim3(64 * kWaves), 0, stream, a);
-  else if (form.half) launch_few<T, TRANSPOSED, TRANSPOSED>(form, tiles, a, stream);
-  else launch_few<T, TRANSPOSED, false>(form, tiles, a, stream);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_kernel<T, 4, kWaves, TRANSPOSED, false, true, PACKED>), dim3(lines.x, lines.y), dim3(64 * kWaves), 0, stream, a);
+  else if (form.half) launch_few<T, TRANSPOSED, TRANSPOSED, PACKED>(form, tiles, a, stream);
+  else launch_few<T, TRANSPOSED, false, PACKED>(form, tiles, a, stream);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
 
-template <typename T>
+template <typename T, bool PACKED>
 int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   constexpr int N = Piece<T>::N;
   a.col_tiles = (p.outer + 16 * N - 1) / (16 * N);
@@ -413,18 +442,19 @@ int launch_weights(ds_ctx* ctx, const ds_grouped& p, MmArgs& a) {
   if (tiles > ds_most_workgroups(64 * kWaves))
     return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", p.inner, p.outer);
   const dim3 grid((unsigned)tiles, p.groups), block(64 * kWaves);
-  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, true>), grid, block, 0, ctx->stream, a);
-  else if (shared) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, false>), grid, block, 0, ctx->stream, a);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, false, false>), grid, block, 0, ctx->stream, a);
+  if (tiny) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, true, PACKED>), grid, block, 0, ctx->stream, a);
+  else if (shared) hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, true, false, PACKED>), grid, block, 0, ctx->stream, a);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(few_rows_weights_kernel<T, false, false, PACKED>), grid, block, 0, ctx->stream, a);
   DS_HIP(ctx, hipGetLastError());
   return DS_OK;
 }
 
-template <typename T>
+template <typename T, bool PACKED>
 int backward(ds_ctx* ctx, const ds_grouped& p, MmArgs& a, void* workspace) {
-  DS_TRY((launch_rows<T, true>(ctx, p, a)));
-  if (ds_weights_in_tiles(sizes(p), element_of<T>())) return ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
-  return launch_weights<T>(ctx, p, a);
+  DS_TRY((launch_rows<T, true, PACKED>(ctx, p, a)));
+  if (ds_weights_in_tiles(sizes(p), element_of<T>()))
+    return PACKED ? ds_launch_weight_tiles_packed(ctx, element_of<T>(), a, workspace) : ds_launch_weight_tiles(ctx, element_of<T>(), a, workspace);
+  return launch_weights<T, PACKED>(ctx, p, a);
 }
 
 }  // namespace
@@ -460,22 +490,27 @@ int ds_launch_grouped_mm_backward(ds_ctx* ctx, int dtype, const ds_grouped& p, d
   a.ys = dx.stride;
   a.dw = dw;
   a.db = db;
-  if (dtype == DS_ELEM_F32) return backward<float>(ctx, p, a, workspace);
-  if (dtype == DS_ELEM_BF16) return backward<__bf16>(ctx, p, a, workspace);
-  return backward<_Float16>(ctx, p, a, workspace);
-}
-
-// Packed rows are unpacked in front of the products
-int64_t ds_grouped_mm_backward_packed_bytes(int dtype, const ds_grouped& p, bool gate) {
-  const int64_t rows = ((int64_t)p.rows * p.inner * (dtype == DS_ELEM_F32 ? 4 : 2) + 15) / 16 * 16;
-  return (gate ? 2 : 1) * rows + ds_grouped_mm_backward_bytes(dtype, p);
+  if (dtype == DS_ELEM_F32) return backward<float, false>(ctx, p, a, workspace);
+  if (dtype == DS_ELEM_BF16) return backward<__bf16, false>(ctx, p, a, workspace);
+  return backward<_Float16, false>(ctx, p, a, workspace);
 }
 
 int ds_launch_grouped_mm_backward_packed(ds_ctx* ctx, int dtype, const ds_grouped& p, ds_rows dy, const ds_packed& x, const uint8_t* gate, int64_t gate_stride,
                                          ds_rows dx, void* dw, float* db, void* workspace) {
-  const int64_t rows = ((int64_t)p.rows * p.inner * (dtype == DS_ELEM_F32 ? 4 : 2) + 15) / 16 * 16;
-  const ds_rows whole = {workspace, p.inner}, open = {(char*)workspace + rows, p.inner};
-  DS_TRY(ds_launch_unpack(ctx, dtype, p.rows, p.inner, x, whole));
-  if (gate) DS_TRY(ds_launch_unpack(ctx, dtype, p.rows, p.inner, {gate, gate_stride, nullptr, 0}, open));
-  return ds_launch_grouped_mm_backward(ctx, dtype, p, dy, whole, gate ? open : ds_rows{nullptr, 0}, dx, dw, db, (char*)workspace + (gate ? 2 : 1) * rows);
+  MmArgs a = arguments(p);
+  a.dy = dy.data;
+  a.dys = dy.stride;
+  a.codes = x.codes;
+  a.xs = x.codes_stride;
+  a.scales = x.scales;
+  a.scales_stride = x.scales_stride;
+  a.gate = gate;
+  a.gs = gate_stride;
+  a.y = (void*)dx.data;
+  a.ys = dx.stride;
+  a.dw = dw;
+  a.db = db;
+  if (dtype == DS_ELEM_F32) return backward<float, true>(ctx, p, a, workspace);
+  if (dtype == DS_ELEM_BF16) return backward<__bf16, true>(ctx, p, a, workspace);
+  return backward<_Float16, true>(ctx, p, a, workspace);
 }

@@ -3,8 +3,6 @@
 // The power is the smallest that leaves the block's finite values at or below 448, so a value is off by at most 2^-4 of itself, or by 2^-10 of that power where it
 // is smaller than 2^-6 of it. Two things are kept exactly: which values are 0, since a ReLU's gate is read from the codes (what would round to 0
 // becomes the smallest code of its sign), and what is finite: no value comes back larger than its type holds, infinities and NaN come back as NaN.
-#include <type_traits>
-
 #include "feature_ops.h"
 #include "packed.h"
 #include "rows.h"
