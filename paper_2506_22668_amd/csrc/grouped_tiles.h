@@ -122,7 +122,7 @@ struct Loader {
         over |= (unsigned)(by <= 0 ? 0 : by < N ? by : N) << (4 * u);
         p = !there ? zeros : by > 0 ? end - N : p;
       }
-      held[u] = *reinterpret_cast<const typename Piece<T>::U*>(p);
+      held[u] = *(const DS_GLOBAL typename Piece<T>::U*)p;   // (a global address, of which the compiler is not sure)
     }
   }
   // into LDS; cut: of each piece its first `keep` elements alone (the contraction ends in it)
@@ -154,8 +154,10 @@ struct PackedLoader {
       scale = there && p < end ? scale : zeros;   // (behind the end: the row's scales may end there)
       p = !there ? zeros : by > 0 ? end - N : p;
     }
-    codes[set][u] = load_codes<N>(p);
-    scales[set][u] = *scale;
+    // (global addresses, all of them, of which the compiler is not sure)
+    typedef PackedPiece<N> U __attribute__((aligned(1)));
+    codes[set][u] = *(const DS_GLOBAL U*)p;
+    scales[set][u] = *(const DS_GLOBAL uint8_t*)scale;
   }
   __device__ __forceinline__ void store(int set, char* stage) {
 #pragma unroll
@@ -586,7 +588,10 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   using DOp = Operand<T, BN, true>;
   constexpr int STAGE = XOp::BYTES + DOp::BYTES, LOADS = STAGE / 16 / THREADS;
   constexpr int LINES = THREADS / DOp::PER_ROW, EACH = DEPTH / LINES;   // of a thread's pieces of a stage: lines apart, and how many
-  __shared__ __attribute__((aligned(128))) char stage0[STAGE], stage1[STAGE], stage2[STAGE], stage3[STAGE];
+  constexpr int RING = 4 * DEPTH;
+  // (x held in 8 bits has arrays of its own: what is written into an array waits for what comes into it directly)
+  constexpr int HELD = PACKED ? DOp::BYTES : STAGE, APART = PACKED ? XOp::BYTES : 16;
+  __shared__ __attribute__((aligned(128))) char stage0[HELD], stage1[HELD], stage2[HELD], stage3[HELD], x0[APART], x1[APART], x2[APART], x3[APART];
   __shared__ float sums[LINES][BN];
   __shared__ int row_of[2][THREADS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -628,71 +633,14 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
     // block ahead (looked up stage by stage, a line of the order a stage, each stage waited for memory: 150 us where sorted rows took 95).
     const int stop = __builtin_amdgcn_readfirstlane(min(end, begin + upto * UNIT)), stages = 2 * (upto - first);
     const int start = __builtin_amdgcn_readfirstlane(begin + first * UNIT);
-    int coming = start, left = stages;
-    const auto row_at = [&](int pos) __attribute__((always_inline)) { return pos < stop ? ds_ordered_row(a.order, a.rows, pos) : -1; };
-    row_of[0][threadIdx.x] = row_at(start + (int)threadIdx.x);
-    int later = row_at(start + THREADS + (int)threadIdx.x);
-    __syncthreads();
     const bool ends = a.outer - col0 < BN || a.inner - in0 < BR;   // (columns that there are not)
-    const auto fetch = [&](char* stage) __attribute__((always_inline)) {
-      if (left == 0) return false;
-      const int block = (coming - start) / THREADS, at = (coming - start) % THREADS;
-      if (at == 0) {   // (nobody reads the block before any more)
-        row_of[(block + 1) & 1][threadIdx.x] = later;
-        later = row_at(start + (block + 2) * THREADS + (int)threadIdx.x);
-      }
-      int now[EACH];
-#pragma unroll
-      for (int u = 0; u < EACH; ++u) now[u] = row_of[block & 1][at + u * LINES + line];
-      const bool over = ends || coming + DEPTH > stop || a.order;   // (an order may name rows that there are not)
-#pragma unroll
-      for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + now[u] * a.dys + (col0 + place), now[u] >= 0, over, dy_end, stage);
-#pragma unroll
-      for (int u = 0; u < EACH; ++u) lx.fetch(u, x + now[u] * a.xs + (in0 + place), now[u] >= 0, over, x_end, stage + DOp::BYTES);
-      coming += DEPTH;
-      --left;
-      return true;
-    };
-    const auto put = [&](char* stage) __attribute__((always_inline)) {
-      ld.store(stage, false, 0);
-      lx.store(stage + DOp::BYTES, false, 0);
-    };
-    // PACKED: x of a stage is asked for one stage further ahead than dy, which then finds the rows looked up
-    int x_coming = start, x_left = stages, rows_of_x[EACH] = {};
-    const auto fetch_x = [&](int set) __attribute__((always_inline)) {
-      if (x_left == 0) return;
-      const int block = (x_coming - start) / THREADS, at = (x_coming - start) % THREADS;
-      if (at == 0) {
-        row_of[(block + 1) & 1][threadIdx.x] = later;
-        later = row_at(start + (block + 2) * THREADS + (int)threadIdx.x);
-      }
-#pragma unroll
-      for (int u = 0; u < EACH; ++u) rows_of_x[u] = row_of[block & 1][at + u * LINES + line];
-      const bool over = ends || x_coming + DEPTH > stop || a.order;
-#pragma unroll
-      for (int u = 0; u < EACH; ++u)
-        lp.fetch(set, u, a.codes + rows_of_x[u] * a.xs + (in0 + place), a.scales + rows_of_x[u] * a.scales_stride + min(in0 + place, a.inner - 1) / kPackBlock, rows_of_x[u] >= 0, over, codes_end);
-      x_coming += DEPTH;
-      --x_left;
-    };
-    const auto fetch_dy = [&](char* stage) __attribute__((always_inline)) {
-      if (left == 0) return false;
-      const bool over = ends || coming + DEPTH > stop || a.order;
-#pragma unroll
-      for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + rows_of_x[u] * a.dys + (col0 + place), rows_of_x[u] >= 0, over, dy_end, stage);
-      coming += DEPTH;
-      --left;
-      return true;
-    };
-    // (in two phases, the waves of a SIMD a phase apart, as in row_tiles_kernel)
-    const auto half = [&](bool fresh, int number, int set, char* now, char* behind, char* before) __attribute__((always_inline)) {
-      PieceV<T> fx[2][NR], fd[2][NN];
+    const auto operands = [&](const char* now, const char* now_x, PieceV<T> (&fx)[2][NR], PieceV<T> (&fd)[2][NN]) __attribute__((always_inline)) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int n = 0; n < NN; ++n) fd[c][n] = rd.read(now, wn + n * 32, c);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) fx[c][r] = rx.read(now + DOp::BYTES, wr + r * 32, c);
+        for (int r = 0; r < NR; ++r) fx[c][r] = rx.read(now_x, wr + r * 32, c);
       }
       if (in0 == 0) {   // db: the column sums of what is in LDS anyway
 #pragma unroll
@@ -702,25 +650,8 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
           for (int i = 0; i < N; ++i) sum[i] += (float)v[i];
         }
       }
-      bool more;
-      if constexpr (PACKED) {
-        // what came of x two halves ago, into the stage after the next; dy of the stage three on, x of the one behind that
-        if (number + 2 < stages) lp.store(set, behind + DOp::BYTES);
-        if constexpr (DIRECT) {
-          more = fetch_dy(before);
-          fetch_x(set);
-        } else {
-          ld.store(before, false, 0);
-          fetch_x(set);
-          more = fetch_dy(before);
-        }
-      } else {
-        put(before);
-        more = fetch(before);
-      }
-      if (!DIRECT || fresh) meet<-1>();
-      else if (more) meet<PACKED ? 2 * (ld.PIECES + lp.LOADS) : 2 * LOADS>();
-      else meet<0>();
+    };
+    const auto multiply_all = [&](PieceV<T> (&fx)[2][NR], PieceV<T> (&fd)[2][NN]) __attribute__((always_inline)) {
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
       products<T, NR, NN>(fd[0], fx[0], acc);
@@ -730,12 +661,63 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
       meet<-1>();
     };
     if constexpr (PACKED) {
+      // The rows of four stages are a block, of which a ring in LDS holds eight; a block comes in three ahead of the one that is read, whether or not there is any: all
+      // loads here are without conditions, so that the compiler knows how many are on their way behind the ones that it waits for. (Two stages at a time
+      // were waited for altogether otherwise: 189 us.)
+      int* ring = &row_of[0][0];
+      static_assert(8 * RING <= 2 * THREADS && THREADS % RING == 0, "");
+      const auto row_at = [&](int block) __attribute__((always_inline)) {
+        const int pos = start + block * RING + (int)threadIdx.x % RING;
+        const int32_t* from = a.order ? a.order + min(pos, a.rows - 1) : (const int32_t*)a.offsets;   // (sorted rows: any address)
+        const int named = *(const DS_GLOBAL int32_t*)from, row = !a.order ? pos : named >= 0 && named < a.rows ? named : -1;
+        return pos < stop ? row : -1;
+      };
+  #pragma unroll
+      for (int q = 0; q < 4; ++q) ring[q * RING + (int)threadIdx.x % RING] = row_at(q);
+      int later = row_at(4), block = 4, x_stage = 0, dy_stage = 0, rows_of_x[EACH];
+      __syncthreads();
+      // x of a stage is asked for one stage further ahead than dy, which then finds the rows looked up
+      const auto fetch_x = [&](int set) __attribute__((always_inline)) {
+        const int at = x_stage * DEPTH;
+  #pragma unroll
+        for (int u = 0; u < EACH; ++u) rows_of_x[u] = ring[at / RING % 8 * RING + at % RING + u * LINES + line];
+        const bool over = ends || start + at + DEPTH > stop || a.order;
+  #pragma unroll
+        for (int u = 0; u < EACH; ++u)
+          lp.fetch(set, u, a.codes + rows_of_x[u] * a.xs + (in0 + place), a.scales + rows_of_x[u] * a.scales_stride + min(in0 + place, a.inner - 1) / kPackBlock,
+                   rows_of_x[u] >= 0, over, codes_end);
+        ++x_stage;
+      };
+      const auto fetch_dy = [&](char* stage) __attribute__((always_inline)) {
+        const bool over = ends || start + (dy_stage + 1) * DEPTH > stop || a.order;
+  #pragma unroll
+        for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + rows_of_x[u] * a.dys + (col0 + place), rows_of_x[u] >= 0, over, dy_end, stage);
+        ++dy_stage;
+      };
+      // (phases as above. What came of x two halves ago goes into the stage after the next; then dy of the stage three on is asked for, and x of the one
+      // behind that. What is waited for at the end is dy of the next stage: behind it are at least the loads of two stages.)
+      const auto half = [&](int set, char* now, char* now_x, char* behind_x, char* before) __attribute__((always_inline)) {
+        PieceV<T> fx[2][NR], fd[2][NN];
+        operands(now, now_x, fx, fd);
+        lp.store(set, behind_x);
+        if constexpr (DIRECT) {
+          fetch_dy(before);
+          fetch_x(set);
+          meet<2 * (EACH + lp.LOADS)>();
+        } else {
+          ld.store(before, false, 0);
+          fetch_x(set);
+          fetch_dy(before);
+          meet<-1>();
+        }
+        multiply_all(fx, fd);
+      };
       fetch_x(0);
-      lp.store(0, stage0 + DOp::BYTES);
+      lp.store(0, x0);
       fetch_dy(stage0);
       ld.store(stage0, false, 0);
       fetch_x(1);
-      lp.store(1, stage1 + DOp::BYTES);
+      lp.store(1, x1);
       fetch_dy(stage1);
       ld.store(stage1, false, 0);
       fetch_x(0);
@@ -743,7 +725,62 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
       ld.store(stage2, false, 0);
       fetch_x(1);
       if (!DIRECT) fetch_dy(stage3);
+      meet<0>();
+      const bool second = wave >= WR * WN / 2;
+      if (second) meet<-1>();
+      for (int s = 0;; s += 4) {
+        ring[block % 8 * RING + (int)threadIdx.x % RING] = later;
+        later = row_at(++block);
+        half(0, stage0, x0, x2, stage3);
+        half(1, stage1, x1, x3, stage0);
+        if (s + 2 >= stages) break;
+        half(0, stage2, x2, x0, stage1);
+        half(1, stage3, x3, x1, stage2);
+        if (s + 4 >= stages) break;
+      }
+      if (!second) meet<-1>();
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing comes into LDS any more)
+      __syncthreads();
     } else {
+      int coming = start, left = stages;
+      const auto row_at = [&](int pos) __attribute__((always_inline)) { return pos < stop ? ds_ordered_row(a.order, a.rows, pos) : -1; };
+      row_of[0][threadIdx.x] = row_at(start + (int)threadIdx.x);
+      int later = row_at(start + THREADS + (int)threadIdx.x);
+      __syncthreads();
+      const auto fetch = [&](char* stage) __attribute__((always_inline)) {
+        if (left == 0) return false;
+        const int block = (coming - start) / THREADS, at = (coming - start) % THREADS;
+        if (at == 0) {   // (nobody reads the block before any more)
+          row_of[(block + 1) & 1][threadIdx.x] = later;
+          later = row_at(start + (block + 2) * THREADS + (int)threadIdx.x);
+        }
+        int now[EACH];
+  #pragma unroll
+        for (int u = 0; u < EACH; ++u) now[u] = row_of[block & 1][at + u * LINES + line];
+        const bool over = ends || coming + DEPTH > stop || a.order;   // (an order may name rows that there are not)
+  #pragma unroll
+        for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + now[u] * a.dys + (col0 + place), now[u] >= 0, over, dy_end, stage);
+  #pragma unroll
+        for (int u = 0; u < EACH; ++u) lx.fetch(u, x + now[u] * a.xs + (in0 + place), now[u] >= 0, over, x_end, stage + DOp::BYTES);
+        coming += DEPTH;
+        --left;
+        return true;
+      };
+      const auto put = [&](char* stage) __attribute__((always_inline)) {
+        ld.store(stage, false, 0);
+        lx.store(stage + DOp::BYTES, false, 0);
+      };
+      // (in two phases, the waves of a SIMD a phase apart, as in row_tiles_kernel)
+      const auto half = [&](bool fresh, char* now, char* before) __attribute__((always_inline)) {
+        PieceV<T> fx[2][NR], fd[2][NN];
+        operands(now, now + DOp::BYTES, fx, fd);
+        put(before);
+        const bool more = fetch(before);
+        if (!DIRECT || fresh) meet<-1>();
+        else if (more) meet<2 * LOADS>();
+        else meet<0>();
+        multiply_all(fx, fd);
+      };
       fetch(stage0);
       put(stage0);
       fetch(stage1);
@@ -751,19 +788,19 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
       fetch(stage2);
       put(stage2);
       if (!DIRECT) fetch(stage3);
-    }
-    meet<0>();
-    const bool second = wave >= WR * WN / 2;
-    if (second) meet<-1>();
-    for (int s = 0; s < stages; s += 4) {
-      half(s == 0, s, 0, stage0, stage2, stage3);
-      half(s == 0, s + 1, 1, stage1, stage3, stage0);
-      if (s + 2 < stages) {
-        half(false, s + 2, 0, stage2, stage0, stage1);
-        half(false, s + 3, 1, stage3, stage1, stage2);
+      meet<0>();
+      const bool second = wave >= WR * WN / 2;
+      if (second) meet<-1>();
+      for (int s = 0; s < stages; s += 4) {
+        half(s == 0, stage0, stage3);
+        half(s == 0, stage1, stage0);
+        if (s + 2 < stages) {
+          half(false, stage2, stage1);
+          half(false, stage3, stage2);
+        }
       }
+      if (!second) meet<-1>();
     }
-    if (!second) meet<-1>();
     const bool whole = first == 0 && upto == steps;
     // slot 0: the group began in an earlier chunk; 1: it begins here and goes on in a later one
     float* to = partial + ((int64_t)place_of * 2 + (first == 0)) * SLOT;

@@ -15,7 +15,7 @@ ROUTE = dict(dtype=1, rows=100_000, experts=9, k=2, renorm=0, x=P, xs=9, ids=P, 
 ROUTE_BACKWARD = dict(dtype=1, rows=5, experts=9, k=2, renorm=1, x=P, xs=9, lse=P, ids=P, counts=P, dweights=P, dloss=P, dx=P, dxs=9)
 PACK = dict(dtype=0, rows=5, cols=40, x=P, xs=40, codes=P, cs=40, scales=P, ss=2)
 UNPACK = dict(dtype=0, rows=5, cols=40, codes=P, cs=40, scales=P, ss=2, y=P, ys=40)
-PACKED_BACKWARD = dict(dtype=1, rows=5, inner=40, outer=8, groups=3, dy=P, dys=8, codes=P, cs=40, scales=P, ss=2, w=P, offsets=P, order=None, gate=P, gs=40,
+PACKED_BACKWARD = dict(dtype=1, rows=100_000, inner=40, outer=8, groups=3, dy=P, dys=8, codes=P, cs=40, scales=P, ss=2, w=P, offsets=P, order=None, gate=P, gs=40,
                        dx=P, dxs=40, dw=P, db=P, ws=P, wsn=1 << 40)
 MANY = (1 << 30) + 1
 NAN, INF = float("nan"), float("inf")
