@@ -580,7 +580,7 @@ __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit,
 
 // PACKED: x is held in 8 bits. Its codes and scales come through registers, two stages ahead, and go into LDS as the numbers that they stand for; dy, and all that is
 // done with what is in LDS, is as without: 65,521 rows by 1,024 x 512 TIME.
-template <typename T, int BR, int BN, int WR, int WN, bool DIRECT, bool PACKED = false>
+template <typename T, int BR, int BN, int WR, int WN, bool DIRECT, int PACKED = 0>
 __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial, int most_chunks) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
   constexpr int NR = BR / WR / 32, NN = BN / WN / 32, SLOT = BR * BN + BN;
@@ -590,8 +590,11 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   constexpr int LINES = THREADS / DOp::PER_ROW, EACH = DEPTH / LINES;   // of a thread's pieces of a stage: lines apart, and how many
   constexpr int RING = 4 * DEPTH;
   // (x held in 8 bits has arrays of its own: what is written into an array waits for what comes into it directly)
-  constexpr int HELD = PACKED ? DOp::BYTES : STAGE, APART = PACKED ? XOp::BYTES : 16;
-  __shared__ __attribute__((aligned(128))) char stage0[HELD], stage1[HELD], stage2[HELD], stage3[HELD], x0[APART], x1[APART], x2[APART], x3[APART];
+  constexpr int HELD = PACKED ? DOp::BYTES : STAGE, APART = PACKED ? XOp::BYTES : 16, CODES = PACKED == 2 ? DEPTH * BR : 16, SCALES = PACKED == 2 ? CODES / kPackBlock : 16;
+  __shared__ __attribute__((aligned(128))) char stage0[HELD], stage1[HELD], stage2[HELD], stage3[HELD], x0[APART], x1[APART];
+  __shared__ __attribute__((aligned(128))) char x2[PACKED == 1 ? APART : 16], x3[PACKED == 1 ? APART : 16];
+  // (codes, and behind them the scales: the compiler tells apart eight arrays that loads go to directly)
+  __shared__ __attribute__((aligned(128))) uint8_t codes0[CODES + SCALES], codes1[CODES + SCALES], codes2[CODES + SCALES], codes3[CODES + SCALES];
   __shared__ float sums[LINES][BN];
   __shared__ int row_of[2][THREADS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -660,7 +663,92 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
       __builtin_amdgcn_sched_barrier(0);
       meet<-1>();
     };
-    if constexpr (PACKED) {
+    if constexpr (PACKED == 2) {
+      // Codes and scales come into LDS as they are, four stages ahead, and a thread turns the 16 (fp32: four) codes that it asked for into numbers a stage before they are
+      // needed: into one of two arrays, since the other is not read any more by then.
+      constexpr int CPT = CODES / THREADS, PARTS = BR / (4 * kPackBlock);   // codes of a thread, words of scales of a row
+      static_assert(CPT == 16 || CPT == 4, "");
+      const int code_line = (int)threadIdx.x / (BR / CPT), code_col = (int)threadIdx.x % (BR / CPT) * CPT;
+      const int scale_line = lane / PARTS, scale_col = in0 + lane % PARTS * (4 * kPackBlock);
+      const auto row_at = [&](int pos) __attribute__((always_inline)) { return pos < stop ? ds_ordered_row(a.order, a.rows, pos) : -1; };
+      row_of[0][threadIdx.x] = row_at(start + (int)threadIdx.x);
+      int later = row_at(start + THREADS + (int)threadIdx.x), x_stage = 0, dy_stage = 0, rows_of_dy[EACH];
+      __syncthreads();
+      const uint8_t* zeros = reinterpret_cast<const uint8_t*>(&kZeros);
+      const auto fetch_x = [&](uint8_t* codes) __attribute__((always_inline)) {
+        if (x_stage == stages) return false;
+        const int block = x_stage * DEPTH / THREADS, at = x_stage * DEPTH % THREADS;
+        if (at == 0) {   // (nobody reads the block before any more)
+          row_of[(block + 1) & 1][threadIdx.x] = later;
+          later = row_at(start + (block + 2) * THREADS + (int)threadIdx.x);
+        }
+        const int* rows = row_of[block & 1] + at;
+        const int row = rows[code_line];
+        const uint8_t* src = row >= 0 && in0 + code_col < a.inner ? a.codes + row * a.xs + (in0 + code_col) : zeros;
+        if constexpr (CPT == 16) __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(codes + wave * 64 * CPT), 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(codes + wave * 64 * CPT), 4, 0, 0);
+        if (lane < SCALES / 4) {   // (each wave the same words)
+          const int scale_row = rows[scale_line];
+          const uint8_t* from = scale_row >= 0 && scale_col < a.inner ? a.scales + scale_row * a.scales_stride + scale_col / kPackBlock : zeros;
+          __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)from, (DS_LDS void*)(codes + CODES), 4, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) rows_of_dy[u] = rows[u * LINES + line];
+        ++x_stage;
+        return true;
+      };
+      const auto fetch_dy = [&](char* stage) __attribute__((always_inline)) {
+        if (dy_stage == stages) return;
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) ld.fetch(u, dy + rows_of_dy[u] * a.dys + (col0 + place), rows_of_dy[u] >= 0, true, dy_end, stage);
+        ++dy_stage;
+      };
+      const auto decode = [&](const uint8_t* codes, char* to) __attribute__((always_inline)) {
+        const uint32_t scale = codes[CODES + code_line * (BR / kPackBlock) + code_col / kPackBlock];
+        uint32_t word[CPT / 4];
+#pragma unroll
+        for (int i = 0; i < CPT / 4; ++i) word[i] = reinterpret_cast<const uint32_t*>(codes)[(int)threadIdx.x * (CPT / 4) + i];
+#pragma unroll
+        for (int p = 0; p < CPT / N; ++p) {
+          PackedPiece<N> piece;
+          if constexpr (N == 8) piece = (uint64_t)word[2 * p] | (uint64_t)word[2 * p + 1] << 32;
+          else piece = word[p];
+          *reinterpret_cast<PieceV<T>*>(to + (code_line * XOp::PER_ROW + XOp::exchange(code_line, code_col / N + p)) * 16) = decoded<T>(piece, scale);
+        }
+      };
+      // (phases as below. At the end of a half what was asked for two halves ago has come: dy of the next stage, and the codes that the next half decodes.)
+      const auto half = [&](int number, char* now, char* now_x, char* next_x, char* before, const uint8_t* codes, uint8_t* to_codes)
+          __attribute__((always_inline)) {
+        PieceV<T> fx[2][NR], fd[2][NN];
+        operands(now, now_x, fx, fd);
+        if (number + 1 < stages) decode(codes, next_x);
+        fetch_dy(before);
+        if (fetch_x(to_codes)) meet<2 * (EACH + 2)>();
+        else meet<0>();
+        multiply_all(fx, fd);
+      };
+      fetch_x(codes0);
+      fetch_dy(stage0);
+      fetch_x(codes1);
+      fetch_dy(stage1);
+      fetch_x(codes2);
+      fetch_dy(stage2);
+      fetch_x(codes3);
+      meet<0>();
+      decode(codes0, x0);
+      meet<-1>();
+      const bool second = wave >= WR * WN / 2;
+      if (second) meet<-1>();
+      for (int s = 0; s < stages; s += 4) {
+        half(s, stage0, x0, x1, stage3, codes1, codes0);
+        half(s + 1, stage1, x1, x0, stage0, codes2, codes1);
+        if (s + 2 < stages) {
+          half(s + 2, stage2, x0, x1, stage1, codes3, codes2);
+          half(s + 3, stage3, x1, x0, stage2, codes0, codes3);
+        }
+      }
+      if (!second) meet<-1>();
+    } else if constexpr (PACKED == 1) {
       // The rows of four stages are a block, of which a ring in LDS holds eight; a block comes in three ahead of the one that is read, whether or not there is any: all
       // loads here are without conditions, so that the compiler knows how many are on their way behind the ones that it waits for. (Two stages at a time
       // were waited for altogether otherwise: 189 us.)
@@ -989,7 +1077,13 @@ int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
   // (x held in 8 bits comes through registers either way)
   const bool direct = (PACKED || (sixteen(a.x, a.xs, sizeof(T)) && a.inner % Piece<T>::N == 0)) && sixteen(a.dy, a.dys, sizeof(T)) && a.outer % Piece<T>::N == 0;
   const dim3 grid((unsigned)wgs), block(64 * WR * WN);
-  if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true, PACKED>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
+  bool codes_direct = false;   // rows of codes and scales that can come into LDS as they are
+  if constexpr (PACKED) {
+    codes_direct = direct && sixteen(a.codes, a.xs, 1) && a.inner % (4 * kPackBlock) == 0 && (uintptr_t)a.scales % 4 == 0 && a.scales_stride % 4 == 0;
+    if (codes_direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true, 2>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
+  }
+  if (codes_direct) ;
+  else if (direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true, PACKED>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
   else hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, false, PACKED>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
   // threads to a unit by the chunks that a group has on average; workgroups for about 2,048 in all
   const int64_t of_group = chunks / (a.groups < chunks ? a.groups : chunks) + 1;
