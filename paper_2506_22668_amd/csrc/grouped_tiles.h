@@ -713,7 +713,10 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
           PackedPiece<N> piece;
           if constexpr (N == 8) piece = (uint64_t)word[2 * p] | (uint64_t)word[2 * p + 1] << 32;
           else piece = word[p];
-          *reinterpret_cast<PieceV<T>*>(to + (code_line * XOp::PER_ROW + XOp::exchange(code_line, code_col / N + p)) * 16) = decoded<T>(piece, scale);
+          // (a store of its own: the compiler has one wait for all that is on its way to LDS, though nothing of it goes here; 122 us, so TIME2)
+          const PieceV<T> v = decoded<T>(piece, scale);
+          const uint32_t at = (uint32_t)(uintptr_t)(DS_LDS char*)to + (code_line * XOp::PER_ROW + XOp::exchange(code_line, code_col / N + p)) * 16;
+          asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory");
         }
       };
       // (phases as below. At the end of a half what was asked for two halves ago has come: dy of the next stage, and the codes that the next half decodes.)
