@@ -37,14 +37,14 @@ __global__ __launch_bounds__(kThreads) void look_up_kernel(LookArgs a) {
   const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   int64_t row = first / a.calls;
   int call = (int)(first % a.calls);
-  while (row < a.rows) {
-    int64_t at[kAhead];
-    int col[kAhead], id[kAhead];
+  int64_t at[kAhead], next_at[kAhead];
+  int col[kAhead], id[kAhead], next_col[kAhead], next_id[kAhead];
+  const auto look = [&]() __attribute__((always_inline)) {   // the ids of the next pieces
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      at[j] = row;
-      col[j] = call * N;
-      id[j] = row < a.rows ? a.ids[row] : -1;
+      next_at[j] = row;
+      next_col[j] = call * N;
+      next_id[j] = row < a.rows ? a.ids[row] : -1;
       row += a.rows_step;
       call += a.calls_step;
       if (call >= a.calls) {
@@ -52,12 +52,18 @@ __global__ __launch_bounds__(kThreads) void look_up_kernel(LookArgs a) {
         ++row;
       }
     }
+  };
+  look();
+  while (next_at[0] < a.rows) {
     typename Elements<T, N>::V v[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if ((uint32_t)id[j] >= (uint32_t)a.vocab) id[j] = -1;
+      at[j] = next_at[j];
+      col[j] = next_col[j];
+      id[j] = (uint32_t)next_id[j] < (uint32_t)a.vocab ? next_id[j] : -1;
       v[j] = load_elements<T, N, TINY>((const T*)a.table + (int64_t)(id[j] < 0 ? 0 : id[j]) * a.ts, col[j], a.cols);
     }
+    look();
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (at[j] >= a.rows) break;

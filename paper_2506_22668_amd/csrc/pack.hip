@@ -29,6 +29,10 @@ __device__ __forceinline__ uint32_t max_of_four(uint32_t v) {
 typedef uint32_t Eight __attribute__((ext_vector_type(2)));
 typedef uint32_t EightU __attribute__((ext_vector_type(2), aligned(1)));
 
+constexpr int kAhead = 2;   // pieces of a thread on their way at a time
+
+// Most pieces take a product and half a conversion a value; those that hold a value which is not finite, which would round to 0, or near the type's largest
+// go through the definition.
 template <typename T, bool TINY>
 __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
   constexpr uint32_t kMostExponent = std::is_same<T, _Float16>::value ? 142 : 254;
@@ -36,51 +40,88 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
   int64_t row = first / a.calls;
   int call = (int)(first % a.calls);
   while (row < a.rows) {   // (the four threads of a block go on together)
-    const int col = call * kCols, have = a.cols - col;
-    float x[kCols] = {};
-    if (have > 0) {
-      auto v = load_elements<T, kCols, TINY>((const T*)a.x + row * a.xs, col, a.cols);
-      settle_elements<T, kCols, TINY>(v, col, a.cols);
+    int64_t at[kAhead];
+    int which[kAhead];
+    typename Elements<T, kCols>::V v[kAhead];
 #pragma unroll
-      for (int i = 0; i < kCols; ++i) x[i] = i < have ? (float)v[i] : 0.f;
-    }
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < kCols; ++i) {
-      const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
-      most = max(most, bits < 0x7f800000u ? bits : 0);
-    }
-    most = max_of_four(most);
-    const uint32_t exponent = most >> 23;
-    const bool wide = (most & 0x7fffffu) > 0x600000u;   // above 448 of the power below
-    const uint32_t scale = most == 0 ? 127 : max((int)exponent - 8 + (int)wide, 1);
-    const float top = wide && exponent == kMostExponent ? 240.f : 448.f, inv = __uint_as_float((254 - scale) << 23);
-    uint32_t word[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < kCols; i += 2) {
-      float q[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float v = x[i + j], s = v * inv;
-        q[j] = fabsf(s) < 0x1p-9f && v != 0.f ? copysignf(0x1p-9f, v) : fminf(fmaxf(s, -top), top);
-        if (!(fabsf(v) < INFINITY)) q[j] = NAN;
+    for (int j = 0; j < kAhead; ++j) {
+      at[j] = row;
+      which[j] = call;
+      if (row < a.rows && call * kCols < a.cols) v[j] = load_elements<T, kCols, TINY>((const T*)a.x + row * a.xs, call * kCols, a.cols);
+      row += a.rows_step;
+      call += a.calls_step;
+      if (call >= a.calls) {
+        call -= a.calls;
+        ++row;
       }
-      word[i / 4] = i % 4 ? __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], word[i / 4], true) : __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], word[i / 4], false);
     }
-    uint8_t* to = a.codes + row * a.cs + col;
-    if (have >= kCols) {
-      *reinterpret_cast<EightU*>(to) = Eight{word[0], word[1]};
-    } else {
 #pragma unroll
-      for (int i = 0; i < kCols - 1; ++i)
-        if (i < have) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
-    }
-    if (call % 4 == 0) a.scales[row * a.ss + call / 4] = (uint8_t)scale;
-    row += a.rows_step;
-    call += a.calls_step;
-    if (call >= a.calls) {
-      call -= a.calls;
-      ++row;
+    for (int j = 0; j < kAhead; ++j) {
+      if (at[j] >= a.rows) break;
+      const int col = which[j] * kCols, have = a.cols - col;
+      float x[kCols] = {};
+      if (have >= kCols) {
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) x[i] = (float)v[j][i];
+      } else if (have > 0) {
+        settle_elements<T, kCols, TINY>(v[j], col, a.cols);
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) x[i] = i < have ? (float)v[j][i] : 0.f;
+      }
+      uint32_t most = 0, least = 0xffffffffu;   // of the values' bits without a sign; of those that are not 0, less 1
+#pragma unroll
+      for (int i = 0; i < kCols; ++i) {
+        const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
+        most = max(most, bits);
+        least = min(least, bits - 1);
+      }
+      const bool fine = most < 0x7f800000u;
+      if (!fine) {
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) {
+          const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
+          most = max(most, bits < 0x7f800000u ? bits : 0);
+        }
+      }
+      most = max_of_four(most);
+      const uint32_t exponent = most >> 23;
+      const bool wide = (most & 0x7fffffu) > 0x600000u;   // above 448 of the power below
+      const uint32_t scale = most == 0 ? 127 : max((int)exponent - 8 + (int)wide, 1);
+      const bool high = wide && exponent == kMostExponent;
+      const float inv = __uint_as_float((254 - scale) << 23);
+      const uint32_t smallest = __float_as_uint(power_of_scale(scale) * 0x1p-9f);   // the bits of what the smallest code stands for
+      uint32_t word[2];
+      if (fine && !high && least >= smallest - 1) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          word[w] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w] * inv, x[4 * w + 1] * inv, 0, false);
+          word[w] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2] * inv, x[4 * w + 3] * inv, word[w], true);
+        }
+      } else {
+        const float top = high ? 240.f : 448.f;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          float q[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float from = x[4 * w + i], s = from * inv;
+            q[i] = fabsf(s) < 0x1p-9f && from != 0.f ? copysignf(0x1p-9f, from) : fminf(fmaxf(s, -top), top);
+            if (!(fabsf(from) < INFINITY)) q[i] = NAN;
+          }
+          word[w] = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+          word[w] = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], word[w], true);
+        }
+      }
+      uint8_t* to = a.codes + at[j] * a.cs + col;
+      if (have >= kCols) {
+        *reinterpret_cast<EightU*>(to) = Eight{word[0], word[1]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < kCols - 1; ++i)
+          if (i < have) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
+      }
+      if (which[j] % 4 == 0) a.scales[at[j] * a.ss + which[j] / 4] = (uint8_t)scale;
     }
   }
 }
