@@ -1,13 +1,16 @@
-"""A learned encoder of node features: residual blocks whose weights depend on the node's type.
+"""Learned encoders of node features: residual blocks whose weights depend on the node's type, or on the experts that a router chooses.
 
-    h = x + dropout(relu(norm(x) W1[type] + b1[type]) W2[type] + b2[type])
+    h = x + dropout(relu(norm(x) W1[type] + b1[type]) W2[type] + b2[type])                                    TypedEncoder
+    h = x + dropout(sum over j of w_j (relu(norm(x) W1[e_j] + b1[e_j]) W2[e_j] + b2[e_j])),  (e, w) = route(norm(x) R), x = s T[id] at first   RoutedEncoder
 
-The block runs on the library's operators on rows (`Context.layer_norm`, `group_rows`, `grouped_mm`, `dropout` and their
-gradients); what it puts out is what `Context.set_features` takes. Run as a program it trains a small encoder on nodes of three types,
-hands the features to a GCN and explains one of its answers:
+The blocks run on the library's operators on rows (`Context.layer_norm`, `group_rows`, `grouped_mm`, `dropout`, `embed`, `route`, `pack_rows` and their
+gradients); what they put out is what `Context.set_features` takes. Run as a program it trains a small encoder on nodes of three types, or (`ids`) on nodes
+that have nothing but an id, hands the features to a GCN and explains one of its answers:
 
-    python -m paper_2506_22668_amd.encoder
+    python -m paper_2506_22668_amd.encoder [ids]
 """
+import sys
+
 import torch
 
 from .binding import DS_EINVAL, DistShapError
@@ -29,14 +32,16 @@ class _State:
 
 class TypedEncoder:
     """`depth` residual blocks over rows of `width` features of `types` kinds. Parameters are fp32; products run in `dtype`
-    (fp32, bf16 or fp16). `forward(..., train=True)` leaves what `backward` needs in `state`; `update` is a step of plain gradient descent."""
+    (fp32, bf16 or fp16). `forward(..., train=True)` leaves what `backward` needs in `state`; `update` is a step of plain gradient descent. With
+    `packed` a training step keeps its normalised rows and its hidden ones in 8 bits, from which the weights' gradients are formed."""
 
-    def __init__(self, ctx, types, width, hidden, depth=1, dtype=torch.bfloat16, p=0.1, seed=0):
+    def __init__(self, ctx, types, width, hidden, depth=1, dtype=torch.bfloat16, p=0.1, seed=0, packed=False):
         g = torch.Generator(device=ctx.device)
         g.manual_seed(seed)
-        self.ctx, self.types, self.dtype, self.p, self.seed = ctx, types, dtype, p, seed
+        self.ctx, self.types, self.dtype, self.p, self.seed, self.packed = ctx, types, dtype, p, seed, packed
         normal = lambda *shape, scale: torch.randn(*shape, generator=g, device=ctx.device) * scale   # noqa: E731
         zeros = lambda *shape: torch.zeros(*shape, device=ctx.device)   # noqa: E731
+        self._normal = normal
         self.blocks = [dict(gain=zeros(width) + 1, shift=zeros(width), w1=normal(types, width, hidden, scale=width ** -0.5), b1=zeros(types, hidden),
                             w2=normal(types, hidden, width, scale=hidden ** -0.5), b2=zeros(types, width)) for _ in range(depth)]
         self.state, self.grads = None, []
@@ -45,6 +50,23 @@ class TypedEncoder:
     @property
     def _kept(self):
         return self.state.blocks if self.state else []
+
+    def _keep(self, rows):
+        """Rows as a training step keeps them."""
+        return self.ctx.pack_rows(rows) if self.packed else rows
+
+    def _state_of(self, dy, state):
+        """The state of the training forward that dy belongs to."""
+        if state is None:
+            if self._waiting != 1:
+                raise DistShapError(DS_EINVAL, "backward without a training forward of its own" if self._waiting == 0 else
+                                    f"{self._waiting} training forwards wait for a backward pass: give the `state` of the one that is meant")
+            state = self.state
+        if state.shape != dy.shape:
+            raise DistShapError(DS_EINVAL, f"dy has shape {tuple(dy.shape)}, {tuple(state.shape)} went out")
+        if state.changed():
+            raise DistShapError(DS_EINVAL, "the rows or the parameters of this forward have been changed since")
+        return state
 
     def forward(self, x, node_type, train=False, step=0):
         """Rows of x through the blocks, in `dtype`. node_type: int32, one a row (a row of no type passes through unchanged). The
@@ -63,7 +85,7 @@ class TypedEncoder:
             h = c.grouped_mm(y, w1, offsets, order=order, bias=b["b1"], relu=True)
             out = c.grouped_mm(h, w2, offsets, order=order, bias=b["b2"])
             if train:
-                state.blocks.append((x, y, h, mean, rstd, w1, w2, offsets, order, b["gain"], tag))
+                state.blocks.append((x, self._keep(y), self._keep(h), mean, rstd, w1, w2, offsets, order, b["gain"], tag))
                 state.hold(b["gain"], *(w for w in (w1, w2) if w is b["w1"] or w is b["w2"]))
             x = c.dropout(out, self.p if train else 0.0, state.seed, tag, residual=x)
         if train:
@@ -75,15 +97,7 @@ class TypedEncoder:
         """The gradient of the rows that went in; those of the parameters are left in `grads`, one dict a block. `state`: what `self.state` was
         after the forward that dy belongs to; it can be left out where there was one training forward since the last backward pass."""
         c, self.grads = self.ctx, []
-        if state is None:
-            if self._waiting != 1:
-                raise DistShapError(DS_EINVAL, "backward without a training forward of its own" if self._waiting == 0 else
-                                    f"{self._waiting} training forwards wait for a backward pass: give the `state` of the one that is meant")
-            state = self.state
-        if state.shape != dy.shape:
-            raise DistShapError(DS_EINVAL, f"dy has shape {tuple(dy.shape)}, {tuple(state.shape)} went out")
-        if state.changed():
-            raise DistShapError(DS_EINVAL, "the rows or the parameters of this forward have been changed since")
+        state = self._state_of(dy, state)
         dy, grads = dy.to(self.dtype), []
         for x, y, h, mean, rstd, w1, w2, offsets, order, gain, tag in reversed(state.blocks):
             dout = c.dropout(dy, state.p, state.seed, tag)
@@ -101,6 +115,89 @@ class TypedEncoder:
         for b, g in zip(self.blocks, self.grads):
             for name, v in b.items():
                 v.sub_(rate * g[name].float())
+
+
+class RoutedEncoder(TypedEncoder):
+    """Features of nodes that have none: rows of a table by the node's id, then blocks as above of `experts`, of which a router gives each row `k`, weighted
+    by its scores. `forward` leaves the balance loss of its blocks (1 for each where the experts are used alike) in `balance` and how often each
+    expert was chosen in `counts`; `backward(dy, balance=b)` is the gradient of what dy belongs to and b times that loss."""
+
+    def __init__(self, ctx, nodes, experts, width, hidden, depth=1, k=2, dtype=torch.bfloat16, p=0.1, seed=0, packed=False):
+        super().__init__(ctx, experts, width, hidden, depth, dtype, p, seed, packed)
+        self.k, self.scale = k, width ** 0.5
+        self.table = self._normal(nodes, width, scale=width ** -0.5)
+        for b in self.blocks:
+            b["router"] = self._normal(width, experts, scale=width ** -0.5)
+        self.dtable, self.balance, self.counts = None, None, []
+
+    def forward(self, ids, train=False, step=0):
+        """Rows of the nodes `ids` (int32; one outside of the table starts at zeros) in `dtype`. ids stay as they are until the backward pass."""
+        c = self.ctx
+        rows = ids.shape[0]
+        whole = torch.arange(2, device=ids.device) * rows
+        state = _State(self.p, self.seed + (step << 32))
+        state.hold(ids)
+        state.ids = ids
+        x = c.embed(self.table, ids, scale=self.scale, dtype=self.dtype)
+        state.shape = x.shape
+        losses, self.counts = [], []
+        for tag, b in enumerate(self.blocks):
+            w1, w2, router = b["w1"].to(self.dtype), b["w2"].to(self.dtype), b["router"].to(self.dtype)[None]
+            y, mean, rstd = c.layer_norm(x, b["gain"], b["shift"], want_stats=True)
+            scores = c.grouped_mm(y, router, whole)
+            experts, weights, counts, loss, lse = c.route(scores, self.k, renorm=True)
+            total, parts = torch.zeros(x.shape, device=x.device), []
+            kept_y = self._keep(y) if train else None
+            for j in range(self.k):
+                offsets, order = c.group_rows(experts[j], self.types)
+                h = c.grouped_mm(y, w1, offsets, order=order, bias=b["b1"], relu=True)
+                out = c.grouped_mm(h, w2, offsets, order=order, bias=b["b2"])
+                total += out.float() * weights[j][:, None]
+                if train:
+                    parts.append((self._keep(h), self._keep(out), offsets, order))
+            losses.append(loss)
+            self.counts.append(counts)
+            if train:
+                state.blocks.append((x, kept_y, mean, rstd, w1, w2, router, whole, scores, experts, weights, counts, lse, parts, b["gain"], tag))
+                state.hold(b["gain"], *(w for w, p in ((w1, "w1"), (w2, "w2"), (router, "router")) if w.data_ptr() == b[p].data_ptr()))
+            x = c.dropout(total.to(self.dtype), self.p if train else 0.0, state.seed, tag, residual=x)
+        self.balance = torch.stack(losses).sum() if losses else torch.zeros((), device=ids.device)
+        if train:
+            self.state = state
+            self._waiting += 1
+        return x
+
+    def backward(self, dy, state=None, balance=0.0):
+        """Leaves the parameters' gradients in `grads` (one dict a block) and `dtable`."""
+        c, self.grads, self.dtable = self.ctx, [], None
+        state = self._state_of(dy, state)
+        dloss = torch.full((), float(balance), device=dy.device)
+        dy, grads = dy.to(self.dtype), []
+        for x, y, mean, rstd, w1, w2, router, whole, scores, experts, weights, counts, lse, parts, gain, tag in reversed(state.blocks):
+            dtotal = c.dropout(dy, state.p, state.seed, tag).float()
+            dweights, sums, dn = torch.empty_like(weights), None, torch.zeros(x.shape, device=x.device)
+            for j, (h, out, offsets, order) in enumerate(parts):
+                out = c.unpack_rows(out) if self.packed else out.float()
+                dweights[j] = (dtotal * out).sum(1)
+                dout = (dtotal * weights[j][:, None]).to(self.dtype)
+                dh, dw2, db2 = c.grouped_mm_backward(dout, h, w2, offsets, order=order, gate=h)
+                dpart, dw1, db1 = c.grouped_mm_backward(dh, y, w1, offsets, order=order)
+                dn += dpart.float()
+                of_part = dict(w1=dw1.float(), b1=db1, w2=dw2.float(), b2=db2)
+                sums = of_part if sums is None else {name: sums[name] + v for name, v in of_part.items()}
+            dscores = c.route_backward(scores, lse, experts, counts, dweights=dweights, dloss=dloss, renorm=True)
+            dpart, drouter, _ = c.grouped_mm_backward(dscores, y, router, whole)
+            dx, dgain, dshift = c.layer_norm_backward((dn + dpart.float()).to(self.dtype), x, mean, rstd, gain)
+            dy = dy + dx
+            grads.insert(0, dict(gain=dgain, shift=dshift, router=drouter[0], **sums))
+        self.dtable = c.embed_backward(dy, state.ids, self.table.shape[0], scale=self.scale, dtype=torch.float32)
+        self.grads, self._waiting = grads, 0
+
+    def update(self, rate):
+        if self.dtable is None:
+            raise DistShapError(DS_EINVAL, "update without the gradients of a backward pass")
+        super().update(rate)
+        self.table.sub_(rate * self.dtable)
 
 
 def main(nodes=2000, width=64, steps=60):
@@ -121,18 +218,45 @@ def main(nodes=2000, width=64, steps=60):
             print(f"step {step}: mean squared error {off.square().mean().item():.4f}", flush=True)
         enc.backward(off * (2.0 / nodes))
         enc.update(0.02)
-    # a ring with chords, a GCN on the learned features, and the edges that one of its answers rests on
+    _explain(ctx, enc.forward(x, kind).float(), rand)
+    ctx.close()
+
+
+def main_ids(nodes=1000, width=32, steps=60):
+    """Nodes that have an id alone learn features that a target asks for, through experts that are chosen for them."""
+    from . import Context
+    ctx = Context("cuda:0")
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(2)
+    rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda:0")   # noqa: E731
+    target = rand(nodes, width)
+    enc = RoutedEncoder(ctx, nodes, 4, width, 2 * width, depth=2, packed=True)
+    for step in range(steps):
+        ids = torch.randint(0, nodes, (2 * nodes,), generator=g, device="cuda:0").to(torch.int32)
+        out = enc.forward(ids, train=True, step=step)
+        off = out.float() - target[ids.long()]
+        if step % 10 == 0 or step == steps - 1:
+            print(f"step {step}: mean squared error {off.square().mean().item():.4f}, balance {enc.balance.item():.3f}", flush=True)
+        enc.backward(off * (2.0 / nodes), balance=0.1)
+        enc.update(0.1)
+    print("experts of the last block:", enc.counts[-1][:-1].tolist())
+    _explain(ctx, enc.forward(torch.arange(nodes, device="cuda:0").to(torch.int32)).float(), rand)
+    ctx.close()
+
+
+def _explain(ctx, features, rand):
+    """A ring with chords, a GCN on the learned features, and the edges that one of its answers rests on."""
+    nodes, width = features.shape
     near = torch.tensor([-7, -1, 1, 7])
     col = ((torch.arange(nodes)[:, None] + near) % nodes).sort(1)[0].reshape(-1).to(torch.int32)
     ctx.set_graph(torch.arange(nodes + 1) * 4, col)
-    ctx.set_features(enc.forward(x, kind).float())
+    ctx.set_features(features)
     ctx.set_gcn([rand(width, 32) * 0.2, rand(32, 4) * 0.2])
     phi, src, dst, report, _ = ctx.explain(5, 4096, seed=3)
     top = phi.abs().topk(3)[1]
     print(f"node 5 is of class {report.pred_class}; of {report.num_players} edges, these weigh most:",
           [(int(src[i]), int(dst[i]), round(float(phi[i]), 4)) for i in top])
-    ctx.close()
 
 
 if __name__ == "__main__":
-    main()
+    main_ids() if sys.argv[1:] == ["ids"] else main()
