@@ -11,8 +11,6 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define DS_LDS __attribute__((address_space(3)))
-#define DS_GLOBAL __attribute__((address_space(1)))
-
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
 
@@ -247,8 +245,8 @@ __device__ __forceinline__ int hidden(int v) {
 // step are read while the matrix cores work on the slice before. Results leave through LDS of their own, while the next tile's steps come in.
 // Long contractions are bound by the matrix cores and the card's power (65,536 rows by 4,096 x 1,024 bf16 in 8 groups 602 us, 910 TFLOP/s; a large
 // library product 1,218), short ones by the results, which no products go on beside (a unit has the registers of one such tile), and by the last
-// round of tiles: 131,072 rows by 1,024 x 1,024, rows gathered and scattered, 340 us, 810 TFLOP/s; dx of 65,521 rows by 1,024 x 512 with its gate 150 us,
-// 460 TFLOP/s, 2.2 TB/s; fp32 30,011 rows by 512 x 256 76 us, 104 TFLOP/s (a large library product: 153).
+// round of tiles: 131,072 rows by 1,024 x 1,024, rows gathered and scattered, 340 us, 810 TFLOP/s; dx of 65,521 rows by 1,024 x 512 111 us, 620 TFLOP/s, and with its
+// gate 135 (bf16) and 143 (codes, which the compiler waited for one by one before: 177); fp32 30,011 rows by 512 x 256 76 us, 104 TFLOP/s (a large library product: 153).
 template <typename T, int BR, int BN, int WR, int WN, bool TRANSPOSED, bool DIRECT, bool PACKED = false>
 __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T);
@@ -416,7 +414,10 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
       const float least = !TRANSPOSED && a.relu ? 0.f : -INFINITY;
       const int chunk = lane % CHUNKS, c = col + chunk * N;
       const int* rows = row_of[number & (HELD - 1)] + wr + lane / CHUNKS;
-      // (a gate is asked for two blocks of rows ahead, in front of stores that its coming would otherwise wait for)
+      // (a gate is asked for in front of stores that its coming would otherwise wait for: one of codes all of it, one of T, for which there are not the
+      // registers, two blocks of rows ahead)
+      constexpr int AHEAD = PACKED ? NR : 2;
+      const bool cut = c + N > width;
       typename Gate::V open[2 * NR][OUTS];
       const auto ask = [&](int r) __attribute__((always_inline)) {
         if constexpr (TRANSPOSED) {
@@ -425,14 +426,14 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
             for (int half = 2 * r; half < 2 * r + 2; ++half)
 #pragma unroll
               for (int i = 0; i < OUTS; ++i) {
-                const int to = rows[half * OUT_ROWS + i * AT_ONCE];
-                if (to >= 0 && c < width) open[half][i] = Gate::load(gate + to * a.gs + c, gate_end);
+                const typename Gate::E* from = gate + max(rows[half * OUT_ROWS + i * AT_ONCE], 0) * a.gs + min(c, width - 1);   // (no row: any)
+                open[half][i] = Gate::at(cut && from + N > gate_end ? gate_end - N : from);
               }
           }
         }
       };
-      ask(0);
-      ask(1);
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r) ask(r);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the next step has come in: see step)
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
                 out[n][p][q + i] = (T)v;
               }
             }
-        if (r) ask(r + 1);
+        if (r) ask(r + AHEAD - 1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // 16 rows at a time
           const int half = 2 * r + h;
@@ -475,8 +476,11 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void row_tiles_kernel(MmArgs a) {
             if (to < 0 || c >= width) continue;
             PieceV<T> v = *reinterpret_cast<const PieceV<T>*>(held);
             if (TRANSPOSED && gate) {
-#pragma unroll
-              for (int j = 0; j < N; ++j) v[j] = Gate::is_open(open[half][i], j) ? v[j] : (T)0.f;
+              if (cut) {   // (read in front of its place?)
+                const int64_t by = (to - (int64_t)(a.rows - 1)) * a.gs + c + N - width;
+                if (by > 0) open[half][i] = Gate::behind(open[half][i], (unsigned)by);
+              }
+              v = Gate::through(open[half][i], v);
             }
             T* target = y + to * a.ys + c;
             if (c + N <= width) *reinterpret_cast<typename Piece<T>::U*>(target) = v;
@@ -578,8 +582,9 @@ __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit,
   return before;
 }
 
-// PACKED: x is held in 8 bits. Its codes and scales come through registers, two stages ahead, and go into LDS as the numbers that they stand for; dy, and all that is
-// done with what is in LDS, is as without: 65,521 rows by 1,024 x 512 TIME.
+// PACKED: x is held in 8 bits; what is done with the numbers in LDS is as without. 2: rows are aligned for it, and codes and scales go into LDS as they are, four stages
+// ahead, from where they are decoded into one of two arrays a stage before they are needed. 1: they come through registers, two stages ahead. 65,521 rows
+// by 1,024 x 512 bf16 in 16 groups: 113 us (2), 122 (1), 93 from bf16 rows; the decoding is in front of the products that it cannot be beside.
 template <typename T, int BR, int BN, int WR, int WN, bool DIRECT, int PACKED = 0>
 __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial, int most_chunks) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
@@ -713,7 +718,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
           PackedPiece<N> piece;
           if constexpr (N == 8) piece = (uint64_t)word[2 * p] | (uint64_t)word[2 * p + 1] << 32;
           else piece = word[p];
-          // (a store of its own: the compiler has one wait for all that is on its way to LDS, though nothing of it goes here; 122 us, so TIME2)
+          // (a store of its own: the compiler has one wait for all that is on its way to LDS, though nothing of it goes here: 122 us with it)
           const PieceV<T> v = decoded<T>(piece, scale);
           const uint32_t at = (uint32_t)(uintptr_t)(DS_LDS char*)to + (code_line * XOp::PER_ROW + XOp::exchange(code_line, code_col / N + p)) * 16;
           asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory");

@@ -12,6 +12,8 @@
 
 namespace {
 
+#define DS_GLOBAL __attribute__((address_space(1)))
+
 constexpr int kPackBlock = 32;   // columns that share a scale
 
 // 2^(s - 127)
@@ -79,14 +81,22 @@ __device__ __forceinline__ typename Piece<T>::V decoded(PackedPiece<Piece<T>::N>
   return v;
 }
 
-// A gate of dx: open where its value is above 0 (an infinity's code is that of a NaN, which is not)
+// A gate of dx: open where its value is above 0 (an infinity's code is that of a NaN, which is not). `load` is a piece, zeros behind the matrix' end; `at` one as it
+// stands, and `behind` what is left of it where it was read `by` elements in front of its place: nothing waits for a load where it is asked for.
 template <typename T, bool PACKED>
 struct RowGate {
   typedef T E;
   typedef typename Piece<T>::V V;
   static __device__ __forceinline__ V load(const T* p, const T* end) { return load_within<T>(p, end); }
+  static __device__ __forceinline__ V at(const T* p) { return *(const DS_GLOBAL typename Piece<T>::U*)p; }
+  static __device__ __forceinline__ V behind(V v, unsigned by) { return shifted<T>(v, by); }
   static __device__ __forceinline__ V load_first(const T* p, int have) { return load_piece<T>(p, have); }
   static __device__ __forceinline__ bool is_open(V v, int i) { return (float)v[i] > 0.f; }
+  static __device__ __forceinline__ PieceV<T> through(V gate, PieceV<T> v) {
+#pragma unroll
+    for (int i = 0; i < Piece<T>::N; ++i) v[i] = is_open(gate, i) ? v[i] : (T)0.f;
+    return v;
+  }
 };
 template <typename T>
 struct RowGate<T, true> {
@@ -98,8 +108,34 @@ struct RowGate<T, true> {
     const V v = load_codes<N>(by <= 0 ? p : end - N);
     return by <= 0 ? v : shifted_codes<N>(v, by < N ? (unsigned)by : N);
   }
+  static __device__ __forceinline__ V at(const uint8_t* p) {
+    typedef V U __attribute__((aligned(1)));
+    return *(const DS_GLOBAL U*)p;
+  }
+  static __device__ __forceinline__ V behind(V v, unsigned by) { return shifted_codes<N>(v, by); }
   static __device__ __forceinline__ V load_first(const uint8_t* p, int have) { return load_first_codes<N>(p, have); }
   static __device__ __forceinline__ bool is_open(V v, int i) { return (uint32_t)((v >> (8 * i)) & 255) - 1u < 126u; }
+  // (four codes at a time: a byte's highest bit says that it is 1 to 126, and then is all of its bits)
+  static __device__ __forceinline__ PieceV<T> through(V gate, PieceV<T> v) {
+    union {
+      PieceV<T> piece;
+      uint32_t word[4];
+    } u;
+    u.piece = v;
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+      const uint32_t c = (uint32_t)((uint64_t)gate >> (32 * q)), low = c & 0x7f7f7f7fu;
+      const uint32_t high = (low + 0x7f7f7f7fu) & ~((low + 0x01010101u) | c) & 0x80808080u, whole = high | (high - (high >> 7));
+      if constexpr (sizeof(T) == 2) {
+        u.word[2 * q] &= __builtin_amdgcn_perm(whole, whole, 0x01010000u);
+        u.word[2 * q + 1] &= __builtin_amdgcn_perm(whole, whole, 0x03030202u);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u.word[4 * q + i] &= (uint32_t)((int32_t)(whole << (24 - 8 * i)) >> 31);
+      }
+    }
+    return u.piece;
+  }
 };
 
 }  // namespace
