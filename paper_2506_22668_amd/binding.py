@@ -790,11 +790,11 @@ class Context:
         ws, wsp, wsn = self._workspace(self.lib.ds_route_workspace, rows, experts)
         if not 1 <= k <= min(8, experts):
             self._refuse(f"{k} experts to a row out of range [1, {min(8, experts)}]")
-        ids = t.empty((k, rows), dtype=t.int32, device=x.device)
-        weights = t.empty((k, rows), dtype=t.float32, device=x.device)
-        counts = t.empty(experts + 1, dtype=t.int64, device=x.device)
-        lse = t.empty(rows, dtype=t.float32, device=x.device)
-        loss = t.empty((), dtype=t.float32, device=x.device)
+        ids = x.new_empty((k, rows), dtype=t.int32)
+        weights = x.new_empty((k, rows), dtype=t.float32)
+        counts = x.new_empty(experts + 1, dtype=t.int64)
+        lse = x.new_empty(rows, dtype=t.float32)
+        loss = x.new_empty((), dtype=t.float32)
         self._queue(self.lib.ds_route, self._elements[x.dtype], rows, experts, k, int(bool(renorm)), x.data_ptr(), xs, ids.data_ptr(), weights.data_ptr(),
                     counts.data_ptr(), loss.data_ptr(), lse.data_ptr(), wsp, wsn)
         return self._outputs("route", (ids, weights, counts, loss, lse), given)

@@ -584,7 +584,7 @@ __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit,
 
 // PACKED: x is held in 8 bits; what is done with the numbers in LDS is as without. 2: rows are aligned for it, and codes and scales go into LDS as they are, four stages
 // ahead, from where they are decoded into one of two arrays a stage before they are needed. 1: they come through registers, two stages ahead. 65,521 rows
-// by 1,024 x 512 bf16 in 16 groups: 113 us (2), 122 (1), 93 from bf16 rows; the decoding is in front of the products that it cannot be beside.
+// by 1,024 x 512 bf16 in 16 groups: 113 us (2), 122 (1), 93 from bf16 rows; 2,870 rows by 608 x 1,064 fp16 in 22 groups 34, 45, 33; the decoding is in front of the products that it cannot be beside.
 template <typename T, int BR, int BN, int WR, int WN, bool DIRECT, int PACKED = 0>
 __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial, int most_chunks) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
@@ -595,10 +595,10 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
   constexpr int LINES = THREADS / DOp::PER_ROW, EACH = DEPTH / LINES;   // of a thread's pieces of a stage: lines apart, and how many
   constexpr int RING = 4 * DEPTH;
   // (x held in 8 bits has arrays of its own: what is written into an array waits for what comes into it directly)
-  constexpr int HELD = PACKED ? DOp::BYTES : STAGE, APART = PACKED ? XOp::BYTES : 16, CODES = PACKED == 2 ? DEPTH * BR : 16, SCALES = PACKED == 2 ? CODES / kPackBlock : 16;
+  constexpr int HELD = PACKED ? DOp::BYTES : STAGE, APART = PACKED ? XOp::BYTES : 16, CODES = PACKED == 2 ? DEPTH * BR : 16, SCALES = PACKED == 2 ? CODES / kPackBlock * 4 : 16;
   __shared__ __attribute__((aligned(128))) char stage0[HELD], stage1[HELD], stage2[HELD], stage3[HELD], x0[APART], x1[APART];
   __shared__ __attribute__((aligned(128))) char x2[PACKED == 1 ? APART : 16], x3[PACKED == 1 ? APART : 16];
-  // (codes, and behind them the scales: the compiler tells apart eight arrays that loads go to directly)
+  // (codes, and behind them the scales, four bytes to each, as a load of bytes leaves them: the compiler tells apart eight arrays that loads go to directly)
   __shared__ __attribute__((aligned(128))) uint8_t codes0[CODES + SCALES], codes1[CODES + SCALES], codes2[CODES + SCALES], codes3[CODES + SCALES];
   __shared__ float sums[LINES][BN];
   __shared__ int row_of[2][THREADS];
@@ -671,10 +671,11 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
     if constexpr (PACKED == 2) {
       // Codes and scales come into LDS as they are, four stages ahead, and a thread turns the 16 (fp32: four) codes that it asked for into numbers a stage before they are
       // needed: into one of two arrays, since the other is not read any more by then.
-      constexpr int CPT = CODES / THREADS, PARTS = BR / (4 * kPackBlock);   // codes of a thread, words of scales of a row
+      constexpr int CPT = CODES / THREADS, PARTS = BR / kPackBlock, ROUND = SCALES / 4;   // codes of a thread; scales of a row, and of a stage
       static_assert(CPT == 16 || CPT == 4, "");
       const int code_line = (int)threadIdx.x / (BR / CPT), code_col = (int)threadIdx.x % (BR / CPT) * CPT;
-      const int scale_line = lane / PARTS, scale_col = in0 + lane % PARTS * (4 * kPackBlock);
+      static_assert(ROUND % 64 == 0 && THREADS % ROUND == 0, "");   // (a scale of a stage comes in by one wave or by several: the same bytes)
+      const int scale_at = wave * 64 % ROUND, scale_line = (scale_at + lane) / PARTS, scale_col = in0 + (scale_at + lane) % PARTS * kPackBlock;
       const auto row_at = [&](int pos) __attribute__((always_inline)) { return pos < stop ? ds_ordered_row(a.order, a.rows, pos) : -1; };
       row_of[0][threadIdx.x] = row_at(start + (int)threadIdx.x);
       int later = row_at(start + THREADS + (int)threadIdx.x), x_stage = 0, dy_stage = 0, rows_of_dy[EACH];
@@ -692,11 +693,9 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
         const uint8_t* src = row >= 0 && in0 + code_col < a.inner ? a.codes + row * a.xs + (in0 + code_col) : zeros;
         if constexpr (CPT == 16) __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(codes + wave * 64 * CPT), 16, 0, 0);
         else __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)src, (DS_LDS void*)(codes + wave * 64 * CPT), 4, 0, 0);
-        if (lane < SCALES / 4) {   // (each wave the same words)
-          const int scale_row = rows[scale_line];
-          const uint8_t* from = scale_row >= 0 && scale_col < a.inner ? a.scales + scale_row * a.scales_stride + scale_col / kPackBlock : zeros;
-          __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)from, (DS_LDS void*)(codes + CODES), 4, 0, 0);
-        }
+        const int scale_row = rows[scale_line];
+        const uint8_t* from = scale_row >= 0 && scale_col < a.inner ? a.scales + scale_row * a.scales_stride + scale_col / kPackBlock : zeros;
+        __builtin_amdgcn_global_load_lds((const DS_GLOBAL void*)from, (DS_LDS void*)(codes + CODES + scale_at * 4), 1, 0, 0);
 #pragma unroll
         for (int u = 0; u < EACH; ++u) rows_of_dy[u] = rows[u * LINES + line];
         ++x_stage;
@@ -709,7 +708,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a,
         ++dy_stage;
       };
       const auto decode = [&](const uint8_t* codes, char* to) __attribute__((always_inline)) {
-        const uint32_t scale = codes[CODES + code_line * (BR / kPackBlock) + code_col / kPackBlock];
+        const uint32_t scale = codes[CODES + (code_line * PARTS + code_col / kPackBlock) * 4];
         uint32_t word[CPT / 4];
 #pragma unroll
         for (int i = 0; i < CPT / 4; ++i) word[i] = reinterpret_cast<const uint32_t*>(codes)[(int)threadIdx.x * (CPT / 4) + i];
@@ -1085,9 +1084,9 @@ int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
   // (x held in 8 bits comes through registers either way)
   const bool direct = (PACKED || (sixteen(a.x, a.xs, sizeof(T)) && a.inner % Piece<T>::N == 0)) && sixteen(a.dy, a.dys, sizeof(T)) && a.outer % Piece<T>::N == 0;
   const dim3 grid((unsigned)wgs), block(64 * WR * WN);
-  bool codes_direct = false;   // rows of codes and scales that can come into LDS as they are
+  bool codes_direct = false;   // rows of codes that can come into LDS as they are
   if constexpr (PACKED) {
-    codes_direct = direct && sixteen(a.codes, a.xs, 1) && a.inner % (4 * kPackBlock) == 0 && (uintptr_t)a.scales % 4 == 0 && a.scales_stride % 4 == 0;
+    codes_direct = direct && sixteen(a.codes, a.xs, 1) && a.inner % 16 == 0;
     if (codes_direct) hipLaunchKernelGGL(HIP_KERNEL_NAME(weight_tiles_kernel<T, BR, BN, WR, WN, true, 2>), grid, block, 0, ctx->stream, a, partial, (int)chunks);
   }
   if (codes_direct) ;

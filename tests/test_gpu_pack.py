@@ -200,6 +200,8 @@ SHAPES = [(1, 1, 1, 1), (1, 16, 16, 3), (5, 40, 24, 4), (8, 256, 1000, 8), (33, 
           (5000, 512, 768, 4), (777, 1032, 40, 1),
           # many tiles
           (70001, 16, 129, 2), (66001, 264, 136, 3), (40003, 131, 259, 7), (33000, 72, 520, 20), (20000, 512, 512, 2),
+          # rows of whole pieces of codes, and of any number of scales
+          (1500, 48, 256, 4), (2100, 272, 264, 3), (4001, 608, 128, 2), (30011, 80, 512, 5),
           # few rows to a group
           (20, 2100, 136, 2), (50, 2101, 131, 2), (20, 136, 2100, 2), (100, 72, 2056, 2), (1000, 515, 257, 40), (2000, 520, 1024, 40),
           # narrow
