@@ -155,7 +155,8 @@ __device__ __forceinline__ void highest(const int (&key)[PER], int (&list)[K]) {
   }
 }
 
-// Counts of a row's experts are added up in LDS (whole numbers: in any order). 1,000,175 rows of 64 bf16, 2 of them each: see the table of times in front of launch_of.
+// Counts of a row's experts are added up in LDS (whole numbers: in any order). Bound by vector instructions, about 18 a score:
+// 1,000,175 rows of 64 bf16, 2 of them each, 38.5 us (29 for the bytes); 30,011 rows of 515 fp32, 8 of them each, 40.1 (12.6 for the bytes: a list of nine places to a score).
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
   constexpr int ROWS = THREADS / TPR, WAVES = THREADS / 64, WIDE = TPR * PER, LIST = sizeof(T) == 4 ? K + 1 : K, OWN = (K + TPR - 1) / TPR;
@@ -362,7 +363,7 @@ struct RouteGradArgs {
 
 // The scores that were chosen are read once more, each by its address: a row's sum takes their gradients from there, and the threads that hold them take them from a row
 // in LDS, which is zero but for them (comparing experts in the registers takes four instructions a score and choice). Only the row's own threads, of one
-// wave, touch it, and a wave's LDS accesses keep their order.
+// wave, touch it, and a wave's LDS accesses keep their order. Bound by memory: 131,072 rows of 256 bf16, 4 of them each, 27.7 us, 5.0 TB/s.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
   constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N, OWN = (K + TPR - 1) / TPR;
