@@ -718,7 +718,7 @@ class Context:
         ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_packed_workspace, element, rows, inner, outer, groups, int(gp is not None))
         self._queue(self.lib.ds_grouped_mm_backward_packed, element, rows, inner, outer, groups, dy.data_ptr(), dys, codes.data_ptr(), cs, scales.data_ptr(), ss,
                     wp, op, rp, gp, gs, dx.data_ptr(), inner, dw.data_ptr(), db.data_ptr(), wsp, wsn)
-        return self._outputs("grouped_mm_backward", (dx, dw, db), dy, w)
+        return self._outputs("grouped_mm_backward", (dx, dw, db), dy, codes, w)
 
     def pack_rows(self, x):
         """The rows of x in 8 bits, as `Packed`: what a training step keeps of an activation, half of 16 bits. Zeros stay zeros, and nothing else becomes

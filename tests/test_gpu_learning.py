@@ -139,7 +139,7 @@ def _inputs(rows, vocab, seed):
                 whole=torch.tensor([0, rows], device="cuda"))
 
 
-SIZES = [(50, 70), (9_000, 300), (70_000, 200_000)]
+SIZES = [(50, 70), (9_000, 300), (70_000, 200_000), (20_000, 600_000)]
 
 
 @pytest.mark.parametrize("rows, vocab", SIZES)
@@ -221,11 +221,52 @@ def test_gradients_are_calls_of_their_own(ctx):
     g = generator(9)
     table, scores = normal(g, 5, 8).requires_grad_(True), normal(g, 6, 4).requires_grad_(True)
     ids = torch.tensor([0, 3, 4], device="cuda").int()
-    for value in (ctx.embed(table, ids).sum(), ctx.route(scores, 2)[1].sum(), ctx.route(scores, 2)[3]):
+    x, w, offsets = normal(g, 6, 4).requires_grad_(True), normal(g, 1, 4, 4), torch.tensor([0, 6], device="cuda")
+    kept = ctx.pack_rows(x)
+    for value in (ctx.embed(table, ids).sum(), ctx.route(scores, 2)[1].sum(), ctx.route(scores, 2)[3], ctx.unpack_rows(kept).sum(),
+                  ctx.grouped_mm_backward(normal(g, 6, 4), kept, w, offsets, gate=kept)[1].sum()):
         with pytest.raises(DistShapError):
             value.backward()
     with torch.no_grad():
         assert not ctx.embed(table, ids).requires_grad
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("rows", [0, 1])
+def test_steps_of_no_row_and_of_one(ctx, rows, packed):
+    from paper_2506_22668_amd.encoder import RoutedEncoder
+    say(f"routed encoder rows={rows} packed={packed}")
+    enc = RoutedEncoder(ctx, 5, 3, 16, 24, depth=2, k=2, dtype=F32, p=0.0, packed=packed)
+    ids = torch.full((rows,), 3, device="cuda").int()
+    out = enc.forward(ids, train=True)
+    assert out.shape == (rows, 16) and [int(c[-1]) for c in enc.counts] == [rows, rows]
+    enc.backward(torch.ones_like(out), balance=1.0)
+    came = enc.dtable.any(1).tolist()
+    assert came == [False, False, False, rows == 1, False] and torch.isfinite(enc.dtable).all()
+    for grads in enc.grads:
+        for k, v in grads.items():
+            assert torch.isfinite(v).all() and (rows == 1 or not v.any()), k
+    enc.update(0.1)
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+def test_gates_that_are_one_row_for_all_and_end_inside_a_piece(ctx, t):
+    """Gates of rows and of codes, the last rows' pieces reaching over the end of the matrix."""
+    say(f"gates {t}")
+    g = generator(11)
+    rows, inner, outer = 3001, 259, 64
+    x, dy, w = normal(g, rows, inner, t=t).relu(), normal(g, rows, outer, t=t), normal(g, 2, inner, outer, t=t, scale=0.1)
+    order = torch.randperm(rows, generator=g, device="cuda").int()
+    offsets = torch.tensor([0, 1000, rows], device="cuda")
+    open_ = ctx.grouped_mm_backward(dy, x, w, offsets, order=order)[0]
+    for gate in (x, x[:1].expand(rows, inner), x[-1:].expand(rows, inner)):
+        want = torch.where(gate > 0, open_, torch.zeros_like(open_))
+        assert torch.equal(ctx.grouped_mm_backward(dy, x, w, offsets, order=order, gate=gate)[0], want)
+        kept = ctx.pack_rows(x)
+        held = ctx.pack_rows(gate.contiguous()) if gate is x else ctx.pack_rows(gate[:1].contiguous())
+        if gate is not x:
+            held = type(held)(held.codes.view(torch.uint8).expand(rows, inner).view(torch.float8_e4m3fn), held.scales.expand(rows, held.scales.shape[1]))
+        assert torch.equal(ctx.grouped_mm_backward(dy, kept, w, offsets, order=order, gate=held)[0], want)
 
 
 def test_the_example_runs(capsys):
