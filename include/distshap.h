@@ -452,8 +452,7 @@ int ds_unpack_rows(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const
                    int64_t scales_stride, void* y, int64_t y_stride);
 
 /* ds_grouped_mm_backward with x held in 8 bits. gate: NULL, or codes of rows like x: dx is 0 where the code is not above 0. */
-int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, int32_t gate,
-                                            int64_t* bytes /* [host] */);
+int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, int64_t* bytes /* [host] */);
 int ds_grouped_mm_backward_packed(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, const void* dy, int64_t dy_stride,
                                   const uint8_t* codes, int64_t codes_stride, const uint8_t* scales, int64_t scales_stride, const void* w,
                                   const int64_t* offsets, const int32_t* order, const uint8_t* gate, int64_t gate_stride, void* dx, int64_t dx_stride,

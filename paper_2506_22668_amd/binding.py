@@ -166,7 +166,7 @@ def load_library():
         "ds_route_backward": [p, i32, i64, i64, i64, i32, p, i64, p, p, p, p, p, p, i64],
         "ds_pack_rows": [p, i32, i64, i64, p, i64, p, i64, p, i64],
         "ds_unpack_rows": [p, i32, i64, i64, p, i64, p, i64, p, i64],
-        "ds_grouped_mm_backward_packed_workspace": [i32, i64, i64, i64, i64, i32, C.POINTER(i64)],
+        "ds_grouped_mm_backward_packed_workspace": [i32, i64, i64, i64, i64, C.POINTER(i64)],
         "ds_grouped_mm_backward_packed": [p, i32, i64, i64, i64, i64, p, i64, p, i64, p, i64, p, p, p, p, i64, p, i64, p, p, p, i64],
     }
     for name, args in sigs.items():
@@ -715,7 +715,7 @@ class Context:
         dw = w.new_empty((groups, inner, outer))
         db = t.empty((groups, outer), dtype=t.float32, device=w.device)
         element = self._elements[w.dtype]
-        ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_packed_workspace, element, rows, inner, outer, groups, int(gp is not None))
+        ws, wsp, wsn = self._workspace(self.lib.ds_grouped_mm_backward_packed_workspace, element, rows, inner, outer, groups)
         self._queue(self.lib.ds_grouped_mm_backward_packed, element, rows, inner, outer, groups, dy.data_ptr(), dys, codes.data_ptr(), cs, scales.data_ptr(), ss,
                     wp, op, rp, gp, gs, dx.data_ptr(), inner, dw.data_ptr(), db.data_ptr(), wsp, wsn)
         return self._outputs("grouped_mm_backward", (dx, dw, db), dy, codes, w)

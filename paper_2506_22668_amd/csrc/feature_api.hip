@@ -268,7 +268,7 @@ int ds_unpack_rows(ds_ctx* ctx, int32_t dtype, int64_t rows, int64_t cols, const
   return ds_launch_unpack(ctx, dtype, rows, (int)cols, {codes, codes_stride, scales, scales_stride}, {y, y_stride});
 }
 
-int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, int32_t gate, int64_t* bytes) {
+int ds_grouped_mm_backward_packed_workspace(int32_t dtype, int64_t rows, int64_t inner, int64_t outer, int64_t groups, int64_t* bytes) {
   if (!bytes || !known(dtype) || rows < 0 || rows > kMostOrdered || inner < 1 || inner > kMostCols || outer < 1 || outer > kMostCols ||
       groups < 1 || groups > kMostGroups)
     return DS_EINVAL;

@@ -65,7 +65,7 @@ def test_a_workspace_of_packed_gradients_that_is_too_small_is_refused(ctx):  # n
     lib = binding.load_library()
     need = C.c_int64()
     big = dict(rows=100_000, inner=512, outer=512, cs=512, ss=16, gs=512, dys=512, dxs=512)
-    assert lib.ds_grouped_mm_backward_packed_workspace(1, 100_000, 512, 512, 3, 1, C.byref(need)) == 0 and need.value > 0
+    assert lib.ds_grouped_mm_backward_packed_workspace(1, 100_000, 512, 512, 3, C.byref(need)) == 0 and need.value > 0
     for change in (dict(wsn=need.value - 1), dict(ws=None)):
         assert lib.ds_grouped_mm_backward_packed(ctx, *{**PACKED_BACKWARD, **big, **change}.values()) == DS_ECAPACITY
 
@@ -78,7 +78,7 @@ def test_sizes_out_of_range_have_no_workspace():
     for args in [(-1, 8), (MANY, 8), (8, 0), (8, 1025)]:
         assert lib.ds_route_workspace(*args, C.byref(need)) == DS_EINVAL
     for args in [(5, 1, 1, 1, 1), (0, -1, 1, 1, 1), (0, 1, 0, 1, 1), (0, 1, 1, 0, 1), (0, 1, 1, 1, 0)]:
-        assert lib.ds_grouped_mm_backward_packed_workspace(*args, 0, C.byref(need)) == DS_EINVAL
+        assert lib.ds_grouped_mm_backward_packed_workspace(*args, C.byref(need)) == DS_EINVAL
     assert lib.ds_embed_backward_workspace(8, 8, 8, None) == lib.ds_route_workspace(8, 8, None) == DS_EINVAL
     # the largest that are allowed have one
     assert lib.ds_embed_backward_workspace(1 << 30, 1 << 20, 1 << 30, C.byref(need)) == 0 and need.value > 1 << 40
