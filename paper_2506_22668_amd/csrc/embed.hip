@@ -574,12 +574,13 @@ __global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int col
 // workers take equal shares of them. What ids that reach over a share's end leave meets in LDS. Every workgroup reads all ids, which is why rows are few: 1,010 rows of 64 fp32 into
 // 2,000 6.1 us in one launch, 16.6 in the six of the other form; bound by latency.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRange = 256;
-constexpr int kFewRows = 4096;
+constexpr int kFewRows = 8192;
+static_assert(kFewRange <= 256 && kFewRows <= 1 << 24, "a pair is 32 bits");
 template <typename D, typename T, int LANES, bool TINY>
 __global__ __launch_bounds__(kFewThreads) void few_sums_kernel(SumArgs a) {
   constexpr int N = Piece<D>::N, WORKERS = kFewThreads / LANES, P = Piece<T>::N;
   __shared__ int count[kFewWaves][kFewRange], start[kFewRange + 1], wave_sum[kFewWaves];
-  __shared__ int2 held[kFewRows];
+  __shared__ uint32_t held[kFewRows];   // (digit, row)
   __shared__ float meet[WORKERS][2][LANES * N];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first_id = (int)blockIdx.x * a.range, range = min(a.range, a.vocab - first_id);
   for (int i = threadIdx.x; i < kFewWaves * kFewRange; i += kFewThreads) (&count[0][0])[i] = 0;
@@ -629,7 +630,7 @@ __global__ __launch_bounds__(kFewThreads) void few_sums_kernel(SumArgs a) {
       }
       if (there) {
         const int rank = __popcll(same & ((1ull << lane) - 1)), at = mine[digit];
-        held[at + rank] = int2{(int)digit, base + lane};
+        held[at + rank] = digit << 24 | (uint32_t)(base + lane);
         if (rank == 0) mine[digit] = at + __popcll(same);   // (a wave's LDS accesses keep their order)
       }
     }
@@ -638,14 +639,15 @@ __global__ __launch_bounds__(kFewThreads) void few_sums_kernel(SumArgs a) {
   T* dtable = (T*)a.dtable + (int64_t)first_id * a.dts;
   const int worker = (int)threadIdx.x / LANES, place = (int)threadIdx.x % LANES * N, col = (int)blockIdx.y * LANES * N + place, have = a.cols - col;
   const int share = (all + WORKERS - 1) / WORKERS, from = min(worker * share, all), to = min(from + share, all);
-  const bool before = from > 0 && from < to && held[from - 1].x == held[from].x, after = to < all && from < to && held[to].x == held[to - 1].x;
+  const auto id_of = [&](int i) { return (int)(held[i] >> 24); };
+  const bool before = from > 0 && from < to && id_of(from - 1) == id_of(from), after = to < all && from < to && id_of(to) == id_of(to - 1);
   if (have > 0) {
     for (int v = worker; v < range; v += WORKERS)
       if (start[v] == start[v + 1])
 #pragma unroll
         for (int p = 0; p < N / P; ++p) store_piece<T>(dtable + (int64_t)v * a.dts + col + p * P, PieceV<T>{}, have - p * P);
     if (from < to)
-      sum_rows<D, TINY>(from, to, col, a.cols, (const D*)a.dy, a.dys, a.range, [&](int i) { return held[i]; },
+      sum_rows<D, TINY>(from, to, col, a.cols, (const D*)a.dy, a.dys, a.range, [&](int i) { return int2{id_of(i), (int)(held[i] & 0xffffffu)}; },
                         [&](int key, const float(&sum)[N], bool first, bool last) {
                           const bool goes_on = last && after, began = first && before;
                           if (goes_on || began) {
@@ -658,15 +660,15 @@ __global__ __launch_bounds__(kFewThreads) void few_sums_kernel(SumArgs a) {
   }
   __syncthreads();
   // an id that begins in this share and goes on behind it
-  if (have > 0 && after && !(before && held[from].x == held[to - 1].x)) {
-    const int key = held[to - 1].x;
+  if (have > 0 && after && !(before && id_of(from) == id_of(to - 1))) {
+    const int key = id_of(to - 1);
     float sum[N] = {};
     int w = worker;
     do {
 #pragma unroll
       for (int i = 0; i < N; ++i) sum[i] += meet[w][1][place + i];
       ++w;
-    } while ((w + 1) * share < all && held[(w + 1) * share].x == key);
+    } while ((w + 1) * share < all && id_of((w + 1) * share) == key);
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] += meet[w][0][place + i];
     store_sums<T, N>(dtable + (int64_t)key * a.dts + col, sum, a.scale, have);
@@ -686,12 +688,14 @@ int digits_of(int vocab, int* passes) {
 }
 int sort_blocks(int rows) {
   const int blocks = (rows + kStretch - 1) / kStretch;
-  return blocks <= 4 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks;
+  return blocks <= 2 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks;
 }
 
 // Few rows: ids of a workgroup, so that there are about 512 workgroups (of 64 columns or more); 0: another form
 int few_range(int rows, int cols, int vocab) {
-  if (rows > kFewRows) return 0;
+  // (the rows of one id are all of one workgroup: of few ids half as many rows. 8,000 rows of 128 bf16 into 5,000 ids 12 us so, 38 sorted first, all of one id 74 and 49;
+  // into 8 ids 67 and 25.)
+  if (rows > (vocab < 512 ? kFewRows / 2 : kFewRows)) return 0;
   const int64_t range = ((int64_t)vocab * ((cols + 63) / 64) + 511) / 512;
   return range > kFewRange ? 0 : range < 8 ? 8 : (int)range;
 }

@@ -118,7 +118,7 @@ def shares(g, rows, vocab, how):
 @pytest.mark.parametrize("t, tt", [(F32, F32), (BF16, F32), (F16, F16)])
 @pytest.mark.parametrize("how", ["one", "none", "once", "sorted", "few", "uneven"])
 @pytest.mark.parametrize("rows, vocab, cols", [(2, 3, 8), (16, 1023, 24), (17, 1024, 8), (255, 300, 40), (1000, 1000, 16), (2049, 5000, 72), (8191, 1_100_000, 4),
-                                               (8192, 8192, 16), (8193, 70_000, 9), (20_011, 40_000, 33), (70_000, 1023, 64), (262_145, 300_000, 12)])
+                                               (8192, 8192, 16), (8193, 70_000, 9), (4096, 511, 24), (4097, 511, 24), (8192, 511, 8), (8192, 512, 131), (6000, 400, 16), (20_011, 40_000, 33), (70_000, 1023, 64), (262_145, 300_000, 12)])
 def test_gradient_of_ids_in_any_shares(ctx, t, tt, how, rows, vocab, cols):
     say(f"embed_backward {how} {t} rows={rows} vocab={vocab} cols={cols}")
     g = generator(rows)
