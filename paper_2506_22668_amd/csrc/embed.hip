@@ -5,7 +5,7 @@
 //
 // The gradient is summed by sorted ids: a stable radix sort of the pairs (id, r) on digits of up to 10 bits, then sums over stretches of equally many sorted
 // rows, whatever ids they hold, so that an id with a large share of the rows costs as much as as many ids with one row. Where a stretch
-// ends inside an id's rows it leaves a partial sum in fp32, and a last launch adds those up in order and clears the rows of ids that did not come up.
+// ends inside an id's rows it leaves a partial sum in fp32, and a last launch adds those up in order. Few rows are sorted and summed in one launch (few_sums_kernel).
 // No atomic decides an order of floating-point sums: the same inputs give the same bits.
 #include "feature_ops.h"
 #include "group_range.h"
