@@ -223,9 +223,9 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
       if (top == none) top = 0.f;
     }
     float q[PER], total = 0.f;
-    // (the second term's rounding is the same for a whole row, so it cancels in p; lse takes the term as it is)
+    // (the second term's rounding is the same for a whole row, so it cancels in p; `shift` is the power that the highest score itself gets by it, exactly, and lse goes without it)
     const bool near = fabsf(top) < 65536.f;
-    const float base = top * kLog2e;
+    const float base = top * kLog2e, shift = near ? fmaf(top, kLog2e, -base) : 0.f;
     if (near) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) q[i] = __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -base));
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
         if (id[c] >= 0) atomicAdd(&count[id[c]], 1);
       }
     }
-    if (t == 0 && a.lse) at_row(a.lse, row) = total == 0.f ? none : near ? (base + __log2f(total)) * kLn2 : fmaf(__log2f(total), kLn2, top);
+    if (t == 0 && a.lse) at_row(a.lse, row) = total == 0.f ? none : fmaf(__log2f(total) - shift, kLn2, top);
   }
   if constexpr (sizeof(T) == 4) __syncthreads();
   // the workgroup's rows: those of a wave first (lanes TPR apart)
