@@ -87,6 +87,11 @@ __device__ __forceinline__ float highest_lane(float v) {
 
 // e^d; 0 below 2^-126
 __device__ __forceinline__ float power_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// e^d with subnormal results
+__device__ __forceinline__ float whole_power_of(float d) {
+  const float e = __builtin_amdgcn_exp2f(d * (0.5f * kLog2e));
+  return e * e;
+}
 // 2^d with subnormal results
 __device__ __forceinline__ float whole_power(float d) {
   const float e = __builtin_amdgcn_exp2f(0.5f * d);
@@ -363,7 +368,8 @@ struct RouteGradArgs {
 
 // The scores that were chosen are read once more, each by its address: a row's sum takes their gradients from there, and the threads that hold them take them from a row
 // in LDS, which is zero but for them (comparing experts in the registers takes four instructions a score and choice). Only the row's own threads, of one
-// wave, touch it, and a wave's LDS accesses keep their order. Bound by memory: 131,072 rows of 256 bf16, 4 of them each, 27.7 us, 5.0 TB/s.
+// wave, touch it, and a wave's LDS accesses keep their order. What e^(x - lse) is off by lse's own rounding, which grows with the scores (1,000: 3e-5; where all are the type's
+// lowest value lse is that value, and each power 1), is the same for a row's experts: their sum takes it out. Bound by memory: 131,072 rows of 256 bf16, 4 of them each, 27.7 us, 5.0 TB/s.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
   constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N, OWN = (K + TPR - 1) / TPR;
@@ -442,14 +448,17 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
     }
     fetch(row + step);
     look_up(row + 2 * step);
-    float p[PER], s = 0.f, own = 0.f;
+    float p[PER], s = 0.f, own = 0.f, sum = 0.f;
     now.read(t, a.experts, none, p);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      p[i] = whole_power((p[i] - base) * kLog2e);   // (a row that is closed throughout: 0)
+      p[i] = whole_power_of(p[i] - base);   // (a row that is closed throughout: 0)
+      sum += p[i];
       s = fmaf(p[i], share[i], s);
     }
-    s = sum_lanes<TPR>(s);
+    sum = sum_lanes<TPR>(sum);
+    const float part = sum > 0.f ? __builtin_amdgcn_rcpf(sum) : 1.f;
+    s = sum_lanes<TPR>(s) * part;
     float g[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) g[i] = share[i];
@@ -457,7 +466,7 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
       float dot = 0.f, total = 0.f;
 #pragma unroll
       for (int c = 0; c < OWN; ++c) {
-        of[c] = id[c] < 0 ? 0.f : whole_power((of[c] - base) * kLog2e);
+        of[c] = id[c] < 0 ? 0.f : whole_power_of(of[c] - base) * part;
         dp[c] = id[c] < 0 ? 0.f : dp[c];
         total += of[c];
         dot = fmaf(dp[c], of[c], dot);
@@ -490,14 +499,14 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
         if (id[c] >= 0) mine[id[c]] = 0.f;
       __builtin_amdgcn_wave_barrier();
     }
-    s += own;
+    s = (s + own) * part;
     T* dx = (T*)a.dx + row * a.ys;
 #pragma unroll
     for (int q = 0; q < PIECES; ++q) {
       const int at = (q * TPR + t) * N;
       PieceV<T> out;
 #pragma unroll
-      for (int i = 0; i < N; ++i) out[i] = (T)(p[q * N + i] * (g[q * N + i] - s));
+      for (int i = 0; i < N; ++i) out[i] = (T)(p[q * N + i] * fmaf(g[q * N + i], part, -s));
       store_piece<T>(dx + at, out, a.experts - at);
     }
   }
