@@ -33,7 +33,8 @@ class _State:
 class TypedEncoder:
     """`depth` residual blocks over rows of `width` features of `types` kinds. Parameters are fp32; products run in `dtype`
     (fp32, bf16 or fp16). `forward(..., train=True)` leaves what `backward` needs in `state`; `update` is a step of plain gradient descent. With
-    `packed` a training step keeps its normalised rows and its hidden ones in 8 bits, from which the weights' gradients are formed."""
+    `packed` a training step keeps its normalised rows and its hidden ones in 8 bits, from which the gradients of w1 and w2 are formed (what goes out, and the
+    gradients of the rows and the other parameters, are as without)."""
 
     def __init__(self, ctx, types, width, hidden, depth=1, dtype=torch.bfloat16, p=0.1, seed=0, packed=False):
         g = torch.Generator(device=ctx.device)
@@ -120,7 +121,9 @@ class TypedEncoder:
 class RoutedEncoder(TypedEncoder):
     """Features of nodes that have none: rows of a table by the node's id, then blocks as above of `experts`, of which a router gives each row `k`, weighted
     by its scores. `forward` leaves the balance loss of its blocks (1 for each where the experts are used alike) in `balance` and how often each
-    expert was chosen in `counts`; `backward(dy, balance=b)` is the gradient of what dy belongs to and b times that loss."""
+    expert was chosen in `counts`; `backward(dy, balance=b)` is the gradient of what dy belongs to and b times that loss. The router's scores are of `dtype`.
+    With `packed` a training step keeps what each expert put out in 8 bits as well, from which the gradient of the chosen experts' weights is formed: the router's
+    gradient, and through it the table's and those of the blocks before, are then those of rounded rows too."""
 
     def __init__(self, ctx, nodes, experts, width, hidden, depth=1, k=2, dtype=torch.bfloat16, p=0.1, seed=0, packed=False):
         super().__init__(ctx, experts, width, hidden, depth, dtype, p, seed, packed)
