@@ -1,8 +1,8 @@
 // Rows into 8 bits and back: e4m3 codes with a power of two for every 32 columns (packed.h).
 //
-// The power is the smallest that leaves the block's finite values at or below 448, so a value is off by at most 2^-4 of itself, or by 2^-10 of that power where it
-// is smaller than 2^-6 of it. Two things are kept exactly: which values are 0, since a ReLU's gate is read from the codes (what would round to 0
-// becomes the smallest code of its sign), and what is finite: no value comes back larger than its type holds, infinities and NaN come back as NaN.
+// The power is the smallest that leaves the block's finite values at or below 448. A value is off by at most 2^-4 of itself where it is 2^-6 of that power or more, and by at
+// most 2^-10 of the power from 2^-9 of it on. Two things are kept exactly: which values are 0, since a ReLU's gate is read from the codes (what is smaller than 2^-9 of the
+// power becomes that, the smallest code, with its sign), and what is finite: no value comes back larger than its type holds, infinities and NaN come back as NaN.
 #include "feature_ops.h"
 #include "packed.h"
 #include "rows.h"
@@ -13,7 +13,7 @@ constexpr int kThreads = 256, kCols = 8;   // columns of a thread: four threads 
 
 struct PackArgs {
   int64_t rows;
-  int cols, calls, blocks;      // pieces of eight columns to a row, the last block's four filled up; blocks of a row
+  int cols, calls;              // pieces of eight columns to a row (pack: the last block's four filled up)
   int64_t rows_step;            // how far a thread's next piece is
   int calls_step;
   const void* x;                // pack: in; unpack: out
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(PackArgs a) {
       for (int i = 0; i < kCols - 1; ++i)
         if (i < have) word[i / 4] |= (uint32_t)from[i] << (8 * (i % 4));
     }
-    const float power = a.scales ? power_of_scale(a.scales[row * a.ss + col / kPackBlock]) : 1.f;
+    const float power = power_of_scale(a.scales[row * a.ss + col / kPackBlock]);
     float x[kCols];
 #pragma unroll
     for (int i = 0; i < kCols; i += 2) {
