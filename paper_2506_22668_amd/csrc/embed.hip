@@ -382,7 +382,7 @@ __device__ __forceinline__ void clear_rows(const SumArgs& a, int block) {
 
 // LANES threads take a.share sorted rows, a piece of 16 bytes of their columns to a thread, and a workgroup a chunk: sums of ids that reach over a share's end meet in
 // LDS, those of ids that reach over the chunk's go to memory. The first workgroups of the launch clear the rows of ids that did not come up beside it.
-// Bound by memory: 1,000,175 rows of 128 bf16 into 50,021 of fp32 59 us, 4.9 TB/s.
+// Bound by memory: 1,000,175 rows of 128 bf16 into 50,021 of fp32 61 us, 4.7 TB/s.
 template <typename D, typename T, int LANES, bool TINY>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   constexpr int N = Piece<D>::N, WORKERS = kThreads / LANES;
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int col
 
 // Few rows, in one launch: a workgroup has the ids [first, first + range) and the columns of its threads, finds its rows among all and sorts them in LDS, and its
 // workers take equal shares of them. What ids that reach over a share's end leave meets in LDS. Every workgroup reads all ids, which is why rows are few: 1,010 rows of 64 fp32 into
-// 2,000 6.1 us in one launch, 16.6 in the six of the other form; bound by latency.
+// 2,000 5.3 us in one launch, 17.8 in the five of the other form (replayed from a graph); bound by latency.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewRange = 256;
 constexpr int kFewRows = 8192;
 static_assert(kFewRange <= 256 && kFewRows <= 1 << 24, "a pair is 32 bits");
@@ -691,13 +691,19 @@ int sort_blocks(int rows) {
   return blocks <= 2 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks;
 }
 
-// Few rows: ids of a workgroup, so that there are about 512 workgroups (of 64 columns or more); 0: another form
+// Few rows: ids of a workgroup, so that there are about 512 workgroups (of 64 columns or more); 0: another form. A workgroup takes all rows of its ids, in about 5 us and 8 more for
+// each 1,000 of them, and the other form 17 to 30 us, more with more ids; how ids are spread is known on the GPU alone. In us, this form and the other, 128 columns of bf16:
+//   rows   into 4,096 ids   1,024    128      32       8        1        4,096 ids, all rows of one
+//   1,000  6 / 22           6 / 22   7 / 17   8 / 16   13 / 17  16 / 18  16 / 23
+//   2,000  7 / 23           8 / 24   8 / 18   11 / 18  21 / 19  24 / 20  24 / 26
+//   4,000  9 / 28           10 / 27  12 / 20  17 / 20  36 / 21  40 / 23  41 / 34
+//   8,000  13 / 29          14 / 28  19 / 21  29 / 21  67 / 21  74 / 25  74 / 36
+// (So many rows of few ids, evenly spread, to a workgroup at the most; and of fewer than 512 ids half as many in all, since more of them are likely to be of one.)
+constexpr int kFewShare = 1024;
 int few_range(int rows, int cols, int vocab) {
-  // (the rows of one id are all of one workgroup: of few ids half as many rows. 8,000 rows of 128 bf16 into 5,000 ids 12 us so, 38 sorted first, all of one id 74 and 49;
-  // into 8 ids 67 and 25.)
   if (rows > (vocab < 512 ? kFewRows / 2 : kFewRows)) return 0;
-  const int64_t range = ((int64_t)vocab * ((cols + 63) / 64) + 511) / 512;
-  return range > kFewRange ? 0 : range < 8 ? 8 : (int)range;
+  const int64_t even = ((int64_t)vocab * ((cols + 63) / 64) + 511) / 512, range = even < 8 ? 8 : even;
+  return range > kFewRange || (int64_t)rows * (range < vocab ? range : vocab) > (int64_t)kFewShare * vocab ? 0 : (int)range;
 }
 
 struct Layout {

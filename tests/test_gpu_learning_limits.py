@@ -2,6 +2,7 @@
 import pytest
 
 from tests.gpu_common import say
+from tests.test_gpu_embed import gradient, shares
 from tests.test_gpu_features import BF16, F16, F32, U, close, generator, normal
 
 pytestmark = pytest.mark.gpu
@@ -45,6 +46,15 @@ def test_the_most_rows_of_a_tables_gradient(ctx, vocab):
     got = ctx.embed_backward(dy, ids, vocab, dtype=F32)
     assert of[1:].max() <= 2 ** 24
     assert torch.equal(got, of[1:, None].float() * torch.tensor([[1.0, -0.5, 0.25]], device="cuda"))
+
+
+@pytest.mark.parametrize("t, tt", [(F32, F32), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("how", ["one", "few", "uneven"])
+@pytest.mark.parametrize("rows, vocab, cols", [(1024, 8, 40), (1025, 8, 40), (1024, 1, 130), (1025, 1, 130), (2048, 16, 64), (2049, 16, 64), (4096, 32, 9), (4000, 24, 72)])
+def test_gradients_of_few_ids_at_the_borders_of_their_forms(ctx, t, tt, how, rows, vocab, cols):
+    say(f"embed_backward {how} {t} rows={rows} vocab={vocab} cols={cols}")
+    g = generator(rows)
+    gradient(ctx, normal(g, rows, cols, t=t), shares(g, rows, vocab, how), vocab, 1.0, tt)
 
 
 def test_the_most_rows_of_a_router(ctx):
