@@ -26,7 +26,7 @@
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f, kHalf = 0.5f * kLog2e, kLn2 = 0.693147180559945309f;
 
 struct RouteArgs {
   int64_t rows;
@@ -87,16 +87,12 @@ __device__ __forceinline__ float highest_lane(float v) {
 
 // e^d; 0 below 2^-126
 __device__ __forceinline__ float power_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
-// e^d with subnormal results
-__device__ __forceinline__ float whole_power_of(float d) {
-  const float e = __builtin_amdgcn_exp2f(d * (0.5f * kLog2e));
+// 2^(2 d) with subnormal results
+__device__ __forceinline__ float squared_power(float d) {
+  const float e = __builtin_amdgcn_exp2f(d);
   return e * e;
 }
-// 2^d with subnormal results
-__device__ __forceinline__ float whole_power(float d) {
-  const float e = __builtin_amdgcn_exp2f(0.5f * d);
-  return e * e;
-}
+__device__ __forceinline__ float whole_power(float d) { return squared_power(0.5f * d); }
 
 // Element `row` (of up to 2^30, each of four bytes) behind an address that all lanes share
 template <typename V>
@@ -160,8 +156,11 @@ __device__ __forceinline__ void highest(const int (&key)[PER], int (&list)[K]) {
   }
 }
 
-// Counts of a row's experts are added up in LDS (whole numbers: in any order). Bound by vector instructions, about 18 a score:
-// 1,000,175 rows of 64 bf16, 2 of them each, 38.5 us (29 for the bytes); 30,011 rows of 515 fp32, 8 of them each, 40.1 (12.6 for the bytes: a list of nine places to a score).
+// Counts of a row's experts are added up in LDS (whole numbers: in any order). Bound by vector instructions: 1,000,175 rows of 64 bf16, 2 of them each, 38.5 us, about 18 a score (29 for the
+// bytes); 30,011 rows of 515 fp32, 8 of them each, 40.1 (12.6 for the bytes). Of the latter a row, a wave, takes about 600: the list of nine places 80, the
+// eight further picks 190, with some 50 waits between dependent steps across lanes, and a third of the places of all threads but one hold no score. 16-bit rows
+// whose experts do not fill the places of a power of two of threads are farthest from their bytes: of 2^25 scores, k 1, 33, 300 and 515 experts 47, 39 and 41 us, 64,
+// 256 and 1,024 28, 28 and 27.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a) {
   constexpr int ROWS = THREADS / TPR, WAVES = THREADS / 64, WIDE = TPR * PER, LIST = sizeof(T) == 4 ? K + 1 : K, OWN = (K + TPR - 1) / TPR;
@@ -369,7 +368,7 @@ struct RouteGradArgs {
 // The scores that were chosen are read once more, each by its address: a row's sum takes their gradients from there, and the threads that hold them take them from a row
 // in LDS, which is zero but for them (comparing experts in the registers takes four instructions a score and choice). Only the row's own threads, of one
 // wave, touch it, and a wave's LDS accesses keep their order. What e^(x - lse) is off by lse's own rounding, which grows with the scores (1,000: 3e-5; where all are the type's
-// lowest value lse is that value, and each power 1), is the same for a row's experts: their sum takes it out. Bound by memory: 131,072 rows of 256 bf16, 4 of them each, 27.7 us, 5.0 TB/s.
+// lowest value lse is that value, and each power 1), is the same for a row's experts: their sum takes it out. Bound by memory: 131,072 rows of 256 bf16, 4 of them each, 28.2 us, 4.9 TB/s.
 template <typename T, int TPR, int PER, int K, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
   constexpr int ROWS = THREADS / TPR, N = Piece<T>::N, PIECES = PER / N, OWN = (K + TPR - 1) / TPR;
@@ -450,9 +449,18 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
     look_up(row + 2 * step);
     float p[PER], s = 0.f, own = 0.f, sum = 0.f;
     now.read(t, a.experts, none, p);
+    // (the exponents of half the power, as in the forward pass, rounded alike for the whole row; a row that is closed throughout: 0)
+    const bool near = fabsf(base) < 65536.f;
+    const float half = base * kHalf;
+    if (near) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) p[i] = squared_power(fmaf(p[i], kHalf, -half));
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) p[i] = squared_power((p[i] - base) * kHalf);
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      p[i] = whole_power_of(p[i] - base);   // (a row that is closed throughout: 0)
       sum += p[i];
       s = fmaf(p[i], share[i], s);
     }
@@ -466,7 +474,7 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteGradArgs a) {
       float dot = 0.f, total = 0.f;
 #pragma unroll
       for (int c = 0; c < OWN; ++c) {
-        of[c] = id[c] < 0 ? 0.f : whole_power_of(of[c] - base) * part;
+        of[c] = id[c] < 0 ? 0.f : squared_power(near ? fmaf(of[c], kHalf, -half) : (of[c] - base) * kHalf) * part;
         dp[c] = id[c] < 0 ? 0.f : dp[c];
         total += of[c];
         dot = fmaf(dp[c], of[c], dot);
