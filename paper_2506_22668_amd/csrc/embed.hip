@@ -447,8 +447,8 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   }
 }
 
-// Adds up what the chunks left of ids that reach over a chunk's end, in order. Bound by latency, 11.6 us behind the sums above, of which most of the ids reach over one end alone: a workgroup looks at kJoinChunks chunks, kJoinCols columns, kJoinLanes threads to an id of up to kShort
-// chunks, all of them to a longer one.
+// Adds up what the chunks left of ids that reach over a chunk's end, in order: a workgroup looks at kJoinChunks chunks and kJoinCols columns, kJoinLanes threads to an id that
+// goes on over fewer than kShort chunks, all of them to a longer one. Bound by latency: 11.6 us behind the sums above, where most of the ids reach over one end alone.
 constexpr int kJoinThreads = 512, kJoinChunks = 64, kJoinCols = 32, kJoinLanes = kJoinCols / 4, kJoinWorkers = kJoinThreads / kJoinLanes, kShort = 32;
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void finish_kernel(SumArgs a, int col_tiles) {

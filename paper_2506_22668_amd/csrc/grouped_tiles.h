@@ -585,6 +585,8 @@ __device__ __forceinline__ int locate_unit(const MmArgs& a, int depth, int unit,
 // PACKED: x is held in 8 bits; what is done with the numbers in LDS is as without. 2: rows are aligned for it, and codes and scales go into LDS as they are, four stages
 // ahead, from where they are decoded into one of two arrays a stage before they are needed. 1: they come through registers, two stages ahead. 65,521 rows
 // by 1,024 x 512 bf16 in 16 groups: 113 us (2), 122 (1), 93 from bf16 rows; 2,870 rows by 608 x 1,064 fp16 in 22 groups 34, 45, 33; the decoding is in front of the products that it cannot be beside.
+// (1 has two sets of codes under way beside the accumulators: in 16 bits 255 or 256 registers and 4 of them spilled, 10 where dy comes through registers too, around the main loop; their
+// loads and stores come on top of those that a wait counts from behind, so it waits longer at the most. fp32, 118, and 2, 251, spill none.)
 template <typename T, int BR, int BN, int WR, int WN, bool DIRECT, int PACKED = 0>
 __global__ __launch_bounds__(64 * WR * WN, 2) void weight_tiles_kernel(MmArgs a, float* partial, int most_chunks) {
   constexpr int THREADS = 64 * WR * WN, N = Piece<T>::N, DEPTH = kDepthBytes / sizeof(T), UNIT = 2 * DEPTH;   // rows of a stage, and of a unit
@@ -1081,7 +1083,7 @@ int launch_weights(ds_ctx* ctx, MmArgs& a, float* partial) {
   const int64_t tiles = weight_tiles<T, BR, BN>(a.inner, a.outer), chunks = ds_weight_chunks(a.rows, tiles, 128 / (int)sizeof(T));
   const int64_t wgs = (tiles * chunks + 7) / 8 * 8;
   if (wgs > ds_most_workgroups(64 * WR * WN)) return ds_fail(ctx, DS_EINVAL, "weights of %d by %d are more tiles than a launch has", a.inner, a.outer);
-  // (x held in 8 bits comes through registers either way)
+  // (of x in 8 bits it is dy alone that this is about: codes come directly where `codes_direct` says so, else through registers)
   const bool direct = (PACKED || (sixteen(a.x, a.xs, sizeof(T)) && a.inner % Piece<T>::N == 0)) && sixteen(a.dy, a.dys, sizeof(T)) && a.outer % Piece<T>::N == 0;
   const dim3 grid((unsigned)wgs), block(64 * WR * WN);
   bool codes_direct = false;   // rows of codes that can come into LDS as they are
